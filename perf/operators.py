@@ -83,6 +83,8 @@ def draw(rng):
             cols = max(64, cols // 64 * 64)
         rows = _log(rng, 1, max(2, min(16384, 2 ** 24 // cols)))
         c = _norm("", rows, cols, rng.choice(["bf16", "bf16", "f16", "f32"]), rng.choice([0.0, 0.1, 0.3]), form)
+        if c["type"] == "f32":
+            c["rows"] = max(1, rows // 2)
     else:
         kind, dim = rng.choice(["bf16", "bf16", "f16"]), rng.choice([32, 40, 64, 64, 80, 96, 128, 128])
         kv_heads, group = rng.choice([1, 2, 4, 6, 8, 16]), rng.choice([1, 1, 2, 3, 4, 8])
