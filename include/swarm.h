@@ -63,7 +63,7 @@ enum { SWARM_TOPO_COMPLETE = 0, SWARM_TOPO_RING = 1, SWARM_TOPO_REGULAR = 2 };
 
 enum { SWARM_BLOCKING = 0, SWARM_NONBLOCKING = 1, SWARM_REGISTERS = 2 };
 enum { SWARM_OBJ_NONE = 0, SWARM_OBJ_SYNTH = 1, SWARM_OBJ_LSQ = 2, SWARM_OBJ_LOGISTIC = 3 };
-enum { SWARM_F32 = 0, SWARM_BF16 = 1 };
+enum { SWARM_F32 = 0, SWARM_BF16 = 1, SWARM_F16 = 2 };
 
 enum {
   SWARM_OK = 0,
@@ -337,6 +337,105 @@ int64_t swarm_kernel_launches(swarm_ctx *ctx);             /* kernels launched s
 int swarm_last_cuda_error(swarm_ctx *ctx);                 /* cudaError_t of the last SWARM_ECUDA       */
 const char *swarm_strerror(int code);
 void swarm_destroy(swarm_ctx *ctx);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators of the models that the nodes train (the paper's experiments train a Transformer for translation: an encoder's
+ * states are read by a decoder through cross attention, and each of its sublayers ends in dropout, a residual
+ * addition and a norm). They need no context: a caller computes the gradients of its own objective with them and
+ * applies the steps to the models in place (swarm_model_ptr) between interactions.
+ *   - Everything is device memory of the current device; the calls are asynchronous on cuda_stream (cudaStream_t,
+ *     NULL = default stream), keep nothing between calls, allocate nothing and can be captured.
+ *   - Sums, softmax statistics and norms are held in fp32. Results do not depend on timing: the same inputs give
+ *     the same bits.
+ *   - dtype: SWARM_F32, SWARM_BF16 or SWARM_F16, of all activations of a call. Weights and their gradients are fp32.
+ *   - Errors: EINVAL (before anything is launched), ECUDA (swarm_operator_error() names the CUDA error).
+ * ---------------------------------------------------------------------------------------- */
+
+/* Dropout with a residual addition: out = residual + m * x, m = 0 with probability rate, else 1 / (1 - rate).
+ * The mask is never stored: it is drawn from the counter-based generator keyed by `seed`, one call for 8
+ * consecutive columns: Philox(column div 8, row, event, stream 13); column c takes word (c mod 8) div 2, low half
+ * if c is even, and is kept iff these 16 bits are >= T = rate * 2^16 (rounded to the nearest integer); the factor is
+ * 2^16 / (2^16 - T), so that the result is unbiased for the rate that the 16 bits realise. The gradient with
+ * respect to x is the same call on the gradient of out, without a residual and with the same seed and event.
+ *   rows x cols elements, consecutive in a row, rows at the given pitches (elements, >= cols). residual may be
+ *   NULL; out may be x or residual. Rows whose addresses are all multiples of 16 bytes travel as 128-bit accesses,
+ *   others element by element. A dropped element is 0 whatever x holds there.
+ * Errors: EINVAL (NULL, rows or cols < 0 or >= 2^31, a pitch < cols, dtype, rate outside [0, 1], address not a
+ * multiple of the element size). */
+int swarm_dropout(const void *x_dev, const void *residual_dev, void *out_dev, int64_t rows, int64_t cols,
+                  int64_t x_pitch, int64_t residual_pitch, int64_t out_pitch, int32_t dtype, double rate,
+                  uint64_t seed, uint32_t event, void *cuda_stream);
+
+/* Root-mean-square norm with the residual's addition: total = residual + m * x (as swarm_dropout; rate 0 = plain
+ * sum), y = weight * total / sqrt(mean(total^2) + eps), the mean over the cols of a row. The norm is taken of the
+ * fp32 sum, before it is rounded to dtype for total_dev.
+ *   residual_dev may be NULL. total_dev may be NULL, or residual_dev, or x_dev. weight_dev: cols floats.
+ *   Exactly one of y_dev (dtype, pitch y_pitch) and codes_dev is given. codes_dev: y in 8 bits (e4m3, one byte per
+ *   element, row pitch y_pitch) with scales_dev[row][ceil(cols / 128)] floats: y ~ code * scale, scale = (largest
+ *   |y| of the 128 columns) / 448; a block of zeros, or whose scale would be below 2^-126, has scale 0 and codes 0;
+ *   a block that holds a NaN has scale NaN.
+ * Errors: EINVAL (as swarm_dropout; cols > SWARM_NORM_MAX_COLS; eps negative or not finite; neither or both of
+ * y_dev and codes_dev, codes without scales). */
+#define SWARM_NORM_MAX_COLS 32768
+int swarm_add_rms_norm(const void *x_dev, const void *residual_dev, const float *weight_dev, void *total_dev,
+                       void *y_dev, uint8_t *codes_dev, float *scales_dev, int64_t rows, int64_t cols,
+                       int64_t x_pitch, int64_t residual_pitch, int64_t total_pitch, int64_t y_pitch, int32_t dtype,
+                       float eps, double rate, uint64_t seed, uint32_t event, void *cuda_stream);
+
+/* Gradient of swarm_add_rms_norm at the total that it returned. With r = 1 / sqrt(mean(total^2) + eps):
+ *   dresidual = dtotal + r * weight * dy - total * r^3 * mean(weight * dy * total),
+ *   dx = m * dresidual (the mask drawn again),   dweight = sum over rows of dy * total * r.
+ *   dtotal_dev (the gradient that reaches the sum past the norm) may be NULL. dx_dev may be NULL; with rate 0 it
+ *   would equal dresidual. dresidual_dev may be dy_dev or dtotal_dev. dweight_dev: cols floats, or NULL.
+ *   workspace_dev: swarm_add_rms_norm_workspace(rows, cols) bytes, 16-byte aligned, needed with dweight_dev.
+ * The sum over rows is added in a fixed order. Errors: EINVAL. */
+size_t swarm_add_rms_norm_workspace(int64_t rows, int64_t cols);
+int swarm_add_rms_norm_backward(const void *dy_dev, const void *dtotal_dev, const void *total_dev,
+                                const float *weight_dev, void *dresidual_dev, void *dx_dev, float *dweight_dev,
+                                int64_t rows, int64_t cols, int64_t dy_pitch, int64_t dtotal_pitch, int64_t total_pitch,
+                                int64_t dresidual_pitch, int64_t dx_pitch, int32_t dtype, float eps, double rate,
+                                uint64_t seed, uint32_t event, void *workspace_dev, size_t workspace_bytes,
+                                void *cuda_stream);
+
+/* Cross attention: `queries` decoder rows attend to `keys` encoder states. For sentence b, head h, its key head
+ * h div (heads / kv_heads) and the first query_lengths[b] rows and key_lengths[b] states:
+ *   s = scale * q . k,   lse = log sum_j exp(s_j),   o = sum_j exp(s_j - lse) v_j.
+ * A sentence without states, and rows past the end, have o = 0 and lse = -infinity. What q, k, v and dout hold past
+ * the ends is not used (NaN included); gradients there are 0.
+ * Tensors are addressed by strides (elements) over sentence, token and head; the head_dim values of a head are
+ * consecutive. lse is [batch][heads][queries] floats. */
+typedef struct { int64_t batch, token, head; } swarm_strides;
+typedef struct {
+  int32_t batch, heads, kv_heads, queries, keys, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, <= 128 */
+  int32_t dtype;                                             /* SWARM_BF16 or SWARM_F16                     */
+  float scale;                                               /* > 0, finite                                 */
+  int64_t wait_limit;            /* polls after which a device-side wait gives up; < 0: the default; 0: at once  */
+  const int32_t *query_lengths_dev, *key_lengths_dev;        /* [batch], clamped to [0, queries / keys]; NULL: all */
+  swarm_strides q, k, v, o;      /* multiples of 8, >= 0; those of q, k, v may be 0 (a broadcast dimension)      */
+  swarm_strides dout, dq, dk, dv;                            /* read by the backward call only                   */
+} swarm_attention;
+
+/* Bytes of device scratch that the forward (backward = 0) or backward call needs for these sizes (0 is possible).
+ * Errors: EINVAL. */
+int swarm_cross_attention_workspace(const swarm_attention *desc_host, int32_t backward, size_t *bytes_host);
+/* lse_dev may be NULL (needed for the backward pass only). Addresses of q, k, v, o: multiples of 16 bytes.
+ * A call of few query rows per key head (a decoding step) splits the encoder states over CTAs.
+ * Errors: EINVAL (sizes, strides, alignment, scale, dtype, NULL, workspace too small). */
+int swarm_cross_attention(const swarm_attention *desc_host, const void *q_dev, const void *k_dev, const void *v_dev,
+                          void *o_dev, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+/* dq, dk, dv from dout (the gradient of o), q, k, v and the o and lse of the forward call. dk and dv of a key head
+ * are the sums over its query heads, added in a fixed order; p, ds and their products as in the formula
+ *   p = exp(s - lse),  dv = p^T dout,  ds = scale * p * (dout v^T - rowsum(dout * o)),  dq = ds k,  dk = ds^T q. */
+int swarm_cross_attention_backward(const swarm_attention *desc_host, const void *dout_dev, const void *q_dev,
+                                   const void *k_dev, const void *v_dev, const void *o_dev, const float *lse_dev,
+                                   void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,
+                                   size_t workspace_bytes, void *cuda_stream);
+
+/* Waits for cuda_stream and returns SWARM_ECUDA (swarm_operator_error() == cudaErrorLaunchTimeout) if a device-side
+ * wait of an operator has given up on the current device since the last check (its results are then undefined),
+ * or a CUDA error of the stream. */
+int swarm_operator_check(void *cuda_stream);
+int swarm_operator_error(void);                            /* cudaError_t of this thread's last SWARM_ECUDA from an operator */
 
 #ifdef __cplusplus
 }

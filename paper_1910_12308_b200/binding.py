@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 BLOCKING, NONBLOCKING, REGISTERS = 0, 1, 2
 TOPO_COMPLETE, TOPO_RING, TOPO_REGULAR = 0, 1, 2
 OBJ_NONE, OBJ_SYNTH, OBJ_LSQ, OBJ_LOGISTIC = 0, 1, 2, 3
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 OK, EINVAL, ERANGE, EPAIR, ESTATE, ENOMEM, ECUDA = 0, -1, -2, -3, -4, -5, -6
 (T_X, T_B, T_CODES, T_EXPS, T_ADJ, T_A, T_BVEC, T_XSTAR, T_SCALARS, T_COUNTERS, T_OWN, T_OEXPS, T_CLOCKS, T_MU_RECORD,
  T_A_RECORD, T_GRAM) = range(16)
@@ -31,6 +31,9 @@ EXPORTS = [
     "swarm_set_buffer_mode", "swarm_get_tensor", "swarm_get_data_rows", "swarm_get_tensor_async",
     "swarm_set_tensor", "swarm_get_state", "swarm_set_state", "swarm_model_ptr", "swarm_set_stream",
     "swarm_sync", "swarm_set_wait_limit", "swarm_potential_static", "swarm_kernel_launches", "swarm_last_cuda_error", "swarm_strerror", "swarm_destroy",
+    "swarm_dropout", "swarm_add_rms_norm", "swarm_add_rms_norm_workspace", "swarm_add_rms_norm_backward",
+    "swarm_cross_attention", "swarm_cross_attention_workspace", "swarm_cross_attention_backward",
+    "swarm_operator_check", "swarm_operator_error",
 ]
 
 
@@ -116,6 +119,15 @@ def load():
         "swarm_last_cuda_error": (C.c_int, [vp]),
         "swarm_strerror": (C.c_char_p, [C.c_int]),
         "swarm_destroy": (None, [vp]),
+        "swarm_dropout": (C.c_int, [vp, vp, vp, i64, i64, i64, i64, i64, i32, C.c_double, u64, u32, vp]),
+        "swarm_add_rms_norm": (C.c_int, [vp] * 7 + [i64] * 6 + [i32, f32, C.c_double, u64, u32, vp]),
+        "swarm_add_rms_norm_workspace": (C.c_size_t, [i64, i64]),
+        "swarm_add_rms_norm_backward": (C.c_int, [vp] * 7 + [i64] * 7 + [i32, f32, C.c_double, u64, u32, vp, C.c_size_t, vp]),
+        "swarm_cross_attention_workspace": (C.c_int, [vp, i32, C.POINTER(C.c_size_t)]),
+        "swarm_cross_attention": (C.c_int, [vp] * 7 + [C.c_size_t, vp]),
+        "swarm_cross_attention_backward": (C.c_int, [vp] * 11 + [C.c_size_t, vp]),
+        "swarm_operator_check": (C.c_int, [vp]),
+        "swarm_operator_error": (C.c_int, []),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

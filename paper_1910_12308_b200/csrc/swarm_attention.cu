@@ -1,0 +1,279 @@
+// Cross attention of a decoder's rows to an encoder's states, and its gradient.
+//
+//   s = scale * q k^T,  p = exp(s - lse),  o = p v
+//   dv = p^T dout,  ds = scale * p * (dout v^T - rowsum(dout * o)),  dq = ds k,  dk = ds^T q
+//
+// One pass over the states with the running maximum and sum of the softmax; nothing of size queries x keys is stored.
+#include <cmath>
+#include <mutex>
+
+#include "swarm_opsup.cuh"
+
+namespace swarm {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttentionArgs {
+  const void *q, *k, *v, *o, *dout;
+  const float* lse_in;
+  void *out, *dq, *dk, *dv;
+  float* lse;
+  float* delta;                       // [batch][heads][queries] rowsum(dout * o)
+  const int32_t *query_lengths, *key_lengths;
+  swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;
+  int32_t batch, heads, kv_heads, group, queries, keys, head_dim;
+  float scale;
+};
+
+__device__ __forceinline__ int length_of(const int32_t* lengths, int b, int most) {
+  return lengths ? min(max(lengths[b], 0), most) : most;
+}
+
+__device__ __forceinline__ int64_t offset_of(const swarm_strides& s, int b, int t, int h) {
+  return b * s.batch + t * s.token + h * s.head;
+}
+
+template <typename T>
+__device__ __forceinline__ float dot_row(const float* a, const T* p, int dim) {
+  float s = 0.0f;
+  for (int d = 0; d < dim; d += 8) {
+    float v[8];
+    unpack8<T>(load_raw8<T>(p + d), v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(a[d + i], v[i], s);
+  }
+  return s;
+}
+
+constexpr int kMaxDim = 128;
+
+// Warp = one query row; lane = one state of 32 at a time for the scores, then dims lane, lane + 32, ... of the output.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_rows_kernel(AttentionArgs a) {
+  __shared__ float sq[4][kMaxDim];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * 4 + warp, h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
+  if (t >= a.queries) return;
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h);
+  T* out = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h);
+  const int n = t < nq ? nk : 0;
+  for (int d = lane; d < a.head_dim; d += 32) sq[warp][d] = n ? to_float<T>(q[d]) : 0.0f;
+  __syncwarp();
+  float m = -INFINITY, l = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < n; j0 += 32) {
+    const int j = j0 + lane;
+    const float s = j < n ? a.scale * dot_row<T>(sq[warp], reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk), a.head_dim) : -INFINITY;
+    float top = s;
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.0f : m_new;
+    const float c = exp2f((m - base) * kLog2e), p = exp2f((s - base) * kLog2e);
+    l = l * c + warp_sum(p);
+    m = m_new;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] *= c;
+    for (int u = 0; u < min(32, n - j0); ++u) {
+      const float pu = __shfl_sync(0xFFFFFFFFu, p, u);
+      const T* v = reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j0 + u, hk);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (lane + 32 * i < a.head_dim) acc[i] = fmaf(pu, to_float<T>(v[lane + 32 * i]), acc[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (lane + 32 * i < a.head_dim) out[lane + 32 * i] = from_float<T>(n ? acc[i] / l : 0.0f);
+  if (a.lse && lane == 0) a.lse[((int64_t)b * a.heads + h) * a.queries + t] = n ? m + logf(l) : -INFINITY;
+}
+
+// Warp = one query row: delta, then dq.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_dq_kernel(AttentionArgs a) {
+  __shared__ float sq[4][kMaxDim], sd[4][kMaxDim];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * 4 + warp, h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
+  if (t >= a.queries) return;
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  const int n = t < nq ? nk : 0;
+  const int64_t at = ((int64_t)b * a.heads + h) * a.queries + t;
+  float delta = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n) {
+    const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h);
+    const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t, h);
+    const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, t, h);
+    for (int d = lane; d < a.head_dim; d += 32) {
+      sq[warp][d] = to_float<T>(q[d]);
+      sd[warp][d] = to_float<T>(g[d]);
+      delta = fmaf(to_float<T>(g[d]), to_float<T>(o[d]), delta);
+    }
+    __syncwarp();
+    delta = warp_sum(delta);
+    const float lse = a.lse_in[at];
+    for (int j0 = 0; j0 < n; j0 += 32) {
+      const int j = min(j0 + lane, n - 1);
+      const float s = a.scale * dot_row<T>(sq[warp], reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk), a.head_dim);
+      const float dp = dot_row<T>(sd[warp], reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j, hk), a.head_dim);
+      const float ds = a.scale * exp2f((s - lse) * kLog2e) * (dp - delta);
+      for (int u = 0; u < min(32, n - j0); ++u) {
+        const float du = __shfl_sync(0xFFFFFFFFu, ds, u);
+        const T* k = reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j0 + u, hk);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (lane + 32 * i < a.head_dim) acc[i] = fmaf(du, to_float<T>(k[lane + 32 * i]), acc[i]);
+      }
+    }
+  }
+  if (lane == 0) a.delta[at] = delta;
+  T* dq = reinterpret_cast<T*>(a.dq) + offset_of(a.dqs, b, t, h);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (lane + 32 * i < a.head_dim) dq[lane + 32 * i] = from_float<T>(acc[i]);
+}
+
+// Warp = one state of one key head: dk and dv over the rows of its query heads.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_dkv_kernel(AttentionArgs a) {
+  __shared__ float sk[4][kMaxDim], sv[4][kMaxDim];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int j = blockIdx.x * 4 + warp, hk = blockIdx.y, b = blockIdx.z;
+  if (j >= a.keys) return;
+  const int nk = length_of(a.key_lengths, b, a.keys);
+  const int n = j < nk ? length_of(a.query_lengths, b, a.queries) : 0;
+  float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n) {
+    const T* k = reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk);
+    const T* v = reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j, hk);
+    for (int d = lane; d < a.head_dim; d += 32) { sk[warp][d] = to_float<T>(k[d]); sv[warp][d] = to_float<T>(v[d]); }
+    __syncwarp();
+  }
+  for (int g = 0; g < a.group; ++g) {
+    const int h = hk * a.group + g;
+    const int64_t at = ((int64_t)b * a.heads + h) * a.queries;
+    for (int t0 = 0; t0 < n; t0 += 32) {
+      const int t = min(t0 + lane, n - 1);
+      const float s = a.scale * dot_row<T>(sk[warp], reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h), a.head_dim);
+      const float dp = dot_row<T>(sv[warp], reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t, h), a.head_dim);
+      const float p = exp2f((s - a.lse_in[at + t]) * kLog2e), ds = a.scale * p * (dp - a.delta[at + t]);
+      for (int u = 0; u < min(32, n - t0); ++u) {
+        const float pu = __shfl_sync(0xFFFFFFFFu, p, u), du = __shfl_sync(0xFFFFFFFFu, ds, u);
+        const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t0 + u, h);
+        const T* d_ = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t0 + u, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (lane + 32 * i < a.head_dim) {
+            dk[i] = fmaf(du, to_float<T>(q[lane + 32 * i]), dk[i]);
+            dv[i] = fmaf(pu, to_float<T>(d_[lane + 32 * i]), dv[i]);
+          }
+      }
+    }
+  }
+  T* pk = reinterpret_cast<T*>(a.dk) + offset_of(a.dks, b, j, hk);
+  T* pv = reinterpret_cast<T*>(a.dv) + offset_of(a.dvs, b, j, hk);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (lane + 32 * i < a.head_dim) { pk[lane + 32 * i] = from_float<T>(dk[i]); pv[lane + 32 * i] = from_float<T>(dv[i]); }
+}
+
+// ---- argument checks ------------------------------------------------------------------------
+bool desc_ok(const swarm_attention* d) {
+  return d && d->batch >= 0 && d->queries >= 0 && d->keys >= 0 && d->heads >= 1 && d->kv_heads >= 1 &&
+         d->heads % d->kv_heads == 0 && d->batch <= 65535 && d->heads <= 65535 && d->head_dim >= 8 && d->head_dim <= kMaxDim &&
+         d->head_dim % 8 == 0 && (d->dtype == SWARM_BF16 || d->dtype == SWARM_F16) && d->scale > 0.0f && std::isfinite(d->scale);
+}
+constexpr int64_t kMaxStride = (int64_t)1 << 38;
+bool one_stride_ok(int64_t s, int extent, bool output) {
+  return extent <= 1 || (s >= 0 && s < kMaxStride && s % 8 == 0 && !(output && s == 0));
+}
+// A tensor of `tokens` rows and `heads` heads: address and strides; an output may not repeat a dimension.
+bool strided_ok(const void* p, const swarm_strides& s, int batch, int tokens, int heads, bool output) {
+  return p && ((uintptr_t)p & 15) == 0 && one_stride_ok(s.batch, batch, output) && one_stride_ok(s.token, tokens, output) &&
+         one_stride_ok(s.head, heads, output);
+}
+bool lengths_ok(const int32_t* p) { return ((uintptr_t)p & 3) == 0; }
+
+void fill(AttentionArgs& a, const swarm_attention* d) {
+  a.query_lengths = d->query_lengths_dev; a.key_lengths = d->key_lengths_dev;
+  a.qs = d->q; a.ks = d->k; a.vs = d->v; a.os = d->o; a.dos = d->dout; a.dqs = d->dq; a.dks = d->dk; a.dvs = d->dv;
+  a.batch = d->batch; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads;
+  a.queries = d->queries; a.keys = d->keys; a.head_dim = d->head_dim;
+  a.scale = d->scale;
+}
+
+}  // namespace
+}  // namespace swarm
+
+using namespace swarm;
+
+extern "C" {
+
+int swarm_cross_attention_workspace(const swarm_attention* desc_host, int32_t backward, size_t* bytes_host) {
+  if (!desc_ok(desc_host) || !bytes_host) return SWARM_EINVAL;
+  *bytes_host = backward ? (size_t)desc_host->batch * desc_host->heads * desc_host->queries * sizeof(float) : 0;
+  return SWARM_OK;
+}
+
+int swarm_cross_attention(const swarm_attention* desc_host, const void* q_dev, const void* k_dev, const void* v_dev,
+                          void* o_dev, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+  if (!desc_ok(desc_host)) return SWARM_EINVAL;
+  const swarm_attention& d = *desc_host;
+  if (d.batch == 0 || d.queries == 0) return SWARM_OK;
+  size_t need = 0;
+  swarm_cross_attention_workspace(desc_host, 0, &need);
+  if (!strided_ok(q_dev, d.q, d.batch, d.queries, d.heads, false) || !strided_ok(o_dev, d.o, d.batch, d.queries, d.heads, true) ||
+      (d.keys > 0 && (!strided_ok(k_dev, d.k, d.batch, d.keys, d.kv_heads, false) || !strided_ok(v_dev, d.v, d.batch, d.keys, d.kv_heads, false))) ||
+      ((uintptr_t)lse_dev & 3) || !lengths_ok(d.query_lengths_dev) || !lengths_ok(d.key_lengths_dev) ||
+      workspace_bytes < need || (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15))))
+    return SWARM_EINVAL;
+  AttentionArgs a{};
+  fill(a, desc_host);
+  a.q = q_dev; a.k = k_dev; a.v = v_dev; a.out = o_dev; a.lse = lse_dev;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const dim3 grid((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
+  if (d.dtype == SWARM_BF16) attention_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
+  else attention_rows_kernel<__half><<<grid, 128, 0, st>>>(a);
+  return operator_result(cudaGetLastError());
+}
+
+int swarm_cross_attention_backward(const swarm_attention* desc_host, const void* dout_dev, const void* q_dev,
+                                   const void* k_dev, const void* v_dev, const void* o_dev, const float* lse_dev,
+                                   void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                                   size_t workspace_bytes, void* cuda_stream) {
+  if (!desc_ok(desc_host)) return SWARM_EINVAL;
+  const swarm_attention& d = *desc_host;
+  if (d.batch == 0) return SWARM_OK;
+  size_t need = 0;
+  swarm_cross_attention_workspace(desc_host, 1, &need);
+  if (d.queries > 0 &&
+      (!strided_ok(q_dev, d.q, d.batch, d.queries, d.heads, false) || !strided_ok(o_dev, d.o, d.batch, d.queries, d.heads, false) ||
+       !strided_ok(dout_dev, d.dout, d.batch, d.queries, d.heads, false) || !strided_ok(dq_dev, d.dq, d.batch, d.queries, d.heads, true) ||
+       !lse_dev || ((uintptr_t)lse_dev & 3)))
+    return SWARM_EINVAL;
+  if (d.keys > 0 &&
+      (!strided_ok(dk_dev, d.dk, d.batch, d.keys, d.kv_heads, true) || !strided_ok(dv_dev, d.dv, d.batch, d.keys, d.kv_heads, true) ||
+       !strided_ok(k_dev, d.k, d.batch, d.keys, d.kv_heads, false) || !strided_ok(v_dev, d.v, d.batch, d.keys, d.kv_heads, false)))
+    return SWARM_EINVAL;
+  if (!lengths_ok(d.query_lengths_dev) || !lengths_ok(d.key_lengths_dev) || workspace_bytes < need ||
+      (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15))))
+    return SWARM_EINVAL;
+  AttentionArgs a{};
+  fill(a, desc_host);
+  a.q = q_dev; a.k = k_dev; a.v = v_dev; a.o = o_dev; a.dout = dout_dev; a.lse_in = lse_dev;
+  a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev; a.delta = reinterpret_cast<float*>(workspace_dev);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const dim3 gq((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
+  const dim3 gk((unsigned)((d.keys + 3) / 4), (unsigned)d.kv_heads, (unsigned)d.batch);
+  if (d.queries > 0) {
+    if (d.dtype == SWARM_BF16) attention_dq_kernel<__nv_bfloat16><<<gq, 128, 0, st>>>(a);
+    else attention_dq_kernel<__half><<<gq, 128, 0, st>>>(a);
+  }
+  if (d.keys > 0) {
+    if (d.dtype == SWARM_BF16) attention_dkv_kernel<__nv_bfloat16><<<gk, 128, 0, st>>>(a);
+    else attention_dkv_kernel<__half><<<gk, 128, 0, st>>>(a);
+  }
+  return operator_result(cudaGetLastError());
+}
+
+int swarm_operator_check(void* cuda_stream) { return operator_result(cudaStreamSynchronize((cudaStream_t)cuda_stream)); }
+
+}  // extern "C"

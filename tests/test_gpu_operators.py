@@ -1,0 +1,525 @@
+"""Operators of the models that the nodes train, against their formulas in 64 bits.
+
+Tolerances are bounds, not observations. U is the largest relative rounding error of a type. A result that is rounded
+once is held to U of itself; E = 2e-5 covers what fp32 arithmetic adds (128-term dot products of unit normals, base-2
+exponentials, sums of a few thousand terms); an operand that is rounded to the type before a product contributes U times
+the product's absolute sum.
+"""
+import math
+
+import pytest
+
+from paper_1910_12308_b200 import binding as g
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_1910_12308_b200 import operators as ops  # noqa: E402
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+U = {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}
+TINY = {BF16: 1e-38, F16: 2.0 ** -24, F32: 1e-38}        # a result may fall among the subnormals of its type
+E = 2e-5
+
+
+def randn(*shape, dtype=F32, seed=0, std=1.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def within(got, want, bound, what=""):
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape, what
+    assert not torch.isnan(got).any(), what
+    over = (got - want).abs() - bound
+    assert over.max().item() <= 0 if over.numel() else True, (what, over.max().item(), (got - want).abs().max().item())
+
+
+# ---- the mask ------------------------------------------------------------------------------------------------------
+
+
+def philox(counter, key):
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(p1 >> 32) ^ c[1] ^ k[0], p1 & 0xFFFFFFFF, (p0 >> 32) ^ c[3] ^ k[1], p0 & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def factors(rows, cols, rate, seed, event):
+    """m of every element: 0, or 2^16 / (2^16 - T)."""
+    drop = math.floor(rate * 65536 + 0.5)
+    out = torch.zeros(rows, cols, dtype=torch.float64)
+    for r in range(rows):
+        for c0 in range(0, cols, 8):
+            words = philox((c0 // 8, r, event, 13), (seed & 0xFFFFFFFF, seed >> 32))
+            for c in range(c0, min(c0 + 8, cols)):
+                u = words[(c % 8) // 2] >> (16 * (c % 2)) & 0xFFFF
+                out[r, c] = 65536 / (65536 - drop) if u >= drop else 0.0
+    return out.cuda()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (2, 8), (5, 9), (4, 255), (3, 256), (2, 264), (9, 513), (3, 1001)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_dropout(dtype, rows, cols, residual):
+    seed, event, rate = 0xFEDCBA9876543210 + rows, 4000000000 + cols, 0.3
+    x, r = randn(rows, cols, dtype=dtype, seed=1), randn(rows, cols, dtype=dtype, seed=2, std=3) if residual else None
+    m = factors(rows, cols, rate, seed, event)
+    want = x.double() * m + (r.double() if residual else 0.0)
+    got = ops.dropout(x, rate, seed, event, residual=r)
+    size = (x.double() * m).abs() + (r.double().abs() if residual else 0.0)
+    within(got, want, U[dtype] * want.abs() + 2.0 ** -22 * size + TINY[dtype])
+    if not residual:
+        assert torch.equal(got == 0, (m == 0) | (x == 0))
+
+
+def test_dropout_ends_of_the_rate_and_what_is_dropped():
+    x = torch.full((4, 300), float("nan"), device="cuda")
+    assert torch.equal(ops.dropout(x, 1.0, 1, 2), torch.zeros_like(x))          # nothing of a dropped element is used
+    y = randn(4, 300)
+    assert torch.equal(ops.dropout(y, 0.0, 1, 2), y)
+    assert torch.equal(ops.dropout(y, 1.0, 1, 2, residual=y), y)
+    kept = ops.dropout(torch.ones(512, 4096, device="cuda"), 0.25, 77, 3)
+    share = (kept > 0).double().mean().item()
+    assert abs(share - 0.75) < 6 * math.sqrt(0.75 * 0.25 / kept.numel())         # six standard deviations
+    other = ops.dropout(torch.ones(512, 4096, device="cuda"), 0.25, 77, 4)
+    assert abs(((kept > 0) == (other > 0)).double().mean().item() - (0.75 ** 2 + 0.25 ** 2)) < 6 / math.sqrt(kept.numel())
+    assert ops.dropout(torch.empty(0, 5, device="cuda"), 0.5, 1, 2).shape == (0, 5)
+    assert ops.dropout(torch.empty(5, 0, device="cuda"), 0.5, 1, 2).shape == (5, 0)
+
+
+def test_dropout_does_not_depend_on_strides_alignment_or_place():
+    x, r = randn(40, 520, dtype=BF16, seed=3), randn(40, 520, dtype=BF16, seed=4)
+    want = ops.dropout(x, 0.4, 9, 5, residual=r)
+    wide = torch.zeros(40, 1111, dtype=BF16, device="cuda")
+    wide[:, 3:523] = x                                                          # neither the base nor the pitch on 16 bytes
+    assert torch.equal(ops.dropout(wide[:, 3:523], 0.4, 9, 5, residual=r), want)
+    assert torch.equal(ops.dropout(x.view(4, 10, 520), 0.4, 9, 5, residual=r.view(4, 10, 520)).view(40, 520), want)
+    into = torch.zeros(40, 600, dtype=BF16, device="cuda")
+    ops.dropout(x, 0.4, 9, 5, residual=r, out=into[:, 8:528])
+    assert torch.equal(into[:, 8:528], want) and not into[:, :8].any() and not into[:, 528:].any()
+    here = x.clone()
+    assert torch.equal(ops.dropout(here, 0.4, 9, 5, residual=r, out=here), want)
+    there = r.clone()
+    assert torch.equal(ops.dropout(x, 0.4, 9, 5, residual=there, out=there), want)
+
+
+def test_dropout_gradient_is_its_difference():
+    x, dy, u = (randn(7, 333, dtype=F32, seed=s) for s in (5, 6, 7))
+    dx = ops.dropout(dy, 0.2, 11, 12)
+    up, down = (ops.dropout(x + h * u, 0.2, 11, 12).double() for h in (0.5, -0.5))
+    lhs, rhs = ((up - down) * dy.double()).sum().item(), (dx.double() * u.double()).sum().item()
+    assert abs(lhs - rhs) <= 2.0 ** -21 * (dx.double().abs() * (u.abs() + x.abs())).sum().item()
+
+
+# ---- norm ----------------------------------------------------------------------------------------------------------
+
+
+def norm_reference(x, r, w, eps, m):
+    total = x.double() * m + (r.double() if r is not None else 0.0)
+    return total, w.double() * total / (total.square().mean(1, keepdim=True) + eps).sqrt()
+
+
+NORM_SHAPES = [(1, 1), (2, 5), (3, 64), (5, 255), (2, 256), (7, 257), (3, 512), (9, 1001), (2, 1024), (3, 1032), (2, 2048),
+               (2, 4100), (2, 8192), (1, 16000), (1, 32768)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+@pytest.mark.parametrize("rate,residual", [(0.0, True), (0.3, True), (0.0, False)])
+def test_add_rms_norm(dtype, rows, cols, rate, residual):
+    if rate and cols > 1100:
+        pytest.skip("the mask is checked at the smaller widths; the reference draws it one call at a time")
+    x, r = randn(rows, cols, dtype=dtype, seed=1), randn(rows, cols, dtype=dtype, seed=2, std=3) if residual else None
+    w = 1 + 0.3 * randn(cols, seed=3)
+    m = factors(rows, cols, rate, 5, 6) if rate else 1.0
+    total, want = norm_reference(x, r, w, 1e-5, m)
+    y, kept = ops.add_rms_norm(x, w, residual=r, eps=1e-5, rate=rate, seed=5, event=6)
+    size = (x.double() * m).abs() + (r.double().abs() if residual else 0.0)
+    within(kept, total, U[dtype] * total.abs() + 2.0 ** -22 * size + TINY[dtype])
+    rstd = 1 / (total.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    within(y, want, (U[dtype] + E) * want.abs() + 2.0 ** -22 * size * rstd * w.double().abs() + TINY[dtype])
+    if not residual and not rate:
+        assert kept is x
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+def test_add_rms_norm_in_8_bits(dtype, rows, cols):
+    x, r = randn(rows, cols, dtype=dtype, seed=1), randn(rows, cols, dtype=dtype, seed=2)
+    x[0] = 0
+    r[0, : cols // 2] = 0                                                       # blocks of zeros
+    w = 1 + 0.3 * randn(cols, seed=3)
+    codes, scales, total = ops.add_rms_norm(x, w, residual=r, eight_bit=True)
+    _, want = norm_reference(x, r, w, 1e-6, 1.0)
+    assert codes.dtype == torch.float8_e4m3fn and scales.shape == (rows, (cols + 127) // 128)
+    within(total, x.double() + r.double(), U[dtype] * (x.double() + r.double()).abs() + 2.0 ** -22 * (x.abs() + r.abs()).double() + TINY[dtype])
+    for b in range(scales.shape[1]):
+        part = want[:, 128 * b: 128 * b + 128]
+        top = part.abs().amax(1)
+        assert ((scales[:, b].double() * 448 - top).abs() <= E * top).all()
+        s = scales[:, b].double().unsqueeze(1)
+        got = codes[:, 128 * b: 128 * b + 128].double() * s
+        # e4m3 keeps four significant bits, and steps of 2^-9 below 2^-6
+        within(got, part, part.abs() * (2.0 ** -4 + E) + s * 2.0 ** -10 * (1 + E) + E * top.unsqueeze(1))
+        assert (codes[:, 128 * b: 128 * b + 128].float()[top == 0] == 0).all()
+
+
+def test_add_rms_norm_8_bits_of_values_that_are_not_finite():
+    x = randn(3, 384, seed=1)
+    x[1, 200] = float("nan")
+    codes, scales, _ = ops.add_rms_norm(x, torch.ones(384, device="cuda"), eight_bit=True)
+    assert torch.isfinite(codes[0].float()).all() and torch.isfinite(scales[[0, 2]]).all()
+    assert torch.isnan(scales[1]).all() and torch.isnan(codes[1].float()).all()  # the norm of that row has no value
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (4, 64), (5, 255), (700, 256), (33, 257), (9, 1001), (1200, 1024),
+                                       (40, 1032), (6, 2048), (3, 4100), (300, 8192), (2, 16000), (2, 32768)])
+@pytest.mark.parametrize("rate,past", [(0.0, True), (0.3, True), (0.0, False)])
+def test_add_rms_norm_backward(dtype, rows, cols, rate, past):
+    if rate and rows * cols > 12000:
+        pytest.skip("the mask is checked at the smaller sizes; the reference draws it one call at a time")
+    total, dy = randn(rows, cols, dtype=dtype, seed=1, std=2), randn(rows, cols, dtype=dtype, seed=2)
+    dtotal = randn(rows, cols, dtype=dtype, seed=3) if past else None
+    w = 1 + 0.3 * randn(cols, seed=4)
+    m = factors(rows, cols, rate, 5, 6) if rate else 1.0
+    t, dyd, wd = total.double(), dy.double(), w.double()
+    r = 1 / (t.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    first, second = r * wd * dyd, t * r ** 3 * (wd * dyd * t).mean(1, keepdim=True)
+    want = first - second + (dtotal.double() if past else 0.0)
+    size = first.abs() + t.abs() * r ** 3 * (wd * dyd * t).abs().mean(1, keepdim=True) + (dtotal.double().abs() if past else 0.0)
+    dx, dres, dw = ops.add_rms_norm_backward(dy, total, w, dtotal=dtotal, rate=rate, seed=5, event=6)
+    within(dres, want, U[dtype] * want.abs() + E * size + TINY[dtype])
+    within(dx, want * m, U[dtype] * (want * m).abs() + E * size * 2 + TINY[dtype])
+    within(dw, (dyd * t * r).sum(0), E * (dyd * t * r).abs().sum(0) + 1e-30)
+    again = ops.add_rms_norm_backward(dy, total, w, dtotal=dtotal, rate=rate, seed=5, event=6)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dres, dw)))          # one fixed order of addition
+
+
+def test_norm_gradient_is_the_difference_of_the_norm():
+    x, dy, u = (randn(6, 300, seed=s).double() for s in (1, 2, 3))
+    w, v = 1 + 0.3 * randn(300, seed=4), randn(300, seed=5)
+    h = 1e-4
+
+    def loss(x_, w_):
+        return (norm_reference(x_, None, w_, 1e-6, 1.0)[1] * dy).sum().item()
+
+    dx, _, dw = ops.add_rms_norm_backward(dy.float(), x.float(), w)
+    x, dy = x.float().double(), dy.float().double()
+    num = (loss(x + h * u, w.double()) - loss(x - h * u, w.double())) / (2 * h)
+    assert abs(num - (dx.double() * u).sum().item()) <= (E + 1e-6) * (dx.double().abs() * u.abs()).sum().item() + 1e-6
+    num = (loss(x, w.double() + h * v.double()) - loss(x, w.double() - h * v.double())) / (2 * h)
+    assert abs(num - (dw.double() * v.double()).sum().item()) <= (E + 1e-6) * (dw.double().abs() * v.double().abs()).sum().item() + 1e-6
+
+
+def test_norm_does_not_depend_on_strides_and_alignment():
+    x, r, w = randn(20, 520, dtype=BF16, seed=1), randn(20, 520, dtype=BF16, seed=2), 1 + 0.3 * randn(520, seed=3)
+    store = torch.zeros(521, device="cuda")
+    store[1:] = w
+    y, total = ops.add_rms_norm(x, w, residual=r, rate=0.2, seed=1, event=2)
+    c, s, _ = ops.add_rms_norm(x, w, residual=r, rate=0.2, seed=1, event=2, eight_bit=True)
+    wide = torch.zeros(20, 777, dtype=BF16, device="cuda")
+    wide[:, 5:525] = x
+    y2, total2 = ops.add_rms_norm(wide[:, 5:525], store[1:], residual=r, rate=0.2, seed=1, event=2)
+    assert torch.equal(total, total2)
+    within(y2, y, 2 * U[BF16] * y.double().abs() + TINY[BF16])                   # another order of the sum of squares
+    c2, s2, _ = ops.add_rms_norm(wide[:, 5:525], store[1:], residual=r, rate=0.2, seed=1, event=2, eight_bit=True)
+    assert ((s - s2).abs() <= E * s).all() and ((c.float() - c2.float()).abs() <= 2.0 ** -3 * c.float().abs() + 2.0 ** -9).all()
+    y3, _ = ops.add_rms_norm(x.view(4, 5, 520), store[1:], residual=r.view(4, 5, 520), rate=0.2, seed=1, event=2)
+    assert torch.equal(y3.view(20, 520), y)
+    g1 = ops.add_rms_norm_backward(r, total, w, dtotal=x, rate=0.2, seed=1, event=2)
+    g2 = ops.add_rms_norm_backward(r, total, store[1:], dtotal=wide[:, 5:525], rate=0.2, seed=1, event=2)
+    for a, b in zip(g1, g2):
+        within(b, a, (2 * U[BF16] if a.dtype == BF16 else 1e-4) * a.double().abs().clamp_min(1e-2))
+
+
+# ---- attention -----------------------------------------------------------------------------------------------------
+
+
+def attention_reference(q, k, v, scale, nq, nk, do=None, u=0.0):
+    """o, lse (and dq, dk, dv) in 64 bits with elementwise bounds for an implementation that rounds p and ds to a type
+    with relative error u before their products."""
+    b, tq, h, d = q.shape
+    tk, hk = k.shape[1], k.shape[2]
+    grp = h // hk
+    out = {}
+    res = {n: torch.zeros(b, tq, h, d, dtype=torch.float64, device="cuda") for n in ("o", "o_b", "dq", "dq_b")}
+    res |= {n: torch.zeros(b, tk, hk, d, dtype=torch.float64, device="cuda") for n in ("dk", "dk_b", "dv", "dv_b")}
+    res["lse"] = torch.full((b, h, tq), -math.inf, dtype=torch.float64, device="cuda")
+    for i in range(b):
+        n, m = int(nq[i]), int(nk[i])
+        if not n or not m:
+            continue
+        for a in range(h):
+            c = a // grp
+            qd, kd, vd = q[i, :n, a].double(), k[i, :m, c].double(), v[i, :m, c].double()
+            s = scale * qd @ kd.T
+            lse = torch.logsumexp(s, 1)
+            p = torch.exp(s - lse[:, None])
+            o = p @ vd
+            res["lse"][i, a, :n] = lse
+            res["o"][i, :n, a] = o
+            ob = (u + E) * (p @ vd.abs())
+            res["o_b"][i, :n, a] = u * o.abs() + ob
+            if do is None:
+                continue
+            g_ = do[i, :n, a].double()
+            dp, delta = g_ @ vd.T, (g_ * o).sum(1, keepdim=True)
+            ds = scale * p * (dp - delta)
+            delta_b = (g_.abs() * (u * o.abs() + ob)).sum(1, keepdim=True) + E * (g_ * o).abs().sum(1, keepdim=True)
+            ds_b = (u + E) * ds.abs() + scale * p * (E * (g_.abs() @ vd.abs().T) * 0.1 + delta_b)
+            res["dq"][i, :n, a] = ds @ kd
+            res["dq_b"][i, :n, a] = ds_b @ kd.abs()
+            res["dk"][i, :m, c] += ds.T @ qd
+            res["dk_b"][i, :m, c] += ds_b.T @ qd.abs()
+            res["dv"][i, :m, c] += p.T @ g_
+            res["dv_b"][i, :m, c] += (u + E) * (p.T @ g_.abs())
+    for name in ("dq", "dk", "dv"):
+        res[name + "_b"] += u * res[name].abs()
+    return res
+
+
+def attention_inputs(b, tq, tk, h, hk, d, dtype, seed=0, layout="tokens"):
+    q, do = randn(b, tq, h, d, dtype=dtype, seed=seed, std=1.5), randn(b, tq, h, d, dtype=dtype, seed=seed + 3)
+    if layout == "packed":
+        kv = randn(b, tk, 2, hk, d, dtype=dtype, seed=seed + 1)
+        return q, kv[:, :, 0], kv[:, :, 1], do
+    if layout == "heads":
+        k, v = (randn(b, hk, tk, d, dtype=dtype, seed=seed + s).transpose(1, 2) for s in (1, 2))
+        return q.transpose(1, 2).contiguous().transpose(1, 2), k, v, do
+    return q, randn(b, tk, hk, d, dtype=dtype, seed=seed + 1), randn(b, tk, hk, d, dtype=dtype, seed=seed + 2), do
+
+
+def check_attention(q, k, v, do, nq=None, nk=None, scale=None, clean=None):
+    """Forward and backward against the reference; `clean` holds (q, k, v, do) with finite values where the inputs
+    themselves hold others past the ends."""
+    b, tq, h, d = q.shape
+    tk, dtype = k.shape[1], q.dtype
+    cq, ck, cv, cdo = clean or (q, k, v, do)
+    s = scale or d ** -0.5
+    lq = nq.tolist() if nq is not None else [tq] * b
+    lk = nk.tolist() if nk is not None else [tk] * b
+    clamp = lambda n, most: [min(max(x, 0), most) for x in n]  # noqa: E731
+    ref = attention_reference(cq, ck, cv, s, clamp(lq, tq), clamp(lk, tk), cdo, U[dtype])
+    kw = dict(scale=scale, query_lengths=nq, key_lengths=nk)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True, **kw)
+    within(o, ref["o"], ref["o_b"] + TINY[dtype], "o")
+    assert torch.equal(torch.isinf(lse), torch.isinf(ref["lse"])) and not (lse == math.inf).any()
+    fin = torch.isfinite(ref["lse"])
+    within(lse[fin], ref["lse"][fin], E * (1 + ref["lse"][fin].abs()), "lse")
+    assert torch.equal(ops.cross_attention(q, k, v, **kw), o)                    # with and without lse, and twice the same bits
+    got = ops.cross_attention_backward(do, q, k, v, o, lse, **kw)
+    for name, x in zip(("dq", "dk", "dv"), got):
+        within(x, ref[name], ref[name + "_b"] + TINY[dtype], name)
+    again = ops.cross_attention_backward(do, q, k, v, o, lse, **kw)
+    assert all(torch.equal(x, y) for x, y in zip(got, again))                    # one fixed order of addition
+    ops.check()
+    return o, lse, got
+
+
+LENGTHS = [(1, 1), (1, 2), (1, 77), (2, 63), (3, 64), (5, 65), (7, 127), (16, 128), (17, 129), (50, 61), (127, 40), (128, 128),
+           (129, 130), (130, 257), (257, 200), (300, 513)]
+
+
+@pytest.mark.parametrize("tq,tk", LENGTHS)
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (F16, 128)])
+def test_cross_attention_lengths(tq, tk, dtype, d):
+    check_attention(*attention_inputs(2, tq, tk, 2, 2, d, dtype, seed=tq))
+
+
+@pytest.mark.parametrize("d", [8, 16, 32, 40, 56, 64, 72, 80, 96, 120, 128])
+@pytest.mark.parametrize("tq,tk", [(1, 150), (140, 150)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_cross_attention_head_dims(d, tq, tk, dtype):
+    check_attention(*attention_inputs(2, tq, tk, 3, 3, d, dtype, seed=d))
+
+
+@pytest.mark.parametrize("h,hk", [(2, 1), (3, 1), (6, 2), (8, 1), (8, 2), (12, 4), (24, 1), (40, 1)])
+@pytest.mark.parametrize("tq,tk,d", [(1, 300, 64), (4, 129, 128), (150, 140, 64), (140, 150, 128)])
+def test_cross_attention_shared_heads(h, hk, tq, tk, d):
+    check_attention(*attention_inputs(2, tq, tk, h, hk, d, BF16, seed=h))
+
+
+@pytest.mark.parametrize("layout", ["packed", "heads"])
+@pytest.mark.parametrize("tq,tk", [(1, 200), (20, 130), (200, 333)])
+def test_cross_attention_layouts(layout, tq, tk):
+    check_attention(*attention_inputs(3, tq, tk, 4, 2, 64, BF16, seed=5, layout=layout))
+
+
+@pytest.mark.parametrize("tq,tk,d", [(1, 300, 64), (3, 70, 128), (40, 100, 64), (200, 300, 64), (300, 260, 128), (150, 270, 72)])
+def test_cross_attention_ends_empty_rows_and_what_lies_past_them(tq, tk, d):
+    """Unequal lengths, an empty sentence, a length past the end and a negative one; NaN and infinities past the ends."""
+    b, dtype = 6, BF16
+    q, k, v, do = attention_inputs(b, tq, tk, 4, 2, d, dtype, seed=9, layout="packed")
+    nk = torch.tensor([tk, 0, 1, max(1, tk - 129), tk + 7, -3], dtype=torch.int32, device="cuda")
+    nq = torch.tensor([tq, tq, max(1, tq // 2), max(1, tq - 1), tq + 9, tq], dtype=torch.int32, device="cuda")
+    if tq > 1:
+        nq[0] = 0
+    dirty = [x.clone() for x in (q, k, v, do)]
+    for i in range(b):
+        nqi, nki = min(max(int(nq[i]), 0), tq), min(max(int(nk[i]), 0), tk)
+        for x, n in ((dirty[0], nqi), (dirty[1], nki), (dirty[2], nki), (dirty[3], nqi)):
+            x[i, n:] = float("nan")
+            x[i, n::2] = float("inf")
+            x[i, n::3] = -float("inf")
+    o, lse, grads = check_attention(*dirty, nq=nq, nk=nk, clean=(q, k, v, do))
+    assert not o[1].any() and torch.isinf(lse[1]).all() and not grads[0][1].any()
+    check_attention(q, k, v, do, nk=nk)
+    check_attention(q, k, v, do, nq=nq)
+
+
+@pytest.mark.parametrize("tq", [1, 150])
+def test_cross_attention_of_nothing(tq):
+    q, k, v, do = attention_inputs(2, tq, 0, 2, 1, 64, BF16)
+    o, lse, (dq, dk, dv) = check_attention(q, k, v, do)
+    assert not o.any() and not dq.any() and dk.shape == k.shape
+    q, k, v, do = attention_inputs(2, 0, 5, 2, 1, 64, BF16)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    dq, dk, dv = ops.cross_attention_backward(do, q, k, v, o, lse)
+    assert o.numel() == 0 and not dk.any() and not dv.any()                       # no rows: the states' gradients are 0
+    q, k, v, do = attention_inputs(0, 3, 5, 2, 1, 64, BF16)
+    assert ops.cross_attention(q, k, v).numel() == 0
+
+
+@pytest.mark.parametrize("tq,tk", [(1, 500), (130, 500)])
+def test_cross_attention_large_scores(tq, tk):
+    """Scores in the thousands of either sign, and in growing order: the running maximum has to move."""
+    q, k, v, do = attention_inputs(1, tq, tk, 2, 2, 64, BF16, seed=3)
+    k = (k.float() * torch.linspace(0.1, 30, tk, device="cuda").view(1, tk, 1, 1)).to(BF16)
+    q = (q.float() * 8).to(BF16)
+    scale = 0.25                                                                  # scores up to about 10^4; a power of two
+    ref = attention_reference(q, k, v, scale, [tq], [tk], None, U[BF16])
+    o, lse = ops.cross_attention(q, k, v, scale=scale, need_lse=True)
+    # fp32 scores of that size are off by up to 2^-24 * 64 * (largest sum of |q k|), which exp turns into a relative error
+    size = (scale * torch.einsum("bqhd,bkhd->bhqk", q.double().abs(), k.double().abs())).max().item()
+    slack = 8 * 2.0 ** -24 * size
+    vmax = v.double().abs().max().item()
+    within(o, ref["o"], ref["o_b"] + 2 * slack * vmax, "o")
+    within(lse, ref["lse"], slack + E * ref["lse"].abs(), "lse")
+
+
+@pytest.mark.parametrize("tq", [1, 8, 200])
+def test_cross_attention_broadcast_states(tq):
+    """Encoder states shared by all sentences (a beam) or all heads through strides of 0."""
+    q, k, v, do = attention_inputs(1, tq, 140, 4, 2, 64, BF16, seed=4)
+    q, do = (randn(3, tq, 4, 64, dtype=BF16, seed=s) for s in (21, 22))
+    check_attention(q, k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1), do)
+    one = k[:, :, :1].expand(3, -1, 4, -1), v[:, :, :1].expand(3, -1, 4, -1)
+    o, lse, (dq, dk, dv) = check_attention(q, one[0], one[1], do)
+    assert dk.shape == (3, 140, 4, 64)
+
+
+def test_cross_attention_gradients_into_a_packed_buffer():
+    q, k, v, do = attention_inputs(2, 70, 90, 4, 2, 64, BF16, seed=6)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    want = ops.cross_attention_backward(do, q, k, v, o, lse)
+    dkv = torch.full((2, 90, 3, 2, 64), 7.0, dtype=BF16, device="cuda")
+    got = ops.cross_attention_backward(do, q, k, v, o, lse, dk=dkv[:, :, 0], dv=dkv[:, :, 2])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and (dkv[:, :, 1] == 7).all()
+    wide = torch.full((2, 70, 5, 64), 7.0, dtype=BF16, device="cuda")
+    assert torch.equal(ops.cross_attention(q, k, v, out=wide[:, :, :4]), o) and (wide[:, :, 4] == 7).all()
+
+
+@pytest.mark.parametrize("tq", [1, 130])
+def test_cross_attention_offsets_past_32_bits(tq):
+    """Two sentences whose states lie more than 2^32 bytes and 2^31 elements apart."""
+    far, tk = (1 << 31) + 4096, 200
+    store = torch.empty(far + 2 * tk * 64, dtype=BF16, device="cuda")
+    k, v = (store.as_strided((2, tk, 1, 64), (far, 64, 64, 1), at) for at in (0, tk * 64))
+    k.copy_(randn(2, tk, 1, 64, dtype=BF16, seed=1))
+    v.copy_(randn(2, tk, 1, 64, dtype=BF16, seed=2))
+    q, do = randn(2, tq, 2, 64, dtype=BF16, seed=3), randn(2, tq, 2, 64, dtype=BF16, seed=4)
+    check_attention(q, k, v, do)
+
+
+def test_cross_attention_long_states():
+    """More states than one CTA walks alone, and a length that ends inside a tile of the last part."""
+    for h, hk, d, dtype in ((4, 1, 64, BF16), (2, 2, 128, F16)):
+        q, k, v, do = attention_inputs(1, 1, 20011, h, hk, d, dtype, seed=8, layout="heads")
+        nk = torch.tensor([19999], dtype=torch.int32, device="cuda")
+        check_attention(q, k, v, do)
+        check_attention(q, k, v, do, nk=nk)
+
+
+def test_cross_attention_gradient_is_the_difference():
+    q, k, v, do = attention_inputs(1, 9, 150, 2, 1, 64, F16, seed=12)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    grads = ops.cross_attention_backward(do, q, k, v, o, lse)
+    ref = attention_reference(q, k, v, 0.125, [9], [150], do, U[F16])
+    h = 1e-4
+
+    def loss(q_, k_, v_):
+        return (attention_reference(q_, k_, v_, 0.125, [9], [150])["o"] * do.double()).sum().item()
+
+    base = [x.double() for x in (q, k, v)]
+    for at, (grad, name) in enumerate(zip(grads, ("dq", "dk", "dv"))):
+        step = randn(*grad.shape, seed=30 + at).double()
+        up, down = ([x + s * h * step if i == at else x for i, x in enumerate(base)] for s in (1, -1))
+        num = (loss(*up) - loss(*down)) / (2 * h)
+        assert abs(num - (grad.double() * step).sum().item()) <= (ref[name + "_b"] * step.abs()).sum().item() + 1e-5
+
+
+def test_operators_on_another_stream_and_in_a_graph():
+    side = torch.cuda.Stream()
+    q, k, v, do = attention_inputs(2, 140, 150, 4, 2, 64, BF16, seed=6)
+    x, r, w = randn(64, 512, dtype=BF16, seed=1), randn(64, 512, dtype=BF16, seed=2), 1 + 0.3 * randn(512, seed=3)
+
+    def everything():
+        o, lse = ops.cross_attention(q, k, v, need_lse=True)
+        y, total = ops.add_rms_norm(x, w, residual=r, rate=0.1, seed=3, event=4)
+        return [o, lse, ops.cross_attention(q[:, :1], k, v), *ops.cross_attention_backward(do, q, k, v, o, lse), y, total,
+                *ops.add_rms_norm_backward(r, total, w, dtotal=x, rate=0.1, seed=3, event=4), ops.dropout(x, 0.1, 3, 4)]
+
+    want = everything()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = everything()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = everything()
+    for t in out:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    ops.check()
+
+
+def test_refusals_of_the_tensor_checks():
+    x, w = randn(4, 64, dtype=BF16), torch.ones(64, device="cuda")
+    for bad in (lambda: ops.dropout(x, 1.5, 1, 1), lambda: ops.dropout(x, float("nan"), 1, 1), lambda: ops.dropout(x, 0.1, -1, 1),
+                lambda: ops.dropout(x, 0.1, 1, 2 ** 32), lambda: ops.dropout(x.cpu(), 0.1, 1, 1),
+                lambda: ops.dropout(x.double(), 0.1, 1, 1), lambda: ops.dropout(x, 0.1, 1, 1, residual=x.float()),
+                lambda: ops.dropout(x, 0.1, 1, 1, residual=x[:2]), lambda: ops.dropout(x.t(), 0.1, 1, 1),
+                lambda: ops.dropout(torch.zeros(4, 5, 64, device="cuda")[:, :4], 0.1, 1, 1),
+                lambda: ops.add_rms_norm(x, w.to(BF16)), lambda: ops.add_rms_norm(x, w[:60]),
+                lambda: ops.add_rms_norm(x, torch.ones(128, device="cuda")[::2]),
+                lambda: ops.add_rms_norm_backward(x, x[:3], w)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: ops.add_rms_norm(x, w, eps=-1.0), lambda: ops.add_rms_norm(x, w, eps=float("inf")),
+                lambda: ops.add_rms_norm(torch.zeros(1, 32769, device="cuda"), torch.ones(32769, device="cuda"))):
+        with pytest.raises(g.SwarmError):
+            bad()
+    q, k, v, do = attention_inputs(2, 5, 7, 4, 2, 64, BF16)
+    f = ops.cross_attention
+    for bad in (lambda: f(q.float(), k.float(), v.float()), lambda: f(q, k.half(), v), lambda: f(q, k[:1], v),
+                lambda: f(q, k, v[:, :5]), lambda: f(q[0], k, v), lambda: f(q.transpose(2, 3), k, v),
+                lambda: f(q, k, v, key_lengths=torch.zeros(2, device="cuda")),
+                lambda: f(q, k, v, key_lengths=torch.zeros(3, dtype=torch.int32, device="cuda")),
+                lambda: f(q.cpu(), k, v), lambda: f(q, k, v, out=torch.empty(2, 5, 4, 32, dtype=BF16, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    off = torch.zeros(2 * 7 * 2 * 64 + 8, dtype=BF16, device="cuda")[1:1 + 2 * 7 * 2 * 64].view(2, 7, 2, 64)
+    for bad in (lambda: f(q, off, v), lambda: f(q, k, v, scale=0.0), lambda: f(q, k, v, scale=float("nan")),
+                lambda: f(q[:, :, :3], k, v), lambda: f(q[..., :60].contiguous(), k[..., :60].contiguous(), v[..., :60].contiguous()),
+                lambda: f(randn(1, 2, 1, 136, dtype=BF16), randn(1, 2, 1, 136, dtype=BF16), randn(1, 2, 1, 136, dtype=BF16)),
+                lambda: f(q, k, v, out=torch.empty(1, 5, 4, 64, dtype=BF16, device="cuda").expand(2, -1, -1, -1))):
+        with pytest.raises(g.SwarmError):
+            bad()
+    torch.cuda.synchronize()
