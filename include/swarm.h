@@ -411,7 +411,7 @@ typedef struct {
   float scale;                                               /* > 0, finite                                 */
   int64_t wait_limit;            /* polls after which a device-side wait gives up; < 0: the default; 0: at once  */
   const int32_t *query_lengths_dev, *key_lengths_dev;        /* [batch], clamped to [0, queries / keys]; NULL: all */
-  swarm_strides q, k, v, o;      /* multiples of 8, >= 0; those of q, k, v may be 0 (a broadcast dimension)      */
+  swarm_strides q, k, v, o;      /* multiples of 8, > 0; inputs may repeat their sentences or heads by strides of 0 */
   swarm_strides dout, dq, dk, dv;                            /* read by the backward call only                   */
 } swarm_attention;
 

@@ -7,31 +7,31 @@
 #include <cmath>
 #include <mutex>
 
-#include "swarm_opsup.cuh"
+#include "swarm_attention.h"
 
 namespace swarm {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxDevices = 64;
+static __device__ int g_operator_status;               // raised by a kernel of this device whose wait gave up
+int* g_status_addr[kMaxDevices] = {};
+std::mutex g_setup_mutex;
 
-struct AttentionArgs {
-  const void *q, *k, *v, *o, *dout;
-  const float* lse_in;
-  void *out, *dq, *dk, *dv;
-  float* lse;
-  float* delta;                       // [batch][heads][queries] rowsum(dout * o)
-  const int32_t *query_lengths, *key_lengths;
-  swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;
-  int32_t batch, heads, kv_heads, group, queries, keys, head_dim;
-  float scale;
-};
-
-__device__ __forceinline__ int length_of(const int32_t* lengths, int b, int most) {
-  return lengths ? min(max(lengths[b], 0), most) : most;
-}
-
-__device__ __forceinline__ int64_t offset_of(const swarm_strides& s, int b, int t, int h) {
-  return b * s.batch + t * s.token + h * s.head;
+// Device address of the status word of the current device.
+cudaError_t status_word(int** out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_setup_mutex);
+  if (!g_status_addr[dev]) {
+    void* p = nullptr;
+    e = cudaGetSymbolAddress(&p, g_operator_status);
+    if (e != cudaSuccess) return e;
+    g_status_addr[dev] = (int*)p;
+  }
+  *out = g_status_addr[dev];
+  return cudaSuccess;
 }
 
 template <typename T>
@@ -45,8 +45,6 @@ __device__ __forceinline__ float dot_row(const float* a, const T* p, int dim) {
   }
   return s;
 }
-
-constexpr int kMaxDim = 128;
 
 // Warp = one query row; lane = one state of 32 at a time for the scores, then dims lane, lane + 32, ... of the output.
 template <typename T>
@@ -182,13 +180,13 @@ bool desc_ok(const swarm_attention* d) {
          d->head_dim % 8 == 0 && (d->dtype == SWARM_BF16 || d->dtype == SWARM_F16) && d->scale > 0.0f && std::isfinite(d->scale);
 }
 constexpr int64_t kMaxStride = (int64_t)1 << 38;
-bool one_stride_ok(int64_t s, int extent, bool output) {
-  return extent <= 1 || (s >= 0 && s < kMaxStride && s % 8 == 0 && !(output && s == 0));
+bool one_stride_ok(int64_t s, int extent, bool repeats) {
+  return extent <= 1 || (s >= 0 && s < kMaxStride && s % 8 == 0 && (repeats || s != 0));
 }
-// A tensor of `tokens` rows and `heads` heads: address and strides; an output may not repeat a dimension.
+// A tensor of `tokens` rows and `heads` heads: address and strides; an input may repeat its sentences or heads.
 bool strided_ok(const void* p, const swarm_strides& s, int batch, int tokens, int heads, bool output) {
-  return p && ((uintptr_t)p & 15) == 0 && one_stride_ok(s.batch, batch, output) && one_stride_ok(s.token, tokens, output) &&
-         one_stride_ok(s.head, heads, output);
+  return p && ((uintptr_t)p & 15) == 0 && one_stride_ok(s.batch, batch, !output) && one_stride_ok(s.token, tokens, false) &&
+         one_stride_ok(s.head, heads, !output);
 }
 bool lengths_ok(const int32_t* p) { return ((uintptr_t)p & 3) == 0; }
 
@@ -198,6 +196,7 @@ void fill(AttentionArgs& a, const swarm_attention* d) {
   a.batch = d->batch; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads;
   a.queries = d->queries; a.keys = d->keys; a.head_dim = d->head_dim;
   a.scale = d->scale;
+  a.wait_limit = d->wait_limit < 0 ? kAttentionWaitLimit : d->wait_limit < (int64_t)1 << 32 ? (uint32_t)d->wait_limit : 0xFFFFFFFFu;
 }
 
 }  // namespace
@@ -229,6 +228,9 @@ int swarm_cross_attention(const swarm_attention* desc_host, const void* q_dev, c
   fill(a, desc_host);
   a.q = q_dev; a.k = k_dev; a.v = v_dev; a.out = o_dev; a.lse = lse_dev;
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return operator_result(e);
+  if ((int64_t)d.queries * a.group > 16 && d.keys > 0) return operator_result(launch_attention_forward_tc(a, d.dtype, st));
   const dim3 grid((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
   if (d.dtype == SWARM_BF16) attention_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
   else attention_rows_kernel<__half><<<grid, 128, 0, st>>>(a);
@@ -274,6 +276,18 @@ int swarm_cross_attention_backward(const swarm_attention* desc_host, const void*
   return operator_result(cudaGetLastError());
 }
 
-int swarm_operator_check(void* cuda_stream) { return operator_result(cudaStreamSynchronize((cudaStream_t)cuda_stream)); }
+int swarm_operator_check(void* cuda_stream) {
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  int *word = nullptr, raised = 0;
+  cudaError_t e = status_word(&word);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(&raised, word, sizeof raised, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && raised) {
+    e = cudaMemsetAsync(word, 0, sizeof raised, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess) e = cudaErrorLaunchTimeout;
+  }
+  return operator_result(e);
+}
 
 }  // extern "C"

@@ -1,0 +1,47 @@
+// The attention kernels as the C entry points launch them.
+#pragma once
+#include <cuda.h>
+
+#include "swarm_opsup.cuh"
+
+namespace swarm {
+
+constexpr int kMaxDim = 128;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kAttentionWaitLimit = 1u << 22;     // default polls of a device-side wait
+
+struct AttentionArgs {
+  const void *q, *k, *v, *o, *dout;
+  const float* lse_in;
+  void *out, *dq, *dk, *dv;
+  float* lse;
+  float* delta;                       // [batch][heads][queries] rowsum(dout * o)
+  const int32_t *query_lengths, *key_lengths;
+  swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;
+  int32_t batch, heads, kv_heads, group, queries, keys, head_dim;
+  float scale;
+  uint32_t wait_limit;
+  int* status;                        // raised when a device-side wait gives up
+};
+
+__device__ __forceinline__ int length_of(const int32_t* lengths, int b, int most) {
+  return lengths ? min(max(lengths[b], 0), most) : most;
+}
+
+__device__ __forceinline__ int64_t offset_of(const swarm_strides& s, int b, int t, int h) {
+  return b * s.batch + t * s.token + h * s.head;
+}
+
+// A strided tensor as tiles of 128 rows x 64 values of one head: coordinates (value, token, head, sentence), rows and
+// values past the ends read as zero and are not written. A broadcast dimension (stride 0) has extent 1 in the map and
+// its coordinate is multiplied by 0.
+struct TileMap {
+  CUtensorMap map;
+  int32_t token_step, head_step, batch_step;
+};
+cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, int dtype, int batch, int tokens, int heads,
+                          int head_dim);
+
+cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
+
+}  // namespace swarm

@@ -1,0 +1,370 @@
+// Cross attention, forward pass on the tensor cores (many query rows).
+#include <mutex>
+
+#include "swarm_attention.h"
+#include "swarm_tc.cuh"
+
+namespace swarm {
+namespace {
+
+constexpr int kTile = 128;                              // query rows and states of a tile
+constexpr int kBlockBytes = kTile * 128;                // 128 rows x 64 values, 128-byte swizzle
+constexpr int kFwdThreads = 320;                        // two softmax warpgroups, the copying warp, the issuing warp
+
+template <int DB> constexpr int kFwdStages = DB == 2 ? 4 : 6;
+template <int DB> constexpr int kFwdSmem = (2 + kFwdStages<DB>) * DB * kBlockBytes + 1024;
+
+struct FwdBars {
+  uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], p_full[2], o_full[2], drain;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Shared-memory address of 16 bytes (8 values) of a row in a swizzled block.
+__device__ __forceinline__ uint32_t swizzled(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
+
+// Zeroes rows [first, last) of a tile of DB blocks; called by one warp. The rows are in an operand of a product whose
+// other factor is 0 there, and hold whatever lies past a sentence's end.
+template <int DB>
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last, int lane) {
+  for (int i = lane; i < (last - first) * 8 * DB; i += 32) {
+    const int row = first + i / (8 * DB), c = i % (8 * DB);
+    *reinterpret_cast<uint4*>(tile + (c >> 3) * kBlockBytes + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async();
+  __syncwarp();
+}
+
+template <typename T, int DB>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
+                         const __grid_constant__ TileMap mo, AttentionArgs a, int row_tiles, int pairs) {
+  constexpr int kStages = kFwdStages<DB>;
+  constexpr uint32_t kTileBytes = DB * kBlockBytes;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* sQ = smem;                                   // two tiles
+  uint8_t* sKV = smem + 2 * kTileBytes;                 // ring of K, V tiles
+  __shared__ FwdBars bars;
+  __shared__ uint32_t tmem_slot;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  // the pair of row tiles of this CTA: tiles are numbered head after head within the group of a key head
+  const int pair = blockIdx.x % pairs, bh = blockIdx.x / pairs, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  const int n = (nk + kTile - 1) / kTile;
+  int head[2], row0[2];
+  bool active[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int tile = pair * 2 + t;
+    head[t] = hk * a.group + tile / row_tiles;
+    row0[t] = tile % row_tiles * kTile;
+    active[t] = tile < row_tiles * a.group && row0[t] < nq && n > 0;
+  }
+  const bool any = active[0] || active[1];
+
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars.q_full[i]), 1);
+      mbar_init(smem_u32(&bars.s_full[i]), 1);
+      mbar_init(smem_u32(&bars.p_full[i]), 4);
+      mbar_init(smem_u32(&bars.o_full[i]), 1);
+    }
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_u32(&bars.kv_full[i]), 1);
+      mbar_init(smem_u32(&bars.kv_empty[i]), 1);
+    }
+    mbar_init(smem_u32(&bars.drain), 1);
+    fence_mbar_init();
+  }
+  if (warp == 9) { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;                      // columns: scores of tile t at 128 t (its weights over them), o at 256 + 128 t
+  const uint32_t limit = a.wait_limit;
+  bool ok = true;
+
+  if (warp == 8) {
+    // ---- copies -------------------------------------------------------------------------------
+    if (any) {
+      int issued = 0;
+      if (lane == 0) { tma_prefetch_map(&mk.map); tma_prefetch_map(&mv.map); }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (active[t] && limit && lane == 0) {
+          const uint32_t bar = smem_u32(&bars.q_full[t]);
+          mbar_expect_tx(bar, kTileBytes);
+          for (int d = 0; d < DB; ++d)
+            tma_load_4d(smem_u32(sQ) + t * kTileBytes + d * kBlockBytes, &mq.map, d * 64, row0[t] * mq.token_step, head[t] * mq.head_step,
+                        b * mq.batch_step, bar);
+        }
+      for (int f = 0; f < 2 * n; ++f) {                 // K of tile 0, V of tile 0, K of tile 1, ...
+        const int st = f % kStages;
+        ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((f / kStages) & 1) ^ 1, limit);
+        if (!ok) break;
+        if (lane == 0) {
+          const TileMap& m = f & 1 ? mv : mk;
+          const uint32_t bar = smem_u32(&bars.kv_full[st]);
+          mbar_expect_tx(bar, kTileBytes);
+          for (int d = 0; d < DB; ++d)
+            tma_load_4d(smem_u32(sKV) + st * kTileBytes + d * kBlockBytes, &m.map, d * 64, (f >> 1) * kTile * m.token_step, hk * m.head_step,
+                        b * m.batch_step, bar);
+        }
+        issued = f + 1;
+      }
+      if (!ok) {
+        // gave up: the copies in flight land before the CTA's shared memory is released
+        for (int f = issued > kStages ? issued - kStages : 0; f < issued; ++f)
+          mbar_wait(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
+        for (int t = 0; t < 2; ++t)
+          if (active[t] && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
+      }
+    }
+  } else if (warp == 9) {
+    // ---- products -----------------------------------------------------------------------------
+    if (any) {
+      const int ksteps = (a.head_dim + 15) / 16;
+      constexpr uint32_t kIdescPV = instr_desc_16<T>(kTile, DB * 64, 0, 1);
+      const uint64_t dq0 = smem_desc_sw128(smem_u32(sQ), 16, 1024), dk0 = smem_desc_sw128(smem_u32(sKV), 16, 1024);
+      const uint64_t dv0 = smem_desc_sw128(smem_u32(sKV), kBlockBytes, 1024);
+      auto scores = [&](int t, int j) {                 // S_t = Q_t K_j^T
+        const int valid = min(kTile, nk - j * kTile), cols = (valid + 15) & ~15;
+        const uint32_t idesc = instr_desc_16<T>(kTile, kTile, 0, 0) - ((uint32_t)(kTile >> 3) << 17) + ((uint32_t)(cols >> 3) << 17);
+        const uint64_t dk = dk0 + (uint64_t)((((2 * j) % kStages) * kTileBytes) >> 4), dq = dq0 + (uint64_t)((t * kTileBytes) >> 4);
+        for (int ks = 0; ks < ksteps; ++ks) {
+          const uint64_t at = (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4);
+          tc_mma(tmem + 128 * t, dq + at, dk + at, idesc, ks != 0);
+        }
+        tc_commit(smem_u32(&bars.s_full[t]));
+      };
+      ok = mbar_wait(smem_u32(&bars.kv_full[0]), 0, limit);
+      for (int t = 0; t < 2 && ok; ++t)
+        if (active[t]) {
+          ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
+          tc_fence_after();
+          if (ok && lane == 0) scores(t, 0);
+        }
+      if (ok && lane == 0) tc_commit(smem_u32(&bars.kv_empty[0]));
+      for (int j = 0; j < n && ok; ++j) {
+        const int fv = 2 * j + 1, sv = fv % kStages, fk = 2 * j + 2;
+        const int valid = min(kTile, nk - j * kTile), rows = (valid + 15) & ~15;
+        ok = mbar_wait(smem_u32(&bars.kv_full[sv]), (fv / kStages) & 1, limit);
+        if (!ok) break;
+        if (valid < rows) zero_rows<DB>(sKV + sv * kTileBytes, valid, rows, lane);
+        for (int t = 0; t < 2 && ok; ++t)
+          if (active[t]) {
+            ok = mbar_wait(smem_u32(&bars.p_full[t]), j & 1, limit);
+            if (!ok) break;
+            tc_fence_after();
+            if (lane == 0) {
+              const uint64_t dv = dv0 + (uint64_t)((sv * kTileBytes) >> 4);
+              for (int ks = 0; ks < rows / 16; ++ks)
+                tc_mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + ks * 8, dv + (uint64_t)((ks * 2048) >> 4), kIdescPV, (j | ks) != 0);
+              if (j == n - 1) tc_commit(smem_u32(&bars.o_full[t]));
+            }
+            __syncwarp();
+            if (j + 1 < n) {
+              ok = mbar_wait(smem_u32(&bars.kv_full[fk % kStages]), (fk / kStages) & 1, limit);
+              tc_fence_after();
+              if (ok && lane == 0) scores(t, j + 1);
+            }
+          }
+        if (ok && lane == 0) {
+          tc_commit(smem_u32(&bars.kv_empty[sv]));
+          if (j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[fk % kStages]));
+        }
+        __syncwarp();
+      }
+      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
+        if (lane == 0) tc_commit(smem_u32(&bars.drain));
+        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
+      }
+    }
+  } else {
+    // ---- softmax ------------------------------------------------------------------------------
+    const int t = warp >> 2, quad = warp & 3;
+    const int row = row0[t] + quad * 32 + lane;         // this thread's query row
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t ts = tmem + 128 * t + lane_base, to = tmem + 256 + 128 * t + lane_base;
+    const float c = a.scale * kLog2e;
+    float m = 0.0f, l = 0.0f;                           // m: the maximum that the weights are taken against
+    if (active[t]) {
+      m = -INFINITY;
+      for (int j = 0; j < n; ++j) {
+        ok = mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+        const int valid = nk - j * kTile;
+        float s[kTile];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, s + g * 32);
+        tmem_wait_ld();
+        if (valid < kTile) {
+#pragma unroll
+          for (int i = 0; i < kTile; ++i) s[i] = i < valid ? s[i] : -INFINITY;
+        }
+        float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int i = 4; i < kTile; i += 4) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], s[i + u]);
+        }
+        const float m_tile = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        if (j == 0) m = m_tile;
+        else if (__any_sync(0xFFFFFFFFu, (m_tile - m) * c > 8.0f)) {
+          // the maximum moved by more than a factor of 2^8 in some row of the warp: rescale the sums so far. Smaller
+          // moves keep the old reference; the weights then reach 2^8, which fp32 sums and 16-bit weights hold as well.
+          const float m_new = fmaxf(m, m_tile), f = m_new == m ? 1.0f : ex2((m - m_new) * c);
+          l *= f;
+          m = m_new;
+#pragma unroll
+          for (int g = 0; g < DB * 2; ++g) {
+            float o[32];
+            tmem_ld32(to + g * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= f;
+            tmem_st32(to + g * 32, o);
+          }
+        }
+        const float mc = m == -INFINITY ? 0.0f : m * c;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float p0 = ex2(fmaf(s[g * 32 + 2 * i], c, -mc)), p1 = ex2(fmaf(s[g * 32 + 2 * i + 1], c, -mc));
+            sum[i & 1] += p0;
+            sum[2 + (i & 1)] += p1;
+            p[i] = pack2<T>(p0, p1);
+          }
+          tmem_st16(ts + g * 16, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[t]));
+      }
+      if (ok) {
+        ok = mbar_wait(smem_u32(&bars.o_full[t]), 0, limit);
+        tc_fence_after();
+      }
+    }
+    // ---- output -------------------------------------------------------------------------------
+    const bool exists = pair * 2 + t < row_tiles * a.group;
+    if (exists && named_barrier_and(1 + t, 128, ok)) {
+      const bool live = active[t] && row < nq;
+      const float inv = live && l != 0.0f ? 1.0f / l : 0.0f;
+      uint8_t* out = sQ + t * kTileBytes;               // the query tile has been read by now
+#pragma unroll
+      for (int g = 0; g < DB * 2; ++g) {
+        float o[32];
+        if (active[t]) { tmem_ld32(to + g * 32, o); tmem_wait_ld(); }
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            w[u] = live ? pack2<T>(o[ch * 8 + 2 * u] * inv, o[ch * 8 + 2 * u + 1] * inv) : 0u;
+          *reinterpret_cast<uint4*>(out + (g >> 1) * kBlockBytes + swizzled(quad * 32 + lane, (g & 1) * 4 + ch)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      if (a.lse && row < a.queries)
+        a.lse[((int64_t)b * a.heads + head[t]) * a.queries + row] = live ? m * a.scale + logf(l) : -INFINITY;
+      fence_proxy_async();
+      named_barrier(1 + t, 128);
+      if ((warp & 3) == 0 && lane == 0) {
+        for (int d = 0; d < DB; ++d)
+          tma_store_4d(&mo.map, smem_u32(out) + d * kBlockBytes, d * 64, row0[t] * mo.token_step, head[t] * mo.head_step, b * mo.batch_step);
+        bulk_commit();
+        bulk_wait_read();
+      }
+    }
+  }
+  if (!ok && lane == 0) atomicExch(a.status, 1);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+template <typename T, int DB>
+cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const TileMap& mk, const TileMap& mv, const TileMap& mo, cudaStream_t st) {
+  static bool attr_set[64] = {};
+  static std::mutex attr_mutex;
+  {
+    std::lock_guard<std::mutex> lock(attr_mutex);
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!attr_set[dev]) {
+      const cudaError_t e = cudaFuncSetAttribute(attention_forward_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFwdSmem<DB>);
+      if (e != cudaSuccess) return e;
+      attr_set[dev] = true;
+    }
+  }
+  const int row_tiles = (a.queries + kTile - 1) / kTile, pairs = (int)(((int64_t)row_tiles * a.group + 1) / 2);
+  const int64_t ctas = (int64_t)pairs * a.kv_heads * a.batch;
+  attention_forward_kernel<T, DB><<<(unsigned)ctas, kFwdThreads, kFwdSmem<DB>, st>>>(mq, mk, mv, mo, a, row_tiles, pairs);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, int dtype, int batch, int tokens, int heads,
+                          int head_dim) {
+  typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static encode_fn encode = nullptr;
+  static std::mutex mutex;
+  {
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!encode) {
+      void* f = nullptr;
+      cudaDriverEntryPointQueryResult found;
+      const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+      if (e != cudaSuccess) return e;
+      if (found != cudaDriverEntryPointSuccess || !f) return cudaErrorNotSupported;
+      encode = (encode_fn)f;
+    }
+  }
+  const int64_t stride[3] = {s.token, s.head, s.batch};
+  const int extent[3] = {tokens, heads, batch};
+  int32_t* step[3] = {&out->token_step, &out->head_step, &out->batch_step};
+  cuuint64_t dims[4] = {(cuuint64_t)head_dim, 1, 1, 1}, bytes[3] = {16, 16, 16};
+  for (int i = 0; i < 3; ++i) {
+    *step[i] = 0;
+    if (extent[i] > 1 && stride[i] != 0) {
+      dims[i + 1] = (cuuint64_t)extent[i];
+      bytes[i] = (cuuint64_t)stride[i] * 2;
+      *step[i] = 1;
+    }
+  }
+  const cuuint32_t box[4] = {64, (cuuint32_t)kTile, 1, 1}, ones[4] = {1, 1, 1, 1};
+  const CUresult r = encode(&out->map, dtype == SWARM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                            const_cast<void*>(p), dims, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st) {
+  TileMap mq, mk, mv, mo;
+  cudaError_t e = make_tile_map(&mq, a.q, a.qs, dtype, a.batch, a.queries, a.heads, a.head_dim);
+  if (e == cudaSuccess) e = make_tile_map(&mo, a.out, a.os, dtype, a.batch, a.queries, a.heads, a.head_dim);
+  if (e == cudaSuccess) e = make_tile_map(&mk, a.k, a.ks, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
+  if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
+  if (e != cudaSuccess) return e;
+  if (dtype == SWARM_BF16)
+    return a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1>(a, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2>(a, mq, mk, mv, mo, st);
+  return a.head_dim <= 64 ? launch_forward<__half, 1>(a, mq, mk, mv, mo, st) : launch_forward<__half, 2>(a, mq, mk, mv, mo, st);
+}
+
+}  // namespace swarm
