@@ -85,92 +85,22 @@ __global__ void __launch_bounds__(128) attention_rows_kernel(AttentionArgs a) {
   if (a.lse && lane == 0) a.lse[((int64_t)b * a.heads + h) * a.queries + t] = n ? m + logf(l) : -INFINITY;
 }
 
-// Warp = one query row: delta, then dq.
-template <typename T>
-__global__ void __launch_bounds__(128) attention_dq_kernel(AttentionArgs a) {
-  __shared__ float sq[4][kMaxDim], sd[4][kMaxDim];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t = blockIdx.x * 4 + warp, h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
-  if (t >= a.queries) return;
-  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const int n = t < nq ? nk : 0;
-  const int64_t at = ((int64_t)b * a.heads + h) * a.queries + t;
-  float delta = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  if (n) {
-    const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h);
-    const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t, h);
-    const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, t, h);
-    for (int d = lane; d < a.head_dim; d += 32) {
-      sq[warp][d] = to_float<T>(q[d]);
-      sd[warp][d] = to_float<T>(g[d]);
-      delta = fmaf(to_float<T>(g[d]), to_float<T>(o[d]), delta);
-    }
-    __syncwarp();
-    delta = warp_sum(delta);
-    const float lse = a.lse_in[at];
-    for (int j0 = 0; j0 < n; j0 += 32) {
-      const int j = min(j0 + lane, n - 1);
-      const float s = a.scale * dot_row<T>(sq[warp], reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk), a.head_dim);
-      const float dp = dot_row<T>(sd[warp], reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j, hk), a.head_dim);
-      const float ds = a.scale * exp2f((s - lse) * kLog2e) * (dp - delta);
-      for (int u = 0; u < min(32, n - j0); ++u) {
-        const float du = __shfl_sync(0xFFFFFFFFu, ds, u);
-        const T* k = reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j0 + u, hk);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (lane + 32 * i < a.head_dim) acc[i] = fmaf(du, to_float<T>(k[lane + 32 * i]), acc[i]);
-      }
-    }
+// Zeros into a strided tensor: the outputs of a call that has no rows or no states to sum over.
+__global__ void __launch_bounds__(256) attention_zero_kernel(uint4* p, swarm_strides s, int tokens, int heads, int chunks) {
+  const int b = blockIdx.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)tokens * heads * chunks; i += (int64_t)gridDim.x * 256) {
+    const int ch = (int)(i % chunks), h = (int)(i / chunks % heads), t = (int)(i / chunks / heads);
+    p[offset_of(s, b, t, h) / 8 + ch] = make_uint4(0, 0, 0, 0);
   }
-  if (lane == 0) a.delta[at] = delta;
-  T* dq = reinterpret_cast<T*>(a.dq) + offset_of(a.dqs, b, t, h);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < a.head_dim) dq[lane + 32 * i] = from_float<T>(acc[i]);
 }
-
-// Warp = one state of one key head: dk and dv over the rows of its query heads.
-template <typename T>
-__global__ void __launch_bounds__(128) attention_dkv_kernel(AttentionArgs a) {
-  __shared__ float sk[4][kMaxDim], sv[4][kMaxDim];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int j = blockIdx.x * 4 + warp, hk = blockIdx.y, b = blockIdx.z;
-  if (j >= a.keys) return;
-  const int nk = length_of(a.key_lengths, b, a.keys);
-  const int n = j < nk ? length_of(a.query_lengths, b, a.queries) : 0;
-  float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-  if (n) {
-    const T* k = reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk);
-    const T* v = reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j, hk);
-    for (int d = lane; d < a.head_dim; d += 32) { sk[warp][d] = to_float<T>(k[d]); sv[warp][d] = to_float<T>(v[d]); }
-    __syncwarp();
-  }
-  for (int g = 0; g < a.group; ++g) {
-    const int h = hk * a.group + g;
-    const int64_t at = ((int64_t)b * a.heads + h) * a.queries;
-    for (int t0 = 0; t0 < n; t0 += 32) {
-      const int t = min(t0 + lane, n - 1);
-      const float s = a.scale * dot_row<T>(sk[warp], reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h), a.head_dim);
-      const float dp = dot_row<T>(sv[warp], reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t, h), a.head_dim);
-      const float p = exp2f((s - a.lse_in[at + t]) * kLog2e), ds = a.scale * p * (dp - a.delta[at + t]);
-      for (int u = 0; u < min(32, n - t0); ++u) {
-        const float pu = __shfl_sync(0xFFFFFFFFu, p, u), du = __shfl_sync(0xFFFFFFFFu, ds, u);
-        const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t0 + u, h);
-        const T* d_ = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t0 + u, h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (lane + 32 * i < a.head_dim) {
-            dk[i] = fmaf(du, to_float<T>(q[lane + 32 * i]), dk[i]);
-            dv[i] = fmaf(pu, to_float<T>(d_[lane + 32 * i]), dv[i]);
-          }
-      }
-    }
-  }
-  T* pk = reinterpret_cast<T*>(a.dk) + offset_of(a.dks, b, j, hk);
-  T* pv = reinterpret_cast<T*>(a.dv) + offset_of(a.dvs, b, j, hk);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < a.head_dim) { pk[lane + 32 * i] = from_float<T>(dk[i]); pv[lane + 32 * i] = from_float<T>(dv[i]); }
+__global__ void __launch_bounds__(256) attention_no_states_kernel(float* lse, int64_t count) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) lse[i] = -INFINITY;
+}
+cudaError_t launch_zero(void* p, const swarm_strides& s, int batch, int tokens, int heads, int head_dim, cudaStream_t st) {
+  const int64_t count = (int64_t)tokens * heads * (head_dim / 8);
+  const unsigned x = (unsigned)(count < 256 * 1024 ? (count + 255) / 256 : 1024);
+  attention_zero_kernel<<<dim3(x, (unsigned)batch), 256, 0, st>>>(reinterpret_cast<uint4*>(p), s, tokens, heads, head_dim / 8);
+  return cudaGetLastError();
 }
 
 // ---- argument checks ------------------------------------------------------------------------
@@ -230,7 +160,14 @@ int swarm_cross_attention(const swarm_attention* desc_host, const void* q_dev, c
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = status_word(&a.status);
   if (e != cudaSuccess) return operator_result(e);
-  if ((int64_t)d.queries * a.group > 16 && d.keys > 0) return operator_result(launch_attention_forward_tc(a, d.dtype, st));
+  if (d.keys == 0) {
+    if (lse_dev) {
+      const int64_t count = (int64_t)d.batch * d.heads * d.queries;
+      attention_no_states_kernel<<<(unsigned)(count < 256 * 1024 ? (count + 255) / 256 : 1024), 256, 0, st>>>(lse_dev, count);
+    }
+    return operator_result(launch_zero(o_dev, d.o, d.batch, d.queries, d.heads, d.head_dim, st));
+  }
+  if ((int64_t)d.queries * a.group > 16) return operator_result(launch_attention_forward_tc(a, d.dtype, st));
   const dim3 grid((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
   if (d.dtype == SWARM_BF16) attention_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
   else attention_rows_kernel<__half><<<grid, 128, 0, st>>>(a);
@@ -263,17 +200,16 @@ int swarm_cross_attention_backward(const swarm_attention* desc_host, const void*
   a.q = q_dev; a.k = k_dev; a.v = v_dev; a.o = o_dev; a.dout = dout_dev; a.lse_in = lse_dev;
   a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev; a.delta = reinterpret_cast<float*>(workspace_dev);
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const dim3 gq((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
-  const dim3 gk((unsigned)((d.keys + 3) / 4), (unsigned)d.kv_heads, (unsigned)d.batch);
-  if (d.queries > 0) {
-    if (d.dtype == SWARM_BF16) attention_dq_kernel<__nv_bfloat16><<<gq, 128, 0, st>>>(a);
-    else attention_dq_kernel<__half><<<gq, 128, 0, st>>>(a);
+  cudaError_t e = status_word(&a.status);
+  if (d.queries > 0 && d.keys > 0) {
+    if (e == cudaSuccess) e = launch_attention_backward_tc(a, d.dtype, st);
+  } else if (d.queries > 0) {
+    if (e == cudaSuccess) e = launch_zero(dq_dev, d.dq, d.batch, d.queries, d.heads, d.head_dim, st);
+  } else if (d.keys > 0) {
+    if (e == cudaSuccess) e = launch_zero(dk_dev, d.dk, d.batch, d.keys, d.kv_heads, d.head_dim, st);
+    if (e == cudaSuccess) e = launch_zero(dv_dev, d.dv, d.batch, d.keys, d.kv_heads, d.head_dim, st);
   }
-  if (d.keys > 0) {
-    if (d.dtype == SWARM_BF16) attention_dkv_kernel<__nv_bfloat16><<<gk, 128, 0, st>>>(a);
-    else attention_dkv_kernel<__half><<<gk, 128, 0, st>>>(a);
-  }
-  return operator_result(cudaGetLastError());
+  return operator_result(e);
 }
 
 int swarm_operator_check(void* cuda_stream) {

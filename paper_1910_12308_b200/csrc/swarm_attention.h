@@ -43,5 +43,6 @@ cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, i
                           int head_dim);
 
 cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
+cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
 
 }  // namespace swarm

@@ -1,14 +1,11 @@
 // Cross attention, forward pass on the tensor cores (many query rows).
 #include <mutex>
 
-#include "swarm_attention.h"
-#include "swarm_tc.cuh"
+#include "swarm_attention_tile.cuh"
 
 namespace swarm {
 namespace {
 
-constexpr int kTile = 128;                              // query rows and states of a tile
-constexpr int kBlockBytes = kTile * 128;                // 128 rows x 64 values, 128-byte swizzle
 constexpr int kFwdThreads = 320;                        // two softmax warpgroups, the copying warp, the issuing warp
 
 template <int DB> constexpr int kFwdStages = DB == 2 ? 4 : 6;
@@ -17,27 +14,6 @@ template <int DB> constexpr int kFwdSmem = (2 + kFwdStages<DB>) * DB * kBlockByt
 struct FwdBars {
   uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], p_full[2], o_full[2], drain;
 };
-
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-// Shared-memory address of 16 bytes (8 values) of a row in a swizzled block.
-__device__ __forceinline__ uint32_t swizzled(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
-
-// Zeroes rows [first, last) of a tile of DB blocks; called by one warp. The rows are in an operand of a product whose
-// other factor is 0 there, and hold whatever lies past a sentence's end.
-template <int DB>
-__device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last, int lane) {
-  for (int i = lane; i < (last - first) * 8 * DB; i += 32) {
-    const int row = first + i / (8 * DB), c = i % (8 * DB);
-    *reinterpret_cast<uint4*>(tile + (c >> 3) * kBlockBytes + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-  }
-  fence_proxy_async();
-  __syncwarp();
-}
 
 template <typename T, int DB>
 __global__ void __launch_bounds__(kFwdThreads, 1)
@@ -100,21 +76,16 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         if (active[t] && limit && lane == 0) {
           const uint32_t bar = smem_u32(&bars.q_full[t]);
           mbar_expect_tx(bar, kTileBytes);
-          for (int d = 0; d < DB; ++d)
-            tma_load_4d(smem_u32(sQ) + t * kTileBytes + d * kBlockBytes, &mq.map, d * 64, row0[t] * mq.token_step, head[t] * mq.head_step,
-                        b * mq.batch_step, bar);
+          load_tile<DB>(smem_u32(sQ) + t * kTileBytes, mq, row0[t], head[t], b, bar);
         }
       for (int f = 0; f < 2 * n; ++f) {                 // K of tile 0, V of tile 0, K of tile 1, ...
         const int st = f % kStages;
         ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((f / kStages) & 1) ^ 1, limit);
         if (!ok) break;
         if (lane == 0) {
-          const TileMap& m = f & 1 ? mv : mk;
           const uint32_t bar = smem_u32(&bars.kv_full[st]);
           mbar_expect_tx(bar, kTileBytes);
-          for (int d = 0; d < DB; ++d)
-            tma_load_4d(smem_u32(sKV) + st * kTileBytes + d * kBlockBytes, &m.map, d * 64, (f >> 1) * kTile * m.token_step, hk * m.head_step,
-                        b * m.batch_step, bar);
+          load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (f >> 1) * kTile, hk, b, bar);
         }
         issued = f + 1;
       }
@@ -131,16 +102,10 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
     if (any) {
       const int ksteps = (a.head_dim + 15) / 16;
       constexpr uint32_t kIdescPV = instr_desc_16<T>(kTile, DB * 64, 0, 1);
-      const uint64_t dq0 = smem_desc_sw128(smem_u32(sQ), 16, 1024), dk0 = smem_desc_sw128(smem_u32(sKV), 16, 1024);
       const uint64_t dv0 = smem_desc_sw128(smem_u32(sKV), kBlockBytes, 1024);
       auto scores = [&](int t, int j) {                 // S_t = Q_t K_j^T
-        const int valid = min(kTile, nk - j * kTile), cols = (valid + 15) & ~15;
-        const uint32_t idesc = instr_desc_16<T>(kTile, kTile, 0, 0) - ((uint32_t)(kTile >> 3) << 17) + ((uint32_t)(cols >> 3) << 17);
-        const uint64_t dk = dk0 + (uint64_t)((((2 * j) % kStages) * kTileBytes) >> 4), dq = dq0 + (uint64_t)((t * kTileBytes) >> 4);
-        for (int ks = 0; ks < ksteps; ++ks) {
-          const uint64_t at = (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4);
-          tc_mma(tmem + 128 * t, dq + at, dk + at, idesc, ks != 0);
-        }
+        mma_rows<T>(tmem + 128 * t, smem_u32(sQ) + t * kTileBytes, smem_u32(sKV) + (2 * j) % kStages * kTileBytes,
+                    (min(kTile, nk - j * kTile) + 15) & ~15, ksteps);
         tc_commit(smem_u32(&bars.s_full[t]));
       };
       ok = mbar_wait(smem_u32(&bars.kv_full[0]), 0, limit);
@@ -233,7 +198,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
             tmem_st32(to + g * 32, o);
           }
         }
-        const float mc = m == -INFINITY ? 0.0f : m * c;
+        const float mc = m == -INFINITY ? 0.0f : m * c - kRunningShift<T>;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -268,22 +233,14 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       for (int g = 0; g < DB * 2; ++g) {
         float o[32];
         if (active[t]) { tmem_ld32(to + g * 32, o); tmem_wait_ld(); }
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          uint32_t w[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            w[u] = live ? pack2<T>(o[ch * 8 + 2 * u] * inv, o[ch * 8 + 2 * u + 1] * inv) : 0u;
-          *reinterpret_cast<uint4*>(out + (g >> 1) * kBlockBytes + swizzled(quad * 32 + lane, (g & 1) * 4 + ch)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        store_row32<T>(out, quad * 32 + lane, g * 32, o, inv, live);
       }
       if (a.lse && row < a.queries)
-        a.lse[((int64_t)b * a.heads + head[t]) * a.queries + row] = live ? m * a.scale + logf(l) : -INFINITY;
+        a.lse[((int64_t)b * a.heads + head[t]) * a.queries + row] = live ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
       fence_proxy_async();
       named_barrier(1 + t, 128);
       if ((warp & 3) == 0 && lane == 0) {
-        for (int d = 0; d < DB; ++d)
-          tma_store_4d(&mo.map, smem_u32(out) + d * kBlockBytes, d * 64, row0[t] * mo.token_step, head[t] * mo.head_step, b * mo.batch_step);
+        store_tile<DB>(mo, smem_u32(out), row0[t], head[t], b);
         bulk_commit();
         bulk_wait_read();
       }

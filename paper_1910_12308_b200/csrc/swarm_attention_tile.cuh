@@ -1,0 +1,79 @@
+// Tiles of the attention kernels: 128 rows of one head in shared memory as blocks of 128 rows x 64 values with the
+// 128-byte swizzle, which TMA writes and reads and the products take as operands (rows by rows or transposed).
+#pragma once
+#include "swarm_attention.h"
+#include "swarm_tc.cuh"
+
+namespace swarm {
+
+constexpr int kTile = 128;                              // rows of a tile
+constexpr int kBlockBytes = kTile * 128;                // 128 rows x 64 values
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Weights exp(s - max) <= 1 are rounded to T before their products. In fp16 those below 2^-14 would lose bits, so they
+// are held as multiples of 2^-shift, with room below the largest fp16 number; bf16 has fp32's range. The exponent's
+// argument takes the shift for nothing, and a power of two is taken out of the sums exactly.
+template <typename T> constexpr float kWeightShift = 0.0f;
+template <> constexpr float kWeightShift<__half> = 15.0f;              // weights against the row's final lse: at most 1
+template <typename T> constexpr float kRunningShift = 0.0f;
+template <> constexpr float kRunningShift<__half> = 7.0f;              // weights against a running maximum: at most 2^8
+__device__ __forceinline__ constexpr float pow2_of(float shift) { return shift == 15.0f ? 0x1p-15f : 1.0f; }
+
+// Offset of 16 bytes (8 values) of a row in a block.
+__device__ __forceinline__ uint32_t swizzled(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
+
+// Zeroes rows [first, last) of a tile of DB blocks; called by one warp. The rows are in an operand of a product whose
+// other factor is 0 there, and hold whatever lies past a sentence's end.
+template <int DB>
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last, int lane) {
+  for (int i = lane; i < (last - first) * 8 * DB; i += 32) {
+    const int row = first + i / (8 * DB), c = i % (8 * DB);
+    *reinterpret_cast<uint4*>(tile + (c >> 3) * kBlockBytes + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async();
+  __syncwarp();
+}
+
+// One thread: the copies of a tile (the barrier is told of its bytes beforehand).
+template <int DB>
+__device__ __forceinline__ void load_tile(uint32_t dst, const TileMap& m, int row0, int head, int b, uint32_t bar) {
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+    tma_load_4d(dst + d * kBlockBytes, &m.map, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step, bar);
+}
+template <int DB>
+__device__ __forceinline__ void store_tile(const TileMap& m, uint32_t src, int row0, int head, int b) {
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+    tma_store_4d(&m.map, src + d * kBlockBytes, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step);
+}
+
+// One thread: D[128 x cols] = A[128 x dim] B[cols x dim]^T, both tiles in shared memory, dim = 16 ksteps.
+template <typename T>
+__device__ __forceinline__ void mma_rows(uint32_t tmem_d, uint32_t tile_a, uint32_t tile_b, int cols, int ksteps) {
+  const uint32_t idesc = instr_desc_16<T>(kTile, 0, 0, 0) + ((uint32_t)(cols >> 3) << 17);
+  const uint64_t da = smem_desc_sw128(tile_a, 16, 1024), db = smem_desc_sw128(tile_b, 16, 1024);
+  for (int ks = 0; ks < ksteps; ++ks) {
+    const uint64_t at = (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4);
+    tc_mma(tmem_d, da + at, db + at, idesc, ks != 0);
+  }
+}
+
+// 32 values of a row times `factor` (zeros unless live) into columns col .. col + 31 of a tile.
+template <typename T>
+__device__ __forceinline__ void store_row32(uint8_t* tile, int row, int col, const float* v, float factor, bool live) {
+#pragma unroll
+  for (int ch = 0; ch < 4; ++ch) {
+    uint32_t w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = live ? pack2<T>(v[ch * 8 + 2 * u] * factor, v[ch * 8 + 2 * u + 1] * factor) : 0u;
+    *reinterpret_cast<uint4*>(tile + (col >> 6) * kBlockBytes + swizzled(row, ((col & 63) >> 3) + ch)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+}  // namespace swarm

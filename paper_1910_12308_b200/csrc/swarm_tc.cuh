@@ -157,4 +157,9 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) 
   return r != 0;
 }
 
+// mbar_wait for warps that stay in step with others after a wait that gave up: nothing is waited for once ok is false.
+__device__ __forceinline__ bool mbar_wait_if(uint32_t bar, uint32_t parity, uint32_t limit, bool ok) {
+  return ok && mbar_wait(bar, parity, limit);
+}
+
 }  // namespace swarm

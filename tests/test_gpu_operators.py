@@ -490,6 +490,24 @@ def test_operators_on_another_stream_and_in_a_graph():
     ops.check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_waits_that_give_up_are_reported_and_leave_the_device_usable(d):
+    """wait_limit 0: every device-side wait gives up at once. The kernels return, the next check says so, and the
+    calls after it are right again."""
+    q, k, v, do = attention_inputs(2, 150, 200, 2, 2, d, BF16, seed=5)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    ops.check()
+    ops.cross_attention(q, k, v, wait_limit=0)
+    with pytest.raises(g.SwarmError) as err:
+        ops.check()
+    assert err.value.code == g.ECUDA and g.load().swarm_operator_error() == 702       # cudaErrorLaunchTimeout
+    ops.check()                                                                       # reported once
+    ops.cross_attention_backward(do, q, k, v, o, lse, wait_limit=0)
+    with pytest.raises(g.SwarmError):
+        ops.check()
+    check_attention(q, k, v, do)
+
+
 def test_refusals_of_the_tensor_checks():
     x, w = randn(4, 64, dtype=BF16), torch.ones(64, device="cuda")
     for bad in (lambda: ops.dropout(x, 1.5, 1, 1), lambda: ops.dropout(x, float("nan"), 1, 1), lambda: ops.dropout(x, 0.1, -1, 1),
