@@ -34,57 +34,6 @@ cudaError_t status_word(int** out) {
   return cudaSuccess;
 }
 
-template <typename T>
-__device__ __forceinline__ float dot_row(const float* a, const T* p, int dim) {
-  float s = 0.0f;
-  for (int d = 0; d < dim; d += 8) {
-    float v[8];
-    unpack8<T>(load_raw8<T>(p + d), v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(a[d + i], v[i], s);
-  }
-  return s;
-}
-
-// Warp = one query row; lane = one state of 32 at a time for the scores, then dims lane, lane + 32, ... of the output.
-template <typename T>
-__global__ void __launch_bounds__(128) attention_rows_kernel(AttentionArgs a) {
-  __shared__ float sq[4][kMaxDim];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t = blockIdx.x * 4 + warp, h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
-  if (t >= a.queries) return;
-  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const T* q = reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, h);
-  T* out = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h);
-  const int n = t < nq ? nk : 0;
-  for (int d = lane; d < a.head_dim; d += 32) sq[warp][d] = n ? to_float<T>(q[d]) : 0.0f;
-  __syncwarp();
-  float m = -INFINITY, l = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j0 = 0; j0 < n; j0 += 32) {
-    const int j = j0 + lane;
-    const float s = j < n ? a.scale * dot_row<T>(sq[warp], reinterpret_cast<const T*>(a.k) + offset_of(a.ks, b, j, hk), a.head_dim) : -INFINITY;
-    float top = s;
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.0f : m_new;
-    const float c = exp2f((m - base) * kLog2e), p = exp2f((s - base) * kLog2e);
-    l = l * c + warp_sum(p);
-    m = m_new;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] *= c;
-    for (int u = 0; u < min(32, n - j0); ++u) {
-      const float pu = __shfl_sync(0xFFFFFFFFu, p, u);
-      const T* v = reinterpret_cast<const T*>(a.v) + offset_of(a.vs, b, j0 + u, hk);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (lane + 32 * i < a.head_dim) acc[i] = fmaf(pu, to_float<T>(v[lane + 32 * i]), acc[i]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < a.head_dim) out[lane + 32 * i] = from_float<T>(n ? acc[i] / l : 0.0f);
-  if (a.lse && lane == 0) a.lse[((int64_t)b * a.heads + h) * a.queries + t] = n ? m + logf(l) : -INFINITY;
-}
-
 // Zeros into a strided tensor: the outputs of a call that has no rows or no states to sum over.
 __global__ void __launch_bounds__(256) attention_zero_kernel(uint4* p, swarm_strides s, int tokens, int heads, int chunks) {
   const int b = blockIdx.y;
@@ -129,6 +78,9 @@ void fill(AttentionArgs& a, const swarm_attention* d) {
   a.wait_limit = d->wait_limit < 0 ? kAttentionWaitLimit : d->wait_limit < (int64_t)1 << 32 ? (uint32_t)d->wait_limit : 0xFFFFFFFFu;
 }
 
+// Whether a call goes to the kernel that streams the states past 16 rows at a time.
+bool few_rows(const AttentionArgs& a) { return (int64_t)a.queries * a.group <= 64; }
+
 }  // namespace
 }  // namespace swarm
 
@@ -138,7 +90,10 @@ extern "C" {
 
 int swarm_cross_attention_workspace(const swarm_attention* desc_host, int32_t backward, size_t* bytes_host) {
   if (!desc_ok(desc_host) || !bytes_host) return SWARM_EINVAL;
-  *bytes_host = backward ? (size_t)desc_host->batch * desc_host->heads * desc_host->queries * sizeof(float) : 0;
+  AttentionArgs a{};
+  fill(a, desc_host);
+  if (backward) *bytes_host = (size_t)a.batch * a.heads * a.queries * sizeof(float);
+  else *bytes_host = a.batch && a.queries && a.keys && few_rows(a) ? attention_rows_workspace(a) : 0;
   return SWARM_OK;
 }
 
@@ -167,11 +122,7 @@ int swarm_cross_attention(const swarm_attention* desc_host, const void* q_dev, c
     }
     return operator_result(launch_zero(o_dev, d.o, d.batch, d.queries, d.heads, d.head_dim, st));
   }
-  if ((int64_t)d.queries * a.group > 16) return operator_result(launch_attention_forward_tc(a, d.dtype, st));
-  const dim3 grid((unsigned)((d.queries + 3) / 4), (unsigned)d.heads, (unsigned)d.batch);
-  if (d.dtype == SWARM_BF16) attention_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
-  else attention_rows_kernel<__half><<<grid, 128, 0, st>>>(a);
-  return operator_result(cudaGetLastError());
+  return operator_result(few_rows(a) ? launch_attention_rows(a, d.dtype, workspace_dev, st) : launch_attention_forward_tc(a, d.dtype, st));
 }
 
 int swarm_cross_attention_backward(const swarm_attention* desc_host, const void* dout_dev, const void* q_dev,

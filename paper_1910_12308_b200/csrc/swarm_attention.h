@@ -43,6 +43,9 @@ cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, i
                           int head_dim);
 
 cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
+// Few query rows; the workspace holds the parts of split states.
+size_t attention_rows_workspace(const AttentionArgs& a);
+cudaError_t launch_attention_rows(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st);
 cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
 
 }  // namespace swarm

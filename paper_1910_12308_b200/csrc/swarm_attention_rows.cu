@@ -1,0 +1,294 @@
+// Cross attention of few query rows (a decoding step): every state is read once, HBM is the bound.
+//
+// CTA = up to 16 rows (query tokens x the query heads of a key head) and a part of the states, four warps on 32 states
+// at a time each. The products run as m16n8k16 on operands that go from global memory straight into registers:
+//   scores  the order of the contraction over the head's values is free, so a lane takes 16 consecutive bytes of a
+//           state (values 32 p + 8 c .. + 7, c = lane % 4) as the operands of two products, and the same of a row of q
+//   sums    a lane takes 16 bytes (values 8 n .. + 7, n = lane / 4) of the states 2 c, 2 c + 1, 2 c + 8, 2 c + 9 and
+//           pairs the states byte-wise; product j then gives values 8 n + j
+// so neither needs shared memory or a transposition. The four warps meet in shared memory; where there are fewer (key
+// head, sentence) pairs than the device has room for, the states are split over CTAs whose parts (maximum, sum, o) a
+// second kernel joins in order.
+#include "swarm_attention.h"
+
+namespace swarm {
+namespace {
+
+constexpr int kRows = 16, kRowsWarps = 4, kRowsStep = 32;
+
+__device__ __forceinline__ float ex2_(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+template <typename T> __device__ __forceinline__ void mma16816(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__half>(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+struct RowsPlan {
+  int32_t rows, row_groups, splits;   // rows of a key head, groups of 16 of them, parts of the states
+  float* part_ml;                     // [batch][kv_heads][rows][splits][2] maximum and sum of a part
+  float* part_o;                      // [batch][kv_heads][rows][splits][head_dim]
+};
+
+// The fp16 weights against a running maximum reach 2^8: held as multiples of 2^-7, see swarm_attention_tile.cuh.
+template <typename T> constexpr float kShift = 0.0f;
+template <> constexpr float kShift<__half> = 7.0f;
+
+template <typename T, int DB>
+__global__ void __launch_bounds__(kRowsWarps * 32)
+attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
+  constexpr int kDim = DB * 64;
+  __shared__ float s_ml[kRowsWarps][kRows][2];
+  extern __shared__ float s_o[];                        // [warps][rows of this group][head_dim]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r8 = lane >> 2, c4 = lane & 3;
+  const int split = blockIdx.x % plan.splits, group = blockIdx.x / plan.splits % plan.row_groups;
+  const int bh = blockIdx.x / plan.splits / plan.row_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int row0 = group * kRows, rows = min(kRows, plan.rows - row0);
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  // this CTA's part of the states: equal runs of whole steps of all warps
+  const int steps = (nk + kRowsStep * kRowsWarps - 1) / (kRowsStep * kRowsWarps);
+  const int begin = (int)((int64_t)steps * split / plan.splits) * kRowsStep * kRowsWarps;
+  const int end = min(nk, (int)((int64_t)steps * (split + 1) / plan.splits) * kRowsStep * kRowsWarps);
+  const int chunks = a.head_dim / 8;                    // 16-byte pieces of a head
+
+  uint32_t q[DB * 2][2][4];                             // [32 values][row r8, row r8 + 8][pair]
+#pragma unroll
+  for (int p = 0; p < DB * 2; ++p)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = row0 + r8 + 8 * u;
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (r < plan.rows && p * 4 + c4 < chunks)
+        w = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, r / a.group, hk * a.group + r % a.group) + p * 32 + c4 * 8);
+      q[p][u][0] = w.x; q[p][u][1] = w.y; q[p][u][2] = w.z; q[p][u][3] = w.w;
+    }
+  const T* kbase = reinterpret_cast<const T*>(a.k) + b * a.ks.batch + hk * a.ks.head;
+  const T* vbase = reinterpret_cast<const T*>(a.v) + b * a.vs.batch + hk * a.vs.head;
+  const float c = a.scale * kLog2e;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, o[DB * 8][4];
+#pragma unroll
+  for (int i = 0; i < DB * 8; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[i][u] = 0.0f;
+
+  for (int j0 = begin + warp * kRowsStep; j0 < end; j0 += kRowsStep * kRowsWarps) {
+    uint4 kw[4][DB * 2], vw[2][4][DB];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {                       // eight states at a time: state r8 of the group
+      const int j = j0 + g * 8 + r8;
+#pragma unroll
+      for (int p = 0; p < DB * 2; ++p)
+        kw[g][p] = j < nk && p * 4 + c4 < chunks ? *reinterpret_cast<const uint4*>(kbase + (int64_t)j * a.ks.token + p * 32 + c4 * 8) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {                     // states 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of sixteen
+        const int j = j0 + g * 16 + c4 * 2 + (u & 1) + (u >> 1) * 8;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          vw[g][u][d] = j < nk && d * 8 + r8 < chunks ? *reinterpret_cast<const uint4*>(vbase + (int64_t)j * a.vs.token + d * 64 + r8 * 8) : make_uint4(0, 0, 0, 0);
+      }
+    float s[4][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[g][u] = 0.0f;
+#pragma unroll
+      for (int p = 0; p < DB * 2; ++p) {
+        const uint32_t a0[4] = {q[p][0][0], q[p][1][0], q[p][0][1], q[p][1][1]};
+        const uint32_t a1[4] = {q[p][0][2], q[p][1][2], q[p][0][3], q[p][1][3]};
+        mma16816<T>(s[g], a0, kw[g][p].x, kw[g][p].y);
+        mma16816<T>(s[g], a1, kw[g][p].z, kw[g][p].w);
+      }
+    }
+    if (j0 + kRowsStep > nk) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (j0 + g * 8 + c4 * 2 + (u & 1) >= nk) s[g][u] = -INFINITY;
+    }
+    float top[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float t = fmaxf(s[0][2 * u], s[0][2 * u + 1]);
+#pragma unroll
+      for (int g = 1; g < 4; ++g) t = fmaxf(t, fmaxf(s[g][2 * u], s[g][2 * u + 1]));
+      t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 1));
+      top[u] = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 2));
+    }
+    if (__any_sync(0xFFFFFFFFu, (top[0] - m[0]) * c > 8.0f || (top[1] - m[1]) * c > 8.0f)) {
+      // the maximum moved by more than 2^8 in some row (or the first step): rescale; smaller moves keep the reference
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float m_new = fmaxf(m[u], top[u]), f = m_new == m[u] ? 1.0f : ex2_((m[u] - m_new) * c);
+        m[u] = m_new;
+        l[u] *= f;
+#pragma unroll
+        for (int i = 0; i < DB * 8; ++i) { o[i][2 * u] *= f; o[i][2 * u + 1] *= f; }
+      }
+    }
+    const float mc[2] = {m[0] == -INFINITY ? 0.0f : m[0] * c - kShift<T>, m[1] == -INFINITY ? 0.0f : m[1] * c - kShift<T>};
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        s[g][u] = ex2_(fmaf(s[g][u], c, -mc[u >> 1]));
+        l[u >> 1] += s[g][u];
+      }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const uint32_t p[4] = {pack2<T>(s[2 * g][0], s[2 * g][1]), pack2<T>(s[2 * g][2], s[2 * g][3]),
+                             pack2<T>(s[2 * g + 1][0], s[2 * g + 1][1]), pack2<T>(s[2 * g + 1][2], s[2 * g + 1][3])};
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vw[g][0][d]);
+        const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vw[g][1][d]);
+        const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vw[g][2][d]);
+        const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vw[g][3][d]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          mma16816<T>(o[d * 8 + 2 * i], p, __byte_perm(v0[i], v1[i], 0x5410), __byte_perm(v2[i], v3[i], 0x5410));
+          mma16816<T>(o[d * 8 + 2 * i + 1], p, __byte_perm(v0[i], v1[i], 0x7632), __byte_perm(v2[i], v3[i], 0x7632));
+        }
+      }
+    }
+  }
+
+  // the warps meet: product j of block d holds values d * 64 + 8 n + j, n = 2 c4, 2 c4 + 1
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 1);
+    l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 2);
+    const int r = r8 + 8 * u;
+    if (r < rows) {
+      if (c4 == 0) { s_ml[warp][r][0] = m[u]; s_ml[warp][r][1] = l[u]; }
+      float* dst = s_o + (warp * rows + r) * a.head_dim;
+#pragma unroll
+      for (int i = 0; i < DB * 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = (i >> 3) * 64 + 8 * (2 * c4 + e) + (i & 7);
+          if (col < a.head_dim) dst[col] = o[i][2 * u + e];
+        }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * chunks; i += kRowsWarps * 32) {
+    const int r = i / chunks, ch = i % chunks, row = row0 + r, t = row / a.group, h = hk * a.group + row % a.group;
+    float top = -INFINITY, sum = 0.0f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kRowsWarps; ++w) top = fmaxf(top, s_ml[w][r][0]);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int w = 0; w < kRowsWarps; ++w) {
+      const float f = ex2_((s_ml[w][r][0] - base) * c);
+      sum = fmaf(s_ml[w][r][1], f, sum);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(s_o[(w * rows + r) * a.head_dim + ch * 8 + e], f, v[e]);
+    }
+    if (plan.splits == 1) {
+      const float inv = t < nq && sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = inv != 0.0f ? v[e] * inv : 0.0f;
+      store8<T>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + ch * 8, v);
+      if (a.lse && ch == 0)
+        a.lse[((int64_t)b * a.heads + h) * a.queries + t] = t < nq && nk > 0 ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
+    } else {
+      const int64_t at = ((int64_t)bh * plan.rows + row) * plan.splits + split;
+      if (ch == 0) { plan.part_ml[at * 2] = top; plan.part_ml[at * 2 + 1] = sum; }
+      store8<float>(plan.part_o + at * a.head_dim + ch * 8, v);
+    }
+  }
+}
+
+// Joins the parts of a row: warp = one row, lane = four values of it, the parts in order.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, RowsPlan plan) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (i >= (int64_t)a.batch * a.kv_heads * plan.rows) return;
+  const int row = (int)(i % plan.rows), bh = (int)(i / plan.rows), hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int t = row / a.group, h = hk * a.group + row % a.group;
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  const float c = a.scale * kLog2e;
+  const float2* ml = reinterpret_cast<const float2*>(plan.part_ml) + i * plan.splits;
+  const float* part = plan.part_o + i * plan.splits * a.head_dim + lane * 4;
+  float top = -INFINITY;
+  for (int s = lane; s < plan.splits; s += 32) top = fmaxf(top, ml[s].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  const float base = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < plan.splits; ++s) {
+    const float f = ex2_((ml[s].x - base) * c);
+    sum = fmaf(ml[s].y, f, sum);
+    if (lane * 4 < a.head_dim) {
+      const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)s * a.head_dim);
+      v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
+    }
+  }
+  const bool live = t < nq && nk > 0;
+  const float inv = live && sum != 0.0f ? 1.0f / sum : 0.0f;
+  if (lane * 4 < a.head_dim) {
+    T* out = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4;
+    uint2 w = make_uint2(0, 0);
+    if (inv != 0.0f) w = make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv));
+    *reinterpret_cast<uint2*>(out) = w;
+  }
+  if (a.lse && lane == 0)
+    a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
+}
+
+RowsPlan make_plan(const AttentionArgs& a) {
+  RowsPlan p{};
+  p.rows = a.queries * a.group;
+  p.row_groups = (p.rows + kRows - 1) / kRows;
+  const int64_t ctas = (int64_t)a.batch * a.kv_heads * p.row_groups, room = 148 * 3;
+  int64_t splits = (room + ctas - 1) / ctas;
+  const int64_t most = ((int64_t)a.keys + kRowsStep * kRowsWarps - 1) / (kRowsStep * kRowsWarps);
+  if (splits > most) splits = most;
+  p.splits = (int32_t)(splits < 1 ? 1 : splits);
+  return p;
+}
+
+template <typename T, int DB>
+cudaError_t launch_rows(const AttentionArgs& a, const RowsPlan& p, cudaStream_t st) {
+  const int64_t ctas = (int64_t)a.batch * a.kv_heads * p.row_groups * p.splits;
+  const int rows = p.rows < kRows ? p.rows : kRows;
+  attention_rows_kernel<T, DB><<<(unsigned)ctas, kRowsWarps * 32, kRowsWarps * rows * a.head_dim * sizeof(float), st>>>(a, p);
+  if (p.splits > 1) {
+    const int64_t rows_all = (int64_t)a.batch * a.kv_heads * p.rows;
+    attention_join_kernel<T><<<(unsigned)((rows_all + 3) / 4), 128, 0, st>>>(a, p);
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t attention_rows_workspace(const AttentionArgs& a) {
+  const RowsPlan p = make_plan(a);
+  if (p.splits == 1) return 0;
+  return (size_t)a.batch * a.kv_heads * p.rows * p.splits * (a.head_dim + 2) * sizeof(float) + 16;
+}
+
+cudaError_t launch_attention_rows(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st) {
+  RowsPlan p = make_plan(a);
+  if (p.splits > 1) {
+    p.part_o = reinterpret_cast<float*>(workspace);
+    p.part_ml = p.part_o + (size_t)a.batch * a.kv_heads * p.rows * p.splits * a.head_dim;
+  }
+  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_rows<__nv_bfloat16, 1>(a, p, st) : launch_rows<__nv_bfloat16, 2>(a, p, st);
+  return a.head_dim <= 64 ? launch_rows<__half, 1>(a, p, st) : launch_rows<__half, 2>(a, p, st);
+}
+
+}  // namespace swarm
