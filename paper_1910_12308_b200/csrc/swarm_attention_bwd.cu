@@ -109,14 +109,14 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
           if (valid < cols) zero_rows<DB>(sKV + 2 * st * kTileBytes, valid, cols, lane);   // k is a factor of dq
           ok = mbar_wait(smem_u32(&bars.s_empty), (j & 1), limit);
           tc_fence_after();
-          if (ok && lane == 0) {
+          if (ok && elect_one()) {
             mma_rows<T>(tmem, aq, akv + 2 * st * kTileBytes, cols, ksteps);
             tc_commit(smem_u32(&bars.s_full));
           }
           __syncwarp();
           if (ok) ok = mbar_wait(smem_u32(&bars.dp_empty), (j & 1), limit);
           tc_fence_after();
-          if (ok && lane == 0) {
+          if (ok && elect_one()) {
             mma_rows<T>(tmem + 128, aq + kTileBytes, akv + (2 * st + 1) * kTileBytes, cols, ksteps);
             tc_commit(smem_u32(&bars.dp_full));
           }
@@ -126,7 +126,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
           const int st = j % kStages;
           ok = mbar_wait(smem_u32(&bars.ds_full), j & 1, limit);
           tc_fence_after();
-          if (ok && lane == 0) {
+          if (ok && elect_one()) {
             const uint64_t dk = smem_desc_sw128(akv + 2 * st * kTileBytes, kBlockBytes, 1024);
             for (int ks = 0; ks < columns(j) / 16; ++ks)
               tc_mma_ts(tmem + 384, tmem + 256 + ks * 8, dk + (uint64_t)((ks * 2048) >> 4), kIdescDq, (j | ks) != 0);
@@ -138,7 +138,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         }
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (lane == 0) tc_commit(smem_u32(&bars.drain));
+        if (elect_one()) tc_commit(smem_u32(&bars.drain));
         mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
@@ -326,7 +326,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         if (i >= 0) {
           ok = mbar_wait(smem_u32(&bars.s_empty), i & 1, limit);
           tc_fence_after();
-          if (ok && lane == 0) outer(tmem + 256, tmem, aq + (2 * st + 1) * kTileBytes, i);
+          if (ok && elect_one()) outer(tmem + 256, tmem, aq + (2 * st + 1) * kTileBytes, i);
           __syncwarp();
         }
         if (i + 1 < n && ok) {
@@ -337,7 +337,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
             zero_rows<DB>(sQ + 2 * next * kTileBytes, valid, cols, lane);
             zero_rows<DB>(sQ + (2 * next + 1) * kTileBytes, valid, cols, lane);
           }
-          if (lane == 0) {
+          if (elect_one()) {
             mma_rows<T>(tmem, akv, aq + 2 * next * kTileBytes, cols, ksteps);
             tc_commit(smem_u32(&bars.s_full));
           }
@@ -346,21 +346,21 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         if (i >= 0 && ok) {
           ok = mbar_wait(smem_u32(&bars.ds_full), i & 1, limit);
           tc_fence_after();
-          if (ok && lane == 0) {
+          if (ok && elect_one()) {
             outer(tmem + 384, tmem + 128, aq + 2 * st * kTileBytes, i);
             tc_commit(smem_u32(&bars.empty[st]));
             if (i == n - 1) tc_commit(smem_u32(&bars.done));
           }
           __syncwarp();
         }
-        if (i + 1 < n && ok && lane == 0) {
+        if (i + 1 < n && ok && elect_one()) {
           mma_rows<T>(tmem + 128, akv + kTileBytes, aq + (2 * next + 1) * kTileBytes, columns(i + 1), ksteps);
           tc_commit(smem_u32(&bars.dp_full));
         }
         __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (lane == 0) tc_commit(smem_u32(&bars.drain));
+        if (elect_one()) tc_commit(smem_u32(&bars.drain));
         mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }

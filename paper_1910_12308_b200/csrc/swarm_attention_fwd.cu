@@ -6,7 +6,8 @@
 namespace swarm {
 namespace {
 
-constexpr int kFwdThreads = 320;                        // two softmax warpgroups, the copying warp, the issuing warp
+constexpr int kFwdThreads = 384;                        // two softmax warpgroups; the third: copying warp, issuing warp
+constexpr int kFwdRegs = 208, kFwdRegsRest = 88;        // 2 * 208 + 88 = 3 * 168, what a thread is launched with
 
 template <int DB> constexpr int kFwdStages = DB == 2 ? 4 : 6;
 template <int DB> constexpr int kFwdSmem = (2 + kFwdStages<DB>) * DB * kBlockBytes + 1024;
@@ -66,6 +67,8 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   const uint32_t limit = a.wait_limit;
   bool ok = true;
 
+  if (warp >= 8) {
+  regs_lower<kFwdRegsRest>();
   if (warp == 8) {
     // ---- copies -------------------------------------------------------------------------------
     if (any) {
@@ -113,9 +116,9 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         if (active[t]) {
           ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
           tc_fence_after();
-          if (ok && lane == 0) scores(t, 0);
+          if (ok && elect_one()) scores(t, 0);
         }
-      if (ok && lane == 0) tc_commit(smem_u32(&bars.kv_empty[0]));
+      if (ok && elect_one()) tc_commit(smem_u32(&bars.kv_empty[0]));
       for (int j = 0; j < n && ok; ++j) {
         const int fv = 2 * j + 1, sv = fv % kStages, fk = 2 * j + 2;
         const int valid = min(kTile, nk - j * kTile), rows = (valid + 15) & ~15;
@@ -127,7 +130,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
             ok = mbar_wait(smem_u32(&bars.p_full[t]), j & 1, limit);
             if (!ok) break;
             tc_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
               const uint64_t dv = dv0 + (uint64_t)((sv * kTileBytes) >> 4);
               for (int ks = 0; ks < rows / 16; ++ks)
                 tc_mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + ks * 8, dv + (uint64_t)((ks * 2048) >> 4), kIdescPV, (j | ks) != 0);
@@ -137,21 +140,23 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
             if (j + 1 < n) {
               ok = mbar_wait(smem_u32(&bars.kv_full[fk % kStages]), (fk / kStages) & 1, limit);
               tc_fence_after();
-              if (ok && lane == 0) scores(t, j + 1);
+              if (ok && elect_one()) scores(t, j + 1);
             }
           }
-        if (ok && lane == 0) {
+        if (ok && elect_one()) {
           tc_commit(smem_u32(&bars.kv_empty[sv]));
           if (j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[fk % kStages]));
         }
         __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (lane == 0) tc_commit(smem_u32(&bars.drain));
+        if (elect_one()) tc_commit(smem_u32(&bars.drain));
         mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
+  }
   } else {
+    regs_raise<kFwdRegs>();
     // ---- softmax ------------------------------------------------------------------------------
     const int t = warp >> 2, quad = warp & 3;
     const int row = row0[t] + quad * 32 + lane;         // this thread's query row
@@ -176,11 +181,11 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         }
         float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int i = 4; i < kTile; i += 4) {
+        for (int i = 4; i + 8 <= kTile; i += 8) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], s[i + u]);
+          for (int u = 0; u < 4; ++u) top[u] = max3(top[u], s[i + u], s[i + 4 + u]);
         }
-        const float m_tile = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float m_tile = fmaxf(max3(top[0], s[124], s[125]), max3(max3(top[1], s[126], s[127]), top[2], top[3]));
         if (j == 0) m = m_tile;
         else if (__any_sync(0xFFFFFFFFu, (m_tile - m) * c > 8.0f)) {
           // the maximum moved by more than a factor of 2^8 in some row of the warp: rescale the sums so far. Smaller
@@ -205,9 +210,11 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
           uint32_t p[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float p0 = ex2(fmaf(s[g * 32 + 2 * i], c, -mc)), p1 = ex2(fmaf(s[g * 32 + 2 * i + 1], c, -mc));
-            sum[i & 1] += p0;
-            sum[2 + (i & 1)] += p1;
+            float p0, p1;
+            fma2(p0, p1, s[g * 32 + 2 * i], s[g * 32 + 2 * i + 1], c, c, -mc, -mc);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+            add2(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], sum[2 * (i & 1)], sum[2 * (i & 1) + 1], p0, p1);
             p[i] = pack2<T>(p0, p1);
           }
           tmem_st16(ts + g * 16, p);
