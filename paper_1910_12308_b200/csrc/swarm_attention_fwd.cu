@@ -6,51 +6,62 @@
 namespace swarm {
 namespace {
 
-constexpr int kFwdThreads = 384;                        // two softmax warpgroups; the third: copying warp, issuing warp
-constexpr int kFwdRegs = 208, kFwdRegsRest = 88;        // 2 * 208 + 88 = 3 * 168, what a thread is launched with
-
-template <int DB> constexpr int kFwdStages = DB == 2 ? 4 : 6;
-template <int DB> constexpr int kFwdSmem = (2 + kFwdStages<DB>) * DB * kBlockBytes + 1024;
-
-struct FwdBars {
-  uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], p_full[2], o_full[2], drain;
+// Shape of a CTA. NT tiles of 128 query rows, each with a softmax warpgroup; a further warpgroup holds the copying warp
+// and the issuing warp. Registers are moved from it to the others: the sum stays what the block was launched with.
+template <int DB, int NT> struct FwdShape {
+  static constexpr int kThreads = 128 * (NT + 1);
+  static constexpr int kCtasPerSm = NT == 1 ? 2 : 1;
+  static constexpr int kRegs = NT == 1 ? 200 : 208, kRegsRest = NT == 1 ? 56 : 88;
+  static constexpr int kStages = NT == 1 ? 4 : DB == 2 ? 4 : 6;
+  static constexpr int kSmem = (NT + kStages) * DB * kBlockBytes + 1024;
+  // tensor memory: scores, weights, sums of tile 0, then of tile 1
+  static constexpr uint32_t kColumns = NT == 1 ? 256 : 512;
+  static constexpr uint32_t kWeights = NT == 1 ? 128 : 0;              // two tiles: the weights overwrite the scores
+  static constexpr uint32_t kSums = NT == 1 ? 192 : 256;
 };
 
-template <typename T, int DB>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+struct FwdBars {
+  uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], s_empty[2], p_full[2], pv_done[2], drain;
+};
+
+// NT = 1 (heads of up to 64 values): scores and weights have tensor memory of their own, so the scores of the next tile
+// are computed while the warps take the exponentials of this one, and two such CTAs share a multiprocessor.
+// NT = 2: two row tiles share every tile of states; while one's products run, the other's softmax does.
+template <typename T, int DB, int NT>
+__global__ void __launch_bounds__(FwdShape<DB, NT>::kThreads, FwdShape<DB, NT>::kCtasPerSm)
 attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
-                         const __grid_constant__ TileMap mo, AttentionArgs a, int row_tiles, int pairs) {
-  constexpr int kStages = kFwdStages<DB>;
+                         const __grid_constant__ TileMap mo, AttentionArgs a, int row_tiles, int tile_groups) {
+  using Shape = FwdShape<DB, NT>;
+  constexpr int kStages = Shape::kStages;
   constexpr uint32_t kTileBytes = DB * kBlockBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* sQ = smem;                                   // two tiles
-  uint8_t* sKV = smem + 2 * kTileBytes;                 // ring of K, V tiles
+  uint8_t* sQ = smem;                                   // NT tiles
+  uint8_t* sKV = smem + NT * kTileBytes;                // ring of K, V tiles
   __shared__ FwdBars bars;
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  // the pair of row tiles of this CTA: tiles are numbered head after head within the group of a key head
-  const int pair = blockIdx.x % pairs, bh = blockIdx.x / pairs, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  // the row tiles of this CTA: tiles are numbered head after head within the group of a key head
+  const int first = blockIdx.x % tile_groups * NT, bh = blockIdx.x / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
   const int n = (nk + kTile - 1) / kTile;
-  int head[2], row0[2];
-  bool active[2];
+  auto head_of = [&](int t) { return hk * a.group + (first + t) / row_tiles; };
+  auto row_of = [&](int t) { return (first + t) % row_tiles * kTile; };
+  auto exists = [&](int t) { return first + t < row_tiles * a.group; };
+  uint32_t act = 0;                                     // bit t: tile t has work
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int tile = pair * 2 + t;
-    head[t] = hk * a.group + tile / row_tiles;
-    row0[t] = tile % row_tiles * kTile;
-    active[t] = tile < row_tiles * a.group && row0[t] < nq && n > 0;
-  }
-  const bool any = active[0] || active[1];
+  for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
+  auto active = [&](int t) { return (act >> t & 1u) != 0; };
+  const bool any = act != 0;
 
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NT; ++i) {
       mbar_init(smem_u32(&bars.q_full[i]), 1);
       mbar_init(smem_u32(&bars.s_full[i]), 1);
+      mbar_init(smem_u32(&bars.s_empty[i]), 4);
       mbar_init(smem_u32(&bars.p_full[i]), 4);
-      mbar_init(smem_u32(&bars.o_full[i]), 1);
+      mbar_init(smem_u32(&bars.pv_done[i]), 1);
     }
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_u32(&bars.kv_full[i]), 1);
@@ -59,113 +70,122 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
     mbar_init(smem_u32(&bars.drain), 1);
     fence_mbar_init();
   }
-  if (warp == 9) { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
+  if (warp == 4 * NT + 1) { tmem_alloc(smem_u32(&tmem_slot), Shape::kColumns); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;                      // columns: scores of tile t at 128 t (its weights over them), o at 256 + 128 t
-  const uint32_t limit = a.wait_limit;
+  const uint32_t tmem = tmem_slot, limit = a.wait_limit;
   bool ok = true;
 
-  if (warp >= 8) {
-  regs_lower<kFwdRegsRest>();
-  if (warp == 8) {
-    // ---- copies -------------------------------------------------------------------------------
-    if (any) {
+  if (warp >= 4 * NT) {
+    regs_lower<Shape::kRegsRest>();
+    if (warp == 4 * NT && any) {
+      // ---- copies -----------------------------------------------------------------------------
       int issued = 0;
-      if (lane == 0) { tma_prefetch_map(&mk.map); tma_prefetch_map(&mv.map); }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (active[t] && limit && lane == 0) {
-          const uint32_t bar = smem_u32(&bars.q_full[t]);
-          mbar_expect_tx(bar, kTileBytes);
-          load_tile<DB>(smem_u32(sQ) + t * kTileBytes, mq, row0[t], head[t], b, bar);
-        }
+      if (limit && elect_one()) {
+        for (int t = 0; t < NT; ++t)
+          if (active(t)) {
+            const uint32_t bar = smem_u32(&bars.q_full[t]);
+            mbar_expect_tx(bar, kTileBytes);
+            load_tile<DB>(smem_u32(sQ) + t * kTileBytes, mq, row_of(t), head_of(t), b, bar);
+          }
+      }
       for (int f = 0; f < 2 * n; ++f) {                 // K of tile 0, V of tile 0, K of tile 1, ...
         const int st = f % kStages;
         ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((f / kStages) & 1) ^ 1, limit);
         if (!ok) break;
-        if (lane == 0) {
+        if (elect_one()) {
           const uint32_t bar = smem_u32(&bars.kv_full[st]);
           mbar_expect_tx(bar, kTileBytes);
           load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (f >> 1) * kTile, hk, b, bar);
         }
+        __syncwarp();
         issued = f + 1;
       }
       if (!ok) {
         // gave up: the copies in flight land before the CTA's shared memory is released
         for (int f = issued > kStages ? issued - kStages : 0; f < issued; ++f)
           mbar_wait(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
-        for (int t = 0; t < 2; ++t)
-          if (active[t] && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
+        for (int t = 0; t < NT; ++t)
+          if (active(t) && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
       }
-    }
-  } else if (warp == 9) {
-    // ---- products -----------------------------------------------------------------------------
-    if (any) {
+    } else if (warp == 4 * NT + 1 && any) {
+      // ---- products ---------------------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
+      const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
       constexpr uint32_t kIdescPV = instr_desc_16<T>(kTile, DB * 64, 0, 1);
-      const uint64_t dv0 = smem_desc_sw128(smem_u32(sKV), kBlockBytes, 1024);
+      auto columns = [&](int j) { return (min(kTile, nk - j * kTile) + 15) & ~15; };
       auto scores = [&](int t, int j) {                 // S_t = Q_t K_j^T
-        mma_rows<T>(tmem + 128 * t, smem_u32(sQ) + t * kTileBytes, smem_u32(sKV) + (2 * j) % kStages * kTileBytes,
-                    (min(kTile, nk - j * kTile) + 15) & ~15, ksteps);
+        mma_rows<T>(tmem + 128 * t, aq + t * kTileBytes, akv + (2 * j) % kStages * kTileBytes, columns(j), ksteps);
         tc_commit(smem_u32(&bars.s_full[t]));
       };
-      ok = mbar_wait(smem_u32(&bars.kv_full[0]), 0, limit);
-      for (int t = 0; t < 2 && ok; ++t)
-        if (active[t]) {
+      auto sums = [&](int t, int j) {                   // O_t += P_t V_j
+        const uint64_t dv = smem_desc_sw128(akv + (2 * j + 1) % kStages * kTileBytes, kBlockBytes, 1024);
+        const uint32_t p = tmem + 128 * t + Shape::kWeights, o = tmem + 128 * t + Shape::kSums;
+        for (int ks = 0; ks < columns(j) / 16; ++ks)
+          tc_mma_ts(o, p + ks * 8, dv + (uint64_t)((ks * 2048) >> 4), kIdescPV, (j | ks) != 0);
+        if (NT == 1 || j == n - 1) tc_commit(smem_u32(&bars.pv_done[t]));
+      };
+      auto wait_kv = [&](int f) { return mbar_wait(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, limit); };
+      ok = wait_kv(0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (active(t) && ok) {
           ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
           tc_fence_after();
           if (ok && elect_one()) scores(t, 0);
+          __syncwarp();
         }
       if (ok && elect_one()) tc_commit(smem_u32(&bars.kv_empty[0]));
       for (int j = 0; j < n && ok; ++j) {
-        const int fv = 2 * j + 1, sv = fv % kStages, fk = 2 * j + 2;
-        const int valid = min(kTile, nk - j * kTile), rows = (valid + 15) & ~15;
-        ok = mbar_wait(smem_u32(&bars.kv_full[sv]), (fv / kStages) & 1, limit);
+        const int sv = (2 * j + 1) % kStages, sk = (2 * j + 2) % kStages;
+        if (NT == 1 && j + 1 < n) {                     // the next scores as soon as these have been read
+          ok = wait_kv(2 * j + 2) && mbar_wait(smem_u32(&bars.s_empty[0]), j & 1, limit);
+          tc_fence_after();
+          if (ok && elect_one()) { scores(0, j + 1); tc_commit(smem_u32(&bars.kv_empty[sk])); }
+          __syncwarp();
+          if (!ok) break;
+        }
+        ok = wait_kv(2 * j + 1);
         if (!ok) break;
-        if (valid < rows) zero_rows<DB>(sKV + sv * kTileBytes, valid, rows, lane);
-        for (int t = 0; t < 2 && ok; ++t)
-          if (active[t]) {
+        const int valid = min(kTile, nk - j * kTile);
+        if (valid < columns(j)) zero_rows<DB>(sKV + sv * kTileBytes, valid, columns(j), lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          if (active(t) && ok) {
             ok = mbar_wait(smem_u32(&bars.p_full[t]), j & 1, limit);
-            if (!ok) break;
             tc_fence_after();
-            if (elect_one()) {
-              const uint64_t dv = dv0 + (uint64_t)((sv * kTileBytes) >> 4);
-              for (int ks = 0; ks < rows / 16; ++ks)
-                tc_mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + ks * 8, dv + (uint64_t)((ks * 2048) >> 4), kIdescPV, (j | ks) != 0);
-              if (j == n - 1) tc_commit(smem_u32(&bars.o_full[t]));
-            }
+            if (ok && elect_one()) sums(t, j);
             __syncwarp();
-            if (j + 1 < n) {
-              ok = mbar_wait(smem_u32(&bars.kv_full[fk % kStages]), (fk / kStages) & 1, limit);
+            if (NT == 2 && j + 1 < n && ok) {
+              ok = wait_kv(2 * j + 2);
               tc_fence_after();
               if (ok && elect_one()) scores(t, j + 1);
+              __syncwarp();
             }
           }
         if (ok && elect_one()) {
           tc_commit(smem_u32(&bars.kv_empty[sv]));
-          if (j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[fk % kStages]));
+          if (NT == 2 && j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[sk]));
         }
         __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
         if (elect_one()) tc_commit(smem_u32(&bars.drain));
+        __syncwarp();
         mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
-  }
   } else {
-    regs_raise<kFwdRegs>();
     // ---- softmax ------------------------------------------------------------------------------
-    const int t = warp >> 2, quad = warp & 3;
-    const int row = row0[t] + quad * 32 + lane;         // this thread's query row
-    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-    const uint32_t ts = tmem + 128 * t + lane_base, to = tmem + 256 + 128 * t + lane_base;
+    regs_raise<Shape::kRegs>();
+    const int t = NT == 1 ? 0 : warp >> 2, quad = warp & 3, head = head_of(t), row0 = row_of(t);
+    const bool work = active(t);
+    const int row = row0 + quad * 32 + lane;            // this thread's query row
+    const uint32_t ts = tmem + 128 * t + ((uint32_t)(quad * 32) << 16), tp = ts + Shape::kWeights, to = ts + Shape::kSums;
     const float c = a.scale * kLog2e;
-    float m = 0.0f, l = 0.0f;                           // m: the maximum that the weights are taken against
-    if (active[t]) {
-      m = -INFINITY;
+    float m = -INFINITY, l = 0.0f;                      // m: the maximum that the weights are taken against
+    if (work) {
       for (int j = 0; j < n; ++j) {
         ok = mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
         if (!ok) break;
@@ -175,6 +195,11 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
 #pragma unroll
         for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, s + g * 32);
         tmem_wait_ld();
+        if (NT == 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty[t]));
+        }
         if (valid < kTile) {
 #pragma unroll
           for (int i = 0; i < kTile; ++i) s[i] = i < valid ? s[i] : -INFINITY;
@@ -186,6 +211,11 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
           for (int u = 0; u < 4; ++u) top[u] = max3(top[u], s[i + u], s[i + 4 + u]);
         }
         const float m_tile = fmaxf(max3(top[0], s[124], s[125]), max3(max3(top[1], s[126], s[127]), top[2], top[3]));
+        if (NT == 1 && j > 0) {                         // the weights and sums of the last tile are free again
+          ok = mbar_wait(smem_u32(&bars.pv_done[t]), (j - 1) & 1, limit);
+          if (!ok) break;
+          tc_fence_after();
+        }
         if (j == 0) m = m_tile;
         else if (__any_sync(0xFFFFFFFFu, (m_tile - m) * c > 8.0f)) {
           // the maximum moved by more than a factor of 2^8 in some row of the warp: rescale the sums so far. Smaller
@@ -217,7 +247,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
             add2(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], sum[2 * (i & 1)], sum[2 * (i & 1) + 1], p0, p1);
             p[i] = pack2<T>(p0, p1);
           }
-          tmem_st16(ts + g * 16, p);
+          tmem_st16(tp + g * 16, p);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tmem_wait_st();
@@ -226,28 +256,27 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[t]));
       }
       if (ok) {
-        ok = mbar_wait(smem_u32(&bars.o_full[t]), 0, limit);
+        ok = mbar_wait(smem_u32(&bars.pv_done[t]), NT == 1 ? (n - 1) & 1 : 0, limit);
         tc_fence_after();
       }
     }
     // ---- output -------------------------------------------------------------------------------
-    const bool exists = pair * 2 + t < row_tiles * a.group;
-    if (exists && named_barrier_and(1 + t, 128, ok)) {
-      const bool live = active[t] && row < nq;
+    if (exists(t) && named_barrier_and(1 + t, 128, ok)) {
+      const bool live = work && row < nq;
       const float inv = live && l != 0.0f ? 1.0f / l : 0.0f;
       uint8_t* out = sQ + t * kTileBytes;               // the query tile has been read by now
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
         float o[32];
-        if (active[t]) { tmem_ld32(to + g * 32, o); tmem_wait_ld(); }
+        if (work) { tmem_ld32(to + g * 32, o); tmem_wait_ld(); }
         store_row32<T>(out, quad * 32 + lane, g * 32, o, inv, live);
       }
       if (a.lse && row < a.queries)
-        a.lse[((int64_t)b * a.heads + head[t]) * a.queries + row] = live ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
+        a.lse[((int64_t)b * a.heads + head) * a.queries + row] = live ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
       fence_proxy_async();
       named_barrier(1 + t, 128);
-      if ((warp & 3) == 0 && lane == 0) {
-        store_tile<DB>(mo, smem_u32(out), row0[t], head[t], b);
+      if (quad == 0 && lane == 0) {
+        store_tile<DB>(mo, smem_u32(out), row0, head, b);
         bulk_commit();
         bulk_wait_read();
       }
@@ -256,11 +285,12 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   if (!ok && lane == 0) atomicExch(a.status, 1);
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) tmem_dealloc(tmem, 512);
+  if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
 }
 
-template <typename T, int DB>
+template <typename T, int DB, int NT>
 cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const TileMap& mk, const TileMap& mv, const TileMap& mo, cudaStream_t st) {
+  using Shape = FwdShape<DB, NT>;
   static bool attr_set[64] = {};
   static std::mutex attr_mutex;
   {
@@ -269,14 +299,14 @@ cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const Tile
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(attention_forward_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFwdSmem<DB>);
+      const cudaError_t e = cudaFuncSetAttribute(attention_forward_kernel<T, DB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
   }
-  const int row_tiles = (a.queries + kTile - 1) / kTile, pairs = (int)(((int64_t)row_tiles * a.group + 1) / 2);
-  const int64_t ctas = (int64_t)pairs * a.kv_heads * a.batch;
-  attention_forward_kernel<T, DB><<<(unsigned)ctas, kFwdThreads, kFwdSmem<DB>, st>>>(mq, mk, mv, mo, a, row_tiles, pairs);
+  const int row_tiles = (a.queries + kTile - 1) / kTile, tile_groups = (int)(((int64_t)row_tiles * a.group + NT - 1) / NT);
+  const int64_t ctas = (int64_t)tile_groups * a.kv_heads * a.batch;
+  attention_forward_kernel<T, DB, NT><<<(unsigned)ctas, Shape::kThreads, Shape::kSmem, st>>>(mq, mk, mv, mo, a, row_tiles, tile_groups);
   return cudaGetLastError();
 }
 
@@ -327,8 +357,8 @@ cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaS
   if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
   if (e != cudaSuccess) return e;
   if (dtype == SWARM_BF16)
-    return a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1>(a, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2>(a, mq, mk, mv, mo, st);
-  return a.head_dim <= 64 ? launch_forward<__half, 1>(a, mq, mk, mv, mo, st) : launch_forward<__half, 2>(a, mq, mk, mv, mo, st);
+    return a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1, 1>(a, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2, 2>(a, mq, mk, mv, mo, st);
+  return a.head_dim <= 64 ? launch_forward<__half, 1, 1>(a, mq, mk, mv, mo, st) : launch_forward<__half, 2, 2>(a, mq, mk, mv, mo, st);
 }
 
 }  // namespace swarm
