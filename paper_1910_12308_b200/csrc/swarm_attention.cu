@@ -92,7 +92,7 @@ int swarm_cross_attention_workspace(const swarm_attention* desc_host, int32_t ba
   if (!desc_ok(desc_host) || !bytes_host) return SWARM_EINVAL;
   AttentionArgs a{};
   fill(a, desc_host);
-  if (backward) *bytes_host = (size_t)a.batch * a.heads * a.queries * sizeof(float);
+  if (backward) *bytes_host = a.batch && a.queries && a.keys ? attention_backward_workspace(a) : 0;
   else *bytes_host = a.batch && a.queries && a.keys && few_rows(a) ? attention_rows_workspace(a) : 0;
   return SWARM_OK;
 }
@@ -149,11 +149,11 @@ int swarm_cross_attention_backward(const swarm_attention* desc_host, const void*
   AttentionArgs a{};
   fill(a, desc_host);
   a.q = q_dev; a.k = k_dev; a.v = v_dev; a.o = o_dev; a.dout = dout_dev; a.lse_in = lse_dev;
-  a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev; a.delta = reinterpret_cast<float*>(workspace_dev);
+  a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e = status_word(&a.status);
   if (d.queries > 0 && d.keys > 0) {
-    if (e == cudaSuccess) e = launch_attention_backward_tc(a, d.dtype, st);
+    if (e == cudaSuccess) e = launch_attention_backward_tc(a, d.dtype, workspace_dev, st);
   } else if (d.queries > 0) {
     if (e == cudaSuccess) e = launch_zero(dq_dev, d.dq, d.batch, d.queries, d.heads, d.head_dim, st);
   } else if (d.keys > 0) {

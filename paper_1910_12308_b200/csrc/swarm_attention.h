@@ -15,7 +15,9 @@ struct AttentionArgs {
   const float* lse_in;
   void *out, *dq, *dk, *dv;
   float* lse;
-  float* delta;                       // [batch][heads][queries] rowsum(dout * o)
+  // backward, per (sentence, head) padded to whole row tiles: lse * log2(e) and rowsum(dout * o) as the kernels use them,
+  // (infinity, 0) in rows that take no part
+  float *stat_lse, *stat_delta;
   const int32_t *query_lengths, *key_lengths;
   swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;
   int32_t batch, heads, kv_heads, group, queries, keys, head_dim;
@@ -32,7 +34,7 @@ __device__ __forceinline__ int64_t offset_of(const swarm_strides& s, int b, int 
   return b * s.batch + t * s.token + h * s.head;
 }
 
-// A strided tensor as tiles of 128 rows x 64 values of one head: coordinates (value, token, head, sentence), rows and
+// A strided tensor as tiles of `rows` rows x 64 values of one head: coordinates (value, token, head, sentence), rows and
 // values past the ends read as zero and are not written. A broadcast dimension (stride 0) has extent 1 in the map and
 // its coordinate is multiplied by 0.
 struct TileMap {
@@ -40,12 +42,13 @@ struct TileMap {
   int32_t token_step, head_step, batch_step;
 };
 cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, int dtype, int batch, int tokens, int heads,
-                          int head_dim);
+                          int head_dim, int rows);
 
 cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
 // Few query rows; the workspace holds the parts of split states.
 size_t attention_rows_workspace(const AttentionArgs& a);
 cudaError_t launch_attention_rows(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st);
-cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
+size_t attention_backward_workspace(const AttentionArgs& a);
+cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* workspace, cudaStream_t st);
 
 }  // namespace swarm

@@ -1,158 +1,200 @@
 // Cross attention, backward pass on the tensor cores.
 //
 // Two kernels, so that every gradient is summed by one CTA in a fixed order and nothing is added with atomics:
-//   attention_dq_kernel   CTA = 128 query rows: s and dp = dout v^T once per tile of states, dq = sum ds k; it also
-//                         writes delta = rowsum(dout * o)
+//   attention_dq_kernel   CTA = tiles of 128 query rows: s and dp = dout v^T once per 64 states, dq = sum ds k; it also
+//                         leaves lse and delta = rowsum(dout * o) as the other kernel wants them
 //   attention_dkv_kernel  CTA = 128 states of a key head: the transposed products, over all rows of all its query
 //                         heads: dv = sum p^T dout, dk = sum ds^T q
 // The price is s and dp computed twice: 7 products instead of 5.
 #include <mutex>
 
-#include "swarm_attention.h"
 #include "swarm_attention_tile.cuh"
 
 namespace swarm {
 namespace {
 
-constexpr int kBwdThreads = 320;                        // two warpgroups on the tile's values, copying warp, issuing warp
+// =================================================================================================
+// dq. NT row tiles per CTA, a warpgroup each (thread = row). Tensor memory of a tile: s (64 columns), dp (64) with ds
+// (16 bits) over it, dq. The scores of the next 64 states are computed as soon as these have been read into registers;
+// dp follows once dq has taken ds. While one tile's warps are at their exponentials, the other tile's products (NT = 2)
+// or the other CTA's of the multiprocessor (NT = 1, heads of up to 64 values) run.
+// =================================================================================================
+constexpr int kStep = 64;                               // states of a step
+constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64 values
 
-template <int DB> constexpr int kBwdStages = DB == 2 ? 2 : 4;          // pairs of tiles in flight
-template <int DB> constexpr int kBwdSmem = (2 + 2 * kBwdStages<DB>) * DB * kBlockBytes + 1024;
-
-struct BwdBars {
-  uint64_t fixed_full, full[4], empty[4], s_full, s_empty, dp_full, dp_empty, ds_full, ds_empty, done, drain;
+template <int DB, int NT> struct DqShape {
+  static constexpr int kThreads = 128 * (NT + 1);
+  static constexpr int kCtasPerSm = NT == 1 ? 2 : 1;
+  static constexpr int kRegs = NT == 1 ? 200 : 208, kRegsRest = NT == 1 ? 56 : 88;
+  static constexpr int kStages = NT == 1 ? 4 : 3;       // of (k, v)
+  static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
+  static constexpr uint32_t kColumns = NT == 1 ? 256 : 512;
 };
 
-// =================================================================================================
-// dq. Tensor memory: s at 0, dp at 128, ds (16 bits, 64 columns) at 256, dq at 384. While the warps turn tile j into
-// ds, the scores and dp of tile j + 1 are computed: each is overwritten as soon as it has been read into registers.
-// The warpgroups share the rows (warp % 4) and split the columns in halves.
-// =================================================================================================
-template <typename T, int DB>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+struct DqBars {
+  uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2], s_empty[2], dp_full[2], ds_full[2], done[2], drain;
+};
+
+template <typename T, int DB, int NT>
+__global__ void __launch_bounds__(DqShape<DB, NT>::kThreads, DqShape<DB, NT>::kCtasPerSm)
 attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
-                    const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdq, AttentionArgs a, int row_tiles) {
-  constexpr int kStages = kBwdStages<DB>;
-  constexpr uint32_t kTileBytes = DB * kBlockBytes;
+                    const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdq, AttentionArgs a, int row_tiles,
+                    int tile_groups) {
+  using Shape = DqShape<DB, NT>;
+  constexpr int kStages = Shape::kStages;
+  constexpr uint32_t kTileBytes = DB * kBlockBytes, kHalfBytes = DB * kStepBlock;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* sQ = smem;                                   // q, dout; dq on the way out
-  uint8_t* sKV = smem + 2 * kTileBytes;                 // ring of (k, v)
-  __shared__ BwdBars bars;
+  uint8_t* sQ = smem;                                   // per tile q, dout; dq on the way out
+  uint8_t* sKV = smem + NT * 2 * kTileBytes;            // ring of (k, v)
+  __shared__ DqBars bars;
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int qt = blockIdx.x % row_tiles, bh = blockIdx.x / row_tiles, h = bh % a.heads, b = bh / a.heads, hk = h / a.group;
+
+  // the row tiles of this CTA: tiles are numbered head after head within the group of a key head
+  const int first = blockIdx.x % tile_groups * NT, bh = blockIdx.x / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const int row0 = qt * kTile, n = row0 < nq ? (nk + kTile - 1) / kTile : 0;
+  const int n = (nk + kStep - 1) / kStep;
+  auto head_of = [&](int t) { return hk * a.group + (first + t) / row_tiles; };
+  auto row_of = [&](int t) { return (first + t) % row_tiles * kTile; };
+  auto exists = [&](int t) { return first + t < row_tiles * a.group; };
+  uint32_t act = 0;                                     // bit t: tile t has work
+#pragma unroll
+  for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
+  auto active = [&](int t) { return (act >> t & 1u) != 0; };
 
   if (tid == 0) {
-    mbar_init(smem_u32(&bars.fixed_full), 1);
-    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.empty[i]), 1); }
-    mbar_init(smem_u32(&bars.s_full), 1);
-    mbar_init(smem_u32(&bars.s_empty), 8);
-    mbar_init(smem_u32(&bars.dp_full), 1);
-    mbar_init(smem_u32(&bars.dp_empty), 8);
-    mbar_init(smem_u32(&bars.ds_full), 8);
-    mbar_init(smem_u32(&bars.ds_empty), 1);
-    mbar_init(smem_u32(&bars.done), 1);
+    for (int i = 0; i < NT; ++i) {
+      mbar_init(smem_u32(&bars.q_full[i]), 1);
+      mbar_init(smem_u32(&bars.s_full[i]), 1);
+      mbar_init(smem_u32(&bars.s_empty[i]), 4);
+      mbar_init(smem_u32(&bars.dp_full[i]), 1);
+      mbar_init(smem_u32(&bars.ds_full[i]), 4);
+      mbar_init(smem_u32(&bars.done[i]), 1);
+    }
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.kv_full[i]), 1); mbar_init(smem_u32(&bars.kv_empty[i]), 1); }
     mbar_init(smem_u32(&bars.drain), 1);
     fence_mbar_init();
   }
-  if (warp == 9) { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
+  if (warp == 4 * NT + 1) { tmem_alloc(smem_u32(&tmem_slot), Shape::kColumns); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot, limit = a.wait_limit;
   bool ok = true;
 
-  if (warp == 8) {
-    if (n) {
+  if (warp >= 4 * NT) {
+    regs_lower<Shape::kRegsRest>();
+    if (warp == 4 * NT && act) {
+      // ---- copies -----------------------------------------------------------------------------
       int issued = 0;
-      if (limit && lane == 0) {
-        const uint32_t bar = smem_u32(&bars.fixed_full);
-        mbar_expect_tx(bar, 2 * kTileBytes);
-        load_tile<DB>(smem_u32(sQ), mq, row0, h, b, bar);
-        load_tile<DB>(smem_u32(sQ) + kTileBytes, mdo, row0, h, b, bar);
+      if (limit && elect_one()) {
+        for (int t = 0; t < NT; ++t)
+          if (active(t)) {
+            const uint32_t bar = smem_u32(&bars.q_full[t]), dst = smem_u32(sQ) + 2 * t * kTileBytes;
+            mbar_expect_tx(bar, 2 * kTileBytes);
+            load_tile<DB>(dst, mq, row_of(t), head_of(t), b, bar);
+            load_tile<DB>(dst + kTileBytes, mdo, row_of(t), head_of(t), b, bar);
+          }
       }
       for (int j = 0; j < n; ++j) {
         const int st = j % kStages;
-        ok = mbar_wait(smem_u32(&bars.empty[st]), ((j / kStages) & 1) ^ 1, limit);
+        ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((j / kStages) & 1) ^ 1, limit);
         if (!ok) break;
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&bars.full[st]);
-          mbar_expect_tx(bar, 2 * kTileBytes);
-          load_tile<DB>(smem_u32(sKV) + 2 * st * kTileBytes, mk, j * kTile, hk, b, bar);
-          load_tile<DB>(smem_u32(sKV) + (2 * st + 1) * kTileBytes, mv, j * kTile, hk, b, bar);
+        if (elect_one()) {
+          const uint32_t bar = smem_u32(&bars.kv_full[st]), dst = smem_u32(sKV) + 2 * st * kHalfBytes;
+          mbar_expect_tx(bar, 2 * kHalfBytes);
+          load_tile<DB, kStep>(dst, mk, j * kStep, hk, b, bar);
+          load_tile<DB, kStep>(dst + kHalfBytes, mv, j * kStep, hk, b, bar);
         }
+        __syncwarp();
         issued = j + 1;
       }
       if (!ok) {
         // gave up: the copies in flight land before the CTA's shared memory is released
         for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
-          mbar_wait(smem_u32(&bars.full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
-        if (limit) mbar_wait(smem_u32(&bars.fixed_full), 0, kAttentionWaitLimit);
+          mbar_wait(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
+        for (int t = 0; t < NT; ++t)
+          if (active(t) && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
       }
-    }
-  } else if (warp == 9) {
-    if (n) {
+    } else if (warp == 4 * NT + 1 && act) {
+      // ---- products ---------------------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
       constexpr uint32_t kIdescDq = instr_desc_16<T>(kTile, DB * 64, 0, 1);
-      auto columns = [&](int j) { return (min(kTile, nk - j * kTile) + 15) & ~15; };
-      ok = mbar_wait(smem_u32(&bars.fixed_full), 0, limit);
-      for (int j = -1; j < n && ok; ++j) {
-        if (j + 1 < n) {
-          const int st = (j + 1) % kStages;
-          ok = mbar_wait(smem_u32(&bars.full[st]), ((j + 1) / kStages) & 1, limit);
-          if (!ok) break;
-          const int valid = min(kTile, nk - (j + 1) * kTile), cols = columns(j + 1);
-          if (valid < cols) zero_rows<DB>(sKV + 2 * st * kTileBytes, valid, cols, lane);   // k is a factor of dq
-          ok = mbar_wait(smem_u32(&bars.s_empty), (j & 1), limit);
+      auto columns = [&](int j) { return (min(kStep, nk - j * kStep) + 15) & ~15; };
+      auto scores = [&](int t, int j) {
+        mma_rows<T, kStep>(tmem + 256 * t, aq + 2 * t * kTileBytes, akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
+        tc_commit(smem_u32(&bars.s_full[t]));
+      };
+      auto dps = [&](int t, int j) {
+        mma_rows<T, kStep>(tmem + 256 * t + 64, aq + (2 * t + 1) * kTileBytes, akv + (2 * (j % kStages) + 1) * kHalfBytes, columns(j), ksteps);
+        tc_commit(smem_u32(&bars.dp_full[t]));
+      };
+      auto dqs = [&](int t, int j) {
+        const uint64_t dk = smem_desc_sw128(akv + 2 * (j % kStages) * kHalfBytes, kStepBlock, 1024);
+        for (int ks = 0; ks < columns(j) / 16; ++ks)
+          tc_mma_ts(tmem + 256 * t + 128, tmem + 256 * t + 64 + ks * 8, dk + (uint64_t)((ks * 2048) >> 4), kIdescDq, (j | ks) != 0);
+        if (j == n - 1) tc_commit(smem_u32(&bars.done[t]));
+      };
+      auto arrive_kv = [&](int j) {                     // waits for the states of step j; k is a factor of dq
+        if (!mbar_wait(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, limit)) return false;
+        const int valid = min(kStep, nk - j * kStep);
+        if (valid < columns(j)) zero_rows<DB, kStep>(sKV + 2 * (j % kStages) * kHalfBytes, valid, columns(j), lane);
+        return true;
+      };
+      ok = arrive_kv(0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (active(t) && ok) {
+          ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
           tc_fence_after();
-          if (ok && elect_one()) {
-            mma_rows<T>(tmem, aq, akv + 2 * st * kTileBytes, cols, ksteps);
-            tc_commit(smem_u32(&bars.s_full));
-          }
-          __syncwarp();
-          if (ok) ok = mbar_wait(smem_u32(&bars.dp_empty), (j & 1), limit);
-          tc_fence_after();
-          if (ok && elect_one()) {
-            mma_rows<T>(tmem + 128, aq + kTileBytes, akv + (2 * st + 1) * kTileBytes, cols, ksteps);
-            tc_commit(smem_u32(&bars.dp_full));
-          }
-          __syncwarp();
-        }
-        if (j >= 0 && ok) {
-          const int st = j % kStages;
-          ok = mbar_wait(smem_u32(&bars.ds_full), j & 1, limit);
-          tc_fence_after();
-          if (ok && elect_one()) {
-            const uint64_t dk = smem_desc_sw128(akv + 2 * st * kTileBytes, kBlockBytes, 1024);
-            for (int ks = 0; ks < columns(j) / 16; ++ks)
-              tc_mma_ts(tmem + 384, tmem + 256 + ks * 8, dk + (uint64_t)((ks * 2048) >> 4), kIdescDq, (j | ks) != 0);
-            tc_commit(smem_u32(&bars.ds_empty));
-            tc_commit(smem_u32(&bars.empty[st]));
-            if (j == n - 1) tc_commit(smem_u32(&bars.done));
-          }
+          if (ok && elect_one()) { scores(t, 0); dps(t, 0); }
           __syncwarp();
         }
+      for (int j = 0; j < n && ok; ++j) {
+        if (j + 1 < n) ok = arrive_kv(j + 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          if (active(t) && ok) {
+            if (j + 1 < n) {
+              ok = mbar_wait(smem_u32(&bars.s_empty[t]), j & 1, limit);
+              tc_fence_after();
+              if (ok && elect_one()) scores(t, j + 1);
+              __syncwarp();
+            }
+            if (ok) ok = mbar_wait(smem_u32(&bars.ds_full[t]), j & 1, limit);
+            tc_fence_after();
+            if (ok && elect_one()) {
+              dqs(t, j);
+              if (j + 1 < n) dps(t, j + 1);
+            }
+            __syncwarp();
+          }
+        if (ok && elect_one()) tc_commit(smem_u32(&bars.kv_empty[j % kStages]));
+        __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
         if (elect_one()) tc_commit(smem_u32(&bars.drain));
+        __syncwarp();
         mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
   } else {
-    const int half = warp >> 2, quad = warp & 3, tile_row = quad * 32 + lane, row = row0 + tile_row;
-    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-    const uint32_t ts = tmem + lane_base + half * 64, tdp = ts + 128, tds = tmem + lane_base + 256 + half * 32;
+    // ---- ds -----------------------------------------------------------------------------------
+    regs_raise<Shape::kRegs>();
+    const int t = NT == 1 ? 0 : warp >> 2, quad = warp & 3, head = head_of(t), row0 = row_of(t), tile_row = quad * 32 + lane;
+    const bool work = active(t);
+    const int row = row0 + tile_row;
+    const uint32_t ts = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = ts + 64;
     const float c = a.scale * kLog2e;
-    const int64_t at = ((int64_t)b * a.heads + h) * a.queries + row;
-    const bool live = row < nq && n > 0;
+    const bool live = work && row < nq;
     float delta = 0.0f, lse2 = INFINITY;
     if (live) {
-      const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, h);
-      const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, row, h);
+      const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
+      const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, row, head);
+      lse2 = a.lse_in[((int64_t)b * a.heads + head) * a.queries + row] * kLog2e;
+#pragma unroll 4
       for (int d = 0; d < a.head_dim; d += 8) {
         float x[8], y[8];
         unpack8<T>(load_raw8<T>(g + d), x);
@@ -160,48 +202,321 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
       }
-      lse2 = a.lse_in[at] * kLog2e;
     }
-    if (half == 0 && row < a.queries) a.delta[at] = delta;
-    for (int j = 0; j < n; ++j) {
-      const int valid = nk - j * kTile - half * 64;     // columns of this half that exist
-      float p[64];
-      ok = mbar_wait(smem_u32(&bars.s_full), j & 1, limit);
+    if (exists(t)) {
+      const int64_t at = ((int64_t)b * a.heads + head) * row_tiles * kTile + row;
+      a.stat_lse[at] = lse2 - kWeightShift<T>;
+      a.stat_delta[at] = delta * pow2_of(kWeightShift<T>);
+    }
+    if (work) {
+      for (int j = 0; j < n; ++j) {
+        const int valid = nk - j * kStep;
+        float p[kStep], dp[kStep];
+        ok = mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32(ts, p);
+        tmem_ld32(ts + 32, p + 32);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty[t]));
+#pragma unroll
+        for (int i = 0; i < kStep; i += 2) {
+          fma2(p[i], p[i + 1], p[i], p[i + 1], c, c, -lse2, -lse2);
+          p[i] = ex2(p[i]);
+          p[i + 1] = ex2(p[i + 1]);
+        }
+        ok = mbar_wait(smem_u32(&bars.dp_full[t]), j & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32(tdp, dp);
+        tmem_ld32(tdp + 32, dp + 32);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < kStep; i += 2) {
+          add2(dp[i], dp[i + 1], dp[i], dp[i + 1], -delta, -delta);
+          mul2(p[i], p[i + 1], p[i], p[i + 1], dp[i], dp[i + 1]);
+        }
+        if (valid < kStep) {
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) p[i] = i < valid ? p[i] : 0.0f;
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+          tmem_st16(tdp + g * 16, w);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.ds_full[t]));
+      }
+      if (ok) {
+        ok = mbar_wait(smem_u32(&bars.done[t]), 0, limit);
+        tc_fence_after();
+      }
+    }
+    if (exists(t) && named_barrier_and(1 + t, 128, ok)) {
+      uint8_t* out = sQ + 2 * t * kTileBytes;
+#pragma unroll
+      for (int g = 0; g < DB * 2; ++g) {
+        float o[32];
+        if (work) { tmem_ld32(ts + 128 + g * 32, o); tmem_wait_ld(); }
+        store_row32<T>(out, tile_row, g * 32, o, a.scale, live);
+      }
+      fence_proxy_async();
+      named_barrier(1 + t, 128);
+      if (quad == 0 && lane == 0) {
+        store_tile<DB>(mdq, smem_u32(out), row0, head, b);
+        bulk_commit();
+        bulk_wait_read();
+      }
+    }
+  }
+  if (!ok && lane == 0) atomicExch(a.status, 1);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
+}
+
+// =================================================================================================
+// dk and dv. Rows of the transposed tile are states (lanes), columns are 64 NW query rows, 64 for each of NW warpgroups.
+// Tensor memory: s^T with p^T (16 bits) over the columns that the same warpgroup read, dp^T with ds^T over it, dv, dk. The
+// warps turn s^T(i) into p^T while dp^T(i) is computed, and dp^T(i) into ds^T while dv takes p^T(i) and s^T(i + 1) is
+// computed. lse and delta of the columns travel with the row tiles.
+// =================================================================================================
+template <int DB, int NW> struct DkvShape {
+  static constexpr int kThreads = 128 * (NW + 1);
+  static constexpr int kCtasPerSm = NW == 1 ? 2 : 1;
+  static constexpr int kRegs = NW == 1 ? 200 : 208, kRegsRest = NW == 1 ? 56 : 88;
+  static constexpr int kRows = 64 * NW;                 // query rows of a step
+  static constexpr int kHalfBytes = DB * kRows * 128;   // of q or dout
+  static constexpr int kStages = NW == 1 ? 4 : 2;
+  static constexpr int kStatBytes = 2 * kRows * 4;
+  static constexpr int kSmem = 2 * DB * kBlockBytes + kStages * (2 * kHalfBytes + kStatBytes) + 1024;
+  static constexpr uint32_t kColumns = NW == 1 ? 256 : 512;
+  static constexpr uint32_t kDp = kRows, kDv = 2 * kRows, kDk = 2 * kRows + DB * 64;
+};
+
+struct DkvBars {
+  uint64_t kv_full, full[4], empty[4], s_full, p_full, dp_full, ds_full, done, drain;
+};
+
+template <typename T, int DB, int NW>
+__global__ void __launch_bounds__(DkvShape<DB, NW>::kThreads, DkvShape<DB, NW>::kCtasPerSm)
+attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
+                     const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdk, const __grid_constant__ TileMap mdv,
+                     AttentionArgs a, int key_tiles, int row_tiles) {
+  using Shape = DkvShape<DB, NW>;
+  constexpr int kStages = Shape::kStages, kRows = Shape::kRows;
+  constexpr uint32_t kTileBytes = DB * kBlockBytes, kHalfBytes = Shape::kHalfBytes;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* sKV = smem;                                  // k, v; dk, dv on the way out
+  uint8_t* sQ = smem + 2 * kTileBytes;                  // ring of (q, dout)
+  uint8_t* sStat = sQ + kStages * 2 * kHalfBytes;       // ring of (lse, delta)
+  __shared__ DkvBars bars;
+  __shared__ uint32_t tmem_slot;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int kt = blockIdx.x % key_tiles, bh = blockIdx.x / key_tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
+  const int key0 = kt * kTile, steps = (nq + kRows - 1) / kRows;       // steps of one head
+  const int n = key0 < nk ? steps * a.group : 0;
+
+  if (tid == 0) {
+    mbar_init(smem_u32(&bars.kv_full), 1);
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.empty[i]), 1); }
+    mbar_init(smem_u32(&bars.s_full), 1);
+    mbar_init(smem_u32(&bars.p_full), 4 * NW);
+    mbar_init(smem_u32(&bars.dp_full), 1);
+    mbar_init(smem_u32(&bars.ds_full), 4 * NW);
+    mbar_init(smem_u32(&bars.done), 1);
+    mbar_init(smem_u32(&bars.drain), 1);
+    fence_mbar_init();
+  }
+  if (warp == 4 * NW + 1) { tmem_alloc(smem_u32(&tmem_slot), Shape::kColumns); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot, limit = a.wait_limit;
+  bool ok = true;
+
+  if (warp >= 4 * NW) {
+    regs_lower<Shape::kRegsRest>();
+    if (warp == 4 * NW && n) {
+      // ---- copies -----------------------------------------------------------------------------
+      int issued = 0;
+      if (limit && elect_one()) {
+        const uint32_t bar = smem_u32(&bars.kv_full);
+        mbar_expect_tx(bar, 2 * kTileBytes);
+        load_tile<DB>(smem_u32(sKV), mk, key0, hk, b, bar);
+        load_tile<DB>(smem_u32(sKV) + kTileBytes, mv, key0, hk, b, bar);
+      }
+      int h = hk * a.group, row0 = 0;
+      for (int i = 0; i < n; ++i) {
+        const int st = i % kStages;
+        ok = mbar_wait(smem_u32(&bars.empty[st]), ((i / kStages) & 1) ^ 1, limit);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t bar = smem_u32(&bars.full[st]), dst = smem_u32(sQ) + 2 * st * kHalfBytes;
+          const uint32_t stat = smem_u32(sStat) + st * Shape::kStatBytes;
+          const int64_t at = ((int64_t)b * a.heads + h) * row_tiles * kTile + row0;
+          mbar_expect_tx(bar, 2 * kHalfBytes + Shape::kStatBytes);
+          load_tile<DB, kRows>(dst, mq, row0, h, b, bar);
+          load_tile<DB, kRows>(dst + kHalfBytes, mdo, row0, h, b, bar);
+          bulk_load(stat, a.stat_lse + at, kRows * 4, bar);
+          bulk_load(stat + kRows * 4, a.stat_delta + at, kRows * 4, bar);
+        }
+        __syncwarp();
+        issued = i + 1;
+        row0 += kRows;
+        if (row0 >= nq) { row0 = 0; ++h; }
+      }
+      if (!ok) {
+        // gave up: the copies in flight land before the CTA's shared memory is released
+        for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
+          mbar_wait(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
+        if (limit) mbar_wait(smem_u32(&bars.kv_full), 0, kAttentionWaitLimit);
+      }
+    } else if (warp == 4 * NW + 1 && n) {
+      // ---- products ---------------------------------------------------------------------------
+      const int ksteps = (a.head_dim + 15) / 16;
+      const uint32_t akv = smem_u32(sKV), aq = smem_u32(sQ);
+      constexpr uint32_t kIdescOut = instr_desc_16<T>(kTile, DB * 64, 0, 1);
+      const int last_valid = nq - (steps - 1) * kRows;  // rows of a head's last step
+      auto valid_rows = [&](int i) { return i % steps == steps - 1 ? last_valid : kRows; };
+      // products with p^T or ds^T: column 16 ks of the step lies at 8 ks of its warpgroup's 64 columns
+      auto outer = [&](uint32_t d, uint32_t left, uint32_t right, int i, int ks_n) {
+        const uint64_t db = smem_desc_sw128(right, kRows * 128, 1024);
+        for (int ks = 0; ks < ks_n; ++ks)
+          tc_mma_ts(d, left + (ks >> 2) * 64 + (ks & 3) * 8, db + (uint64_t)((ks * 2048) >> 4), kIdescOut, (i | ks) != 0);
+      };
+      ok = mbar_wait(smem_u32(&bars.kv_full), 0, limit);
+      int cols = 0, cols_next = 0;                      // of steps i and i + 1
+      for (int i = -1; i < n && ok; ++i) {
+        const int st = i % kStages, next = (i + 1) % kStages;
+        cols = cols_next;
+        if (i >= 0) {
+          ok = mbar_wait(smem_u32(&bars.p_full), i & 1, limit);
+          tc_fence_after();
+          if (ok && elect_one()) outer(tmem + Shape::kDv, tmem, aq + (2 * st + 1) * kHalfBytes, i, cols / 16);
+          __syncwarp();
+        }
+        if (i + 1 < n && ok) {
+          ok = mbar_wait(smem_u32(&bars.full[next]), ((i + 1) / kStages) & 1, limit);
+          if (!ok) break;
+          const int valid = valid_rows(i + 1);
+          cols_next = (valid + 15) & ~15;
+          if (valid < cols_next) {                      // q and dout are factors of dk and dv
+            zero_rows<DB, kRows>(sQ + 2 * next * kHalfBytes, valid, cols_next, lane);
+            zero_rows<DB, kRows>(sQ + (2 * next + 1) * kHalfBytes, valid, cols_next, lane);
+          }
+          tc_fence_after();
+          if (elect_one()) {
+            mma_rows<T, kRows>(tmem, akv, aq + 2 * next * kHalfBytes, cols_next, ksteps);
+            tc_commit(smem_u32(&bars.s_full));
+          }
+          __syncwarp();
+        }
+        if (i >= 0 && ok) {
+          ok = mbar_wait(smem_u32(&bars.ds_full), i & 1, limit);
+          tc_fence_after();
+          if (ok && elect_one()) {
+            outer(tmem + Shape::kDk, tmem + Shape::kDp, aq + 2 * st * kHalfBytes, i, cols / 16);
+            tc_commit(smem_u32(&bars.empty[st]));
+            if (i == n - 1) tc_commit(smem_u32(&bars.done));
+          }
+          __syncwarp();
+        }
+        if (i + 1 < n && ok && elect_one()) {
+          mma_rows<T, kRows>(tmem + Shape::kDp, akv + kTileBytes, aq + (2 * next + 1) * kHalfBytes, cols_next, ksteps);
+          tc_commit(smem_u32(&bars.dp_full));
+        }
+        __syncwarp();
+      }
+      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
+        if (elect_one()) tc_commit(smem_u32(&bars.drain));
+        __syncwarp();
+        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
+      }
+    }
+  } else {
+    // ---- p and ds -----------------------------------------------------------------------------
+    regs_raise<Shape::kRegs>();
+    const int half = NW == 1 ? 0 : warp >> 2, quad = warp & 3, tile_row = quad * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t ts = tmem + lane_base + half * 64, tdp = ts + Shape::kDp;
+    const float c = a.scale * kLog2e;
+    constexpr float kUnshift = pow2_of(kWeightShift<T>);
+    int step = 0;
+    for (int i = 0; i < n; ++i) {
+      const int cols = (step == steps - 1 ? nq - step * kRows : kRows) - half * 64;   // columns of this warpgroup that exist
+      if (++step == steps) step = 0;
+      const float* lse2 = reinterpret_cast<const float*>(sStat + i % kStages * Shape::kStatBytes) + half * 64;
+      const float* delta = lse2 + kRows;
+      float p[64], stat[32];
+      ok = mbar_wait(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, limit);
+      if (!ok) break;
+      load_stats(stat, lse2);
+      ok = mbar_wait(smem_u32(&bars.s_full), i & 1, limit);
       if (!ok) break;
       tc_fence_after();
       tmem_ld32(ts, p);
       tmem_ld32(ts + 32, p + 32);
       tmem_wait_ld();
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        uint32_t w[16];
+#pragma unroll
+        for (int q = 0; q < 32; q += 2) fma2(p[g * 32 + q], p[g * 32 + q + 1], p[g * 32 + q], p[g * 32 + q + 1], c, c, -stat[q], -stat[q + 1]);
+        if (g == 0) load_stats(stat, lse2 + 32);        // arrive under the exponentials
+        else load_stats(stat, delta);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) p[g * 32 + q] = ex2(p[g * 32 + q]);
+        if (cols < 64) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q) p[g * 32 + q] = g * 32 + q < cols ? p[g * 32 + q] : 0.0f;   // what lies there is not a score
+        }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) w[q] = pack2<T>(p[g * 32 + 2 * q], p[g * 32 + 2 * q + 1]);
+        tmem_st16(ts + g * 16, w);
+      }
+      tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty));
-#pragma unroll
-      for (int i = 0; i < 64; ++i) p[i] = ex2(fmaf(p[i], c, -lse2));
-      ok = mbar_wait(smem_u32(&bars.dp_full), j & 1, limit);
+      if (lane == 0) mbar_arrive(smem_u32(&bars.p_full));
+      ok = mbar_wait(smem_u32(&bars.dp_full), i & 1, limit);
       if (!ok) break;
       tc_fence_after();
       float dp[64];
       tmem_ld32(tdp, dp);
       tmem_ld32(tdp + 32, dp + 32);
       tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.dp_empty));
-#pragma unroll
-      for (int i = 0; i < 64; ++i) p[i] = p[i] * (dp[i] - delta);
-      if (valid < 64) {
-#pragma unroll
-        for (int i = 0; i < 64; ++i) p[i] = i < valid ? p[i] : 0.0f;
-      }
-      ok = mbar_wait(smem_u32(&bars.ds_empty), (j & 1) ^ 1, limit);
-      if (!ok) break;
-      tc_fence_after();
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
-        tmem_st16(tds + g * 16, w);
+        for (int q = 0; q < 32; q += 2) {
+          float* d = dp + g * 32 + q;
+          if (kUnshift == 1.0f) add2(d[0], d[1], d[0], d[1], -stat[q], -stat[q + 1]);
+          else fma2(d[0], d[1], d[0], d[1], kUnshift, kUnshift, -stat[q], -stat[q + 1]);
+        }
+        if (g == 0) load_stats(stat, delta + 32);
+#pragma unroll
+        for (int q = 0; q < 32; q += 2) {
+          float* d = dp + g * 32 + q;
+          mul2(d[0], d[1], d[0], d[1], p[g * 32 + q], p[g * 32 + q + 1]);
+        }
+        if (cols < 64) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q) dp[g * 32 + q] = g * 32 + q < cols ? dp[g * 32 + q] : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) w[q] = pack2<T>(dp[g * 32 + 2 * q], dp[g * 32 + 2 * q + 1]);
+        tmem_st16(tdp + g * 16, w);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -212,260 +527,25 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       ok = mbar_wait(smem_u32(&bars.done), 0, limit);
       tc_fence_after();
     }
-    if (named_barrier_and(1, 256, ok)) {
-      // warpgroup `half` takes the output's columns [32 DB half, +32 DB)
-#pragma unroll
-      for (int g = 0; g < DB; ++g) {
-        const int col = half * 32 * DB + g * 32;
-        float o[32];
-        if (n) { tmem_ld32(tmem + lane_base + 384 + col, o); tmem_wait_ld(); }
-        store_row32<T>(sQ, tile_row, col, o, live ? a.scale : 0.0f, live);
-      }
-      fence_proxy_async();
-      named_barrier(1, 256);
-      if (tid == 0) {
-        store_tile<DB>(mdq, smem_u32(sQ), row0, h, b);
-        bulk_commit();
-        bulk_wait_read();
-      }
-    }
-  }
-  if (!ok && lane == 0) atomicExch(a.status, 1);
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 9) tmem_dealloc(tmem, 512);
-}
-
-// =================================================================================================
-// dk and dv. Rows of the transposed tile are states (lanes), columns are query rows. Tensor memory: s^T at 0 with p^T
-// (16 bits) written over the half that each warpgroup read, dp^T at 128 with ds^T over it, dv at 256, dk at 384. The
-// warps turn s^T(i) into p^T while dp^T(i) is computed, and dp^T(i) into ds^T while dv takes p^T(i) and s^T(i + 1) is
-// computed.
-// =================================================================================================
-template <typename T, int DB>
-__global__ void __launch_bounds__(kBwdThreads, 1)
-attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
-                     const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdk, const __grid_constant__ TileMap mdv,
-                     AttentionArgs a, int key_tiles) {
-  constexpr int kStages = kBwdStages<DB>;
-  constexpr uint32_t kTileBytes = DB * kBlockBytes;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* sKV = smem;                                  // k, v; dk, dv on the way out
-  uint8_t* sQ = smem + 2 * kTileBytes;                  // ring of (q, dout)
-  __shared__ BwdBars bars;
-  __shared__ uint32_t tmem_slot;
-  __shared__ __align__(16) float s_lse[2][kTile], s_delta[2][kTile];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int kt = blockIdx.x % key_tiles, bh = blockIdx.x / key_tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
-  const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const int key0 = kt * kTile, row_tiles = (nq + kTile - 1) / kTile;
-  const int n = key0 < nk ? row_tiles * a.group : 0;
-
-  if (tid == 0) {
-    mbar_init(smem_u32(&bars.fixed_full), 1);
-    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.empty[i]), 1); }
-    mbar_init(smem_u32(&bars.s_full), 1);
-    mbar_init(smem_u32(&bars.s_empty), 8);              // p^T has been written
-    mbar_init(smem_u32(&bars.dp_full), 1);
-    mbar_init(smem_u32(&bars.ds_full), 8);
-    mbar_init(smem_u32(&bars.done), 1);
-    mbar_init(smem_u32(&bars.drain), 1);
-    fence_mbar_init();
-  }
-  if (warp == 9) { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_slot, limit = a.wait_limit;
-  bool ok = true;
-
-  if (warp == 8) {
-    if (n) {
-      int issued = 0;
-      if (limit && lane == 0) {
-        const uint32_t bar = smem_u32(&bars.fixed_full);
-        mbar_expect_tx(bar, 2 * kTileBytes);
-        load_tile<DB>(smem_u32(sKV), mk, key0, hk, b, bar);
-        load_tile<DB>(smem_u32(sKV) + kTileBytes, mv, key0, hk, b, bar);
-      }
-      for (int i = 0; i < n; ++i) {
-        const int st = i % kStages, h = hk * a.group + i / row_tiles, row0 = i % row_tiles * kTile;
-        ok = mbar_wait(smem_u32(&bars.empty[st]), ((i / kStages) & 1) ^ 1, limit);
-        if (!ok) break;
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&bars.full[st]);
-          mbar_expect_tx(bar, 2 * kTileBytes);
-          load_tile<DB>(smem_u32(sQ) + 2 * st * kTileBytes, mq, row0, h, b, bar);
-          load_tile<DB>(smem_u32(sQ) + (2 * st + 1) * kTileBytes, mdo, row0, h, b, bar);
-        }
-        issued = i + 1;
-      }
-      if (!ok) {
-        // gave up: the copies in flight land before the CTA's shared memory is released
-        for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-          mbar_wait(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
-        if (limit) mbar_wait(smem_u32(&bars.fixed_full), 0, kAttentionWaitLimit);
-      }
-    }
-  } else if (warp == 9) {
-    if (n) {
-      const int ksteps = (a.head_dim + 15) / 16;
-      const uint32_t akv = smem_u32(sKV), aq = smem_u32(sQ);
-      constexpr uint32_t kIdescOut = instr_desc_16<T>(kTile, DB * 64, 0, 1);
-      auto columns = [&](int i) { return (min(kTile, nq - i % row_tiles * kTile) + 15) & ~15; };
-      // products with p^T or ds^T: column 16 ks of the tile lies at 8 ks of its warpgroup's half
-      auto outer = [&](uint32_t d, uint32_t left, uint32_t right, int i) {
-        const uint64_t db = smem_desc_sw128(right, kBlockBytes, 1024);
-        for (int ks = 0; ks < columns(i) / 16; ++ks)
-          tc_mma_ts(d, left + (ks >> 2) * 64 + (ks & 3) * 8, db + (uint64_t)((ks * 2048) >> 4), kIdescOut, (i | ks) != 0);
-      };
-      ok = mbar_wait(smem_u32(&bars.fixed_full), 0, limit);
-      for (int i = -1; i < n && ok; ++i) {
-        const int st = i % kStages, next = (i + 1) % kStages;
-        if (i >= 0) {
-          ok = mbar_wait(smem_u32(&bars.s_empty), i & 1, limit);
-          tc_fence_after();
-          if (ok && elect_one()) outer(tmem + 256, tmem, aq + (2 * st + 1) * kTileBytes, i);
-          __syncwarp();
-        }
-        if (i + 1 < n && ok) {
-          ok = mbar_wait(smem_u32(&bars.full[next]), ((i + 1) / kStages) & 1, limit);
-          if (!ok) break;
-          const int valid = min(kTile, nq - (i + 1) % row_tiles * kTile), cols = columns(i + 1);
-          if (valid < cols) {                           // q and dout are factors of dk and dv
-            zero_rows<DB>(sQ + 2 * next * kTileBytes, valid, cols, lane);
-            zero_rows<DB>(sQ + (2 * next + 1) * kTileBytes, valid, cols, lane);
-          }
-          if (elect_one()) {
-            mma_rows<T>(tmem, akv, aq + 2 * next * kTileBytes, cols, ksteps);
-            tc_commit(smem_u32(&bars.s_full));
-          }
-          __syncwarp();
-        }
-        if (i >= 0 && ok) {
-          ok = mbar_wait(smem_u32(&bars.ds_full), i & 1, limit);
-          tc_fence_after();
-          if (ok && elect_one()) {
-            outer(tmem + 384, tmem + 128, aq + 2 * st * kTileBytes, i);
-            tc_commit(smem_u32(&bars.empty[st]));
-            if (i == n - 1) tc_commit(smem_u32(&bars.done));
-          }
-          __syncwarp();
-        }
-        if (i + 1 < n && ok && elect_one()) {
-          mma_rows<T>(tmem + 128, akv + kTileBytes, aq + (2 * next + 1) * kTileBytes, columns(i + 1), ksteps);
-          tc_commit(smem_u32(&bars.dp_full));
-        }
-        __syncwarp();
-      }
-      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (elect_one()) tc_commit(smem_u32(&bars.drain));
-        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
-      }
-    }
-  } else {
-    const int half = warp >> 2, quad = warp & 3, tile_row = quad * 32 + lane;
-    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-    const uint32_t ts = tmem + lane_base + half * 64, tdp = ts + 128;
-    const float c = a.scale * kLog2e;
-    constexpr float kUnshift = pow2_of(kWeightShift<T>);
-    // lse and delta of tile i, shifted so that p comes out as a multiple of 2^-shift and ds does not: thread r of a warpgroup fetches row r (warpgroup 0 lse, warpgroup 1 delta)
-    auto fetch = [&](int i) {
-      const int h = hk * a.group + i / row_tiles, row = i % row_tiles * kTile + tile_row;
-      const int64_t at = ((int64_t)b * a.heads + h) * a.queries + row;
-      if (row >= nq) return half == 0 ? INFINITY : 0.0f;
-      return half == 0 ? a.lse_in[at] * kLog2e - kWeightShift<T> : a.delta[at] * kUnshift;
-    };
-    float ahead = n ? fetch(0) : 0.0f;
-    for (int i = 0; i < n; ++i) {
-      const int cols = min(kTile, nq - i % row_tiles * kTile) - half * 64;            // columns of this half that exist
-      (half == 0 ? s_lse : s_delta)[i & 1][tile_row] = ahead;
-      named_barrier(1, 256);                            // both sets are there; their last readers passed two barriers ago
-      if (i + 1 < n) ahead = fetch(i + 1);
-      const float* lse2 = s_lse[i & 1] + half * 64;
-      const float* delta = s_delta[i & 1] + half * 64;
-      float p[64];
-      ok = mbar_wait_if(smem_u32(&bars.s_full), i & 1, limit, ok);
-      tc_fence_after();
-      if (ok) {
-        tmem_ld32(ts, p);
-        tmem_ld32(ts + 32, p + 32);
-        tmem_wait_ld();
-#pragma unroll
-        for (int q = 0; q < 64; q += 4) {
-          const float4 l4 = *reinterpret_cast<const float4*>(lse2 + q);
-          p[q] = ex2(fmaf(p[q], c, -l4.x));
-          p[q + 1] = ex2(fmaf(p[q + 1], c, -l4.y));
-          p[q + 2] = ex2(fmaf(p[q + 2], c, -l4.z));
-          p[q + 3] = ex2(fmaf(p[q + 3], c, -l4.w));
-        }
-        if (cols < 64) {
-#pragma unroll
-          for (int q = 0; q < 64; ++q) p[q] = q < cols ? p[q] : 0.0f;                 // what lies there is not a score
-        }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          uint32_t w[16];
-#pragma unroll
-          for (int q = 0; q < 16; ++q) w[q] = pack2<T>(p[g * 32 + 2 * q], p[g * 32 + 2 * q + 1]);
-          tmem_st16(ts + g * 16, w);
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty));
-      }
-      ok = mbar_wait_if(smem_u32(&bars.dp_full), i & 1, limit, ok);
-      tc_fence_after();
-      if (ok) {
-        float dp[64];
-        tmem_ld32(tdp, dp);
-        tmem_ld32(tdp + 32, dp + 32);
-        tmem_wait_ld();
-#pragma unroll
-        for (int q = 0; q < 64; q += 4) {
-          const float4 d4 = *reinterpret_cast<const float4*>(delta + q);
-          dp[q] = p[q] * fmaf(dp[q], kUnshift, -d4.x);
-          dp[q + 1] = p[q + 1] * fmaf(dp[q + 1], kUnshift, -d4.y);
-          dp[q + 2] = p[q + 2] * fmaf(dp[q + 2], kUnshift, -d4.z);
-          dp[q + 3] = p[q + 3] * fmaf(dp[q + 3], kUnshift, -d4.w);
-        }
-        if (cols < 64) {
-#pragma unroll
-          for (int q = 0; q < 64; ++q) dp[q] = q < cols ? dp[q] : 0.0f;
-        }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          uint32_t w[16];
-#pragma unroll
-          for (int q = 0; q < 16; ++q) w[q] = pack2<T>(dp[g * 32 + 2 * q], dp[g * 32 + 2 * q + 1]);
-          tmem_st16(tdp + g * 16, w);
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.ds_full));
-      }
-    }
-    if (ok && n) {
-      ok = mbar_wait(smem_u32(&bars.done), 0, limit);
-      tc_fence_after();
-    }
-    if (named_barrier_and(1, 256, ok)) {
-      // warpgroup 0 writes dv, warpgroup 1 dk
+    if (named_barrier_and(1, 128 * NW, ok)) {
+      // two warpgroups write dv and dk, one writes both
       const bool live = n > 0 && key0 + tile_row < nk;
-      uint8_t* out = sKV + (half == 0 ? kTileBytes : 0u);
 #pragma unroll
-      for (int g = 0; g < DB * 2; ++g) {
-        float o[32];
-        if (n) { tmem_ld32(tmem + lane_base + 256 + half * 128 + g * 32, o); tmem_wait_ld(); }
-        store_row32<T>(out, tile_row, g * 32, o, half == 0 ? kUnshift : a.scale, live);
+      for (int which = 0; which < 2; ++which) {
+        if (NW == 2 && which != half) continue;
+        uint8_t* out = sKV + (which == 0 ? kTileBytes : 0u);
+#pragma unroll
+        for (int g = 0; g < DB * 2; ++g) {
+          float o[32];
+          if (n) { tmem_ld32(tmem + lane_base + (which == 0 ? Shape::kDv : Shape::kDk) + g * 32, o); tmem_wait_ld(); }
+          store_row32<T>(out, tile_row, g * 32, o, which == 0 ? kUnshift : a.scale, live);
+        }
       }
       fence_proxy_async();
-      named_barrier(2 + half, 128);
-      if ((warp & 3) == 0 && lane == 0) {
-        store_tile<DB>(half == 0 ? mdv : mdk, smem_u32(out), key0, hk, b);
+      named_barrier(1, 128 * NW);
+      if (tid == 0) {
+        store_tile<DB>(mdv, smem_u32(sKV) + kTileBytes, key0, hk, b);
+        store_tile<DB>(mdk, smem_u32(sKV), key0, hk, b);
         bulk_commit();
         bulk_wait_read();
       }
@@ -474,11 +554,13 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
   if (!ok && lane == 0) atomicExch(a.status, 1);
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) tmem_dealloc(tmem, 512);
+  if (warp == 4 * NW + 1) tmem_dealloc(tmem, Shape::kColumns);
 }
 
 template <typename T, int DB>
 cudaError_t launch_backward(const AttentionArgs& a, int dtype, cudaStream_t st) {
+  using Dq = DqShape<DB, DB>;                           // heads of up to 64 values: one tile and two CTAs per multiprocessor
+  using Dkv = DkvShape<DB, DB>;
   static bool attr_set[64] = {};
   static std::mutex attr_mutex;
   {
@@ -487,32 +569,48 @@ cudaError_t launch_backward(const AttentionArgs& a, int dtype, cudaStream_t st) 
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      cudaError_t e = cudaFuncSetAttribute(attention_dq_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBwdSmem<DB>);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBwdSmem<DB>);
+      cudaError_t e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dkv::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
   }
   TileMap mq, mk, mv, mdo, mdq, mdk, mdv;
-  cudaError_t e = make_tile_map(&mq, a.q, a.qs, dtype, a.batch, a.queries, a.heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mdo, a.dout, a.dos, dtype, a.batch, a.queries, a.heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mdq, a.dq, a.dqs, dtype, a.batch, a.queries, a.heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mk, a.k, a.ks, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mdk, a.dk, a.dks, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mdv, a.dv, a.dvs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
+  auto rows = [&](TileMap* m, const void* p, const swarm_strides& s, int box) { return make_tile_map(m, p, s, dtype, a.batch, a.queries, a.heads, a.head_dim, box); };
+  auto states = [&](TileMap* m, const void* p, const swarm_strides& s, int box) { return make_tile_map(m, p, s, dtype, a.batch, a.keys, a.kv_heads, a.head_dim, box); };
+  cudaError_t e = rows(&mq, a.q, a.qs, kTile);
+  if (e == cudaSuccess) e = rows(&mdo, a.dout, a.dos, kTile);
+  if (e == cudaSuccess) e = rows(&mdq, a.dq, a.dqs, kTile);
+  if (e == cudaSuccess) e = states(&mk, a.k, a.ks, kStep);
+  if (e == cudaSuccess) e = states(&mv, a.v, a.vs, kStep);
   if (e != cudaSuccess) return e;
   const int row_tiles = (a.queries + kTile - 1) / kTile, key_tiles = (a.keys + kTile - 1) / kTile;
-  attention_dq_kernel<T, DB><<<(unsigned)((int64_t)row_tiles * a.heads * a.batch), kBwdThreads, kBwdSmem<DB>, st>>>(mq, mk, mv, mdo, mdq, a, row_tiles);
-  attention_dkv_kernel<T, DB><<<(unsigned)((int64_t)key_tiles * a.kv_heads * a.batch), kBwdThreads, kBwdSmem<DB>, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles);
+  const int tile_groups = (int)(((int64_t)row_tiles * a.group + DB - 1) / DB);
+  attention_dq_kernel<T, DB, DB><<<(unsigned)((int64_t)tile_groups * a.kv_heads * a.batch), Dq::kThreads, Dq::kSmem, st>>>(
+      mq, mk, mv, mdo, mdq, a, row_tiles, tile_groups);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = rows(&mq, a.q, a.qs, Dkv::kRows);
+  if (e == cudaSuccess) e = rows(&mdo, a.dout, a.dos, Dkv::kRows);
+  if (e == cudaSuccess) e = states(&mk, a.k, a.ks, kTile);
+  if (e == cudaSuccess) e = states(&mv, a.v, a.vs, kTile);
+  if (e == cudaSuccess) e = states(&mdk, a.dk, a.dks, kTile);
+  if (e == cudaSuccess) e = states(&mdv, a.dv, a.dvs, kTile);
+  if (e != cudaSuccess) return e;
+  attention_dkv_kernel<T, DB, DB><<<(unsigned)((int64_t)key_tiles * a.kv_heads * a.batch), Dkv::kThreads, Dkv::kSmem, st>>>(
+      mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles);
   return cudaGetLastError();
 }
 
+int64_t stat_count(const AttentionArgs& a) { return (int64_t)a.batch * a.heads * ((a.queries + kTile - 1) / kTile) * kTile; }
+
 }  // namespace
 
-cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int dtype, cudaStream_t st) {
-  if (dtype == SWARM_BF16)
-    return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, dtype, st);
+size_t attention_backward_workspace(const AttentionArgs& a) { return (size_t)stat_count(a) * 2 * sizeof(float); }
+
+cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* workspace, cudaStream_t st) {
+  a.stat_lse = reinterpret_cast<float*>(workspace);
+  a.stat_delta = a.stat_lse + stat_count(a);
+  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, dtype, st);
   return a.head_dim <= 64 ? launch_backward<__half, 1>(a, dtype, st) : launch_backward<__half, 2>(a, dtype, st);
 }
 

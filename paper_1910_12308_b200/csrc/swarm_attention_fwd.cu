@@ -313,7 +313,7 @@ cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const Tile
 }  // namespace
 
 cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, int dtype, int batch, int tokens, int heads,
-                          int head_dim) {
+                          int head_dim, int rows) {
   typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -342,7 +342,7 @@ cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, i
       *step[i] = 1;
     }
   }
-  const cuuint32_t box[4] = {64, (cuuint32_t)kTile, 1, 1}, ones[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, ones[4] = {1, 1, 1, 1};
   const CUresult r = encode(&out->map, dtype == SWARM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
                             const_cast<void*>(p), dims, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -351,10 +351,10 @@ cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, i
 
 cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st) {
   TileMap mq, mk, mv, mo;
-  cudaError_t e = make_tile_map(&mq, a.q, a.qs, dtype, a.batch, a.queries, a.heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mo, a.out, a.os, dtype, a.batch, a.queries, a.heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mk, a.k, a.ks, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
-  if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim);
+  cudaError_t e = make_tile_map(&mq, a.q, a.qs, dtype, a.batch, a.queries, a.heads, a.head_dim, kTile);
+  if (e == cudaSuccess) e = make_tile_map(&mo, a.out, a.os, dtype, a.batch, a.queries, a.heads, a.head_dim, kTile);
+  if (e == cudaSuccess) e = make_tile_map(&mk, a.k, a.ks, dtype, a.batch, a.keys, a.kv_heads, a.head_dim, kTile);
+  if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim, kTile);
   if (e != cudaSuccess) return e;
   if (dtype == SWARM_BF16)
     return a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1, 1>(a, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2, 2>(a, mq, mk, mv, mo, st);

@@ -1,4 +1,4 @@
-// Tiles of the attention kernels: 128 rows of one head in shared memory as blocks of 128 rows x 64 values with the
+// Tiles of the attention kernels: rows of one head in shared memory (64 or 128 of them) as blocks of their rows x 64 values with the
 // 128-byte swizzle, which TMA writes and reads and the products take as operands (rows by rows or transposed).
 #pragma once
 #include "swarm_attention.h"
@@ -29,22 +29,22 @@ __device__ __forceinline__ uint32_t swizzled(int row, int chunk) { return (uint3
 
 // Zeroes rows [first, last) of a tile of DB blocks; called by one warp. The rows are in an operand of a product whose
 // other factor is 0 there, and hold whatever lies past a sentence's end.
-template <int DB>
+template <int DB, int ROWS = kTile>
 __device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last, int lane) {
   for (int i = lane; i < (last - first) * 8 * DB; i += 32) {
     const int row = first + i / (8 * DB), c = i % (8 * DB);
-    *reinterpret_cast<uint4*>(tile + (c >> 3) * kBlockBytes + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(tile + (c >> 3) * (ROWS * 128) + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
   }
   fence_proxy_async();
   __syncwarp();
 }
 
 // One thread: the copies of a tile (the barrier is told of its bytes beforehand).
-template <int DB>
+template <int DB, int ROWS = kTile>
 __device__ __forceinline__ void load_tile(uint32_t dst, const TileMap& m, int row0, int head, int b, uint32_t bar) {
 #pragma unroll
   for (int d = 0; d < DB; ++d)
-    tma_load_4d(dst + d * kBlockBytes, &m.map, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step, bar);
+    tma_load_4d(dst + d * (ROWS * 128), &m.map, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step, bar);
 }
 template <int DB>
 __device__ __forceinline__ void store_tile(const TileMap& m, uint32_t src, int row0, int head, int b) {
@@ -53,14 +53,15 @@ __device__ __forceinline__ void store_tile(const TileMap& m, uint32_t src, int r
     tma_store_4d(&m.map, src + d * kBlockBytes, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step);
 }
 
-// One thread: D[128 x cols] = A[128 x dim] B[cols x dim]^T, both tiles in shared memory, dim = 16 ksteps.
-template <typename T>
+// One thread: D[128 x cols] = A[128 x dim] B[cols x dim]^T, dim = 16 ksteps; tile A in shared memory with 128 rows, tile
+// B with ROWS.
+template <typename T, int ROWS = kTile>
 __device__ __forceinline__ void mma_rows(uint32_t tmem_d, uint32_t tile_a, uint32_t tile_b, int cols, int ksteps) {
   const uint32_t idesc = instr_desc_16<T>(kTile, 0, 0, 0) + ((uint32_t)(cols >> 3) << 17);
   const uint64_t da = smem_desc_sw128(tile_a, 16, 1024), db = smem_desc_sw128(tile_b, 16, 1024);
   for (int ks = 0; ks < ksteps; ++ks) {
-    const uint64_t at = (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4);
-    tc_mma(tmem_d, da + at, db + at, idesc, ks != 0);
+    tc_mma(tmem_d, da + (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4),
+           db + (uint64_t)(((ks >> 2) * (ROWS * 128) + (ks & 3) * 32) >> 4), idesc, ks != 0);
   }
 }
 
@@ -73,6 +74,15 @@ __device__ __forceinline__ void store_row32(uint8_t* tile, int row, int col, con
 #pragma unroll
     for (int u = 0; u < 4; ++u) w[u] = live ? pack2<T>(v[ch * 8 + 2 * u] * factor, v[ch * 8 + 2 * u + 1] * factor) : 0u;
     *reinterpret_cast<uint4*>(tile + (col >> 6) * kBlockBytes + swizzled(row, ((col & 63) >> 3) + ch)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// 32 consecutive floats of shared memory, the same for all threads.
+__device__ __forceinline__ void load_stats(float* v, const float* p) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float4 x = reinterpret_cast<const float4*>(p)[i];
+    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
   }
 }
 

@@ -142,6 +142,11 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t sr
   asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
                :: "l"((uint64_t)map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
+// Copy of `bytes` (a multiple of 16) consecutive bytes between 16-byte boundaries.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               :: "r"(dst), "l"((uint64_t)__cvta_generic_to_global(src)), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 // Barrier of a part of the CTA (id 1..15).
@@ -155,11 +160,6 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) 
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)ok) : "memory");
   return r != 0;
-}
-
-// mbar_wait for warps that stay in step with others after a wait that gave up: nothing is waited for once ok is false.
-__device__ __forceinline__ bool mbar_wait_if(uint32_t bar, uint32_t parity, uint32_t limit, bool ok) {
-  return ok && mbar_wait(bar, parity, limit);
 }
 
 // True in one lane of a whole warp. Products issued under it (rather than under lane == 0) are known to the compiler to
