@@ -25,14 +25,14 @@ constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64
 template <int DB, int NT> struct DqShape {
   static constexpr int kThreads = 128 * (NT + 1);
   static constexpr int kCtasPerSm = NT == 1 ? 2 : 1;
-  static constexpr int kRegs = NT == 1 ? 200 : 208, kRegsRest = NT == 1 ? 56 : 88;
+  static constexpr int kRegs = NT == 1 ? 184 : 208, kRegsRest = NT == 1 ? 72 : 88;
   static constexpr int kStages = NT == 1 ? 4 : 3;       // of (k, v)
   static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
   static constexpr uint32_t kColumns = NT == 1 ? 256 : 512;
 };
 
 struct DqBars {
-  uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2], s_empty[2], dp_full[2], ds_full[2], done[2], drain;
+  uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2], s_empty[2], dp_full[2], ds_full[2], done[2], edge_here, edge_done, drain;
 };
 
 template <typename T, int DB, int NT>
@@ -62,6 +62,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 #pragma unroll
   for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
   auto active = [&](int t) { return (act >> t & 1u) != 0; };
+  const int edge = nk % 16 ? nk % kStep : 0;            // states of the last step, where they end inside a product's sixteen
 
   if (tid == 0) {
     for (int i = 0; i < NT; ++i) {
@@ -73,6 +74,8 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       mbar_init(smem_u32(&bars.done[i]), 1);
     }
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars.kv_full[i]), 1); mbar_init(smem_u32(&bars.kv_empty[i]), 1); }
+    mbar_init(smem_u32(&bars.edge_here), 1);
+    mbar_init(smem_u32(&bars.edge_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     fence_mbar_init();
   }
@@ -85,10 +88,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 
   if (warp >= 4 * NT) {
     regs_lower<Shape::kRegsRest>();
-    if (warp == 4 * NT && act) {
-      // ---- copies -----------------------------------------------------------------------------
+    if (warp == 4 * NT && act && elect_one()) {
+      // ---- copies (one thread) ----------------------------------------------------------------
       int issued = 0;
-      if (limit && elect_one()) {
+      if (limit) {
         for (int t = 0; t < NT; ++t)
           if (active(t)) {
             const uint32_t bar = smem_u32(&bars.q_full[t]), dst = smem_u32(sQ) + 2 * t * kTileBytes;
@@ -99,87 +102,87 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
       for (int j = 0; j < n; ++j) {
         const int st = j % kStages;
-        ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((j / kStages) & 1) ^ 1, limit);
+        ok = mbar_wait_one(smem_u32(&bars.kv_empty[st]), ((j / kStages) & 1) ^ 1, limit);
         if (!ok) break;
-        if (elect_one()) {
-          const uint32_t bar = smem_u32(&bars.kv_full[st]), dst = smem_u32(sKV) + 2 * st * kHalfBytes;
-          mbar_expect_tx(bar, 2 * kHalfBytes);
-          load_tile<DB, kStep>(dst, mk, j * kStep, hk, b, bar);
-          load_tile<DB, kStep>(dst + kHalfBytes, mv, j * kStep, hk, b, bar);
-        }
-        __syncwarp();
+        const uint32_t bar = smem_u32(&bars.kv_full[st]), dst = smem_u32(sKV) + 2 * st * kHalfBytes;
+        mbar_expect_tx(bar, 2 * kHalfBytes);
+        load_tile<DB, kStep>(dst, mk, j * kStep, hk, b, bar);
+        load_tile<DB, kStep>(dst + kHalfBytes, mv, j * kStep, hk, b, bar);
         issued = j + 1;
       }
       if (!ok) {
         // gave up: the copies in flight land before the CTA's shared memory is released
         for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
-          mbar_wait(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
+          mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
         for (int t = 0; t < NT; ++t)
-          if (active(t) && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
+          if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
       }
-    } else if (warp == 4 * NT + 1 && act) {
-      // ---- products ---------------------------------------------------------------------------
+    } else if (warp == 4 * NT + 2 && act && edge) {
+      // ---- the last step's end: k is a factor of dq -------------------------------------------
+      const int st = (n - 1) % kStages;
+      ok = mbar_wait(smem_u32(&bars.edge_here), 0, limit);
+      if (ok) {
+        zero_rows<DB, kStep>(sKV + 2 * st * kHalfBytes, edge, (edge + 15) & ~15, lane);
+        if (lane == 0) mbar_arrive(smem_u32(&bars.edge_done));
+      }
+    } else if (warp == 4 * NT + 1 && act && elect_one()) {
+      // ---- products (one thread) --------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
-      constexpr uint32_t kIdescDq = instr_desc_16<T>(kTile, DB * 64, 0, 1);
       auto columns = [&](int j) { return (min(kStep, nk - j * kStep) + 15) & ~15; };
       auto scores = [&](int t, int j) {
-        mma_rows<T, kStep>(tmem + 256 * t, aq + 2 * t * kTileBytes, akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
+        mma_rows<T, DB, kStep>(tmem + 256 * t, aq + 2 * t * kTileBytes, akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
         tc_commit(smem_u32(&bars.s_full[t]));
       };
       auto dps = [&](int t, int j) {
-        mma_rows<T, kStep>(tmem + 256 * t + 64, aq + (2 * t + 1) * kTileBytes, akv + (2 * (j % kStages) + 1) * kHalfBytes, columns(j), ksteps);
+        mma_rows<T, DB, kStep>(tmem + 256 * t + 64, aq + (2 * t + 1) * kTileBytes, akv + (2 * (j % kStages) + 1) * kHalfBytes, columns(j), ksteps);
         tc_commit(smem_u32(&bars.dp_full[t]));
       };
       auto dqs = [&](int t, int j) {
-        const uint64_t dk = smem_desc_sw128(akv + 2 * (j % kStages) * kHalfBytes, kStepBlock, 1024);
-        for (int ks = 0; ks < columns(j) / 16; ++ks)
-          tc_mma_ts(tmem + 256 * t + 128, tmem + 256 * t + 64 + ks * 8, dk + (uint64_t)((ks * 2048) >> 4), kIdescDq, (j | ks) != 0);
+        mma_weights<T, DB, kStep, false>(tmem + 256 * t + 128, tmem + 256 * t + 64, akv + 2 * (j % kStages) * kHalfBytes, columns(j) / 16, j != 0);
         if (j == n - 1) tc_commit(smem_u32(&bars.done[t]));
       };
-      auto arrive_kv = [&](int j) {                     // waits for the states of step j; k is a factor of dq
-        if (!mbar_wait(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, limit)) return false;
-        const int valid = min(kStep, nk - j * kStep);
-        if (valid < columns(j)) zero_rows<DB, kStep>(sKV + 2 * (j % kStages) * kHalfBytes, valid, columns(j), lane);
-        return true;
-      };
-      ok = arrive_kv(0);
+      auto wait_kv = [&](int j) { return mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, limit); };
+      auto at_edge = [&](int j) { return j == n - 1 && edge; };
+      ok = wait_kv(0);
+      if (ok && at_edge(0)) {
+        mbar_arrive(smem_u32(&bars.edge_here));
+        ok = mbar_wait_one(smem_u32(&bars.edge_done), 0, limit);
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         if (active(t) && ok) {
-          ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
+          ok = mbar_wait_one(smem_u32(&bars.q_full[t]), 0, limit);
           tc_fence_after();
-          if (ok && elect_one()) { scores(t, 0); dps(t, 0); }
-          __syncwarp();
+          if (ok) { scores(t, 0); dps(t, 0); }
         }
       for (int j = 0; j < n && ok; ++j) {
-        if (j + 1 < n) ok = arrive_kv(j + 1);
+        if (j + 1 < n) ok = wait_kv(j + 1);
+        if (at_edge(j + 1) && ok) mbar_arrive(smem_u32(&bars.edge_here));
 #pragma unroll
         for (int t = 0; t < NT; ++t)
           if (active(t) && ok) {
             if (j + 1 < n) {
-              ok = mbar_wait(smem_u32(&bars.s_empty[t]), j & 1, limit);
+              ok = mbar_wait_one(smem_u32(&bars.s_empty[t]), j & 1, limit) &&
+                   (!at_edge(j + 1) || mbar_wait_one(smem_u32(&bars.edge_done), 0, limit));
               tc_fence_after();
-              if (ok && elect_one()) scores(t, j + 1);
-              __syncwarp();
+              if (ok) scores(t, j + 1);
             }
-            if (ok) ok = mbar_wait(smem_u32(&bars.ds_full[t]), j & 1, limit);
+            if (ok) ok = mbar_wait_one(smem_u32(&bars.ds_full[t]), j & 1, limit);
             tc_fence_after();
-            if (ok && elect_one()) {
+            if (ok) {
               dqs(t, j);
               if (j + 1 < n) dps(t, j + 1);
             }
-            __syncwarp();
           }
-        if (ok && elect_one()) tc_commit(smem_u32(&bars.kv_empty[j % kStages]));
-        __syncwarp();
+        if (ok) tc_commit(smem_u32(&bars.kv_empty[j % kStages]));
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (elect_one()) tc_commit(smem_u32(&bars.drain));
-        __syncwarp();
-        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
+        tc_commit(smem_u32(&bars.drain));
+        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
+    __syncwarp();
   } else {
     // ---- ds -----------------------------------------------------------------------------------
     regs_raise<Shape::kRegs>();
@@ -276,7 +279,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
     }
   }
-  if (!ok && lane == 0) atomicExch(a.status, 1);
+  if (!ok) atomicExch(a.status, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
@@ -291,7 +294,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 template <int DB, int NW> struct DkvShape {
   static constexpr int kThreads = 128 * (NW + 1);
   static constexpr int kCtasPerSm = NW == 1 ? 2 : 1;
-  static constexpr int kRegs = NW == 1 ? 200 : 208, kRegsRest = NW == 1 ? 56 : 88;
+  static constexpr int kRegs = NW == 1 ? 184 : 208, kRegsRest = NW == 1 ? 72 : 88;
   static constexpr int kRows = 64 * NW;                 // query rows of a step
   static constexpr int kHalfBytes = DB * kRows * 128;   // of q or dout
   static constexpr int kStages = NW == 1 ? 4 : 2;
@@ -302,7 +305,7 @@ template <int DB, int NW> struct DkvShape {
 };
 
 struct DkvBars {
-  uint64_t kv_full, full[4], empty[4], s_full, p_full, dp_full, ds_full, done, drain;
+  uint64_t kv_full, full[4], empty[4], s_full, p_full, dp_full, ds_full, done, edge_here, edge_done, drain;
 };
 
 template <typename T, int DB, int NW>
@@ -325,6 +328,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
   const int key0 = kt * kTile, steps = (nq + kRows - 1) / kRows;       // steps of one head
   const int n = key0 < nk ? steps * a.group : 0;
+  const int edge = nq % 16 ? nq % kRows : 0;            // rows of a head's last step, where they end inside a product's sixteen
 
   if (tid == 0) {
     mbar_init(smem_u32(&bars.kv_full), 1);
@@ -334,6 +338,8 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
     mbar_init(smem_u32(&bars.dp_full), 1);
     mbar_init(smem_u32(&bars.ds_full), 4 * NW);
     mbar_init(smem_u32(&bars.done), 1);
+    mbar_init(smem_u32(&bars.edge_here), 1);
+    mbar_init(smem_u32(&bars.edge_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     fence_mbar_init();
   }
@@ -346,10 +352,10 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
 
   if (warp >= 4 * NW) {
     regs_lower<Shape::kRegsRest>();
-    if (warp == 4 * NW && n) {
-      // ---- copies -----------------------------------------------------------------------------
+    if (warp == 4 * NW && n && elect_one()) {
+      // ---- copies (one thread) ----------------------------------------------------------------
       int issued = 0;
-      if (limit && elect_one()) {
+      if (limit) {
         const uint32_t bar = smem_u32(&bars.kv_full);
         mbar_expect_tx(bar, 2 * kTileBytes);
         load_tile<DB>(smem_u32(sKV), mk, key0, hk, b, bar);
@@ -358,19 +364,16 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       int h = hk * a.group, row0 = 0;
       for (int i = 0; i < n; ++i) {
         const int st = i % kStages;
-        ok = mbar_wait(smem_u32(&bars.empty[st]), ((i / kStages) & 1) ^ 1, limit);
+        ok = mbar_wait_one(smem_u32(&bars.empty[st]), ((i / kStages) & 1) ^ 1, limit);
         if (!ok) break;
-        if (elect_one()) {
-          const uint32_t bar = smem_u32(&bars.full[st]), dst = smem_u32(sQ) + 2 * st * kHalfBytes;
-          const uint32_t stat = smem_u32(sStat) + st * Shape::kStatBytes;
-          const int64_t at = ((int64_t)b * a.heads + h) * row_tiles * kTile + row0;
-          mbar_expect_tx(bar, 2 * kHalfBytes + Shape::kStatBytes);
-          load_tile<DB, kRows>(dst, mq, row0, h, b, bar);
-          load_tile<DB, kRows>(dst + kHalfBytes, mdo, row0, h, b, bar);
-          bulk_load(stat, a.stat_lse + at, kRows * 4, bar);
-          bulk_load(stat + kRows * 4, a.stat_delta + at, kRows * 4, bar);
-        }
-        __syncwarp();
+        const uint32_t bar = smem_u32(&bars.full[st]), dst = smem_u32(sQ) + 2 * st * kHalfBytes;
+        const uint32_t stat = smem_u32(sStat) + st * Shape::kStatBytes;
+        const int64_t at = ((int64_t)b * a.heads + h) * row_tiles * kTile + row0;
+        mbar_expect_tx(bar, 2 * kHalfBytes + Shape::kStatBytes);
+        load_tile<DB, kRows>(dst, mq, row0, h, b, bar);
+        load_tile<DB, kRows>(dst + kHalfBytes, mdo, row0, h, b, bar);
+        bulk_load(stat, a.stat_lse + at, kRows * 4, bar);
+        bulk_load(stat + kRows * 4, a.stat_delta + at, kRows * 4, bar);
         issued = i + 1;
         row0 += kRows;
         if (row0 >= nq) { row0 = 0; ++h; }
@@ -378,71 +381,70 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       if (!ok) {
         // gave up: the copies in flight land before the CTA's shared memory is released
         for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-          mbar_wait(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
-        if (limit) mbar_wait(smem_u32(&bars.kv_full), 0, kAttentionWaitLimit);
+          mbar_wait_one(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
+        if (limit) mbar_wait_one(smem_u32(&bars.kv_full), 0, kAttentionWaitLimit);
       }
-    } else if (warp == 4 * NW + 1 && n) {
-      // ---- products ---------------------------------------------------------------------------
+    } else if (warp == 4 * NW + 2 && edge) {
+      // ---- the end of each head's last step: q and dout are factors of dk and dv ----------------
+      for (int i = steps - 1, g = 0; i < n && ok; i += steps, ++g) {
+        const int st = i % kStages;
+        ok = mbar_wait(smem_u32(&bars.edge_here), g & 1, limit);
+        if (!ok) break;
+        zero_rows<DB, kRows>(sQ + 2 * st * kHalfBytes, edge, (edge + 15) & ~15, lane);
+        zero_rows<DB, kRows>(sQ + (2 * st + 1) * kHalfBytes, edge, (edge + 15) & ~15, lane);
+        if (lane == 0) mbar_arrive(smem_u32(&bars.edge_done));
+      }
+    } else if (warp == 4 * NW + 1 && n && elect_one()) {
+      // ---- products (one thread) --------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t akv = smem_u32(sKV), aq = smem_u32(sQ);
-      constexpr uint32_t kIdescOut = instr_desc_16<T>(kTile, DB * 64, 0, 1);
-      const int last_valid = nq - (steps - 1) * kRows;  // rows of a head's last step
-      auto valid_rows = [&](int i) { return i % steps == steps - 1 ? last_valid : kRows; };
-      // products with p^T or ds^T: column 16 ks of the step lies at 8 ks of its warpgroup's 64 columns
-      auto outer = [&](uint32_t d, uint32_t left, uint32_t right, int i, int ks_n) {
-        const uint64_t db = smem_desc_sw128(right, kRows * 128, 1024);
-        for (int ks = 0; ks < ks_n; ++ks)
-          tc_mma_ts(d, left + (ks >> 2) * 64 + (ks & 3) * 8, db + (uint64_t)((ks * 2048) >> 4), kIdescOut, (i | ks) != 0);
-      };
-      ok = mbar_wait(smem_u32(&bars.kv_full), 0, limit);
-      int cols = 0, cols_next = 0;                      // of steps i and i + 1
+      const int last_cols = (nq - (steps - 1) * kRows + 15) & ~15;     // columns of a head's last step
+      ok = mbar_wait_one(smem_u32(&bars.kv_full), 0, limit);
+      int cols = 0, cols_next = 0, step = 0, head = 0;  // columns of steps i and i + 1; the latter's place
       for (int i = -1; i < n && ok; ++i) {
         const int st = i % kStages, next = (i + 1) % kStages;
+        const bool last = step == steps - 1, at_edge = i + 1 < n && last && edge;
         cols = cols_next;
-        if (i >= 0) {
-          ok = mbar_wait(smem_u32(&bars.p_full), i & 1, limit);
-          tc_fence_after();
-          if (ok && elect_one()) outer(tmem + Shape::kDv, tmem, aq + (2 * st + 1) * kHalfBytes, i, cols / 16);
-          __syncwarp();
-        }
-        if (i + 1 < n && ok) {
-          ok = mbar_wait(smem_u32(&bars.full[next]), ((i + 1) / kStages) & 1, limit);
+        if (at_edge) {
+          ok = mbar_wait_one(smem_u32(&bars.full[next]), ((i + 1) / kStages) & 1, limit);
           if (!ok) break;
-          const int valid = valid_rows(i + 1);
-          cols_next = (valid + 15) & ~15;
-          if (valid < cols_next) {                      // q and dout are factors of dk and dv
-            zero_rows<DB, kRows>(sQ + 2 * next * kHalfBytes, valid, cols_next, lane);
-            zero_rows<DB, kRows>(sQ + (2 * next + 1) * kHalfBytes, valid, cols_next, lane);
-          }
-          tc_fence_after();
-          if (elect_one()) {
-            mma_rows<T, kRows>(tmem, akv, aq + 2 * next * kHalfBytes, cols_next, ksteps);
-            tc_commit(smem_u32(&bars.s_full));
-          }
-          __syncwarp();
+          mbar_arrive(smem_u32(&bars.edge_here));
         }
-        if (i >= 0 && ok) {
-          ok = mbar_wait(smem_u32(&bars.ds_full), i & 1, limit);
+        if (i >= 0) {
+          ok = mbar_wait_one(smem_u32(&bars.p_full), i & 1, limit);
+          if (!ok) break;
           tc_fence_after();
-          if (ok && elect_one()) {
-            outer(tmem + Shape::kDk, tmem + Shape::kDp, aq + 2 * st * kHalfBytes, i, cols / 16);
-            tc_commit(smem_u32(&bars.empty[st]));
-            if (i == n - 1) tc_commit(smem_u32(&bars.done));
-          }
-          __syncwarp();
+          mma_weights<T, DB, kRows, true>(tmem + Shape::kDv, tmem, aq + (2 * st + 1) * kHalfBytes, cols / 16, i != 0);
         }
-        if (i + 1 < n && ok && elect_one()) {
-          mma_rows<T, kRows>(tmem + Shape::kDp, akv + kTileBytes, aq + (2 * next + 1) * kHalfBytes, cols_next, ksteps);
+        if (i + 1 < n) {
+          ok = mbar_wait_one(smem_u32(&bars.full[next]), ((i + 1) / kStages) & 1, limit) &&
+               (!at_edge || mbar_wait_one(smem_u32(&bars.edge_done), head & 1, limit));
+          if (!ok) break;
+          cols_next = last ? last_cols : kRows;
+          if (last) { step = 0; ++head; } else ++step;
+          tc_fence_after();
+          mma_rows<T, DB, kRows>(tmem, akv, aq + 2 * next * kHalfBytes, cols_next, ksteps);
+          tc_commit(smem_u32(&bars.s_full));
+        }
+        if (i >= 0) {
+          ok = mbar_wait_one(smem_u32(&bars.ds_full), i & 1, limit);
+          if (!ok) break;
+          tc_fence_after();
+          mma_weights<T, DB, kRows, true>(tmem + Shape::kDk, tmem + Shape::kDp, aq + 2 * st * kHalfBytes, cols / 16, i != 0);
+          tc_commit(smem_u32(&bars.empty[st]));
+          if (i == n - 1) tc_commit(smem_u32(&bars.done));
+        }
+        if (i + 1 < n) {
+          mma_rows<T, DB, kRows>(tmem + Shape::kDp, akv + kTileBytes, aq + (2 * next + 1) * kHalfBytes, cols_next, ksteps);
           tc_commit(smem_u32(&bars.dp_full));
         }
-        __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (elect_one()) tc_commit(smem_u32(&bars.drain));
-        __syncwarp();
-        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
+        tc_commit(smem_u32(&bars.drain));
+        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
+    __syncwarp();
   } else {
     // ---- p and ds -----------------------------------------------------------------------------
     regs_raise<Shape::kRegs>();
@@ -551,7 +553,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       }
     }
   }
-  if (!ok && lane == 0) atomicExch(a.status, 1);
+  if (!ok) atomicExch(a.status, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NW + 1) tmem_dealloc(tmem, Shape::kColumns);

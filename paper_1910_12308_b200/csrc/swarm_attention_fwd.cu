@@ -21,7 +21,7 @@ template <int DB, int NT> struct FwdShape {
 };
 
 struct FwdBars {
-  uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], s_empty[2], p_full[2], pv_done[2], drain;
+  uint64_t q_full[2], kv_full[6], kv_empty[6], s_full[2], s_empty[2], p_full[2], pv_done[2], edge_here, edge_done, drain;
 };
 
 // NT = 1 (heads of up to 64 values): scores and weights have tensor memory of their own, so the scores of the next tile
@@ -54,6 +54,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
   auto active = [&](int t) { return (act >> t & 1u) != 0; };
   const bool any = act != 0;
+  const int edge = nk % 16 ? nk % kTile : 0;            // rows of the last tile, where they end inside a product's sixteen
 
   if (tid == 0) {
     for (int i = 0; i < NT; ++i) {
@@ -67,6 +68,8 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       mbar_init(smem_u32(&bars.kv_full[i]), 1);
       mbar_init(smem_u32(&bars.kv_empty[i]), 1);
     }
+    mbar_init(smem_u32(&bars.edge_here), 1);
+    mbar_init(smem_u32(&bars.edge_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     fence_mbar_init();
   }
@@ -79,10 +82,10 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
 
   if (warp >= 4 * NT) {
     regs_lower<Shape::kRegsRest>();
-    if (warp == 4 * NT && any) {
-      // ---- copies -----------------------------------------------------------------------------
+    if (warp == 4 * NT && any && elect_one()) {
+      // ---- copies (one thread) ----------------------------------------------------------------
       int issued = 0;
-      if (limit && elect_one()) {
+      if (limit) {
         for (int t = 0; t < NT; ++t)
           if (active(t)) {
             const uint32_t bar = smem_u32(&bars.q_full[t]);
@@ -92,90 +95,87 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       }
       for (int f = 0; f < 2 * n; ++f) {                 // K of tile 0, V of tile 0, K of tile 1, ...
         const int st = f % kStages;
-        ok = mbar_wait(smem_u32(&bars.kv_empty[st]), ((f / kStages) & 1) ^ 1, limit);
+        ok = mbar_wait_one(smem_u32(&bars.kv_empty[st]), ((f / kStages) & 1) ^ 1, limit);
         if (!ok) break;
-        if (elect_one()) {
-          const uint32_t bar = smem_u32(&bars.kv_full[st]);
-          mbar_expect_tx(bar, kTileBytes);
-          load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (f >> 1) * kTile, hk, b, bar);
-        }
-        __syncwarp();
+        const uint32_t bar = smem_u32(&bars.kv_full[st]);
+        mbar_expect_tx(bar, kTileBytes);
+        load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (f >> 1) * kTile, hk, b, bar);
         issued = f + 1;
       }
       if (!ok) {
         // gave up: the copies in flight land before the CTA's shared memory is released
         for (int f = issued > kStages ? issued - kStages : 0; f < issued; ++f)
-          mbar_wait(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
+          mbar_wait_one(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
         for (int t = 0; t < NT; ++t)
-          if (active(t) && limit) mbar_wait(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
+          if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
       }
-    } else if (warp == 4 * NT + 1 && any) {
-      // ---- products ---------------------------------------------------------------------------
+    } else if (warp == 4 * NT + 2 && any && edge) {
+      // ---- the last tile's end: v is a factor of the sums ---------------------------------------
+      const int f = 2 * n - 1;
+      ok = mbar_wait(smem_u32(&bars.edge_here), 0, limit);
+      if (ok) {
+        zero_rows<DB, kTile>(sKV + f % kStages * kTileBytes, edge, (edge + 15) & ~15, lane);
+        if (lane == 0) mbar_arrive(smem_u32(&bars.edge_done));
+      }
+    } else if (warp == 4 * NT + 1 && any && elect_one()) {
+      // ---- products (one thread) --------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
-      constexpr uint32_t kIdescPV = instr_desc_16<T>(kTile, DB * 64, 0, 1);
       auto columns = [&](int j) { return (min(kTile, nk - j * kTile) + 15) & ~15; };
       auto scores = [&](int t, int j) {                 // S_t = Q_t K_j^T
-        mma_rows<T>(tmem + 128 * t, aq + t * kTileBytes, akv + (2 * j) % kStages * kTileBytes, columns(j), ksteps);
+        mma_rows<T, DB, kTile>(tmem + 128 * t, aq + t * kTileBytes, akv + (2 * j) % kStages * kTileBytes, columns(j), ksteps);
         tc_commit(smem_u32(&bars.s_full[t]));
       };
       auto sums = [&](int t, int j) {                   // O_t += P_t V_j
-        const uint64_t dv = smem_desc_sw128(akv + (2 * j + 1) % kStages * kTileBytes, kBlockBytes, 1024);
-        const uint32_t p = tmem + 128 * t + Shape::kWeights, o = tmem + 128 * t + Shape::kSums;
-        for (int ks = 0; ks < columns(j) / 16; ++ks)
-          tc_mma_ts(o, p + ks * 8, dv + (uint64_t)((ks * 2048) >> 4), kIdescPV, (j | ks) != 0);
+        mma_weights<T, DB, kTile, false>(tmem + 128 * t + Shape::kSums, tmem + 128 * t + Shape::kWeights,
+                                         akv + (2 * j + 1) % kStages * kTileBytes, columns(j) / 16, j != 0);
         if (NT == 1 || j == n - 1) tc_commit(smem_u32(&bars.pv_done[t]));
       };
-      auto wait_kv = [&](int f) { return mbar_wait(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, limit); };
+      auto wait_kv = [&](int f) { return mbar_wait_one(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, limit); };
       ok = wait_kv(0);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         if (active(t) && ok) {
-          ok = mbar_wait(smem_u32(&bars.q_full[t]), 0, limit);
+          ok = mbar_wait_one(smem_u32(&bars.q_full[t]), 0, limit);
           tc_fence_after();
-          if (ok && elect_one()) scores(t, 0);
-          __syncwarp();
+          if (ok) scores(t, 0);
         }
-      if (ok && elect_one()) tc_commit(smem_u32(&bars.kv_empty[0]));
+      if (ok) tc_commit(smem_u32(&bars.kv_empty[0]));
       for (int j = 0; j < n && ok; ++j) {
         const int sv = (2 * j + 1) % kStages, sk = (2 * j + 2) % kStages;
         if (NT == 1 && j + 1 < n) {                     // the next scores as soon as these have been read
-          ok = wait_kv(2 * j + 2) && mbar_wait(smem_u32(&bars.s_empty[0]), j & 1, limit);
-          tc_fence_after();
-          if (ok && elect_one()) { scores(0, j + 1); tc_commit(smem_u32(&bars.kv_empty[sk])); }
-          __syncwarp();
+          ok = wait_kv(2 * j + 2) && mbar_wait_one(smem_u32(&bars.s_empty[0]), j & 1, limit);
           if (!ok) break;
+          tc_fence_after();
+          scores(0, j + 1);
+          tc_commit(smem_u32(&bars.kv_empty[sk]));
         }
         ok = wait_kv(2 * j + 1);
-        if (!ok) break;
-        const int valid = min(kTile, nk - j * kTile);
-        if (valid < columns(j)) zero_rows<DB>(sKV + sv * kTileBytes, valid, columns(j), lane);
+        if (j == n - 1 && edge && ok) mbar_arrive(smem_u32(&bars.edge_here));
 #pragma unroll
         for (int t = 0; t < NT; ++t)
           if (active(t) && ok) {
-            ok = mbar_wait(smem_u32(&bars.p_full[t]), j & 1, limit);
+            ok = mbar_wait_one(smem_u32(&bars.p_full[t]), j & 1, limit) &&
+                 (j < n - 1 || !edge || mbar_wait_one(smem_u32(&bars.edge_done), 0, limit));
             tc_fence_after();
-            if (ok && elect_one()) sums(t, j);
-            __syncwarp();
+            if (ok) sums(t, j);
             if (NT == 2 && j + 1 < n && ok) {
               ok = wait_kv(2 * j + 2);
               tc_fence_after();
-              if (ok && elect_one()) scores(t, j + 1);
-              __syncwarp();
+              if (ok) scores(t, j + 1);
             }
           }
-        if (ok && elect_one()) {
+        if (ok) {
           tc_commit(smem_u32(&bars.kv_empty[sv]));
           if (NT == 2 && j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[sk]));
         }
-        __syncwarp();
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        if (elect_one()) tc_commit(smem_u32(&bars.drain));
-        __syncwarp();
-        mbar_wait(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
+        tc_commit(smem_u32(&bars.drain));
+        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
       }
     }
+    __syncwarp();
   } else {
     // ---- softmax ------------------------------------------------------------------------------
     regs_raise<Shape::kRegs>();
@@ -282,7 +282,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       }
     }
   }
-  if (!ok && lane == 0) atomicExch(a.status, 1);
+  if (!ok) atomicExch(a.status, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);

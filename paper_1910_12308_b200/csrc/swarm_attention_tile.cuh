@@ -53,16 +53,30 @@ __device__ __forceinline__ void store_tile(const TileMap& m, uint32_t src, int r
     tma_store_4d(&m.map, src + d * kBlockBytes, d * 64, row0 * m.token_step, head * m.head_step, b * m.batch_step);
 }
 
-// One thread: D[128 x cols] = A[128 x dim] B[cols x dim]^T, dim = 16 ksteps; tile A in shared memory with 128 rows, tile
-// B with ROWS.
-template <typename T, int ROWS = kTile>
+// One thread: D[128 x cols] = A[128 x dim] B[cols x dim]^T, dim = 16 ksteps <= 64 DB; tile A in shared memory with 128
+// rows, tile B with ROWS. The whole width is unrolled: issue, not the tensor pipe, would otherwise set the pace.
+template <typename T, int DB, int ROWS>
 __device__ __forceinline__ void mma_rows(uint32_t tmem_d, uint32_t tile_a, uint32_t tile_b, int cols, int ksteps) {
   const uint32_t idesc = instr_desc_16<T>(kTile, 0, 0, 0) + ((uint32_t)(cols >> 3) << 17);
   const uint64_t da = smem_desc_sw128(tile_a, 16, 1024), db = smem_desc_sw128(tile_b, 16, 1024);
-  for (int ks = 0; ks < ksteps; ++ks) {
-    tc_mma(tmem_d, da + (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4),
-           db + (uint64_t)(((ks >> 2) * (ROWS * 128) + (ks & 3) * 32) >> 4), idesc, ks != 0);
-  }
+#pragma unroll
+  for (int ks = 0; ks < DB * 4; ++ks)
+    if (ks < ksteps)
+      tc_mma(tmem_d, da + (uint64_t)(((ks >> 2) * kBlockBytes + (ks & 3) * 32) >> 4),
+             db + (uint64_t)(((ks >> 2) * (ROWS * 128) + (ks & 3) * 32) >> 4), idesc, ks != 0);
+}
+
+// One thread: D[128 x 64 DB] (+)= W[128 x 16 ksteps] B, the left factor in tensor memory (16-bit pairs, columns 64 apart for
+// each 64 of it if SPLIT, else consecutive), tile B in shared memory with ROWS rows.
+template <typename T, int DB, int ROWS, bool SPLIT>
+__device__ __forceinline__ void mma_weights(uint32_t tmem_d, uint32_t tmem_w, uint32_t tile_b, int ksteps, bool accumulate) {
+  constexpr uint32_t idesc = instr_desc_16<T>(kTile, DB * 64, 0, 1);
+  const uint64_t db = smem_desc_sw128(tile_b, ROWS * 128, 1024);
+#pragma unroll
+  for (int ks = 0; ks < ROWS / 16; ++ks)
+    if (ks < ksteps)
+      tc_mma_ts(tmem_d, tmem_w + (SPLIT ? (ks >> 2) * 64 + (ks & 3) * 8 : ks * 8), db + (uint64_t)((ks * 2048) >> 4), idesc,
+                accumulate || ks != 0);
 }
 
 // 32 values of a row times `factor` (zeros unless live) into columns col .. col + 31 of a tile.

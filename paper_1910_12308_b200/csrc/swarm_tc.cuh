@@ -32,6 +32,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
   for (uint32_t i = 0; i < limit && !done; ++i) done = mbar_try_wait(bar, parity);
   return __all_sync(0xFFFFFFFFu, done);
 }
+// The same for a single thread.
+__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, uint32_t limit) {
+  for (uint32_t i = 0; i < limit; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return false;
+}
 __device__ __forceinline__ void tmem_alloc(uint32_t slot_smem, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(slot_smem), "r"(cols) : "memory");
 }
@@ -162,9 +168,9 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) 
   return r != 0;
 }
 
-// True in one lane of a whole warp. Products issued under it (rather than under lane == 0) are known to the compiler to
-// come from one thread, so their descriptors go to uniform registers without a loop over the lanes: 128 to 190 cycles
-// for each product became a few.
+// True in one lane of a whole warp. Code under it (rather than under lane == 0) is known to the compiler to run in one
+// thread, so the descriptors of its products go to uniform registers without a loop over the lanes: measured, 128 to 190
+// cycles of issue for each product under lane == 0.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
