@@ -82,43 +82,51 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float v
   }
 }
 
-// A segment is 256 consecutive columns of a row, taken by one warp. Element i (0..7) of a lane is column
-//   VEC:  lane * 8 + i   one 128-bit access per lane (two in fp32), for rows that start on 16-byte boundaries
-//   else: i * 32 + lane  one coalesced access per element, for any other base, pitch or width
+// A segment is 8 LPR consecutive columns of a row, taken by LPR lanes (8, 16 or 32) of a warp, l = lane % LPR; narrow rows
+// put 32 / LPR rows into a warp. Element i (0..7) of a lane is column
+//   l * 8 + i    if the rows start on 16-byte boundaries (VEC): one 128-bit access per lane (two in fp32); also of narrow
+//                rows that do not, element by element
+//   i * 32 + l   of wide rows with any other base, pitch or width: one coalesced access per element
 // `valid` counts the segment's columns that exist (<= 0: none).
-constexpr int kSegment = 256;
-template <bool VEC> __device__ __forceinline__ int segment_column(int lane, int i) { return VEC ? lane * 8 + i : i * 32 + lane; }
+template <bool VEC, int LPR> __device__ __forceinline__ int segment_column(int l, int i) { return VEC || LPR < 32 ? l * 8 + i : i * 32 + l; }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void segment_load(const T* p, int valid, int lane, float v[8]) {
-  if (VEC && lane * 8 + 8 <= valid) {
-    unpack8<T>(load_raw8<T>(p + lane * 8), v);
-  } else {
+// Elements as they are stored: 128 bits where that is possible, so that a prefetched row takes few registers.
+template <typename T, bool VEC, int LPR> struct Segment {
+  Raw8<T> raw;
+  __device__ __forceinline__ void load(const T* p, int valid, int l) {
+    if (VEC && l * 8 + 8 <= valid) {
+      raw = load_raw8<T>(p + l * 8);
+    } else {
+      T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = segment_column<VEC>(lane, i);
-      v[i] = c < valid ? to_float<T>(p[c]) : 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        const int c = segment_column<VEC, LPR>(l, i);
+        e[i] = c < valid ? p[c] : from_float<T>(0.0f);
+      }
     }
   }
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void segment_store(T* p, int valid, int lane, const float v[8]) {
-  if (VEC && lane * 8 + 8 <= valid) {
-    store8<T>(p + lane * 8, v);
+  __device__ __forceinline__ void get(float v[8]) const { unpack8<T>(raw, v); }
+};
+template <typename T, bool VEC, int LPR>
+__device__ __forceinline__ void segment_store(T* p, int valid, int l, const float v[8]) {
+  if (VEC && l * 8 + 8 <= valid) {
+    store8<T>(p + l * 8, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int c = segment_column<VEC>(lane, i);
+      const int c = segment_column<VEC, LPR>(l, i);
       if (c < valid) p[c] = from_float<T>(v[i]);
     }
   }
 }
 
-// Mask of a dropout call. threshold: 16-bit draws below it drop the element (0: nothing is dropped, 65536: all).
+// Mask of a dropout call. threshold: 16-bit draws below it drop the element (0: nothing is dropped). Rate 1 drops
+// everything: the threshold then stays below 2^16, the factor is 0 and `all` is set.
 struct DropoutMask {
   PhiloxRoundKeys rk;
   uint32_t event, threshold;
   float factor;
+  int32_t all;
 };
 
 inline DropoutMask make_dropout_mask(double rate, uint64_t seed, uint32_t event) {
@@ -126,26 +134,33 @@ inline DropoutMask make_dropout_mask(double rate, uint64_t seed, uint32_t event)
   m.rk = philox_round_keys((uint32_t)seed, (uint32_t)(seed >> 32));
   m.event = event;
   m.threshold = (uint32_t)(rate * 65536.0 + 0.5);
-  m.factor = m.threshold >= 65536 ? 0.0f : (float)(65536.0 / (double)(65536 - m.threshold));
+  m.all = m.threshold >= 65536;
+  if (m.all) m.threshold = 65535;
+  m.factor = m.all ? 0.0f : (float)(65536.0 / (double)(65536 - m.threshold));
   return m;
 }
 
-// v = m * v on a segment: one generator call per lane and segment covers the lane's eight columns of the VEC order; in
-// the other order the keep bits of a column's call come from the lane that made it. All lanes of the warp call it.
-template <bool VEC>
-__device__ __forceinline__ void segment_dropout(float v[8], uint32_t group0, uint32_t row, int lane, const DropoutMask& m) {
-  const uint4 w = philox4x32_10(group0 + (uint32_t)lane, row, m.event, kStreamDropout, m.rk);
-  if constexpr (VEC) {
+// Zeroes the dropped elements of a segment (the factor is left to the caller): one generator call per lane and segment
+// covers the lane's eight consecutive columns; where the lane's elements are others, the keep bits of a column come from
+// the lane that drew them. group0: the segment's first column div 8. All lanes of the warp call it.
+template <bool VEC, int LPR>
+__device__ __forceinline__ void segment_drop(float v[8], uint32_t group0, uint32_t row, int l, const DropoutMask& m) {
+  const uint4 w = philox4x32_10(group0 + (uint32_t)l, row, m.event, kStreamDropout, m.rk);
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w}, high = m.threshold << 16;     // threshold 65536: handled by the caller
+  if constexpr (VEC || LPR < 32) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = sr_u16(w, i) >= m.threshold ? v[i] * m.factor : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = (word[i] << 16) >= high ? v[2 * i] : 0.0f;                    // low half
+      v[2 * i + 1] = word[i] >= high ? v[2 * i + 1] : 0.0f;                    // high half: the low bits cannot decide
+    }
   } else {
     uint32_t keep = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) keep |= (sr_u16(w, i) >= m.threshold ? 1u : 0u) << i;
+    for (int i = 0; i < 4; ++i) keep |= ((word[i] << 16) >= high ? 1u << (2 * i) : 0u) | (word[i] >= high ? 2u << (2 * i) : 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, i * 4 + (lane >> 3));
-      v[i] = (bits >> (lane & 7)) & 1u ? v[i] * m.factor : 0.0f;
+      const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, i * 4 + (l >> 3));
+      v[i] = (bits >> (l & 7)) & 1u ? v[i] : 0.0f;
     }
   }
 }

@@ -33,75 +33,116 @@ cudaError_t operator_sm_count(int* out) {
 
 namespace {
 
+// CTAs of a kernel that the device holds at once, looked up once per kernel and device.
+template <typename K>
+cudaError_t resident_ctas(K kernel, int threads, int64_t* out) {
+  static int per_device[64] = {};
+  static std::mutex mutex;
+  int sms = 0, dev = 0;
+  cudaError_t e = operator_sm_count(&sms);
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mutex);
+  if (!per_device[dev]) {
+    int n = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0);
+    if (e != cudaSuccess) return e;
+    per_device[dev] = n < 1 ? 1 : n;
+  }
+  *out = (int64_t)per_device[dev] * sms;
+  return cudaSuccess;
+}
+
 // =================================================================================================
-// Dropout. Warp = one 256-column segment of a row at a time; the warps of the grid walk the (row, segment) list with
-// a fixed stride, whose quotient and remainder by the segments of a row come from the host, so that the walk needs
-// no division.
+// Dropout. A warp takes one segment of 32 / LPR rows at a time, two such items in flight; the warps of the grid walk the
+// (rows, segment) list with a fixed stride, whose quotient and remainder by the segments of a row come from the host,
+// so that the walk needs no division.
 // =================================================================================================
-constexpr int kDropThreads = 256;
+constexpr int kRowThreads = 256;
 
 struct DropoutArgs {
   const void* x;
   const void* residual;
   void* out;
   int64_t x_pitch, residual_pitch, out_pitch;
-  int64_t rows, cols;
+  int64_t rows, cols, row_groups;     // groups of 32 / LPR rows
   uint32_t segments;                  // per row
-  int64_t row_step;                   // the stride of the walk: this many rows
+  int64_t row_step;                   // the stride of the walk: this many groups
   uint32_t segment_step;              // and this many segments
 };
 
-template <typename T, bool VEC, bool RES>
-__global__ void __launch_bounds__(kDropThreads)
+template <typename T, bool VEC, int LPR, bool RES>
+__global__ void __launch_bounds__(kRowThreads)
 dropout_kernel(DropoutArgs a, DropoutMask m) {
-  const int lane = threadIdx.x & 31;
-  const int64_t first = (int64_t)blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5);
-  int64_t row = first / a.segments;
-  uint32_t seg = (uint32_t)(first - row * a.segments);
-  while (row < a.rows) {
-    const int64_t col = (int64_t)seg * kSegment;
-    const int valid = (int)min((int64_t)kSegment, a.cols - col);
-    float v[8], r[8];
-    segment_load<T, VEC>(reinterpret_cast<const T*>(a.x) + row * a.x_pitch + col, valid, lane, v);
-    if constexpr (RES) segment_load<T, VEC>(reinterpret_cast<const T*>(a.residual) + row * a.residual_pitch + col, valid, lane, r);
-    if (m.threshold != 0) segment_dropout<VEC>(v, seg * (kSegment / 8), (uint32_t)row, lane, m);
-    if constexpr (RES) {
+  constexpr int kItems = 2;
+  const int lane = threadIdx.x & 31, l = lane % LPR, sub = lane / LPR;
+  const int64_t first = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  int64_t group = first / a.segments;
+  uint32_t seg = (uint32_t)(first - group * a.segments);
+  while (group < a.row_groups) {
+    Segment<T, VEC, LPR> x[kItems], r[kItems];
+    int64_t row[kItems], col[kItems];
+    int valid[kItems];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += r[i];
+    for (int u = 0; u < kItems; ++u) {
+      row[u] = group * (32 / LPR) + sub;
+      col[u] = (int64_t)seg * (LPR * 8);
+      valid[u] = group < a.row_groups && row[u] < a.rows ? (int)min((int64_t)LPR * 8, a.cols - col[u]) : 0;
+      if (valid[u] > 0) {
+        x[u].load(reinterpret_cast<const T*>(a.x) + row[u] * a.x_pitch + col[u], valid[u], l);
+        if constexpr (RES) r[u].load(reinterpret_cast<const T*>(a.residual) + row[u] * a.residual_pitch + col[u], valid[u], l);
+      }
+      group += a.row_step;
+      seg += a.segment_step;
+      if (seg >= a.segments) { seg -= a.segments; ++group; }
     }
-    segment_store<T, VEC>(reinterpret_cast<T*>(a.out) + row * a.out_pitch + col, valid, lane, v);
-    row += a.row_step;
-    seg += a.segment_step;
-    if (seg >= a.segments) { seg -= a.segments; ++row; }
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      float v[8], w[8];
+      x[u].get(v);
+      if (m.threshold != 0) segment_drop<VEC, LPR>(v, (uint32_t)(col[u] >> 3), (uint32_t)row[u], l, m);
+      if constexpr (RES) {
+        r[u].get(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = m.all ? w[i] : fmaf(v[i], m.factor, w[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = m.all ? 0.0f : v[i] * m.factor;
+      }
+      if (valid[u] > 0) segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.out) + row[u] * a.out_pitch + col[u], valid[u], l, v);
+    }
   }
 }
 
-template <typename T>
-cudaError_t launch_dropout(DropoutArgs a, const DropoutMask& m, bool vec, cudaStream_t st) {
-  int sms = 0;
-  const cudaError_t e = operator_sm_count(&sms);
+template <typename T, bool VEC, int LPR, bool RES>
+cudaError_t launch_dropout_as(DropoutArgs a, const DropoutMask& m, cudaStream_t st) {
+  int64_t most = 0;
+  const cudaError_t e = resident_ctas(dropout_kernel<T, VEC, LPR, RES>, kRowThreads, &most);
   if (e != cudaSuccess) return e;
-  const int64_t items = a.rows * (int64_t)a.segments, per_cta = kDropThreads / 32;
-  const int64_t most = (int64_t)sms * (2048 / kDropThreads);
+  a.segments = (uint32_t)((a.cols + LPR * 8 - 1) / (LPR * 8));
+  a.row_groups = (a.rows + 32 / LPR - 1) / (32 / LPR);
+  const int64_t items = a.row_groups * (int64_t)a.segments, per_cta = kRowThreads / 32;
   const int64_t ctas = items < most * per_cta ? (items + per_cta - 1) / per_cta : most;
-  const int64_t stride = ctas * per_cta;
-  a.row_step = stride / a.segments;
-  a.segment_step = (uint32_t)(stride % a.segments);
-  const unsigned grid = (unsigned)ctas;
-  if (vec) {
-    if (a.residual) dropout_kernel<T, true, true><<<grid, kDropThreads, 0, st>>>(a, m);
-    else dropout_kernel<T, true, false><<<grid, kDropThreads, 0, st>>>(a, m);
-  } else {
-    if (a.residual) dropout_kernel<T, false, true><<<grid, kDropThreads, 0, st>>>(a, m);
-    else dropout_kernel<T, false, false><<<grid, kDropThreads, 0, st>>>(a, m);
-  }
+  a.row_step = ctas * per_cta / a.segments;
+  a.segment_step = (uint32_t)(ctas * per_cta % a.segments);
+  dropout_kernel<T, VEC, LPR, RES><<<(unsigned)ctas, kRowThreads, 0, st>>>(a, m);
   return cudaGetLastError();
 }
 
+template <typename T, bool VEC>
+cudaError_t launch_dropout(const DropoutArgs& a, const DropoutMask& m, cudaStream_t st) {
+#define SWARM_DROPOUT_LPR(L) (a.residual ? launch_dropout_as<T, VEC, L, true>(a, m, st) : launch_dropout_as<T, VEC, L, false>(a, m, st))
+  return a.cols <= 64 ? SWARM_DROPOUT_LPR(8) : a.cols <= 128 ? SWARM_DROPOUT_LPR(16) : SWARM_DROPOUT_LPR(32);
+#undef SWARM_DROPOUT_LPR
+}
+
 // =================================================================================================
-// Norm. A row belongs to WPR warps (a group), each holding VPL segments of it in registers: segment v of warp w is
-// segment w + v * WPR of the row. WPR = 1 reduces with shuffles alone and a CTA holds several rows; a wider row is a
-// CTA of its own and meets once in shared memory.
+// Norm. A row belongs to LPR lanes of a warp (rows of up to 256 columns) or to WPR whole warps, each lane with VPL times
+// eight of its elements in registers: segment v of warp w is segment w + v * WPR of the row. The warps of a CTA form
+// groups of WPR that walk the rows with a fixed stride and fetch their next row before they reduce this one; a group of
+// several warps meets once per row in shared memory at a barrier of its own.
+// Few registers and many warps carry it: with a whole row of 1024 in each warp (four segments, 88 registers) 16384
+// rows took 44 us forward and, with 225 registers, 69 us backward.
 // =================================================================================================
 constexpr int kNormBlock = 128;                        // columns that share one scale in the 8-bit output
 
@@ -118,13 +159,20 @@ struct NormArgs {
   float eps, inv_cols;
 };
 
-template <bool VEC>
-__device__ __forceinline__ void weight_load(const float* w, int valid, int lane, bool aligned, float v[8]) {
-  if (VEC && aligned) segment_load<float, true>(w, valid, lane, v);
-  else {
+template <int LPR, int WPR> struct NormShape {
+  static constexpr int kThreads = WPR <= 8 ? 256 : WPR * 32;
+  static constexpr int kGroups = kThreads / (32 * WPR);                // of a CTA
+  static constexpr int kRows = kGroups * (32 / LPR);                   // rows of a CTA at a time
+};
+
+template <bool VEC, int LPR>
+__device__ __forceinline__ void weight_load(const float* w, int valid, int l, bool aligned, float v[8]) {
+  if (VEC && aligned && l * 8 + 8 <= valid) {
+    unpack8<float>(load_raw8<float>(w + l * 8), v);
+  } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int c = segment_column<VEC>(lane, i);
+      const int c = segment_column<VEC, LPR>(l, i);
       v[i] = c < valid ? w[c] : 0.0f;
     }
   }
@@ -134,102 +182,128 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
 
-// Sum over the warps of a row's group: the same value, added in warp order, in every thread.
-template <int WPR>
-__device__ __forceinline__ float group_sum(float v, float* slots, int warp) {
-  v = warp_sum(v);
-  if constexpr (WPR > 1) {
-    if ((threadIdx.x & 31) == 0) slots[warp] = v;
-    __syncthreads();
-    v = 0.0f;
+template <int LPR> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-    for (int w = 0; w < WPR; ++w) v += slots[w];
-  }
+  for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
 
-template <typename T, bool VEC, int WPR, int VPL, bool CODES>
-__global__ void __launch_bounds__(WPR == 1 ? 128 : WPR * 32)
+// Sums of two values over the lanes and warps of a row, the warps added in order: the same in every thread. `slots`: two
+// sets of [WPR][2] floats of the group, taken in turn (a set is written again two barriers later).
+template <int LPR, int WPR>
+__device__ __forceinline__ void row_sums(float& u, float& v, float (*slots)[WPR][2], int& turn, int warp_of_row, int group) {
+  u = lanes_sum<LPR>(u);
+  v = lanes_sum<LPR>(v);
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 31) == 0) { slots[turn][warp_of_row][0] = u; slots[turn][warp_of_row][1] = v; }
+    asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(WPR * 32) : "memory");
+    u = v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) { u += slots[turn][w][0]; v += slots[turn][w][1]; }
+    turn ^= 1;
+  }
+}
+
+template <typename T, bool VEC, int LPR, int WPR, int VPL, bool RES, bool CODES>
+__global__ void __launch_bounds__(NormShape<LPR, WPR>::kThreads)
 add_rms_norm_kernel(NormArgs a, DropoutMask m) {
-  constexpr int kRowsPerCta = WPR == 1 ? 4 : 1;
-  __shared__ float slots[2][WPR];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * kRowsPerCta + (WPR == 1 ? warp : 0);
-  if (WPR == 1 && row >= a.rows) return;
-  const int seg0 = WPR == 1 ? 0 : warp;
-  float t[VPL][8], r[VPL][8];
-#pragma unroll
-  for (int s = 0; s < VPL; ++s) {
-    const int64_t col = (int64_t)(seg0 + s * WPR) * kSegment;
-    const int valid = (int)min((int64_t)kSegment, a.cols - col);
-    segment_load<T, VEC>(reinterpret_cast<const T*>(a.x) + row * a.x_pitch + col, valid, lane, t[s]);
-    if (a.residual) segment_load<T, VEC>(reinterpret_cast<const T*>(a.residual) + row * a.residual_pitch + col, valid, lane, r[s]);
-  }
-  float sq = 0.0f;
-#pragma unroll
-  for (int s = 0; s < VPL; ++s) {
-    const int seg = seg0 + s * WPR;
-    if (m.threshold != 0) segment_dropout<VEC>(t[s], (uint32_t)seg * (kSegment / 8), (uint32_t)row, lane, m);
-    if (a.residual) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[s][i] += r[s][i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sq = fmaf(t[s][i], t[s][i], sq);
-  }
-  sq = group_sum<WPR>(sq, slots[0], warp);
-  const float rstd = 1.0f / sqrtf(fmaf(sq, a.inv_cols, a.eps));
+  using Shape = NormShape<LPR, WPR>;
+  __shared__ float slots[Shape::kGroups][2][WPR][2];
+  const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, group = warp / WPR, seg0 = warp % WPR;
   const bool w_aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
+  int64_t row = (int64_t)blockIdx.x * Shape::kRows + group * (32 / LPR) + lane / LPR;
+  // narrow rows: a warp goes on while any of its rows exists
+  int64_t lead = (int64_t)blockIdx.x * Shape::kRows + group * (32 / LPR);
+  Segment<T, VEC, LPR> x[VPL], r[VPL];
+  auto columns = [&](int s) { return (int)min((int64_t)LPR * 8, a.cols - (int64_t)(seg0 + s * WPR) * (LPR * 8)); };
+  auto fetch = [&]() {
 #pragma unroll
-  for (int s = 0; s < VPL; ++s) {
-    const int seg = seg0 + s * WPR;
-    const int64_t col = (int64_t)seg * kSegment;
-    const int valid = (int)min((int64_t)kSegment, a.cols - col);
-    if (valid <= 0) continue;                                          // the same for the whole warp
-    if (a.total) segment_store<T, VEC>(reinterpret_cast<T*>(a.total) + row * a.total_pitch + col, valid, lane, t[s]);
-    float w[8];
-    weight_load<VEC>(a.weight + col, valid, lane, w_aligned, w);
+    for (int s = 0; s < VPL; ++s) {
+      const int64_t col = (int64_t)(seg0 + s * WPR) * (LPR * 8);
+      const int valid = row < a.rows ? columns(s) : 0;
+      x[s].load(reinterpret_cast<const T*>(a.x) + row * a.x_pitch + col, valid, l);
+      if constexpr (RES) r[s].load(reinterpret_cast<const T*>(a.residual) + row * a.residual_pitch + col, valid, l);
+    }
+  };
+  fetch();
+  int turn = 0;
+  while (lead < a.rows) {
+    float t[VPL][8], sq = 0.0f, none = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[s][i] = t[s][i] * rstd * w[i];
-    if constexpr (!CODES) {
-      segment_store<T, VEC>(reinterpret_cast<T*>(a.y) + row * a.y_pitch + col, valid, lane, t[s]);
-    } else {
-      // largest magnitude of each 128-column block, as bit patterns, so that a NaN is the largest: VEC lanes 0..15 hold
-      // the first block and 16..31 the second, else elements 0..3 and 4..7 of every lane do
-      uint32_t top[2] = {0u, 0u};
+    for (int s = 0; s < VPL; ++s) {
+      x[s].get(t[s]);
+      if (m.threshold != 0) segment_drop<VEC, LPR>(t[s], (uint32_t)(seg0 + s * WPR) * LPR, (uint32_t)row, l, m);
+      float w[8];
+      if constexpr (RES) r[s].get(w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t mag = segment_column<VEC>(lane, i) < valid ? __float_as_uint(t[s][i]) & 0x7FFFFFFFu : 0u;
-        const int b = VEC ? (lane >> 4) : (i >> 2);
-        if (b == 0) top[0] = max(top[0], mag); else top[1] = max(top[1], mag);
+        t[s][i] = m.all ? 0.0f : t[s][i] * m.factor;
+        if constexpr (RES) t[s][i] += w[i];
+        sq = fmaf(t[s][i], t[s][i], sq);
       }
-      top[0] = __reduce_max_sync(0xFFFFFFFFu, top[0]);
-      top[1] = __reduce_max_sync(0xFFFFFFFFu, top[1]);
-      float scale[2], inv[2];
+    }
+    const int64_t here = row;
+    row += (int64_t)gridDim.x * Shape::kRows;
+    lead += (int64_t)gridDim.x * Shape::kRows;
+    if (lead < a.rows) fetch();
+    row_sums<LPR, WPR>(sq, none, slots[group], turn, seg0, group);
+    const float rstd = 1.0f / sqrtf(fmaf(sq, a.inv_cols, a.eps));
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        scale[b] = __uint_as_float(top[b]) * (1.0f / 448.0f);
-        if (scale[b] < 0x1p-126f) scale[b] = 0.0f;                     // its reciprocal could overflow
-        inv[b] = scale[b] == 0.0f ? 0.0f : 1.0f / scale[b];
-        const int64_t block = (int64_t)seg * 2 + b;
-        if (lane == 0 && block < a.blocks) a.scales[row * a.blocks + block] = scale[b];
-      }
-      uint8_t* out = a.codes + row * a.y_pitch + col;
-      if constexpr (VEC) {
-        const float f = lane >> 4 ? inv[1] : inv[0];
-        const uint32_t lo = e4m3x2(t[s][0] * f, t[s][1] * f) | e4m3x2(t[s][2] * f, t[s][3] * f) << 16;
-        const uint32_t hi = e4m3x2(t[s][4] * f, t[s][5] * f) | e4m3x2(t[s][6] * f, t[s][7] * f) << 16;
-        if (lane * 8 + 8 <= valid) *reinterpret_cast<uint2*>(out + lane * 8) = make_uint2(lo, hi);
-        else {
+    for (int s = 0; s < VPL; ++s) {
+      const int seg = seg0 + s * WPR;
+      const int64_t col = (int64_t)seg * (LPR * 8);
+      const int valid = here < a.rows ? columns(s) : 0;
+      if (LPR == 32 && valid <= 0) continue;                           // the same for the whole warp
+      if (a.total) segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.total) + here * a.total_pitch + col, valid, l, t[s]);
+      float w[8];
+      weight_load<VEC, LPR>(a.weight + col, valid, l, w_aligned, w);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (lane * 8 + i < valid) out[lane * 8 + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
-        }
+      for (int i = 0; i < 8; ++i) t[s][i] = t[s][i] * rstd * w[i];
+      if constexpr (!CODES) {
+        segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.y) + here * a.y_pitch + col, valid, l, t[s]);
       } else {
+        // largest magnitude of each 128-column block, as bit patterns, so that a NaN is the largest. Consecutive elements:
+        // a block is 16 lanes (or a narrow row's 8); else elements 0..3 of all lanes, and 4..7
+        constexpr bool kConsecutive = VEC || LPR < 32;
+        constexpr int kParts = kConsecutive ? 1 : 2;                   // blocks that a lane has elements of
+        uint32_t top[2] = {0u, 0u};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int c = i * 32 + lane;
-          if (c < valid) out[c] = (uint8_t)e4m3x2(t[s][i] * inv[i >> 2], 0.0f);
+          const uint32_t mag = segment_column<VEC, LPR>(l, i) < valid ? __float_as_uint(t[s][i]) & 0x7FFFFFFFu : 0u;
+          top[kConsecutive ? 0 : i >> 2] = max(top[kConsecutive ? 0 : i >> 2], mag);
+        }
+        float scale[2], inv[2];
+#pragma unroll
+        for (int b = 0; b < kParts; ++b) {
+          if constexpr (kConsecutive) {
+#pragma unroll
+            for (int o = (LPR < 16 ? LPR : 16) / 2; o > 0; o >>= 1) top[b] = max(top[b], __shfl_xor_sync(0xFFFFFFFFu, top[b], o));
+          } else {
+            top[b] = __reduce_max_sync(0xFFFFFFFFu, top[b]);
+          }
+          scale[b] = __uint_as_float(top[b]) * (1.0f / 448.0f);
+          if (scale[b] < 0x1p-126f) scale[b] = 0.0f;                   // its reciprocal could overflow
+          inv[b] = scale[b] == 0.0f ? 0.0f : 1.0f / scale[b];
+          const int64_t block = kConsecutive ? (col >> 7) + (l >> 4) : (col >> 7) + b;
+          if ((kConsecutive ? (l & 15) == 0 : l == 0) && block < a.blocks && valid > 0) a.scales[here * a.blocks + block] = scale[b];
+        }
+        uint8_t* out = a.codes + here * a.y_pitch + col;
+        if constexpr (kConsecutive) {
+          const float f = inv[0];
+          const uint32_t lo = e4m3x2(t[s][0] * f, t[s][1] * f) | e4m3x2(t[s][2] * f, t[s][3] * f) << 16;
+          const uint32_t hi = e4m3x2(t[s][4] * f, t[s][5] * f) | e4m3x2(t[s][6] * f, t[s][7] * f) << 16;
+          if (VEC && l * 8 + 8 <= valid) *reinterpret_cast<uint2*>(out + l * 8) = make_uint2(lo, hi);
+          else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (l * 8 + i < valid) out[l * 8 + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int c = i * 32 + l;
+            if (c < valid) out[c] = (uint8_t)e4m3x2(t[s][i] * inv[i >> 2], 0.0f);
+          }
         }
       }
     }
@@ -237,9 +311,9 @@ add_rms_norm_kernel(NormArgs a, DropoutMask m) {
 }
 
 // =================================================================================================
-// Gradient of the norm. The groups of the grid walk the rows with a fixed stride and keep their part of dweight in
-// registers; the parts of a CTA meet in shared memory in warp order, those of the CTAs in a second kernel in CTA
-// order, so the sum over rows has one fixed association.
+// Gradient of the norm: the same walk. The weights and the lanes' parts of dweight stay in registers; the parts of a CTA
+// meet in shared memory in group order, those of the CTAs in a second kernel in CTA order, so the sum over rows has one
+// fixed association.
 // =================================================================================================
 struct NormGradArgs {
   const void* dy;
@@ -254,99 +328,102 @@ struct NormGradArgs {
   float eps, inv_cols;
 };
 
-template <typename T, bool VEC, int WPR, int VPL>
-__global__ void __launch_bounds__(WPR == 1 ? 128 : WPR * 32)
+template <typename T, bool VEC, int LPR, int WPR, int VPL, bool PAST>
+__global__ void __launch_bounds__(NormShape<LPR, WPR>::kThreads)
 add_rms_norm_grad_kernel(NormGradArgs a, DropoutMask m) {
-  constexpr int kRowsPerCta = WPR == 1 ? 4 : 1;
-  __shared__ float slots[2][2][WPR];
-  __shared__ float parts[WPR == 1 ? 4 * VPL * kSegment : 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int seg0 = WPR == 1 ? 0 : warp;
+  using Shape = NormShape<LPR, WPR>;
+  constexpr int kCols = LPR * 8 * WPR * VPL;                           // columns that the registers of a group cover
+  constexpr int kParts = Shape::kGroups * (32 / LPR);                  // parts of dweight in a CTA
+  __shared__ float slots[Shape::kGroups][2][WPR][2];
+  __shared__ float parts[kParts > 1 ? kParts * kCols : 1];
+  const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, group = warp / WPR, seg0 = warp % WPR;
   const bool w_aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
-  float dw[VPL][8];
+  int64_t row = (int64_t)blockIdx.x * Shape::kRows + group * (32 / LPR) + lane / LPR;
+  int64_t lead = (int64_t)blockIdx.x * Shape::kRows + group * (32 / LPR);
+  auto columns = [&](int s) { return (int)min((int64_t)LPR * 8, a.cols - (int64_t)(seg0 + s * WPR) * (LPR * 8)); };
+  float dw[VPL][8], w[VPL][8];
+  Segment<T, VEC, LPR> dy[VPL], tot[VPL], past[VPL];
+  auto fetch = [&]() {
 #pragma unroll
-  for (int s = 0; s < VPL; ++s)
+    for (int s = 0; s < VPL; ++s) {
+      const int64_t col = (int64_t)(seg0 + s * WPR) * (LPR * 8);
+      const int valid = row < a.rows ? columns(s) : 0;
+      dy[s].load(reinterpret_cast<const T*>(a.dy) + row * a.dy_pitch + col, valid, l);
+      tot[s].load(reinterpret_cast<const T*>(a.total) + row * a.total_pitch + col, valid, l);
+      if constexpr (PAST) past[s].load(reinterpret_cast<const T*>(a.dtotal) + row * a.dtotal_pitch + col, valid, l);
+    }
+  };
+  fetch();
+#pragma unroll
+  for (int s = 0; s < VPL; ++s) {
+    weight_load<VEC, LPR>(a.weight + (int64_t)(seg0 + s * WPR) * (LPR * 8), columns(s), l, w_aligned, w[s]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[s][i] = 0.0f;
-  int flip = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kRowsPerCta + (WPR == 1 ? warp : 0); row < a.rows; row += (int64_t)gridDim.x * kRowsPerCta) {
-    float g[VPL][8], t[VPL][8];                                        // weight * dy, total
-    float sq = 0.0f, dot = 0.0f;
+  }
+  int turn = 0;
+  while (lead < a.rows) {
+    float g[VPL][8], t[VPL][8], d[VPL][8], sq = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int s = 0; s < VPL; ++s) {
-      const int64_t col = (int64_t)(seg0 + s * WPR) * kSegment;
-      const int valid = (int)min((int64_t)kSegment, a.cols - col);
-      segment_load<T, VEC>(reinterpret_cast<const T*>(a.dy) + row * a.dy_pitch + col, valid, lane, g[s]);
-      segment_load<T, VEC>(reinterpret_cast<const T*>(a.total) + row * a.total_pitch + col, valid, lane, t[s]);
-    }
-    float w[VPL][8];
-#pragma unroll
-    for (int s = 0; s < VPL; ++s) {
-      const int64_t col = (int64_t)(seg0 + s * WPR) * kSegment;
-      weight_load<VEC>(a.weight + col, (int)min((int64_t)kSegment, a.cols - col), lane, w_aligned, w[s]);
+      dy[s].get(g[s]);
+      tot[s].get(t[s]);
+      if constexpr (PAST) past[s].get(d[s]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sq = fmaf(t[s][i], t[s][i], sq);
         dot = fmaf(g[s][i] * w[s][i], t[s][i], dot);
       }
     }
-    if constexpr (WPR == 1) {
-      sq = warp_sum(sq);
-      dot = warp_sum(dot);
-    } else {
-      sq = warp_sum(sq);
-      dot = warp_sum(dot);
-      if (lane == 0) { slots[flip][0][warp] = sq; slots[flip][1][warp] = dot; }
-      __syncthreads();
-      sq = dot = 0.0f;
-#pragma unroll
-      for (int q = 0; q < WPR; ++q) { sq += slots[flip][0][q]; dot += slots[flip][1][q]; }
-      flip ^= 1;                                                       // the other set is written before the next barrier
-    }
+    const int64_t here = row;
+    row += (int64_t)gridDim.x * Shape::kRows;
+    lead += (int64_t)gridDim.x * Shape::kRows;
+    if (lead < a.rows) fetch();
+    row_sums<LPR, WPR>(sq, dot, slots[group], turn, seg0, group);
     const float r = 1.0f / sqrtf(fmaf(sq, a.inv_cols, a.eps));
     const float c = r * r * r * (dot * a.inv_cols);
 #pragma unroll
     for (int s = 0; s < VPL; ++s) {
       const int seg = seg0 + s * WPR;
-      const int64_t col = (int64_t)seg * kSegment;
-      const int valid = (int)min((int64_t)kSegment, a.cols - col);
-      if (valid <= 0) continue;
-      float d[8];
-      if (a.dtotal) segment_load<T, VEC>(reinterpret_cast<const T*>(a.dtotal) + row * a.dtotal_pitch + col, valid, lane, d);
+      const int64_t col = (int64_t)seg * (LPR * 8);
+      const int valid = here < a.rows ? columns(s) : 0;
+      if (LPR == 32 && valid <= 0) continue;                           // the same for the whole warp
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        dw[s][i] = fmaf(g[s][i] * t[s][i], r, dw[s][i]);
+        if (here < a.rows) dw[s][i] = fmaf(g[s][i] * t[s][i], r, dw[s][i]);
         const float v = r * (g[s][i] * w[s][i]) - t[s][i] * c;
-        d[i] = a.dtotal ? d[i] + v : v;
+        d[s][i] = PAST ? d[s][i] + v : v;
       }
-      segment_store<T, VEC>(reinterpret_cast<T*>(a.dresidual) + row * a.dresidual_pitch + col, valid, lane, d);
+      segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.dresidual) + here * a.dresidual_pitch + col, valid, l, d[s]);
       if (a.dx) {
-        if (m.threshold != 0) segment_dropout<VEC>(d, (uint32_t)seg * (kSegment / 8), (uint32_t)row, lane, m);
-        segment_store<T, VEC>(reinterpret_cast<T*>(a.dx) + row * a.dx_pitch + col, valid, lane, d);
+        if (m.threshold != 0) segment_drop<VEC, LPR>(d[s], (uint32_t)seg * LPR, (uint32_t)here, l, m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[s][i] = m.all ? 0.0f : d[s][i] * m.factor;
+        segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.dx) + here * a.dx_pitch + col, valid, l, d[s]);
       }
     }
   }
   if (!a.partial) return;
   float* out = a.partial + (int64_t)blockIdx.x * a.cols;
-  if constexpr (WPR == 1) {
+  if constexpr (kParts > 1) {
+    float* mine = parts + (group * (32 / LPR) + lane / LPR) * kCols;
 #pragma unroll
     for (int s = 0; s < VPL; ++s)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) parts[(warp * VPL + s) * kSegment + segment_column<VEC>(lane, i)] = dw[s][i];
+      for (int i = 0; i < 8; ++i) mine[(seg0 + s * WPR) * (LPR * 8) + segment_column<VEC, LPR>(l, i)] = dw[s][i];
     __syncthreads();
-    for (int c = threadIdx.x; c < a.cols; c += 128) {
+    for (int c = threadIdx.x; c < a.cols; c += Shape::kThreads) {
       float v = parts[c];
 #pragma unroll
-      for (int q = 1; q < 4; ++q) v += parts[q * VPL * kSegment + c];
+      for (int q = 1; q < kParts; ++q) v += parts[q * kCols + c];
       out[c] = v;
     }
   } else {
 #pragma unroll
     for (int s = 0; s < VPL; ++s) {
-      const int64_t col = (int64_t)(seg0 + s * WPR) * kSegment;
+      const int64_t col = (int64_t)(seg0 + s * WPR) * (LPR * 8);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int64_t c = col + segment_column<VEC>(lane, i);
+        const int64_t c = col + segment_column<VEC, LPR>(l, i);
         if (c < a.cols) out[c] = dw[s][i];
       }
     }
@@ -372,48 +449,58 @@ norm_dweight_kernel(const float* __restrict__ partial, int parts, int64_t cols, 
   }
 }
 
-constexpr int kNormGradMaxCtas = 148 * 8;              // the workspace holds this many parts at most
+// Runs CALL(lanes per row, warps per row, segments per warp) for rows of `cols` columns.
+#define SWARM_NORM_SHAPES(cols, CALL)             \
+  ((cols) <= 64 ? CALL(8, 1, 1)                   \
+   : (cols) <= 128 ? CALL(16, 1, 1)               \
+   : (cols) <= 256 ? CALL(32, 1, 1)               \
+   : (cols) <= 512 ? CALL(32, 2, 1)               \
+   : (cols) <= 1024 ? CALL(32, 4, 1)              \
+   : (cols) <= 2048 ? CALL(32, 8, 1)              \
+   : (cols) <= 4096 ? CALL(32, 8, 2)              \
+   : (cols) <= 8192 ? CALL(32, 16, 2)             \
+   : (cols) <= 16384 ? CALL(32, 16, 4)            \
+                     : CALL(32, 32, 4))
 
-// Runs CALL with WPR warps per row and VPL segments per warp for rows of `cols` columns.
-#define SWARM_NORM_SHAPES(cols, CALL)                      \
-  do {                                                     \
-    const int64_t segs_ = ((cols) + kSegment - 1) / kSegment; \
-    if (segs_ <= 1) CALL(1, 1)                             \
-    else if (segs_ <= 2) CALL(1, 2)                        \
-    else if (segs_ <= 4) CALL(1, 4)                        \
-    else if (segs_ <= 8) CALL(4, 2)                        \
-    else if (segs_ <= 16) CALL(8, 2)                       \
-    else if (segs_ <= 32) CALL(16, 2)                      \
-    else if (segs_ <= 64) CALL(16, 4)                      \
-    else CALL(32, 4)                                       \
-  } while (0)
+template <typename T, bool VEC, int LPR, int WPR, int VPL, bool RES, bool CODES>
+cudaError_t launch_norm_as(const NormArgs& a, const DropoutMask& m, cudaStream_t st) {
+  using Shape = NormShape<LPR, WPR>;
+  int64_t most = 0;
+  const cudaError_t e = resident_ctas(add_rms_norm_kernel<T, VEC, LPR, WPR, VPL, RES, CODES>, Shape::kThreads, &most);
+  if (e != cudaSuccess) return e;
+  const int64_t ctas = (a.rows + Shape::kRows - 1) / Shape::kRows;
+  add_rms_norm_kernel<T, VEC, LPR, WPR, VPL, RES, CODES><<<(unsigned)(ctas < most ? ctas : most), Shape::kThreads, 0, st>>>(a, m);
+  return cudaGetLastError();
+}
 
 template <typename T, bool VEC, bool CODES>
 cudaError_t launch_norm(const NormArgs& a, const DropoutMask& m, cudaStream_t st) {
-#define SWARM_CALL(W, V)                                                                                  \
-  {                                                                                                       \
-    const unsigned grid_ = (unsigned)(W == 1 ? (a.rows + 3) / 4 : a.rows);                                \
-    add_rms_norm_kernel<T, VEC, W, V, CODES><<<grid_, W == 1 ? 128 : W * 32, 0, st>>>(a, m);              \
-  }
-  SWARM_NORM_SHAPES(a.cols, SWARM_CALL);
+#define SWARM_CALL(L, W, V) (a.residual ? launch_norm_as<T, VEC, L, W, V, true, CODES>(a, m, st) : launch_norm_as<T, VEC, L, W, V, false, CODES>(a, m, st))
+  return SWARM_NORM_SHAPES(a.cols, SWARM_CALL);
 #undef SWARM_CALL
-  return cudaGetLastError();
 }
 
-// CTAs of the gradient kernel for these sizes.
-int64_t norm_grad_ctas(int64_t rows, int64_t cols) {
-  const int64_t groups = cols <= 4 * kSegment ? (rows + 3) / 4 : rows;
-  const int64_t most = cols <= 4 * kSegment ? 148 * 4 : cols <= 16 * kSegment ? 148 * 2 : 148;
-  const int64_t ctas = groups < most ? groups : most;
-  return ctas < kNormGradMaxCtas ? ctas : kNormGradMaxCtas;
+// Parts of dweight that the workspace has room for: no gradient kernel runs with more CTAs.
+constexpr int64_t kNormGradCtas = 148 * 4;
+
+template <typename T, bool VEC, int LPR, int WPR, int VPL, bool PAST>
+cudaError_t launch_norm_grad_as(const NormGradArgs& a, const DropoutMask& m, int64_t* ctas, cudaStream_t st) {
+  using Shape = NormShape<LPR, WPR>;
+  int64_t most = 0;
+  const cudaError_t e = resident_ctas(add_rms_norm_grad_kernel<T, VEC, LPR, WPR, VPL, PAST>, Shape::kThreads, &most);
+  if (e != cudaSuccess) return e;
+  if (most > kNormGradCtas) most = kNormGradCtas;
+  *ctas = (a.rows + Shape::kRows - 1) / Shape::kRows;
+  if (*ctas > most) *ctas = most;
+  add_rms_norm_grad_kernel<T, VEC, LPR, WPR, VPL, PAST><<<(unsigned)*ctas, Shape::kThreads, 0, st>>>(a, m);
+  return cudaGetLastError();
 }
 
 template <typename T, bool VEC>
-cudaError_t launch_norm_grad(const NormGradArgs& a, const DropoutMask& m, cudaStream_t st) {
-#define SWARM_CALL(W, V) add_rms_norm_grad_kernel<T, VEC, W, V><<<(unsigned)norm_grad_ctas(a.rows, a.cols), W == 1 ? 128 : W * 32, 0, st>>>(a, m);
-  SWARM_NORM_SHAPES(a.cols, SWARM_CALL);
+cudaError_t launch_norm_grad(const NormGradArgs& a, const DropoutMask& m, int64_t* ctas, cudaStream_t st) {
+#define SWARM_CALL(L, W, V) (a.dtotal ? launch_norm_grad_as<T, VEC, L, W, V, true>(a, m, ctas, st) : launch_norm_grad_as<T, VEC, L, W, V, false>(a, m, ctas, st))
+  return SWARM_NORM_SHAPES(a.cols, SWARM_CALL);
 #undef SWARM_CALL
-  return cudaGetLastError();
 }
 
 // ---- argument checks ------------------------------------------------------------------------
@@ -450,13 +537,13 @@ int swarm_dropout(const void* x_dev, const void* residual_dev, void* out_dev, in
   a.x = x_dev; a.residual = residual_dev; a.out = out_dev;
   a.x_pitch = x_pitch; a.residual_pitch = residual_pitch; a.out_pitch = out_pitch;
   a.rows = rows; a.cols = cols;
-  a.segments = (uint32_t)((cols + kSegment - 1) / kSegment);
   const DropoutMask m = make_dropout_mask(rate, seed, event);
   const bool vec = on16(x_dev, x_pitch, size) && on16(residual_dev, residual_pitch, size) && on16(out_dev, out_pitch, size);
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (dtype == SWARM_F32) return operator_result(launch_dropout<float>(a, m, vec, st));
-  if (dtype == SWARM_BF16) return operator_result(launch_dropout<__nv_bfloat16>(a, m, vec, st));
-  return operator_result(launch_dropout<__half>(a, m, vec, st));
+  if (dtype == SWARM_F32) return operator_result(vec ? launch_dropout<float, true>(a, m, st) : launch_dropout<float, false>(a, m, st));
+  if (dtype == SWARM_BF16)
+    return operator_result(vec ? launch_dropout<__nv_bfloat16, true>(a, m, st) : launch_dropout<__nv_bfloat16, false>(a, m, st));
+  return operator_result(vec ? launch_dropout<__half, true>(a, m, st) : launch_dropout<__half, false>(a, m, st));
 }
 
 int swarm_add_rms_norm(const void* x_dev, const void* residual_dev, const float* weight_dev, void* total_dev,
@@ -495,7 +582,7 @@ int swarm_add_rms_norm(const void* x_dev, const void* residual_dev, const float*
 
 size_t swarm_add_rms_norm_workspace(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || cols > SWARM_NORM_MAX_COLS) return 0;
-  return (size_t)(norm_grad_ctas(rows, cols) * cols) * sizeof(float);
+  return (size_t)((rows < kNormGradCtas ? rows : kNormGradCtas) * cols) * sizeof(float);
 }
 
 int swarm_add_rms_norm_backward(const void* dy_dev, const void* dtotal_dev, const void* total_dev,
@@ -526,12 +613,13 @@ int swarm_add_rms_norm_backward(const void* dy_dev, const void* dtotal_dev, cons
   const DropoutMask m = make_dropout_mask(rate, seed, event);
   const bool vec = on16(dy_dev, dy_pitch, size) && on16(dtotal_dev, dtotal_pitch, size) && on16(total_dev, total_pitch, size) &&
                    on16(dresidual_dev, dresidual_pitch, size) && on16(dx_dev, dx_pitch, size);
+  int64_t ctas = 0;
   cudaError_t e;
-  if (dtype == SWARM_F32) e = vec ? launch_norm_grad<float, true>(a, m, st) : launch_norm_grad<float, false>(a, m, st);
-  else if (dtype == SWARM_BF16) e = vec ? launch_norm_grad<__nv_bfloat16, true>(a, m, st) : launch_norm_grad<__nv_bfloat16, false>(a, m, st);
-  else e = vec ? launch_norm_grad<__half, true>(a, m, st) : launch_norm_grad<__half, false>(a, m, st);
+  if (dtype == SWARM_F32) e = vec ? launch_norm_grad<float, true>(a, m, &ctas, st) : launch_norm_grad<float, false>(a, m, &ctas, st);
+  else if (dtype == SWARM_BF16) e = vec ? launch_norm_grad<__nv_bfloat16, true>(a, m, &ctas, st) : launch_norm_grad<__nv_bfloat16, false>(a, m, &ctas, st);
+  else e = vec ? launch_norm_grad<__half, true>(a, m, &ctas, st) : launch_norm_grad<__half, false>(a, m, &ctas, st);
   if (e == cudaSuccess && dweight_dev) {
-    norm_dweight_kernel<<<(unsigned)((cols + 31) / 32), 1024, 0, st>>>(a.partial, (int)norm_grad_ctas(rows, cols), cols, dweight_dev);
+    norm_dweight_kernel<<<(unsigned)((cols + 31) / 32), 1024, 0, st>>>(a.partial, (int)ctas, cols, dweight_dev);
     e = cudaGetLastError();
   }
   return operator_result(e);
