@@ -34,8 +34,8 @@ cudaError_t operator_sm_count(int* out) {
 namespace {
 
 // CTAs of a kernel that the device holds at once, looked up once per kernel and device.
-template <typename K>
-cudaError_t resident_ctas(K kernel, int threads, int64_t* out) {
+template <auto Kernel>
+cudaError_t resident_ctas(int threads, int64_t* out) {
   static int per_device[64] = {};
   static std::mutex mutex;
   int sms = 0, dev = 0;
@@ -45,7 +45,7 @@ cudaError_t resident_ctas(K kernel, int threads, int64_t* out) {
   std::lock_guard<std::mutex> lock(mutex);
   if (!per_device[dev]) {
     int n = 0;
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, 0);
     if (e != cudaSuccess) return e;
     per_device[dev] = n < 1 ? 1 : n;
   }
@@ -117,7 +117,7 @@ dropout_kernel(DropoutArgs a, DropoutMask m) {
 template <typename T, bool VEC, int LPR, bool RES>
 cudaError_t launch_dropout_as(DropoutArgs a, const DropoutMask& m, cudaStream_t st) {
   int64_t most = 0;
-  const cudaError_t e = resident_ctas(dropout_kernel<T, VEC, LPR, RES>, kRowThreads, &most);
+  const cudaError_t e = resident_ctas<dropout_kernel<T, VEC, LPR, RES>>(kRowThreads, &most);
   if (e != cudaSuccess) return e;
   a.segments = (uint32_t)((a.cols + LPR * 8 - 1) / (LPR * 8));
   a.row_groups = (a.rows + 32 / LPR - 1) / (32 / LPR);
@@ -466,7 +466,7 @@ template <typename T, bool VEC, int LPR, int WPR, int VPL, bool RES, bool CODES>
 cudaError_t launch_norm_as(const NormArgs& a, const DropoutMask& m, cudaStream_t st) {
   using Shape = NormShape<LPR, WPR>;
   int64_t most = 0;
-  const cudaError_t e = resident_ctas(add_rms_norm_kernel<T, VEC, LPR, WPR, VPL, RES, CODES>, Shape::kThreads, &most);
+  const cudaError_t e = resident_ctas<add_rms_norm_kernel<T, VEC, LPR, WPR, VPL, RES, CODES>>(Shape::kThreads, &most);
   if (e != cudaSuccess) return e;
   const int64_t ctas = (a.rows + Shape::kRows - 1) / Shape::kRows;
   add_rms_norm_kernel<T, VEC, LPR, WPR, VPL, RES, CODES><<<(unsigned)(ctas < most ? ctas : most), Shape::kThreads, 0, st>>>(a, m);
@@ -487,7 +487,7 @@ template <typename T, bool VEC, int LPR, int WPR, int VPL, bool PAST>
 cudaError_t launch_norm_grad_as(const NormGradArgs& a, const DropoutMask& m, int64_t* ctas, cudaStream_t st) {
   using Shape = NormShape<LPR, WPR>;
   int64_t most = 0;
-  const cudaError_t e = resident_ctas(add_rms_norm_grad_kernel<T, VEC, LPR, WPR, VPL, PAST>, Shape::kThreads, &most);
+  const cudaError_t e = resident_ctas<add_rms_norm_grad_kernel<T, VEC, LPR, WPR, VPL, PAST>>(Shape::kThreads, &most);
   if (e != cudaSuccess) return e;
   if (most > kNormGradCtas) most = kNormGradCtas;
   *ctas = (a.rows + Shape::kRows - 1) / Shape::kRows;
