@@ -120,23 +120,23 @@ __device__ __forceinline__ void segment_store(T* p, int valid, int l, const floa
   }
 }
 
-// Mask of a dropout call. threshold: 16-bit draws below it drop the element (0: nothing is dropped). Rate 1 drops
-// everything: the threshold then stays below 2^16, the factor is 0 and `all` is set.
+// Mask of a dropout call with threshold T: a 16-bit draw below T drops the element. `limit` = T * 2^16 - 1, so that a draw in
+// the high half of a word is kept iff word > limit, whatever its low half holds (T = 2^16 keeps nothing).
 struct DropoutMask {
   PhiloxRoundKeys rk;
-  uint32_t event, threshold;
+  uint32_t event, limit;
   float factor;
-  int32_t all;
+  int32_t active;                     // 0: T = 0, nothing is dropped
 };
 
 inline DropoutMask make_dropout_mask(double rate, uint64_t seed, uint32_t event) {
   DropoutMask m;
   m.rk = philox_round_keys((uint32_t)seed, (uint32_t)(seed >> 32));
   m.event = event;
-  m.threshold = (uint32_t)(rate * 65536.0 + 0.5);
-  m.all = m.threshold >= 65536;
-  if (m.all) m.threshold = 65535;
-  m.factor = m.all ? 0.0f : (float)(65536.0 / (double)(65536 - m.threshold));
+  const uint32_t threshold = (uint32_t)(rate * 65536.0 + 0.5);
+  m.active = threshold != 0;
+  m.limit = (threshold << 16) - 1u;
+  m.factor = threshold >= 65536 ? 0.0f : (float)(65536.0 / (double)(65536 - threshold));
   return m;
 }
 
@@ -146,17 +146,17 @@ inline DropoutMask make_dropout_mask(double rate, uint64_t seed, uint32_t event)
 template <bool VEC, int LPR>
 __device__ __forceinline__ void segment_drop(float v[8], uint32_t group0, uint32_t row, int l, const DropoutMask& m) {
   const uint4 w = philox4x32_10(group0 + (uint32_t)l, row, m.event, kStreamDropout, m.rk);
-  const uint32_t word[4] = {w.x, w.y, w.z, w.w}, high = m.threshold << 16;     // threshold 65536: handled by the caller
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
   if constexpr (VEC || LPR < 32) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v[2 * i] = (word[i] << 16) >= high ? v[2 * i] : 0.0f;                    // low half
-      v[2 * i + 1] = word[i] >= high ? v[2 * i + 1] : 0.0f;                    // high half: the low bits cannot decide
+      v[2 * i] = (word[i] << 16) > m.limit ? v[2 * i] : 0.0f;                  // low half
+      v[2 * i + 1] = word[i] > m.limit ? v[2 * i + 1] : 0.0f;                  // high half
     }
   } else {
     uint32_t keep = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) keep |= ((word[i] << 16) >= high ? 1u << (2 * i) : 0u) | (word[i] >= high ? 2u << (2 * i) : 0u);
+    for (int i = 0; i < 4; ++i) keep |= ((word[i] << 16) > m.limit ? 1u << (2 * i) : 0u) | (word[i] > m.limit ? 2u << (2 * i) : 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, i * 4 + (l >> 3));

@@ -100,14 +100,14 @@ dropout_kernel(DropoutArgs a, DropoutMask m) {
     for (int u = 0; u < kItems; ++u) {
       float v[8], w[8];
       x[u].get(v);
-      if (m.threshold != 0) segment_drop<VEC, LPR>(v, (uint32_t)(col[u] >> 3), (uint32_t)row[u], l, m);
+      if (m.active) segment_drop<VEC, LPR>(v, (uint32_t)(col[u] >> 3), (uint32_t)row[u], l, m);
       if constexpr (RES) {
         r[u].get(w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = m.all ? w[i] : fmaf(v[i], m.factor, w[i]);
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], m.factor, w[i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = m.all ? 0.0f : v[i] * m.factor;
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * m.factor;
       }
       if (valid[u] > 0) segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.out) + row[u] * a.out_pitch + col[u], valid[u], l, v);
     }
@@ -232,12 +232,12 @@ add_rms_norm_kernel(NormArgs a, DropoutMask m) {
 #pragma unroll
     for (int s = 0; s < VPL; ++s) {
       x[s].get(t[s]);
-      if (m.threshold != 0) segment_drop<VEC, LPR>(t[s], (uint32_t)(seg0 + s * WPR) * LPR, (uint32_t)row, l, m);
+      if (m.active) segment_drop<VEC, LPR>(t[s], (uint32_t)(seg0 + s * WPR) * LPR, (uint32_t)row, l, m);
       float w[8];
       if constexpr (RES) r[s].get(w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        t[s][i] = m.all ? 0.0f : t[s][i] * m.factor;
+        t[s][i] = t[s][i] * m.factor;
         if constexpr (RES) t[s][i] += w[i];
         sq = fmaf(t[s][i], t[s][i], sq);
       }
@@ -395,9 +395,9 @@ add_rms_norm_grad_kernel(NormGradArgs a, DropoutMask m) {
       }
       segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.dresidual) + here * a.dresidual_pitch + col, valid, l, d[s]);
       if (a.dx) {
-        if (m.threshold != 0) segment_drop<VEC, LPR>(d[s], (uint32_t)seg * LPR, (uint32_t)here, l, m);
+        if (m.active) segment_drop<VEC, LPR>(d[s], (uint32_t)seg * LPR, (uint32_t)here, l, m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[s][i] = m.all ? 0.0f : d[s][i] * m.factor;
+        for (int i = 0; i < 8; ++i) d[s][i] = d[s][i] * m.factor;
         segment_store<T, VEC, LPR>(reinterpret_cast<T*>(a.dx) + here * a.dx_pitch + col, valid, l, d[s]);
       }
     }
