@@ -1,7 +1,7 @@
 // Cross attention of few query rows (a decoding step): every state is read once, HBM is the bound.
 //
-// CTA = up to 16 rows (query tokens x the query heads of a key head) and a part of the states, four warps on 32 states
-// at a time each. The products run as m16n8k16 on operands that go from global memory straight into registers:
+// CTA = up to 16 rows (query tokens x the query heads of a key head) and a part of the states, four warps on 16 states at
+// a time each, the next ones fetched before these are used. The products run as m16n8k16 on operands that go from global memory straight into registers:
 //   scores  the order of the contraction over the head's values is free, so a lane takes 16 consecutive bytes of a
 //           state (values 32 p + 8 c .. + 7, c = lane % 4) as the operands of two products, and the same of a row of q
 //   sums    a lane takes 16 bytes (values 8 n .. + 7, n = lane / 4) of the states 2 c, 2 c + 1, 2 c + 8, 2 c + 9 and
@@ -14,7 +14,9 @@
 namespace swarm {
 namespace {
 
-constexpr int kRows = 16, kRowsWarps = 4, kRowsStep = 32;
+constexpr int kRows = 16, kRowsWarps = 4;
+
+constexpr int kRowsStep = 16;                           // states that a warp takes at a time
 
 __device__ __forceinline__ float ex2_(float x) {
   float r;
@@ -54,9 +56,10 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
   const int row0 = group * kRows, rows = min(kRows, plan.rows - row0);
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
   // this CTA's part of the states: equal runs of whole steps of all warps
-  const int steps = (nk + kRowsStep * kRowsWarps - 1) / (kRowsStep * kRowsWarps);
-  const int begin = (int)((int64_t)steps * split / plan.splits) * kRowsStep * kRowsWarps;
-  const int end = min(nk, (int)((int64_t)steps * (split + 1) / plan.splits) * kRowsStep * kRowsWarps);
+  constexpr int kWhole = kRowsStep * kRowsWarps;
+  const int steps = (nk + kWhole - 1) / kWhole;
+  const int begin = (int)((int64_t)steps * split / plan.splits) * kWhole;
+  const int end = min(nk, (int)((int64_t)steps * (split + 1) / plan.splits) * kWhole);
   const int chunks = a.head_dim / 8;                    // 16-byte pieces of a head
 
   uint32_t q[DB * 2][2][4];                             // [32 values][row r8, row r8 + 8][pair]
@@ -79,40 +82,43 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) o[i][u] = 0.0f;
 
-  for (int j0 = begin + warp * kRowsStep; j0 < end; j0 += kRowsStep * kRowsWarps) {
-    uint4 kw[4][DB * 2], vw[2][4][DB];
+  constexpr int kStep = kRowsStep, kStride = kStep * kRowsWarps;
+  struct States { uint4 k[kStep / 8][DB * 2], v[kStep / 16][4][DB]; };
+  auto fetch = [&](States& x, int j0) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {                       // eight states at a time: state r8 of the group
+    for (int g = 0; g < kStep / 8; ++g) {               // eight states at a time: state r8 of the group
       const int j = j0 + g * 8 + r8;
 #pragma unroll
       for (int p = 0; p < DB * 2; ++p)
-        kw[g][p] = j < nk && p * 4 + c4 < chunks ? *reinterpret_cast<const uint4*>(kbase + (int64_t)j * a.ks.token + p * 32 + c4 * 8) : make_uint4(0, 0, 0, 0);
+        x.k[g][p] = j < nk && p * 4 + c4 < chunks ? *reinterpret_cast<const uint4*>(kbase + (int64_t)j * a.ks.token + p * 32 + c4 * 8) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < kStep / 16; ++g)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {                     // states 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of sixteen
         const int j = j0 + g * 16 + c4 * 2 + (u & 1) + (u >> 1) * 8;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
-          vw[g][u][d] = j < nk && d * 8 + r8 < chunks ? *reinterpret_cast<const uint4*>(vbase + (int64_t)j * a.vs.token + d * 64 + r8 * 8) : make_uint4(0, 0, 0, 0);
+          x.v[g][u][d] = j < nk && d * 8 + r8 < chunks ? *reinterpret_cast<const uint4*>(vbase + (int64_t)j * a.vs.token + d * 64 + r8 * 8) : make_uint4(0, 0, 0, 0);
       }
-    float s[4][4];
+  };
+  auto compute = [&](const States& x, int j0) {
+    float s[kStep / 8][4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < kStep / 8; ++g) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) s[g][u] = 0.0f;
 #pragma unroll
       for (int p = 0; p < DB * 2; ++p) {
         const uint32_t a0[4] = {q[p][0][0], q[p][1][0], q[p][0][1], q[p][1][1]};
         const uint32_t a1[4] = {q[p][0][2], q[p][1][2], q[p][0][3], q[p][1][3]};
-        mma16816<T>(s[g], a0, kw[g][p].x, kw[g][p].y);
-        mma16816<T>(s[g], a1, kw[g][p].z, kw[g][p].w);
+        mma16816<T>(s[g], a0, x.k[g][p].x, x.k[g][p].y);
+        mma16816<T>(s[g], a1, x.k[g][p].z, x.k[g][p].w);
       }
     }
-    if (j0 + kRowsStep > nk) {
+    if (j0 + kStep > nk) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
+      for (int g = 0; g < kStep / 8; ++g)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           if (j0 + g * 8 + c4 * 2 + (u & 1) >= nk) s[g][u] = -INFINITY;
@@ -122,7 +128,7 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
     for (int u = 0; u < 2; ++u) {
       float t = fmaxf(s[0][2 * u], s[0][2 * u + 1]);
 #pragma unroll
-      for (int g = 1; g < 4; ++g) t = fmaxf(t, fmaxf(s[g][2 * u], s[g][2 * u + 1]));
+      for (int g = 1; g < kStep / 8; ++g) t = fmaxf(t, fmaxf(s[g][2 * u], s[g][2 * u + 1]));
       t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 1));
       top[u] = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 2));
     }
@@ -139,28 +145,43 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
     }
     const float mc[2] = {m[0] == -INFINITY ? 0.0f : m[0] * c - kShift<T>, m[1] == -INFINITY ? 0.0f : m[1] * c - kShift<T>};
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+    for (int g = 0; g < kStep / 8; ++g)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         s[g][u] = ex2_(fmaf(s[g][u], c, -mc[u >> 1]));
         l[u >> 1] += s[g][u];
       }
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < kStep / 16; ++g) {
       const uint32_t p[4] = {pack2<T>(s[2 * g][0], s[2 * g][1]), pack2<T>(s[2 * g][2], s[2 * g][3]),
                              pack2<T>(s[2 * g + 1][0], s[2 * g + 1][1]), pack2<T>(s[2 * g + 1][2], s[2 * g + 1][3])};
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
-        const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vw[g][0][d]);
-        const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vw[g][1][d]);
-        const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vw[g][2][d]);
-        const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vw[g][3][d]);
+        const uint32_t v[4][4] = {{x.v[g][0][d].x, x.v[g][0][d].y, x.v[g][0][d].z, x.v[g][0][d].w},
+                                  {x.v[g][1][d].x, x.v[g][1][d].y, x.v[g][1][d].z, x.v[g][1][d].w},
+                                  {x.v[g][2][d].x, x.v[g][2][d].y, x.v[g][2][d].z, x.v[g][2][d].w},
+                                  {x.v[g][3][d].x, x.v[g][3][d].y, x.v[g][3][d].z, x.v[g][3][d].w}};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          mma16816<T>(o[d * 8 + 2 * i], p, __byte_perm(v0[i], v1[i], 0x5410), __byte_perm(v2[i], v3[i], 0x5410));
-          mma16816<T>(o[d * 8 + 2 * i + 1], p, __byte_perm(v0[i], v1[i], 0x7632), __byte_perm(v2[i], v3[i], 0x7632));
+          mma16816<T>(o[d * 8 + 2 * i], p, __byte_perm(v[0][i], v[1][i], 0x5410), __byte_perm(v[2][i], v[3][i], 0x5410));
+          mma16816<T>(o[d * 8 + 2 * i + 1], p, __byte_perm(v[0][i], v[1][i], 0x7632), __byte_perm(v[2][i], v[3][i], 0x7632));
         }
       }
+    }
+  };
+  int j0 = begin + warp * kStep;
+  if (j0 < end) {
+    States even, odd;
+    fetch(even, j0);
+    while (true) {
+      if (j0 + kStride < end) fetch(odd, j0 + kStride);
+      compute(even, j0);
+      j0 += kStride;
+      if (j0 >= end) break;
+      if (j0 + kStride < end) fetch(even, j0 + kStride);
+      compute(odd, j0);
+      j0 += kStride;
+      if (j0 >= end) break;
     }
   }
 
@@ -249,15 +270,28 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Ro
     a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
 }
 
+constexpr int kMaxSplits = 32;
+
+// The number of parts of the states that this model of a multiprocessor's time likes best, in states of one CTA: its share
+// of the CTAs, each with its states and a cost of its own (its start, the meeting of its warps, its share of the join:
+// measured, about 64 states and 24 more for each row), divided by the share of the bandwidth that its resident CTAs
+// draw (up to three for heads of up to 64 values, two for longer ones); and the join's launch, about 4 us.
+// Measured (both sides): 16 x 16 heads of 64 over 2048 states 35 us whole and 40 us in five parts; 8 x 8 grouped heads of
+// 128 over 16384 states 101 us in nine parts and 115 us in seven, which leave half a wave empty.
 RowsPlan make_plan(const AttentionArgs& a) {
   RowsPlan p{};
   p.rows = a.queries * a.group;
   p.row_groups = (p.rows + kRows - 1) / kRows;
-  const int64_t ctas = (int64_t)a.batch * a.kv_heads * p.row_groups, room = 148 * 3;
-  int64_t splits = (room + ctas - 1) / ctas;
-  const int64_t most = ((int64_t)a.keys + kRowsStep * kRowsWarps - 1) / (kRowsStep * kRowsWarps);
-  if (splits > most) splits = most;
-  p.splits = (int32_t)(splits < 1 ? 1 : splits);
+  p.splits = 1;
+  const int64_t ctas = (int64_t)a.batch * a.kv_heads * p.row_groups, sms = 148;
+  const double own = 64.0 + 24.0 * (p.rows < kRows ? p.rows : kRows), join = a.head_dim <= 64 ? 480.0 : 320.0;
+  double best = 0.0;
+  for (int s = 1; s <= kMaxSplits && (int64_t)(s - 1) * 128 < a.keys; ++s) {
+    const int64_t each = (ctas * s + sms - 1) / sms;
+    const double drawn = a.head_dim <= 64 ? (each == 1 ? 0.55 : each == 2 ? 0.85 : 1.0) : each == 1 ? 0.6 : 1.0;
+    const double time = (double)each * ((double)a.keys / s + own) / drawn + (s > 1 ? join : 0.0);
+    if (s == 1 || time < best * 0.97) { best = time; p.splits = s; }
+  }
   return p;
 }
 
