@@ -14,10 +14,14 @@ namespace swarm {
 namespace {
 
 // =================================================================================================
-// dq. NT row tiles per CTA, a warpgroup each (thread = row). Tensor memory of a tile: s (64 columns), dp (64) with ds
-// (16 bits) over it, dq. The scores of the next 64 states are computed as soon as these have been read into registers;
-// dp follows once dq has taken ds. While one tile's warps are at their exponentials, the other tile's products (NT = 2)
-// or the other CTA's of the multiprocessor (NT = 1, heads of up to 64 values) run.
+// dq. NT row tiles per CTA, a warpgroup each (thread = row). Tensor memory of a tile: s (64 columns, two sets of them for
+// NT = 1), dp (64) with ds (16 bits) over it, dq. The scores are computed one step ahead (NT = 1) or as soon as those of the
+// step have been read into registers; dp follows once dq has taken ds. While one tile's warps are at their exponentials,
+// the other tile's products (NT = 2) or the other CTA's of the multiprocessor (NT = 1, heads of up to 64 values) run. With
+// two tiles the issuing thread takes up whichever barrier has completed: in a fixed order either tile's scores waited for
+// the other's ds.
+// delta = rowsum(dout * o) is off by what the rounding of o left; the sum of ds over a row, 0 in exact arithmetic, is that
+// error, and the other kernel gets delta without it.
 // =================================================================================================
 constexpr int kStep = 64;                               // states of a step
 constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64 values
@@ -28,11 +32,12 @@ template <int DB, int NT> struct DqShape {
   static constexpr int kRegs = NT == 1 ? 184 : 208, kRegsRest = NT == 1 ? 72 : 88;
   static constexpr int kStages = NT == 1 ? 4 : 3;       // of (k, v)
   static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
-  static constexpr uint32_t kColumns = NT == 1 ? 256 : 512;
+  static constexpr uint32_t kColumns = NT == 1 ? 256 : 512, kDp = NT == 1 ? 128 : 64, kDq = kDp + 64;
 };
 
 struct DqBars {
-  uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2], s_empty[2], dp_full[2], ds_full[2], done[2], edge_here, edge_done, drain;
+  uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2],   // s_full: of the tiles, or of the two sets of one tile's scores
+      s_empty[2], dp_full[2], ds_full[2], done[2], edge_here, edge_done, drain;
 };
 
 template <typename T, int DB, int NT>
@@ -65,7 +70,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
   const int edge = nk % 16 ? nk % kStep : 0;            // states of the last step, where they end inside a product's sixteen
 
   if (tid == 0) {
-    for (int i = 0; i < NT; ++i) {
+    for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars.q_full[i]), 1);
       mbar_init(smem_u32(&bars.s_full[i]), 1);
       mbar_init(smem_u32(&bars.s_empty[i]), 4);
@@ -131,24 +136,28 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
       auto columns = [&](int j) { return (min(kStep, nk - j * kStep) + 15) & ~15; };
       auto scores = [&](int t, int j) {
-        mma_rows<T, DB, kStep>(tmem + 256 * t, aq + 2 * t * kTileBytes, akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
-        tc_commit(smem_u32(&bars.s_full[t]));
+        mma_rows<T, DB, kStep>(tmem + 256 * t + (NT == 1 ? 64 * (j & 1) : 0), aq + 2 * t * kTileBytes,
+                               akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
+        tc_commit(smem_u32(&bars.s_full[NT == 1 ? j & 1 : t]));
       };
       auto dps = [&](int t, int j) {
-        mma_rows<T, DB, kStep>(tmem + 256 * t + 64, aq + (2 * t + 1) * kTileBytes, akv + (2 * (j % kStages) + 1) * kHalfBytes, columns(j), ksteps);
+        mma_rows<T, DB, kStep>(tmem + 256 * t + Shape::kDp, aq + (2 * t + 1) * kTileBytes, akv + (2 * (j % kStages) + 1) * kHalfBytes,
+                               columns(j), ksteps);
         tc_commit(smem_u32(&bars.dp_full[t]));
       };
       auto dqs = [&](int t, int j) {
-        mma_weights<T, DB, kStep, false>(tmem + 256 * t + 128, tmem + 256 * t + 64, akv + 2 * (j % kStages) * kHalfBytes, columns(j) / 16, j != 0);
+        mma_weights<T, DB, kStep, false>(tmem + 256 * t + Shape::kDq, tmem + 256 * t + Shape::kDp, akv + 2 * (j % kStages) * kHalfBytes,
+                                         columns(j) / 16, j != 0);
         if (j == n - 1) tc_commit(smem_u32(&bars.done[t]));
       };
-      auto wait_kv = [&](int j) { return mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, limit); };
-      auto at_edge = [&](int j) { return j == n - 1 && edge; };
-      ok = wait_kv(0);
-      if (ok && at_edge(0)) {
+      // the states of step j have landed, and what lies past their end is zeros where they end inside a product's sixteen
+      auto wait_kv = [&](int j) {
+        if (!mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, limit)) return false;
+        if (j < n - 1 || !edge) return true;
         mbar_arrive(smem_u32(&bars.edge_here));
-        ok = mbar_wait_one(smem_u32(&bars.edge_done), 0, limit);
-      }
+        return mbar_wait_one(smem_u32(&bars.edge_done), 0, limit);
+      };
+      ok = wait_kv(0);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         if (active(t) && ok) {
@@ -156,26 +165,63 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
           tc_fence_after();
           if (ok) { scores(t, 0); dps(t, 0); }
         }
-      for (int j = 0; j < n && ok; ++j) {
-        if (j + 1 < n) ok = wait_kv(j + 1);
-        if (at_edge(j + 1) && ok) mbar_arrive(smem_u32(&bars.edge_here));
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          if (active(t) && ok) {
-            if (j + 1 < n) {
-              ok = mbar_wait_one(smem_u32(&bars.s_empty[t]), j & 1, limit) &&
-                   (!at_edge(j + 1) || mbar_wait_one(smem_u32(&bars.edge_done), 0, limit));
-              tc_fence_after();
-              if (ok) scores(t, j + 1);
-            }
-            if (ok) ok = mbar_wait_one(smem_u32(&bars.ds_full[t]), j & 1, limit);
+      if constexpr (NT == 1) {
+        if (n > 1 && ok) {
+          ok = wait_kv(1);
+          tc_fence_after();
+          if (ok) scores(0, 1);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+          ok = mbar_wait_one(smem_u32(&bars.ds_full[0]), j & 1, limit);
+          if (!ok) break;
+          tc_fence_after();
+          dqs(0, j);
+          if (j + 1 < n) dps(0, j + 1);
+          tc_commit(smem_u32(&bars.kv_empty[j % kStages]));
+          if (j + 2 < n) {                              // ds(j) has been written, so s(j) has been read
+            ok = wait_kv(j + 2);
             tc_fence_after();
-            if (ok) {
-              dqs(t, j);
-              if (j + 1 < n) dps(t, j + 1);
+            if (ok) scores(0, j + 2);
+          }
+        }
+      } else {
+        int next_s[2] = {active(0) ? 1 : n, active(1) ? 1 : n}, next_ds[2] = {active(0) ? 0 : n, active(1) ? 0 : n};
+        int here = 1, freed = 0;                        // steps whose states have landed; whose states are done with
+        bool waits_edge = false;
+        uint32_t idle = 0;
+        while (ok && (next_ds[0] < n || next_ds[1] < n)) {
+          bool moved = false;
+          if (here < n && (next_s[0] == here || next_s[1] == here)) {
+            if (!waits_edge && mbar_test(smem_u32(&bars.kv_full[here % kStages]), (here / kStages) & 1)) {
+              waits_edge = here == n - 1 && edge;
+              if (waits_edge) mbar_arrive(smem_u32(&bars.edge_here));
+              else ++here;
+              moved = true;
+            } else if (waits_edge && mbar_test(smem_u32(&bars.edge_done), 0)) {
+              ++here;
+              moved = true;
             }
           }
-        if (ok) tc_commit(smem_u32(&bars.kv_empty[j % kStages]));
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (next_s[t] < here && mbar_test(smem_u32(&bars.s_empty[t]), (next_s[t] - 1) & 1)) {
+              tc_fence_after();
+              scores(t, next_s[t]);
+              ++next_s[t];
+              moved = true;
+            }
+            if (next_ds[t] < n && next_s[t] > min(next_ds[t] + 1, n - 1) && mbar_test(smem_u32(&bars.ds_full[t]), next_ds[t] & 1)) {
+              tc_fence_after();
+              dqs(t, next_ds[t]);
+              ++next_ds[t];
+              if (next_ds[t] < n) dps(t, next_ds[t]);
+              if (min(next_ds[0], next_ds[1]) > freed) { tc_commit(smem_u32(&bars.kv_empty[freed % kStages])); ++freed; }
+              moved = true;
+            }
+          }
+          if (moved) idle = 0;
+          else if (++idle > limit) ok = false;
+        }
       }
       if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
         tc_commit(smem_u32(&bars.drain));
@@ -189,10 +235,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const int t = NT == 1 ? 0 : warp >> 2, quad = warp & 3, head = head_of(t), row0 = row_of(t), tile_row = quad * 32 + lane;
     const bool work = active(t);
     const int row = row0 + tile_row;
-    const uint32_t ts = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = ts + 64;
+    const uint32_t tile = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = tile + Shape::kDp;
     const float c = a.scale * kLog2e;
     const bool live = work && row < nq;
-    float delta = 0.0f, lse2 = INFINITY;
+    float delta = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
     if (live) {
       const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
       const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, row, head);
@@ -206,24 +252,22 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
       }
     }
-    if (exists(t)) {
-      const int64_t at = ((int64_t)b * a.heads + head) * row_tiles * kTile + row;
-      a.stat_lse[at] = lse2 - kWeightShift<T>;
-      a.stat_delta[at] = delta * pow2_of(kWeightShift<T>);
-    }
     if (work) {
       for (int j = 0; j < n; ++j) {
         const int valid = nk - j * kStep;
         float p[kStep], dp[kStep];
-        ok = mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
+        ok = NT == 1 ? mbar_wait(smem_u32(&bars.s_full[j & 1]), (j >> 1) & 1, limit) : mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
         if (!ok) break;
         tc_fence_after();
+        const uint32_t ts = tile + (NT == 1 ? 64 * (j & 1) : 0);
         tmem_ld32(ts, p);
         tmem_ld32(ts + 32, p + 32);
         tmem_wait_ld();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty[t]));
+        if (NT == 2) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars.s_empty[t]));
+        }
 #pragma unroll
         for (int i = 0; i < kStep; i += 2) {
           fma2(p[i], p[i + 1], p[i], p[i + 1], c, c, -lse2, -lse2);
@@ -249,7 +293,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         for (int g = 0; g < 2; ++g) {
           uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+          for (int i = 0; i < 16; ++i) {
+            add2(off[0], off[1], off[0], off[1], p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+            w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+          }
           tmem_st16(tdp + g * 16, w);
         }
         tmem_wait_st();
@@ -263,11 +310,14 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
     }
     if (exists(t) && named_barrier_and(1 + t, 128, ok)) {
+      const int64_t at = ((int64_t)b * a.heads + head) * row_tiles * kTile + row;
+      a.stat_lse[at] = lse2 - kWeightShift<T>;
+      a.stat_delta[at] = live ? (delta + (off[0] + off[1])) * pow2_of(kWeightShift<T>) : 0.0f;
       uint8_t* out = sQ + 2 * t * kTileBytes;
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
         float o[32];
-        if (work) { tmem_ld32(ts + 128 + g * 32, o); tmem_wait_ld(); }
+        if (work) { tmem_ld32(tile + Shape::kDq + g * 32, o); tmem_wait_ld(); }
         store_row32<T>(out, tile_row, g * 32, o, a.scale, live);
       }
       fence_proxy_async();
