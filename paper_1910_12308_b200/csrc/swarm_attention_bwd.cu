@@ -253,10 +253,12 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
     }
     if (work) {
+      bool ahead = false;                               // the scores of the step have been seen to be there
       for (int j = 0; j < n; ++j) {
         const int valid = nk - j * kStep;
         float p[kStep], dp[kStep];
-        ok = NT == 1 ? mbar_wait(smem_u32(&bars.s_full[j & 1]), (j >> 1) & 1, limit) : mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
+        ok = NT == 1 ? mbar_wait_after(ahead, smem_u32(&bars.s_full[j & 1]), (j >> 1) & 1, limit)
+                     : mbar_wait_after(ahead, smem_u32(&bars.s_full[t]), j & 1, limit);
         if (!ok) break;
         tc_fence_after();
         const uint32_t ts = tile + (NT == 1 ? 64 * (j & 1) : 0);
@@ -299,6 +301,8 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
           }
           tmem_st16(tdp + g * 16, w);
         }
+        ahead = j + 1 < n && (NT == 1 ? mbar_test(smem_u32(&bars.s_full[(j + 1) & 1]), ((j + 1) >> 1) & 1)
+                                      : mbar_test(smem_u32(&bars.s_full[t]), (j + 1) & 1));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -504,13 +508,14 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
     const float c = a.scale * kLog2e;
     constexpr float kUnshift = pow2_of(kWeightShift<T>);
     int step = 0;
+    bool ahead = false;                                 // the step's copies have been seen to be there
     for (int i = 0; i < n; ++i) {
       const int cols = (step == steps - 1 ? nq - step * kRows : kRows) - half * 64;   // columns of this warpgroup that exist
       if (++step == steps) step = 0;
       const float* lse2 = reinterpret_cast<const float*>(sStat + i % kStages * Shape::kStatBytes) + half * 64;
       const float* delta = lse2 + kRows;
       float p[64], stat[32];
-      ok = mbar_wait(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, limit);
+      ok = mbar_wait_after(ahead, smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, limit);
       if (!ok) break;
       load_stats(stat, lse2);
       ok = mbar_wait(smem_u32(&bars.s_full), i & 1, limit);
@@ -570,6 +575,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         for (int q = 0; q < 16; ++q) w[q] = pack2<T>(dp[g * 32 + 2 * q], dp[g * 32 + 2 * q + 1]);
         tmem_st16(tdp + g * 16, w);
       }
+      ahead = i + 1 < n && mbar_test(smem_u32(&bars.full[(i + 1) % kStages]), ((i + 1) / kStages) & 1);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();

@@ -186,8 +186,9 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
     const float c = a.scale * kLog2e;
     float m = -INFINITY, l = 0.0f;                      // m: the maximum that the weights are taken against
     if (work) {
+      bool ahead = false;                               // the scores of the step have been seen to be there
       for (int j = 0; j < n; ++j) {
-        ok = mbar_wait(smem_u32(&bars.s_full[t]), j & 1, limit);
+        ok = mbar_wait_after(ahead, smem_u32(&bars.s_full[t]), j & 1, limit);
         if (!ok) break;
         tc_fence_after();
         const int valid = nk - j * kTile;
@@ -211,13 +212,19 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
           for (int u = 0; u < 4; ++u) top[u] = max3(top[u], s[i + u], s[i + 4 + u]);
         }
         const float m_tile = fmaxf(max3(top[0], s[124], s[125]), max3(max3(top[1], s[126], s[127]), top[2], top[3]));
-        if (NT == 1 && j > 0) {                         // the weights and sums of the last tile are free again
-          ok = mbar_wait(smem_u32(&bars.pv_done[t]), (j - 1) & 1, limit);
-          if (!ok) break;
-          tc_fence_after();
-        }
+        // NT = 1: the weights and sums of the last tile are free again once its product has completed
+        bool pv_waits = NT == 1 && j > 0;
+        auto wait_pv = [&]() {
+          if (pv_waits) {
+            ok = mbar_wait(smem_u32(&bars.pv_done[t]), (j - 1) & 1, limit);
+            tc_fence_after();
+          }
+          pv_waits = false;
+        };
         if (j == 0) m = m_tile;
         else if (__any_sync(0xFFFFFFFFu, (m_tile - m) * c > 8.0f)) {
+          wait_pv();
+          if (!ok) break;
           // the maximum moved by more than a factor of 2^8 in some row of the warp: rescale the sums so far. Smaller
           // moves keep the old reference; the weights then reach 2^8, which fp32 sums and 16-bit weights hold as well.
           const float m_new = fmaxf(m, m_tile), f = m_new == m ? 1.0f : ex2((m - m_new) * c);
@@ -247,8 +254,14 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
             add2(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], sum[2 * (i & 1)], sum[2 * (i & 1) + 1], p0, p1);
             p[i] = pack2<T>(p0, p1);
           }
+          if (NT == 1 && g == 0) {
+            wait_pv();
+            if (!ok) break;
+          }
           tmem_st16(tp + g * 16, p);
         }
+        if (!ok) break;
+        if (NT == 1) ahead = j + 1 < n && mbar_test(smem_u32(&bars.s_full[t]), (j + 1) & 1);
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tmem_wait_st();
         tc_fence_before();
