@@ -15,9 +15,9 @@ struct AttentionArgs {
   const float* lse_in;
   void *out, *dq, *dk, *dv;
   float* lse;
-  // backward, per (sentence, head) padded to whole row tiles: lse * log2(e) and rowsum(dout * o) as the kernels use them,
-  // (infinity, 0) in rows that take no part
-  float *stat_lse, *stat_delta;
+  // backward, per (sentence, head) padded to whole row tiles: lse and rowsum(dout * o) as factors of a product (see the
+  // backward kernels), 32 bytes a row each
+  uint8_t *stat_lse, *stat_delta;
   const int32_t *query_lengths, *key_lengths;
   swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;
   int32_t batch, heads, kv_heads, group, queries, keys, head_dim;

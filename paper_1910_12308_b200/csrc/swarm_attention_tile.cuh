@@ -91,13 +91,19 @@ __device__ __forceinline__ void store_row32(uint8_t* tile, int row, int col, con
   }
 }
 
-// 32 consecutive floats of shared memory, the same for all threads.
-__device__ __forceinline__ void load_stats(float* v, const float* p) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float4 x = reinterpret_cast<const float4*>(p)[i];
-    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-  }
+// A number per row as an operand of a product: 16 values of T of which the first three add up to it (24 bits or more), against
+// a row of kStatOne in the same places. Rows are stored as the unswizzled operand wants them, eight of them in 256 bytes: their
+// first eight values (16 bytes a row), then the others. fp16 has its range widened by kStatOne.
+template <typename T> constexpr float kStatOne = 1.0f;
+template <> constexpr float kStatOne<__half> = 64.0f;
+__device__ __forceinline__ int64_t stat_offset(int64_t row) { return (row >> 3) * 256 + (row & 7) * 16; }
+template <typename T>
+__device__ __forceinline__ void store_stat(uint8_t* p, float v) {
+  v *= 1.0f / kStatOne<T>;
+  const float hi = to_float<T>(from_float<T>(v)), r1 = isinf(hi) ? 0.0f : v - hi;
+  const float mid = to_float<T>(from_float<T>(r1)), lo = r1 - mid;
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(hi, mid), pack2<T>(lo, 0.0f), 0u, 0u);
+  *reinterpret_cast<uint4*>(p + 128) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 }  // namespace swarm
