@@ -29,7 +29,7 @@ constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64
 template <int DB, int NT> struct DqShape {
   static constexpr int kThreads = 128 * (NT + 1);
   static constexpr int kCtasPerSm = NT == 1 ? 2 : 1;
-  static constexpr int kRegs = NT == 1 ? 184 : 208, kRegsRest = NT == 1 ? 72 : 88;
+  static constexpr int kRegs = NT == 1 ? 192 : 208, kRegsRest = NT == 1 ? 64 : 88;
   static constexpr int kStages = NT == 1 ? 4 : 3;       // of (k, v)
   static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
   static constexpr uint32_t kColumns = NT == 1 ? 256 : 512, kDp = NT == 1 ? 128 : 64, kDq = kDp + 64;
@@ -351,7 +351,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 template <int DB, int NW> struct DkvShape {
   static constexpr int kThreads = 128 * (NW + 1);
   static constexpr int kCtasPerSm = NW == 1 ? 2 : 1;
-  static constexpr int kRegs = NW == 1 ? 184 : 208, kRegsRest = NW == 1 ? 72 : 88;
+  static constexpr int kRegs = NW == 1 ? 192 : 208, kRegsRest = NW == 1 ? 64 : 88;
   static constexpr int kRows = 64 * NW;                 // query rows of a step
   static constexpr int kHalfBytes = DB * kRows * 128;   // of q or dout
   static constexpr int kStages = NW == 1 ? 3 : 2;
