@@ -21,7 +21,9 @@ namespace {
 // two tiles the issuing thread takes up whichever barrier has completed: in a fixed order either tile's scores waited for
 // the other's ds.
 // delta = rowsum(dout * o) is off by what the rounding of o left; the sum of ds over a row, 0 in exact arithmetic, is that
-// error, and the other kernel gets delta without it.
+// error, and the other kernel gets delta without it. Here it stays in ds, beside the rounding of ds to eight bits where T is
+// bf16; the two together would leave dq 1.55 times as far from its value as its own rounding does. So in bf16 ds is the
+// sum of two numbers of T, both of which dq takes (the second lies beside the first, over the rest of dp): 1.2 times.
 // =================================================================================================
 constexpr int kStep = 64;                               // states of a step
 constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64 values
@@ -34,6 +36,8 @@ template <int DB, int NT> struct DqShape {
   static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
   static constexpr uint32_t kColumns = NT == 1 ? 256 : 512, kDp = NT == 1 ? 128 : 64, kDq = kDp + 64;
 };
+
+template <typename T> constexpr bool kTwoParts = sizeof(T) == 2 && kWeightShift<T> == 0.0f;            // bf16
 
 struct DqBars {
   uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2],   // s_full: of the tiles, or of the two sets of one tile's scores
@@ -146,8 +150,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         tc_commit(smem_u32(&bars.dp_full[t]));
       };
       auto dqs = [&](int t, int j) {
-        mma_weights<T, DB, kStep, false>(tmem + 256 * t + Shape::kDq, tmem + 256 * t + Shape::kDp, akv + 2 * (j % kStages) * kHalfBytes,
-                                         columns(j) / 16, j != 0);
+#pragma unroll
+        for (int part = 0; part < (kTwoParts<T> ? 2 : 1); ++part)
+          mma_weights<T, DB, kStep, false>(tmem + 256 * t + Shape::kDq, tmem + 256 * t + Shape::kDp + 32 * part,
+                                           akv + 2 * (j % kStages) * kHalfBytes, columns(j) / 16, part != 0 || j != 0);
         if (j == n - 1) tc_commit(smem_u32(&bars.done[t]));
       };
       // the states of step j have landed, and what lies past their end is zeros where they end inside a product's sixteen
@@ -300,6 +306,16 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
             w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
           }
           tmem_st16(tdp + g * 16, w);
+          if (kTwoParts<T>) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float a0, a1;
+              unpack2<T>(w[i], a0, a1);
+              fma2(a0, a1, a0, a1, -1.0f, -1.0f, p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+              w[i] = pack2<T>(a0, a1);
+            }
+            tmem_st16(tdp + 32 + g * 16, w);
+          }
         }
         ahead = j + 1 < n && (NT == 1 ? mbar_test(smem_u32(&bars.s_full[(j + 1) & 1]), ((j + 1) >> 1) & 1)
                                       : mbar_test(smem_u32(&bars.s_full[t]), (j + 1) & 1));
