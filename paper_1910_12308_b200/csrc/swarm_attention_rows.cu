@@ -242,20 +242,21 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Ro
   const int t = row / a.group, h = hk * a.group + row % a.group;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
   const float c = a.scale * kLog2e;
-  const float2* ml = reinterpret_cast<const float2*>(plan.part_ml) + i * plan.splits;
+  // lane s weighs part s; the parts' values are then added in order
   const float* part = plan.part_o + i * plan.splits * a.head_dim + lane * 4;
-  float top = -INFINITY;
-  for (int s = lane; s < plan.splits; s += 32) top = fmaxf(top, ml[s].x);
+  float2 ml = make_float2(-INFINITY, 0.0f);
+  if (lane < plan.splits) ml = reinterpret_cast<const float2*>(plan.part_ml)[i * plan.splits + lane];
+  float top = ml.x;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  const float base = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  const float f = ex2_((ml.x - (top == -INFINITY ? 0.0f : top)) * c), sum = warp_sum(ml.y * f);
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (int s = 0; s < plan.splits; ++s) {
-    const float f = ex2_((ml[s].x - base) * c);
-    sum = fmaf(ml[s].y, f, sum);
+    const float fs = __shfl_sync(0xFFFFFFFFu, f, s);
     if (lane * 4 < a.head_dim) {
       const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)s * a.head_dim);
-      v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
+      v[0] = fmaf(x.x, fs, v[0]); v[1] = fmaf(x.y, fs, v[1]); v[2] = fmaf(x.z, fs, v[2]); v[3] = fmaf(x.w, fs, v[3]);
     }
   }
   const bool live = t < nq && nk > 0;
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Ro
     a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
 }
 
-constexpr int kMaxSplits = 32;
+constexpr int kMaxSplits = 32;                         // a lane of the joining warp each
 
 // The number of parts of the states that this model of a multiprocessor's time likes best, in states of one CTA: its share
 // of the CTAs, each with its states and a cost of its own (its start, the meeting of its warps, its share of the join:
