@@ -17,7 +17,8 @@
  *     call changes no state and no counter.
  *   - Device work is asynchronous on the context's stream and ordered by call order.
  *     swarm_potential, swarm_get_tensor, swarm_sample_pairs and swarm_sync wait for it.
- *   - Device-side waits are bounded (only the tensor-core local-step kernels have any). A kernel whose wait
+ *   - Device-side waits are bounded (only the tensor-core kernels have any; for those of the operators without a
+ *     context see swarm_operator_check). In the local-step kernels, a kernel whose wait
  *     runs out raises a status word, writes no result and returns; later kernels of the context that would
  *     build on its result return at once. Every synchronising call checks that word: from then on each of them
  *     returns SWARM_ECUDA with swarm_last_cuda_error() == cudaErrorLaunchTimeout (the models are in an
@@ -344,10 +345,13 @@ void swarm_destroy(swarm_ctx *ctx);
  * addition and a norm). They need no context: a caller computes the gradients of its own objective with them and
  * applies the steps to the models in place (swarm_model_ptr) between interactions.
  *   - Everything is device memory of the current device; the calls are asynchronous on cuda_stream (cudaStream_t,
- *     NULL = default stream), keep nothing between calls, allocate nothing and can be captured.
+ *     NULL = default stream), keep nothing between calls, allocate nothing and can be captured (after one call of the
+ *     kind outside a capture, which loads its kernels).
  *   - Sums, softmax statistics and norms are held in fp32. Results do not depend on timing: the same inputs give
  *     the same bits.
  *   - dtype: SWARM_F32, SWARM_BF16 or SWARM_F16, of all activations of a call. Weights and their gradients are fp32.
+ *   - The waits of the attention kernels are bounded. A kernel whose wait gives up writes nothing, frees what it holds
+ *     and raises a word that swarm_operator_check reads; other calls do not look at it.
  *   - Errors: EINVAL (before anything is launched), ECUDA (swarm_operator_error() names the CUDA error).
  * ---------------------------------------------------------------------------------------- */
 
@@ -403,10 +407,11 @@ int swarm_add_rms_norm_backward(const void *dy_dev, const void *dtotal_dev, cons
  * A sentence without states, and rows past the end, have o = 0 and lse = -infinity. What q, k, v and dout hold past
  * the ends is not used (NaN included); gradients there are 0.
  * Tensors are addressed by strides (elements) over sentence, token and head; the head_dim values of a head are
- * consecutive. lse is [batch][heads][queries] floats. */
+ * consecutive. lse is [batch][heads][queries] floats. Outputs must not overlap inputs. */
 typedef struct { int64_t batch, token, head; } swarm_strides;
 typedef struct {
-  int32_t batch, heads, kv_heads, queries, keys, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, <= 128 */
+  int32_t batch, heads, kv_heads, queries, keys, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, <= 128;
+                                                                queries, keys <= 2^30; batch, heads <= 65535        */
   int32_t dtype;                                             /* SWARM_BF16 or SWARM_F16                     */
   float scale;                                               /* > 0, finite                                 */
   int64_t wait_limit;            /* polls after which a device-side wait gives up; < 0: the default; 0: at once  */

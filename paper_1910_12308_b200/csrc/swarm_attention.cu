@@ -53,10 +53,17 @@ cudaError_t launch_zero(void* p, const swarm_strides& s, int batch, int tokens, 
 }
 
 // ---- argument checks ------------------------------------------------------------------------
+constexpr int32_t kMaxTokens = 1 << 30;                 // tile arithmetic stays in 32 bits
+// CTAs of the largest grid that any kernel of the call may take.
+bool grid_ok(const swarm_attention* d) {
+  const int64_t rows = ((int64_t)d->queries + 127) / 128, states = ((int64_t)d->keys + 127) / 128;
+  return (rows > 32 ? rows : 32) * d->heads < ((int64_t)1 << 31) / (d->batch > 0 ? d->batch : 1) &&
+         states * d->kv_heads < ((int64_t)1 << 31) / (d->batch > 0 ? d->batch : 1);
+}
 bool desc_ok(const swarm_attention* d) {
-  return d && d->batch >= 0 && d->queries >= 0 && d->keys >= 0 && d->heads >= 1 && d->kv_heads >= 1 &&
+  return d && d->queries <= kMaxTokens && d->keys <= kMaxTokens && d->batch >= 0 && d->queries >= 0 && d->keys >= 0 && d->heads >= 1 && d->kv_heads >= 1 &&
          d->heads % d->kv_heads == 0 && d->batch <= 65535 && d->heads <= 65535 && d->head_dim >= 8 && d->head_dim <= kMaxDim &&
-         d->head_dim % 8 == 0 && (d->dtype == SWARM_BF16 || d->dtype == SWARM_F16) && d->scale > 0.0f && std::isfinite(d->scale);
+         d->head_dim % 8 == 0 && (d->dtype == SWARM_BF16 || d->dtype == SWARM_F16) && d->scale > 0.0f && std::isfinite(d->scale) && grid_ok(d);
 }
 constexpr int64_t kMaxStride = (int64_t)1 << 38;
 bool one_stride_ok(int64_t s, int extent, bool repeats) {

@@ -76,7 +76,8 @@ def test_attention_refusals():
 
     for bad in (dict(batch=-1), dict(heads=0), dict(kv_heads=0), dict(kv_heads=3), dict(queries=-1), dict(keys=-1), dict(dim=0),
                 dict(dim=4), dict(dim=60), dict(dim=136), dict(dtype=g.F32), dict(dtype=5), dict(scale=0.0), dict(scale=-1.0),
-                dict(scale=float("inf")), dict(scale=float("nan")), dict(batch=65536)):
+                dict(scale=float("inf")), dict(scale=float("nan")), dict(batch=65536),
+                dict(queries=(1 << 30) + 1), dict(keys=(1 << 30) + 1), dict(batch=60000, heads=60000, kv_heads=60000)):
         if bad.get("heads") == 0 or bad.get("dim") == 0:
             strides = [(64, 64, 64)] * 8
         else:
