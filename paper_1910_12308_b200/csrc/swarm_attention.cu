@@ -103,7 +103,8 @@ int swarm_cross_attention_workspace(const swarm_attention* desc_host, int32_t ba
   AttentionArgs a{};
   fill(a, desc_host);
   if (backward) *bytes_host = a.batch && a.queries && a.keys ? attention_backward_workspace(a) : 0;
-  else *bytes_host = a.batch && a.queries && a.keys && few_rows(a) ? attention_rows_workspace(a) : 0;
+  else if (!a.batch || !a.queries || !a.keys) *bytes_host = 0;
+  else *bytes_host = few_rows(a) ? attention_rows_workspace(a) : attention_forward_workspace(a);
   return SWARM_OK;
 }
 
@@ -132,7 +133,7 @@ int swarm_cross_attention(const swarm_attention* desc_host, const void* q_dev, c
     }
     return operator_result(launch_zero(o_dev, d.o, d.batch, d.queries, d.heads, d.head_dim, st));
   }
-  return operator_result(few_rows(a) ? launch_attention_rows(a, d.dtype, workspace_dev, st) : launch_attention_forward_tc(a, d.dtype, st));
+  return operator_result(few_rows(a) ? launch_attention_rows(a, d.dtype, workspace_dev, st) : launch_attention_forward_tc(a, d.dtype, workspace_dev, st));
 }
 
 int swarm_cross_attention_backward(const swarm_attention* desc_host, const void* dout_dev, const void* q_dev,

@@ -44,7 +44,27 @@ struct TileMap {
 cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, int dtype, int batch, int tokens, int heads,
                           int head_dim, int rows);
 
-cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st);
+// A call whose states are split over CTAs: their parts of every row (query token x query head of a key head), joined by a
+// kernel of their own.
+constexpr int kMaxSplits = 32;                          // a lane of the joining warp each
+struct SplitPlan {
+  int32_t rows;                       // of a key head: queries * group
+  int32_t splits;
+  float* part_o;                      // [batch][kv_heads][rows][splits][head_dim] weighted sums
+  float* part_ml;                     // [batch][kv_heads][rows][splits][2] their maximum and the sum of the weights
+};
+inline size_t split_parts(const AttentionArgs& a, const SplitPlan& p) { return (size_t)a.batch * a.kv_heads * p.rows * p.splits; }
+inline size_t split_bytes(const AttentionArgs& a, const SplitPlan& p) {
+  return p.splits == 1 ? 0 : split_parts(a, p) * (a.head_dim + 2) * sizeof(float) + 16;
+}
+inline void place_parts(const AttentionArgs& a, SplitPlan* p, void* workspace) {
+  p->part_o = reinterpret_cast<float*>(workspace);
+  p->part_ml = p->part_o + split_parts(a, *p) * a.head_dim;
+}
+cudaError_t launch_attention_join(const AttentionArgs& a, const SplitPlan& p, int dtype, cudaStream_t st);
+
+size_t attention_forward_workspace(const AttentionArgs& a);
+cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st);
 // Few query rows; the workspace holds the parts of split states.
 size_t attention_rows_workspace(const AttentionArgs& a);
 cudaError_t launch_attention_rows(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st);

@@ -36,10 +36,10 @@ struct FwdBars {
 // NT = 1 (heads of up to 64 values): scores and weights have tensor memory of their own, so the scores of the next tile
 // are computed while the warps take the exponentials of this one, and two such CTAs share a multiprocessor.
 // NT = 2: two row tiles share every tile of states; while one's products run, the other's softmax does.
-template <typename T, int DB, int NT>
+template <typename T, int DB, int NT, bool SPLIT>
 __global__ void __launch_bounds__(FwdShape<DB, NT>::kThreads, FwdShape<DB, NT>::kCtasPerSm)
 attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
-                         const __grid_constant__ TileMap mo, AttentionArgs a, int row_tiles, int tile_groups) {
+                         const __grid_constant__ TileMap mo, AttentionArgs a, int row_tiles, int tile_groups, SplitPlan plan) {
   using Shape = FwdShape<DB, NT>;
   constexpr int kStages = Shape::kStages;
   constexpr uint32_t kTileBytes = DB * kBlockBytes;
@@ -52,9 +52,12 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   // the row tiles of this CTA: tiles are numbered head after head within the group of a key head
-  const int first = blockIdx.x % tile_groups * NT, bh = blockIdx.x / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int split = SPLIT ? blockIdx.x % plan.splits : 0, cta = SPLIT ? blockIdx.x / plan.splits : blockIdx.x;
+  const int first = cta % tile_groups * NT, bh = cta / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const int n = (nk + kTile - 1) / kTile;
+  const int tiles = (nk + kTile - 1) / kTile;           // of states; this CTA has n of them, the first of them `start`
+  const int start = SPLIT ? (int)((int64_t)tiles * split / plan.splits) : 0;
+  const int n = SPLIT ? (int)((int64_t)tiles * (split + 1) / plan.splits) - start : tiles;
   auto head_of = [&](int t) { return hk * a.group + (first + t) / row_tiles; };
   auto row_of = [&](int t) { return (first + t) % row_tiles * kTile; };
   auto exists = [&](int t) { return first + t < row_tiles * a.group; };
@@ -63,7 +66,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
   auto active = [&](int t) { return (act >> t & 1u) != 0; };
   const bool any = act != 0;
-  const int edge = nk % 16 ? nk % kTile : 0;            // rows of the last tile, where they end inside a product's sixteen
+  const int edge = nk % 16 && start + n == tiles ? nk % kTile : 0;     // rows of the last tile, where they end inside a product's sixteen
 
   if (tid == 0) {
     for (int i = 0; i < NT; ++i) {
@@ -108,7 +111,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         if (!ok) break;
         const uint32_t bar = smem_u32(&bars.kv_full[st]);
         mbar_expect_tx(bar, kTileBytes);
-        load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (f >> 1) * kTile, hk, b, bar);
+        load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (start + (f >> 1)) * kTile, hk, b, bar);
         issued = f + 1;
       }
       if (!ok) {
@@ -130,7 +133,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       // ---- products (one thread) --------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
-      auto columns = [&](int j) { return (min(kTile, nk - j * kTile) + 15) & ~15; };
+      auto columns = [&](int j) { return (min(kTile, nk - (start + j) * kTile) + 15) & ~15; };
       auto scores = [&](int t, int j) {                 // S_t = Q_t K_j^T
         mma_rows<T, DB, kTile>(tmem + 128 * t, aq + t * kTileBytes, akv + (2 * j) % kStages * kTileBytes, columns(j), ksteps);
         tc_commit(smem_u32(&bars.s_full[t]));
@@ -200,7 +203,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         ok = mbar_wait_after(ahead, smem_u32(&bars.s_full[t]), j & 1, limit);
         if (!ok) break;
         tc_fence_after();
-        const int valid = nk - j * kTile;
+        const int valid = nk - (start + j) * kTile;
         float s[kTile];
 #pragma unroll
         for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, s + g * 32);
@@ -283,8 +286,24 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       }
     }
     // ---- output -------------------------------------------------------------------------------
-    if (exists(t) && named_barrier_and(1 + t, 128, ok)) {
-      const bool live = work && row < nq;
+    const bool live = work && row < nq;
+    if (!exists(t) || !named_barrier_and(1 + t, 128, ok)) {
+      // nothing to write
+    } else if (SPLIT) {
+      // this CTA's part of the row: its sums as they are, their maximum and the sum of the weights
+      const int64_t at = (((int64_t)bh * a.queries + row) * a.group + (head - hk * a.group)) * plan.splits + split;
+#pragma unroll
+      for (int g = 0; g < DB * 2; ++g) {
+        float o[32];
+        if (work) { tmem_ld32(to + g * 32, o); tmem_wait_ld(); }
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          if (row < a.queries && g * 32 + i < a.head_dim)
+            *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + g * 32 + i) =
+                live ? make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+    } else {
       const float inv = live && l != 0.0f ? 1.0f / l : 0.0f;
       uint8_t* out = sQ + t * kTileBytes;               // the query tile has been read by now
 #pragma unroll
@@ -310,8 +329,9 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
 }
 
-template <typename T, int DB, int NT>
-cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const TileMap& mk, const TileMap& mv, const TileMap& mo, cudaStream_t st) {
+template <typename T, int DB, int NT, bool SPLIT>
+cudaError_t launch_forward_as(const AttentionArgs& a, const SplitPlan& plan, const TileMap& mq, const TileMap& mk, const TileMap& mv,
+                           const TileMap& mo, cudaStream_t st) {
   using Shape = FwdShape<DB, NT>;
   static bool attr_set[64] = {};
   static std::mutex attr_mutex;
@@ -321,15 +341,40 @@ cudaError_t launch_forward(const AttentionArgs& a, const TileMap& mq, const Tile
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(attention_forward_kernel<T, DB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
+      const cudaError_t e = cudaFuncSetAttribute(attention_forward_kernel<T, DB, NT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
   }
   const int row_tiles = (a.queries + kTile - 1) / kTile, tile_groups = (int)(((int64_t)row_tiles * a.group + NT - 1) / NT);
-  const int64_t ctas = (int64_t)tile_groups * a.kv_heads * a.batch;
-  attention_forward_kernel<T, DB, NT><<<(unsigned)ctas, Shape::kThreads, Shape::kSmem, st>>>(mq, mk, mv, mo, a, row_tiles, tile_groups);
+  const int64_t ctas = (int64_t)tile_groups * a.kv_heads * a.batch * plan.splits;
+  attention_forward_kernel<T, DB, NT, SPLIT><<<(unsigned)ctas, Shape::kThreads, Shape::kSmem, st>>>(mq, mk, mv, mo, a, row_tiles, tile_groups, plan);
   return cudaGetLastError();
+}
+
+template <typename T, int DB, int NT>
+cudaError_t launch_forward(const AttentionArgs& a, const SplitPlan& plan, const TileMap& mq, const TileMap& mk, const TileMap& mv,
+                           const TileMap& mo, cudaStream_t st) {
+  return plan.splits > 1 ? launch_forward_as<T, DB, NT, true>(a, plan, mq, mk, mv, mo, st)
+                         : launch_forward_as<T, DB, NT, false>(a, plan, mq, mk, mv, mo, st);
+}
+
+// Few row tiles leave multiprocessors idle while each CTA walks all states: these are then split, as far as the CTAs still
+// run at once and four steps or more are left to each, where that saves twelve steps (a step is about 1.4 us, the parts'
+// way through memory and the joining kernel 10 to 15). Measured: 8 heads of 64, 128 rows, 4096 states 42 us whole and 24 in
+// parts, 8 heads of 128, 512 rows 66 and 31; 2 x 8 heads of 64, 300 rows, 1000 states (eight steps) 16 and 25.
+SplitPlan make_forward_plan(const AttentionArgs& a) {
+  SplitPlan p{};
+  const int nt = a.head_dim <= 64 ? 1 : 2;
+  const int64_t row_tiles = (a.queries + kTile - 1) / kTile, steps = (a.keys + kTile - 1) / kTile;
+  const int64_t ctas = (row_tiles * a.group + nt - 1) / nt * a.kv_heads * a.batch, room = 148 * (nt == 1 ? 2 : 1);
+  int64_t s = room / ctas;
+  if (s > kMaxSplits) s = kMaxSplits;
+  if (s > steps / 4) s = steps / 4;
+  if (s < 2 || steps - (steps + s - 1) / s < 12) s = 1;
+  p.splits = (int32_t)s;
+  p.rows = s > 1 ? a.queries * a.group : 0;             // at most 128 rows for each of the 296 CTAs
+  return p;
 }
 
 }  // namespace
@@ -371,7 +416,11 @@ cudaError_t make_tile_map(TileMap* out, const void* p, const swarm_strides& s, i
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaStream_t st) {
+size_t attention_forward_workspace(const AttentionArgs& a) { return split_bytes(a, make_forward_plan(a)); }
+
+cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st) {
+  SplitPlan plan = make_forward_plan(a);
+  if (plan.splits > 1) place_parts(a, &plan, workspace);
   TileMap mq, mk, mv, mo;
   cudaError_t e = make_tile_map(&mq, a.q, a.qs, dtype, a.batch, a.queries, a.heads, a.head_dim, kTile);
   if (e == cudaSuccess) e = make_tile_map(&mo, a.out, a.os, dtype, a.batch, a.queries, a.heads, a.head_dim, kTile);
@@ -379,8 +428,11 @@ cudaError_t launch_attention_forward_tc(const AttentionArgs& a, int dtype, cudaS
   if (e == cudaSuccess) e = make_tile_map(&mv, a.v, a.vs, dtype, a.batch, a.keys, a.kv_heads, a.head_dim, kTile);
   if (e != cudaSuccess) return e;
   if (dtype == SWARM_BF16)
-    return a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1, 1>(a, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2, 2>(a, mq, mk, mv, mo, st);
-  return a.head_dim <= 64 ? launch_forward<__half, 1, 1>(a, mq, mk, mv, mo, st) : launch_forward<__half, 2, 2>(a, mq, mk, mv, mo, st);
+    e = a.head_dim <= 64 ? launch_forward<__nv_bfloat16, 1, 1>(a, plan, mq, mk, mv, mo, st) : launch_forward<__nv_bfloat16, 2, 2>(a, plan, mq, mk, mv, mo, st);
+  else
+    e = a.head_dim <= 64 ? launch_forward<__half, 1, 1>(a, plan, mq, mk, mv, mo, st) : launch_forward<__half, 2, 2>(a, plan, mq, mk, mv, mo, st);
+  if (e == cudaSuccess && plan.splits > 1) e = launch_attention_join(a, plan, dtype, st);
+  return e;
 }
 
 }  // namespace swarm

@@ -36,10 +36,8 @@ template <> __device__ __forceinline__ void mma16816<__half>(float c[4], const u
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-struct RowsPlan {
-  int32_t rows, row_groups, splits;   // rows of a key head, groups of 16 of them, parts of the states
-  float* part_ml;                     // [batch][kv_heads][rows][splits][2] maximum and sum of a part
-  float* part_o;                      // [batch][kv_heads][rows][splits][head_dim]
+struct RowsPlan : SplitPlan {
+  int32_t row_groups;                 // groups of 16 rows
 };
 
 // The fp16 weights against a running maximum reach 2^8: held as multiples of 2^-7, see swarm_attention_tile.cuh.
@@ -236,7 +234,7 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
 
 // Joins the parts of a row: warp = one row, lane = four values of it, the parts in order.
 template <typename T>
-__global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, RowsPlan plan) {
+__global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, SplitPlan plan) {
   const int lane = threadIdx.x & 31;
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (i >= (int64_t)a.batch * a.kv_heads * plan.rows) return;
@@ -273,7 +271,6 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Ro
     a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
 }
 
-constexpr int kMaxSplits = 32;                         // a lane of the joining warp each
 
 // The number of parts of the states that this model of a multiprocessor's time likes best, in states of one CTA: its share
 // of the CTAs, each with its states and a cost of its own (its start, the meeting of its warps, its share of the join:
@@ -303,29 +300,28 @@ cudaError_t launch_rows(const AttentionArgs& a, const RowsPlan& p, cudaStream_t 
   const int64_t ctas = (int64_t)a.batch * a.kv_heads * p.row_groups * p.splits;
   const int rows = p.rows < kRows ? p.rows : kRows;
   attention_rows_kernel<T, DB><<<(unsigned)ctas, kRowsWarps * 32, kRowsWarps * rows * a.head_dim * sizeof(float), st>>>(a, p);
-  if (p.splits > 1) {
-    const int64_t rows_all = (int64_t)a.batch * a.kv_heads * p.rows;
-    attention_join_kernel<T><<<(unsigned)((rows_all + 3) / 4), 128, 0, st>>>(a, p);
-  }
   return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t attention_rows_workspace(const AttentionArgs& a) {
-  const RowsPlan p = make_plan(a);
-  if (p.splits == 1) return 0;
-  return (size_t)a.batch * a.kv_heads * p.rows * p.splits * (a.head_dim + 2) * sizeof(float) + 16;
+cudaError_t launch_attention_join(const AttentionArgs& a, const SplitPlan& p, int dtype, cudaStream_t st) {
+  const unsigned grid = (unsigned)(((int64_t)a.batch * a.kv_heads * p.rows + 3) / 4);
+  if (dtype == SWARM_BF16) attention_join_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a, p);
+  else attention_join_kernel<__half><<<grid, 128, 0, st>>>(a, p);
+  return cudaGetLastError();
 }
+
+size_t attention_rows_workspace(const AttentionArgs& a) { return split_bytes(a, make_plan(a)); }
 
 cudaError_t launch_attention_rows(const AttentionArgs& a, int dtype, void* workspace, cudaStream_t st) {
   RowsPlan p = make_plan(a);
-  if (p.splits > 1) {
-    p.part_o = reinterpret_cast<float*>(workspace);
-    p.part_ml = p.part_o + (size_t)a.batch * a.kv_heads * p.rows * p.splits * a.head_dim;
-  }
-  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_rows<__nv_bfloat16, 1>(a, p, st) : launch_rows<__nv_bfloat16, 2>(a, p, st);
-  return a.head_dim <= 64 ? launch_rows<__half, 1>(a, p, st) : launch_rows<__half, 2>(a, p, st);
+  if (p.splits > 1) place_parts(a, &p, workspace);
+  cudaError_t e;
+  if (dtype == SWARM_BF16) e = a.head_dim <= 64 ? launch_rows<__nv_bfloat16, 1>(a, p, st) : launch_rows<__nv_bfloat16, 2>(a, p, st);
+  else e = a.head_dim <= 64 ? launch_rows<__half, 1>(a, p, st) : launch_rows<__half, 2>(a, p, st);
+  if (e == cudaSuccess && p.splits > 1) e = launch_attention_join(a, p, dtype, st);
+  return e;
 }
 
 }  // namespace swarm
