@@ -48,11 +48,11 @@ struct DqBars {
       s_empty[2], dp_full[2], ds_full[2], done[2], edge_here, edge_done, drain;
 };
 
-template <typename T, int DB, int NT>
+template <typename T, int DB, int NT, bool SPLIT>
 __global__ void __launch_bounds__(DqShape<DB, NT>::kThreads, DqShape<DB, NT>::kCtasPerSm)
 attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
                     const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdq, AttentionArgs a, int row_tiles,
-                    int tile_groups) {
+                    int tile_groups, SplitPlan plan) {
   using Shape = DqShape<DB, NT>;
   constexpr int kStages = Shape::kStages;
   constexpr uint32_t kTileBytes = DB * kBlockBytes, kHalfBytes = DB * kStepBlock;
@@ -65,9 +65,12 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   // the row tiles of this CTA: tiles are numbered head after head within the group of a key head
-  const int first = blockIdx.x % tile_groups * NT, bh = blockIdx.x / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int split = SPLIT ? blockIdx.x % plan.splits : 0, cta = SPLIT ? blockIdx.x / plan.splits : blockIdx.x;
+  const int first = cta % tile_groups * NT, bh = cta / tile_groups, hk = bh % a.kv_heads, b = bh / a.kv_heads;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
-  const int n = (nk + kStep - 1) / kStep;
+  const int all = (nk + kStep - 1) / kStep;             // steps; this CTA has n of them, the first of them `start`
+  const int start = SPLIT ? (int)((int64_t)all * split / plan.splits) : 0;
+  const int n = SPLIT ? (int)((int64_t)all * (split + 1) / plan.splits) - start : all;
   auto head_of = [&](int t) { return hk * a.group + (first + t) / row_tiles; };
   auto row_of = [&](int t) { return (first + t) % row_tiles * kTile; };
   auto exists = [&](int t) { return first + t < row_tiles * a.group; };
@@ -75,7 +78,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 #pragma unroll
   for (int t = 0; t < NT; ++t) act |= exists(t) && row_of(t) < nq && n > 0 ? 1u << t : 0u;
   auto active = [&](int t) { return (act >> t & 1u) != 0; };
-  const int edge = nk % 16 ? nk % kStep : 0;            // states of the last step, where they end inside a product's sixteen
+  const int edge = nk % 16 && start + n == all ? nk % kStep : 0;       // states of the last step, where they end inside a product's sixteen
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -119,8 +122,8 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         if (!ok) break;
         const uint32_t bar = smem_u32(&bars.kv_full[st]), dst = smem_u32(sKV) + 2 * st * kHalfBytes;
         mbar_expect_tx(bar, 2 * kHalfBytes);
-        load_tile<DB, kStep>(dst, mk, j * kStep, hk, b, bar);
-        load_tile<DB, kStep>(dst + kHalfBytes, mv, j * kStep, hk, b, bar);
+        load_tile<DB, kStep>(dst, mk, (start + j) * kStep, hk, b, bar);
+        load_tile<DB, kStep>(dst + kHalfBytes, mv, (start + j) * kStep, hk, b, bar);
         issued = j + 1;
       }
       if (!ok) {
@@ -142,7 +145,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       // ---- products (one thread) --------------------------------------------------------------
       const int ksteps = (a.head_dim + 15) / 16;
       const uint32_t aq = smem_u32(sQ), akv = smem_u32(sKV);
-      auto columns = [&](int j) { return (min(kStep, nk - j * kStep) + 15) & ~15; };
+      auto columns = [&](int j) { return (min(kStep, nk - (start + j) * kStep) + 15) & ~15; };
       auto scores = [&](int t, int j) {
         mma_rows<T, DB, kStep>(tmem + 256 * t + (NT == 1 ? 64 * (j & 1) : 0), aq + 2 * t * kTileBytes,
                                akv + 2 * (j % kStages) * kHalfBytes, columns(j), ksteps);
@@ -265,7 +268,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     if (work) {
       bool ahead = false;                               // the scores of the step have been seen to be there
       for (int j = 0; j < n; ++j) {
-        const int valid = nk - j * kStep;
+        const int valid = nk - (start + j) * kStep;
         float p[kStep], dp[kStep];
         ok = NT == 1 ? mbar_wait_after(ahead, smem_u32(&bars.s_full[j & 1]), (j >> 1) & 1, limit)
                      : mbar_wait_after(ahead, smem_u32(&bars.s_full[t]), j & 1, limit);
@@ -333,10 +336,30 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         tc_fence_after();
       }
     }
-    if (exists(t) && named_barrier_and(1 + t, 128, ok)) {
-      const int64_t at = stat_offset(((int64_t)b * a.heads + head) * row_tiles * kTile + row);
-      store_stat<T>(a.stat_lse + at, (kWeightShift<T> - lse2) / c);    // in units of a score; -infinity in rows that take no part
-      store_stat<T>(a.stat_delta + at, live ? -(delta + (off[0] + off[1])) : 0.0f);
+    const int64_t stat = stat_offset(((int64_t)b * a.heads + head) * row_tiles * kTile + row);
+    if (!exists(t) || !named_barrier_and(1 + t, 128, ok)) {
+      // nothing to write
+    } else if (SPLIT) {
+      // this CTA's part of the row: dq without its factor, and the sum of ds
+      const int64_t at = (((int64_t)bh * a.queries + row) * a.group + (head - hk * a.group)) * plan.splits + split;
+#pragma unroll
+      for (int g = 0; g < DB * 2; ++g) {
+        float o[32];
+        if (work) { tmem_ld32(tile + Shape::kDq + g * 32, o); tmem_wait_ld(); }
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          if (row < a.queries && g * 32 + i < a.head_dim)
+            *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + g * 32 + i) =
+                live ? make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? off[0] + off[1] : 0.0f, 0.0f);
+      else if (split == 0) {                            // rows of the tile past the tensor's
+        store_stat<T>(a.stat_lse + stat, -INFINITY);
+        store_stat<T>(a.stat_delta + stat, 0.0f);
+      }
+    } else {
+      store_stat<T>(a.stat_lse + stat, (kWeightShift<T> - lse2) / c);    // in units of a score; -infinity in rows that take no part
+      store_stat<T>(a.stat_delta + stat, live ? -(delta + (off[0] + off[1])) : 0.0f);
       uint8_t* out = sQ + 2 * t * kTileBytes;
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
@@ -357,6 +380,61 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
+}
+
+// Joins the parts of a row's dq and leaves its statistics: warp = one row, lane = four of its values, the parts in order.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_dq_join_kernel(AttentionArgs a, SplitPlan plan, int row_tiles) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (i >= (int64_t)a.batch * a.kv_heads * plan.rows) return;
+  const int r = (int)(i % plan.rows), bh = (int)(i / plan.rows), hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int t = r / a.group, h = hk * a.group + r % a.group;
+  const bool live = t < length_of(a.query_lengths, b, a.queries) && length_of(a.key_lengths, b, a.keys) > 0;
+  const bool mine = lane * 4 < a.head_dim;
+  float delta = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (live && mine) {
+    const uint2 g = *reinterpret_cast<const uint2*>(reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, t, h) + lane * 4);
+    const uint2 o = *reinterpret_cast<const uint2*>(reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, t, h) + lane * 4);
+    float g0, g1, o0, o1;
+    unpack2<T>(g.x, g0, g1); unpack2<T>(o.x, o0, o1);
+    delta = fmaf(g0, o0, g1 * o1);
+    unpack2<T>(g.y, g0, g1); unpack2<T>(o.y, o0, o1);
+    delta = fmaf(g0, o0, fmaf(g1, o1, delta));
+  }
+  delta = warp_sum(delta) + warp_sum(lane < plan.splits ? plan.part_ml[(i * plan.splits + lane) * 2] : 0.0f);
+  const float* part = plan.part_o + i * plan.splits * a.head_dim + lane * 4;
+#pragma unroll 8
+  for (int s = 0; s < plan.splits; ++s)
+    if (mine) {
+      const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)s * a.head_dim);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    }
+  if (mine) {
+    const uint2 w = live ? make_uint2(pack2<T>(v[0] * a.scale, v[1] * a.scale), pack2<T>(v[2] * a.scale, v[3] * a.scale)) : make_uint2(0, 0);
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.dq) + offset_of(a.dqs, b, t, h) + lane * 4) = w;
+  }
+  if (lane == 0) {
+    const int64_t head = (int64_t)b * a.heads + h, stat = stat_offset(head * row_tiles * kTile + t);
+    store_stat<T>(a.stat_lse + stat, live ? (kWeightShift<T> - a.lse_in[head * a.queries + t] * kLog2e) / (a.scale * kLog2e) : -INFINITY);
+    store_stat<T>(a.stat_delta + stat, live ? -delta : 0.0f);
+  }
+}
+
+// As for the forward pass (make_forward_plan): few row tiles over many states are split, eight steps of 64 or more to each
+// part, where that saves 24 steps of about 1 us.
+SplitPlan make_dq_plan(const AttentionArgs& a) {
+  SplitPlan p{};
+  const int nt = a.head_dim <= 64 ? 1 : 2;
+  const int64_t row_tiles = (a.queries + kTile - 1) / kTile, steps = (a.keys + kStep - 1) / kStep;
+  const int64_t ctas = (row_tiles * a.group + nt - 1) / nt * a.kv_heads * a.batch, room = 148 * (nt == 1 ? 2 : 1);
+  int64_t s = room / ctas;
+  if (s > kMaxSplits) s = kMaxSplits;
+  if (s > steps / 8) s = steps / 8;
+  if (s < 2 || steps - (steps + s - 1) / s < 24) s = 1;
+  p.splits = (int32_t)s;
+  p.rows = s > 1 ? a.queries * a.group : 0;
+  return p;
 }
 
 // =================================================================================================
@@ -643,7 +721,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
 }
 
 template <typename T, int DB>
-cudaError_t launch_backward(const AttentionArgs& a, int dtype, cudaStream_t st) {
+cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, int dtype, cudaStream_t st) {
   using Dq = DqShape<DB, DB>;                           // heads of up to 64 values: one tile and two CTAs per multiprocessor
   using Dkv = DkvShape<DB, DB>;
   static bool attr_set[64] = {};
@@ -654,7 +732,8 @@ cudaError_t launch_backward(const AttentionArgs& a, int dtype, cudaStream_t st) 
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      cudaError_t e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
+      cudaError_t e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
       if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dkv::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
@@ -671,8 +750,13 @@ cudaError_t launch_backward(const AttentionArgs& a, int dtype, cudaStream_t st) 
   if (e != cudaSuccess) return e;
   const int row_tiles = (a.queries + kTile - 1) / kTile, key_tiles = (a.keys + kTile - 1) / kTile;
   const int tile_groups = (int)(((int64_t)row_tiles * a.group + DB - 1) / DB);
-  attention_dq_kernel<T, DB, DB><<<(unsigned)((int64_t)tile_groups * a.kv_heads * a.batch), Dq::kThreads, Dq::kSmem, st>>>(
-      mq, mk, mv, mdo, mdq, a, row_tiles, tile_groups);
+  const unsigned dq_ctas = (unsigned)((int64_t)tile_groups * a.kv_heads * a.batch * plan.splits);
+  if (plan.splits > 1) {
+    attention_dq_kernel<T, DB, DB, true><<<dq_ctas, Dq::kThreads, Dq::kSmem, st>>>(mq, mk, mv, mdo, mdq, a, row_tiles, tile_groups, plan);
+    attention_dq_join_kernel<T><<<(unsigned)(((int64_t)a.batch * a.kv_heads * plan.rows + 3) / 4), 128, 0, st>>>(a, plan, row_tiles);
+  } else {
+    attention_dq_kernel<T, DB, DB, false><<<dq_ctas, Dq::kThreads, Dq::kSmem, st>>>(mq, mk, mv, mdo, mdq, a, row_tiles, tile_groups, plan);
+  }
   e = cudaGetLastError();
   if (e == cudaSuccess) e = rows(&mq, a.q, a.qs, Dkv::kRows);
   if (e == cudaSuccess) e = rows(&mdo, a.dout, a.dos, Dkv::kRows);
@@ -690,13 +774,15 @@ int64_t stat_count(const AttentionArgs& a) { return (int64_t)a.batch * a.heads *
 
 }  // namespace
 
-size_t attention_backward_workspace(const AttentionArgs& a) { return (size_t)stat_count(a) * 2 * 32; }
+size_t attention_backward_workspace(const AttentionArgs& a) { return (size_t)stat_count(a) * 2 * 32 + split_bytes(a, make_dq_plan(a)); }
 
 cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* workspace, cudaStream_t st) {
   a.stat_lse = reinterpret_cast<uint8_t*>(workspace);
   a.stat_delta = a.stat_lse + stat_count(a) * 32;
-  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, dtype, st);
-  return a.head_dim <= 64 ? launch_backward<__half, 1>(a, dtype, st) : launch_backward<__half, 2>(a, dtype, st);
+  SplitPlan plan = make_dq_plan(a);
+  if (plan.splits > 1) place_parts(a, &plan, a.stat_delta + stat_count(a) * 32);
+  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, plan, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, plan, dtype, st);
+  return a.head_dim <= 64 ? launch_backward<__half, 1>(a, plan, dtype, st) : launch_backward<__half, 2>(a, plan, dtype, st);
 }
 
 }  // namespace swarm
