@@ -464,11 +464,11 @@ struct DkvBars {
   uint64_t kv_full, full[4], empty[4], s_full, p_full, dp_full, ds_full, done, edge_here, edge_done, drain;
 };
 
-template <typename T, int DB, int NW>
+template <typename T, int DB, int NW, bool SPLIT>
 __global__ void __launch_bounds__(DkvShape<DB, NW>::kThreads, DkvShape<DB, NW>::kCtasPerSm)
 attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
                      const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdk, const __grid_constant__ TileMap mdv,
-                     AttentionArgs a, int key_tiles, int row_tiles) {
+                     AttentionArgs a, int key_tiles, int row_tiles, SplitPlan plan) {
   using Shape = DkvShape<DB, NW>;
   constexpr int kStages = Shape::kStages, kRows = Shape::kRows;
   constexpr uint32_t kTileBytes = DB * kBlockBytes, kHalfBytes = Shape::kHalfBytes;
@@ -481,10 +481,14 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
   __shared__ DkvBars bars;
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int kt = blockIdx.x % key_tiles, bh = blockIdx.x / key_tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const int split = SPLIT ? blockIdx.x % plan.splits : 0, cta = SPLIT ? blockIdx.x / plan.splits : blockIdx.x;
+  const int kt = cta % key_tiles, bh = cta / key_tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
   const int nq = length_of(a.query_lengths, b, a.queries), nk = length_of(a.key_lengths, b, a.keys);
   const int key0 = kt * kTile, steps = (nq + kRows - 1) / kRows;       // steps of one head
-  const int n = key0 < nk ? steps * a.group : 0;
+  const int64_t all = key0 < nk ? (int64_t)steps * a.group : 0;        // steps of all heads; this CTA has n, from `start`
+  const int start = SPLIT ? (int)(all * split / plan.splits) : 0;
+  const int n = SPLIT ? (int)(all * (split + 1) / plan.splits) - start : (int)all;
+  const int step0 = SPLIT && n ? start % steps : 0;                    // the first one's place within its head
   const int edge = nq % 16 ? nq % kRows : 0;            // rows of a head's last step, where they end inside a product's sixteen
 
   if (tid == 0) {
@@ -525,7 +529,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         load_tile<DB>(smem_u32(sKV), mk, key0, hk, b, bar);
         load_tile<DB>(smem_u32(sKV) + kTileBytes, mv, key0, hk, b, bar);
       }
-      int h = hk * a.group, row0 = 0;
+      int h = hk * a.group + (SPLIT ? start / steps : 0), row0 = step0 * kRows;
       for (int i = 0; i < n; ++i) {
         const int st = i % kStages;
         ok = mbar_wait_one(smem_u32(&bars.empty[st]), ((i / kStages) & 1) ^ 1, limit);
@@ -550,7 +554,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       }
     } else if (warp == 4 * NW + 2 && edge) {
       // ---- the end of each head's last step: q and dout are factors of dk and dv ----------------
-      for (int i = steps - 1, g = 0; i < n && ok; i += steps, ++g) {
+      for (int i = steps - 1 - step0, g = 0; i < n && ok; i += steps, ++g) {
         const int st = i % kStages;
         ok = mbar_wait(smem_u32(&bars.edge_here), g & 1, limit);
         if (!ok) break;
@@ -570,7 +574,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
                instr_desc_16<T>(kTile, 0, 0, 0) + ((uint32_t)(columns >> 3) << 17), 1);
       };
       ok = mbar_wait_one(smem_u32(&bars.kv_full), 0, limit);
-      int cols = 0, cols_next = 0, step = 0, head = 0;  // columns of steps i and i + 1; the latter's place
+      int cols = 0, cols_next = 0, step = step0, head = 0;  // columns of steps i and i + 1; the latter's place
       for (int i = -1; i < n && ok; ++i) {
         const int st = i % kStages, next = (i + 1) % kStages;
         const bool last = step == steps - 1, at_edge = i + 1 < n && last && edge;
@@ -625,7 +629,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
     const uint32_t ts = tmem + lane_base + half * 64, tdp = ts + Shape::kDp;
     const float c = a.scale * kLog2e;
     constexpr float kUnshift = pow2_of(kWeightShift<T>);
-    int step = 0;
+    int step = step0;
     for (int i = 0; i < n; ++i) {
       const int cols = (step == steps - 1 ? nq - step * kRows : kRows) - half * 64;   // columns of this warpgroup that exist
       if (++step == steps) step = 0;
@@ -690,9 +694,29 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       ok = mbar_wait(smem_u32(&bars.done), 0, limit);
       tc_fence_after();
     }
-    if (named_barrier_and(1, 128 * NW, ok)) {
-      // two warpgroups write dv and dk, one writes both
-      const bool live = n > 0 && key0 + tile_row < nk;
+    const bool live = n > 0 && key0 + tile_row < nk;
+    // two warpgroups write dv and dk, one writes both
+    if (!named_barrier_and(1, 128 * NW, ok)) {
+      // nothing to write
+    } else if (SPLIT) {
+      // this CTA's part of the state's dk and dv, with their factors
+      const int64_t at = ((int64_t)bh * a.keys + key0 + tile_row) * plan.splits + split;
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        if (NW == 2 && which != half) continue;
+        const float factor = which == 0 ? kUnshift : a.scale;
+#pragma unroll
+        for (int g = 0; g < DB * 2; ++g) {
+          float o[32];
+          if (n) { tmem_ld32(tmem + lane_base + (which == 0 ? Shape::kDv : Shape::kDk) + g * 32, o); tmem_wait_ld(); }
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            if (key0 + tile_row < a.keys && g * 32 + i < a.head_dim)
+              *reinterpret_cast<float4*>(plan.part_o + (at * 2 + which) * a.head_dim + g * 32 + i) =
+                  live ? make_float4(o[i] * factor, o[i + 1] * factor, o[i + 2] * factor, o[i + 3] * factor) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    } else {
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
         if (NW == 2 && which != half) continue;
@@ -720,8 +744,46 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
   if (warp == 4 * NW + 1) tmem_dealloc(tmem, Shape::kColumns);
 }
 
+// Joins the parts of a state's dk and dv: warp = one state of one key head, lane = four values of each, the parts in order.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_dkv_join_kernel(AttentionArgs a, SplitPlan plan) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (i >= (int64_t)a.batch * a.kv_heads * a.keys || lane * 4 >= a.head_dim) return;
+  const int j = (int)(i % a.keys), bh = (int)(i / a.keys), hk = bh % a.kv_heads, b = bh / a.kv_heads;
+  const float* part = plan.part_o + i * plan.splits * 2 * a.head_dim + lane * 4;
+  float v[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+  for (int s = 0; s < plan.splits; ++s)
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)(2 * s + which) * a.head_dim);
+      v[which][0] += x.x; v[which][1] += x.y; v[which][2] += x.z; v[which][3] += x.w;
+    }
+  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.dv) + offset_of(a.dvs, b, j, hk) + lane * 4) = make_uint2(pack2<T>(v[0][0], v[0][1]), pack2<T>(v[0][2], v[0][3]));
+  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.dk) + offset_of(a.dks, b, j, hk) + lane * 4) = make_uint2(pack2<T>(v[1][0], v[1][1]), pack2<T>(v[1][2], v[1][3]));
+}
+
+// The same for few states under many rows: eight steps of 64 rows (or four of 128) or more to each part, where that saves 24
+// (or 12) of them.
+SplitPlan make_dkv_plan(const AttentionArgs& a) {
+  SplitPlan p{};
+  const int rows = a.head_dim <= 64 ? DkvShape<1, 1>::kRows : DkvShape<2, 2>::kRows;
+  const int64_t steps = (int64_t)((a.queries + rows - 1) / rows) * a.group;
+  const int64_t ctas = (int64_t)((a.keys + kTile - 1) / kTile) * a.kv_heads * a.batch, room = 148 * (a.head_dim <= 64 ? 2 : 1);
+  int64_t s = room / ctas;
+  if (s > kMaxSplits) s = kMaxSplits;
+  if (s > steps * rows / 512) s = steps * rows / 512;
+  if (s < 2 || (steps - (steps + s - 1) / s) * rows < 24 * 64) s = 1;
+  p.splits = (int32_t)s;
+  return p;
+}
+size_t dkv_part_bytes(const AttentionArgs& a, const SplitPlan& p) {
+  return p.splits == 1 ? 0 : (size_t)a.batch * a.kv_heads * a.keys * p.splits * 2 * a.head_dim * sizeof(float);
+}
+
 template <typename T, int DB>
-cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, int dtype, cudaStream_t st) {
+cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, const SplitPlan& dkv, int dtype, cudaStream_t st) {
   using Dq = DqShape<DB, DB>;                           // heads of up to 64 values: one tile and two CTAs per multiprocessor
   using Dkv = DkvShape<DB, DB>;
   static bool attr_set[64] = {};
@@ -734,7 +796,8 @@ cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, int d
     if (!attr_set[dev]) {
       cudaError_t e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
       if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dq_kernel<T, DB, DB, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dq::kSmem);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dkv::kSmem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB, DB, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dkv::kSmem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_dkv_kernel<T, DB, DB, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Dkv::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
@@ -765,8 +828,13 @@ cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, int d
   if (e == cudaSuccess) e = states(&mdk, a.dk, a.dks, kTile);
   if (e == cudaSuccess) e = states(&mdv, a.dv, a.dvs, kTile);
   if (e != cudaSuccess) return e;
-  attention_dkv_kernel<T, DB, DB><<<(unsigned)((int64_t)key_tiles * a.kv_heads * a.batch), Dkv::kThreads, Dkv::kSmem, st>>>(
-      mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles);
+  const unsigned dkv_ctas = (unsigned)((int64_t)key_tiles * a.kv_heads * a.batch * dkv.splits);
+  if (dkv.splits > 1) {
+    attention_dkv_kernel<T, DB, DB, true><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, dkv);
+    attention_dkv_join_kernel<T><<<(unsigned)(((int64_t)a.batch * a.kv_heads * a.keys + 3) / 4), 128, 0, st>>>(a, dkv);
+  } else {
+    attention_dkv_kernel<T, DB, DB, false><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, dkv);
+  }
   return cudaGetLastError();
 }
 
@@ -774,15 +842,20 @@ int64_t stat_count(const AttentionArgs& a) { return (int64_t)a.batch * a.heads *
 
 }  // namespace
 
-size_t attention_backward_workspace(const AttentionArgs& a) { return (size_t)stat_count(a) * 2 * 32 + split_bytes(a, make_dq_plan(a)); }
+size_t attention_backward_workspace(const AttentionArgs& a) {
+  return (size_t)stat_count(a) * 2 * 32 + dkv_part_bytes(a, make_dkv_plan(a)) + split_bytes(a, make_dq_plan(a));
+}
 
 cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* workspace, cudaStream_t st) {
   a.stat_lse = reinterpret_cast<uint8_t*>(workspace);
   a.stat_delta = a.stat_lse + stat_count(a) * 32;
-  SplitPlan plan = make_dq_plan(a);
-  if (plan.splits > 1) place_parts(a, &plan, a.stat_delta + stat_count(a) * 32);
-  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, plan, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, plan, dtype, st);
-  return a.head_dim <= 64 ? launch_backward<__half, 1>(a, plan, dtype, st) : launch_backward<__half, 2>(a, plan, dtype, st);
+  SplitPlan dq = make_dq_plan(a), dkv = make_dkv_plan(a);
+  uint8_t* rest = a.stat_delta + stat_count(a) * 32;
+  dkv.part_o = reinterpret_cast<float*>(rest);          // head_dim is a multiple of 8: 16-byte boundaries throughout
+  if (dq.splits > 1) place_parts(a, &dq, rest + dkv_part_bytes(a, dkv));
+  if (dtype == SWARM_BF16)
+    return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, dq, dkv, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, dq, dkv, dtype, st);
+  return a.head_dim <= 64 ? launch_backward<__half, 1>(a, dq, dkv, dtype, st) : launch_backward<__half, 2>(a, dq, dkv, dtype, st);
 }
 
 }  // namespace swarm

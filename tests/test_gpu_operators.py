@@ -454,6 +454,16 @@ def test_cross_attention_split_states_of_many_rows(h, hk, d, dtype):
     check_attention(q, k, v, do, nq=nq, nk=nk)
 
 
+@pytest.mark.parametrize("h,hk,d,dtype", [(4, 2, 64, BF16), (2, 2, 128, F16), (3, 1, 96, BF16)])
+def test_cross_attention_split_rows_of_few_states(h, hk, d, dtype):
+    """Few tiles of states under many rows, whole, and of lengths that leave some parts without rows."""
+    q, k, v, do = attention_inputs(2, 4100, 130, h, hk, d, dtype, seed=15, layout="packed")
+    check_attention(q, k, v, do)
+    nq = torch.tensor([4033, 70], dtype=torch.int32, device="cuda")
+    nk = torch.tensor([129, 130], dtype=torch.int32, device="cuda")
+    check_attention(q, k, v, do, nq=nq, nk=nk)
+
+
 def test_cross_attention_gradient_is_the_difference():
     q, k, v, do = attention_inputs(1, 9, 150, 2, 1, 64, F16, seed=12)
     o, lse = ops.cross_attention(q, k, v, need_lse=True)
