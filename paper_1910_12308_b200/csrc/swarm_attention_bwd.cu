@@ -5,7 +5,7 @@
 //                         leaves lse and delta = rowsum(dout * o) as the other kernel wants them
 //   attention_dkv_kernel  CTA = 128 states of a key head: the transposed products, over all rows of all its query
 //                         heads: dv = sum p^T dout, dk = sum ds^T q
-// The price is s and dp computed twice: 7 products instead of 5 (8 in bf16, see dq).
+// The price is s and dp computed twice: 8 products instead of 5 (one for ds's second part, see dq).
 // Measured: 32 x 16 heads of 64, 512 rows and states, 210 us (104 dq, 91 dkv in the kernels' own time with lengths of three
 // quarters); 4 x 16 heads of 128 on 4 key heads, 2048 rows, 4096 states, 930 us (dq 467, dkv 470), 660 TFLOP/s of the five
 // products. The tensor pipe is busy 40 % (dq) and 59 % (dkv) of the long case; a tile's chain of products, their latency
@@ -25,9 +25,10 @@ namespace {
 // two tiles the issuing thread takes up whichever barrier has completed: in a fixed order either tile's scores waited for
 // the other's ds.
 // delta = rowsum(dout * o) is off by what the rounding of o left; the sum of ds over a row, 0 in exact arithmetic, is that
-// error, and the other kernel gets delta without it. Here it stays in ds, beside the rounding of ds to eight bits where T is
-// bf16; the two together would leave dq 1.55 times as far from its value as its own rounding does. So in bf16 ds is the
-// sum of two numbers of T, both of which dq takes (the second lies beside the first, over the rest of dp): 1.2 times.
+// error, and the other kernel gets delta without it. Here it stays in ds (but for sentences of one step, where it can be
+// taken out: with 6 states it doubled the error of dq), beside the rounding of ds to T; the two together would leave dq 1.55
+// times as far from its value as its own rounding does. So ds is the sum of two numbers of T, both of which dq takes (the
+// second lies beside the first, over the rest of dp): 1.2 times.
 // =================================================================================================
 constexpr int kStep = 64;                               // states of a step
 constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64 values
@@ -40,8 +41,6 @@ template <int DB, int NT> struct DqShape {
   static constexpr int kSmem = NT * 2 * DB * kBlockBytes + kStages * 2 * DB * kStepBlock + 1024;
   static constexpr uint32_t kColumns = NT == 1 ? 256 : 512, kDp = NT == 1 ? 128 : 64, kDq = kDp + 64;
 };
-
-template <typename T> constexpr bool kTwoParts = sizeof(T) == 2 && kWeightShift<T> == 0.0f;            // bf16
 
 struct DqBars {
   uint64_t q_full[2], kv_full[4], kv_empty[4], s_full[2],   // s_full: of the tiles, or of the two sets of one tile's scores
@@ -158,7 +157,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       };
       auto dqs = [&](int t, int j) {
 #pragma unroll
-        for (int part = 0; part < (kTwoParts<T> ? 2 : 1); ++part)
+        for (int part = 0; part < 2; ++part)
           mma_weights<T, DB, kStep, false>(tmem + 256 * t + Shape::kDq, tmem + 256 * t + Shape::kDp + 32 * part,
                                            akv + 2 * (j % kStages) * kHalfBytes, columns(j) / 16, part != 0 || j != 0);
         if (j == n - 1) tc_commit(smem_u32(&bars.done[t]));
@@ -295,6 +294,12 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         tmem_ld32(tdp, dp);
         tmem_ld32(tdp + 32, dp + 32);
         tmem_wait_ld();
+        if (all == 1) {                                 // all states are here: take delta's error out
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) sum += i < valid ? p[i] * (dp[i] - delta) : 0.0f;
+          delta += sum;
+        }
 #pragma unroll
         for (int i = 0; i < kStep; i += 2) {
           add2(dp[i], dp[i + 1], dp[i], dp[i + 1], -delta, -delta);
@@ -313,16 +318,14 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
             w[i] = pack2<T>(p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
           }
           tmem_st16(tdp + g * 16, w);
-          if (kTwoParts<T>) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float a0, a1;
-              unpack2<T>(w[i], a0, a1);
-              fma2(a0, a1, a0, a1, -1.0f, -1.0f, p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
-              w[i] = pack2<T>(a0, a1);
-            }
-            tmem_st16(tdp + 32 + g * 16, w);
+          for (int i = 0; i < 16; ++i) {
+            float a0, a1;
+            unpack2<T>(w[i], a0, a1);
+            fma2(a0, a1, a0, a1, -1.0f, -1.0f, p[g * 32 + 2 * i], p[g * 32 + 2 * i + 1]);
+            w[i] = pack2<T>(a0, a1);
           }
+          tmem_st16(tdp + 32 + g * 16, w);
         }
         ahead = j + 1 < n && (NT == 1 ? mbar_test(smem_u32(&bars.s_full[(j + 1) & 1]), ((j + 1) >> 1) & 1)
                                       : mbar_test(smem_u32(&bars.s_full[t]), (j + 1) & 1));

@@ -11,7 +11,7 @@
 // joining kernel; the tensor pipe is busy a seventh of the time. The four warps meet in shared memory; where there are fewer (key
 // head, sentence) pairs than the device has room for, the states are split over CTAs whose parts (maximum, sum, o) a
 // second kernel joins in order.
-#include "swarm_attention.h"
+#include "swarm_attention_tile.cuh"
 
 namespace swarm {
 namespace {
@@ -19,12 +19,6 @@ namespace {
 constexpr int kRows = 16, kRowsWarps = 4;
 
 constexpr int kRowsStep = 16;                           // states that a warp takes at a time
-
-__device__ __forceinline__ float ex2_(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 
 template <typename T> __device__ __forceinline__ void mma16816(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1);
 template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
@@ -39,10 +33,6 @@ template <> __device__ __forceinline__ void mma16816<__half>(float c[4], const u
 struct RowsPlan : SplitPlan {
   int32_t row_groups;                 // groups of 16 rows
 };
-
-// The fp16 weights against a running maximum reach 2^8: held as multiples of 2^-7, see swarm_attention_tile.cuh.
-template <typename T> constexpr float kShift = 0.0f;
-template <> constexpr float kShift<__half> = 7.0f;
 
 template <typename T, int DB>
 __global__ void __launch_bounds__(kRowsWarps * 32)
@@ -136,19 +126,19 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
       // the maximum moved by more than 2^8 in some row (or the first step): rescale; smaller moves keep the reference
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float m_new = fmaxf(m[u], top[u]), f = m_new == m[u] ? 1.0f : ex2_((m[u] - m_new) * c);
+        const float m_new = fmaxf(m[u], top[u]), f = m_new == m[u] ? 1.0f : ex2((m[u] - m_new) * c);
         m[u] = m_new;
         l[u] *= f;
 #pragma unroll
         for (int i = 0; i < DB * 8; ++i) { o[i][2 * u] *= f; o[i][2 * u + 1] *= f; }
       }
     }
-    const float mc[2] = {m[0] == -INFINITY ? 0.0f : m[0] * c - kShift<T>, m[1] == -INFINITY ? 0.0f : m[1] * c - kShift<T>};
+    const float mc[2] = {m[0] == -INFINITY ? 0.0f : m[0] * c - kRunningShift<T>, m[1] == -INFINITY ? 0.0f : m[1] * c - kRunningShift<T>};
 #pragma unroll
     for (int g = 0; g < kStep / 8; ++g)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        s[g][u] = ex2_(fmaf(s[g][u], c, -mc[u >> 1]));
+        s[g][u] = ex2(fmaf(s[g][u], c, -mc[u >> 1]));
         l[u >> 1] += s[g][u];
       }
 #pragma unroll
@@ -212,7 +202,7 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
     const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
     for (int w = 0; w < kRowsWarps; ++w) {
-      const float f = ex2_((s_ml[w][r][0] - base) * c);
+      const float f = ex2((s_ml[w][r][0] - base) * c);
       sum = fmaf(s_ml[w][r][1], f, sum);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaf(s_o[(w * rows + r) * a.head_dim + ch * 8 + e], f, v[e]);
@@ -223,7 +213,7 @@ attention_rows_kernel(AttentionArgs a, RowsPlan plan) {
       for (int e = 0; e < 8; ++e) v[e] = inv != 0.0f ? v[e] * inv : 0.0f;
       store8<T>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + ch * 8, v);
       if (a.lse && ch == 0)
-        a.lse[((int64_t)b * a.heads + h) * a.queries + t] = t < nq && nk > 0 ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
+        a.lse[((int64_t)b * a.heads + h) * a.queries + t] = t < nq && nk > 0 ? top * a.scale + (logf(sum) - kRunningShift<T> * 0.69314718f) : -INFINITY;
     } else {
       const int64_t at = ((int64_t)bh * plan.rows + row) * plan.splits + split;
       if (ch == 0) { plan.part_ml[at * 2] = top; plan.part_ml[at * 2 + 1] = sum; }
@@ -249,7 +239,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Sp
   float top = ml.x;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  const float f = ex2_((ml.x - (top == -INFINITY ? 0.0f : top)) * c), sum = warp_sum(ml.y * f);
+  const float f = ex2((ml.x - (top == -INFINITY ? 0.0f : top)) * c), sum = warp_sum(ml.y * f);
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int s = 0; s < plan.splits; ++s) {
@@ -268,7 +258,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(AttentionArgs a, Sp
     *reinterpret_cast<uint2*>(out) = w;
   }
   if (a.lse && lane == 0)
-    a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kShift<T> * 0.69314718f) : -INFINITY;
+    a.lse[((int64_t)b * a.heads + h) * a.queries + t] = live ? top * a.scale + (logf(sum) - kRunningShift<T> * 0.69314718f) : -INFINITY;
 }
 
 

@@ -18,8 +18,6 @@ from . import binding as _b
 _DTYPES = {torch.float32: _b.F32, torch.bfloat16: _b.BF16, torch.float16: _b.F16}
 _DESC = struct.Struct("=7ifq2Q24q")                        # swarm_attention: 8 tensors of 3 strides at the end
 _NO_GRADS = (0,) * 12
-_workspace_bytes = C.c_size_t()
-_workspace_ref = C.byref(_workspace_bytes)
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -215,8 +213,9 @@ def _attention_desc(device, q, k, v, o, scale, query_lengths, key_lengths, wait_
 
 
 def _workspace(L, desc, backward, x):
-    _check(L.swarm_cross_attention_workspace(desc, backward, _workspace_ref), "swarm_cross_attention_workspace")
-    n = _workspace_bytes.value
+    size = C.c_size_t()
+    _check(L.swarm_cross_attention_workspace(desc, backward, C.byref(size)), "swarm_cross_attention_workspace")
+    n = size.value
     return (x.new_empty((n,), dtype=torch.uint8) if n else None), n
 
 
