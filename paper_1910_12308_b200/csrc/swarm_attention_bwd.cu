@@ -125,13 +125,11 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         load_tile<DB, kStep>(dst + kHalfBytes, mv, (start + j) * kStep, hk, b, bar);
         issued = j + 1;
       }
-      if (!ok) {
-        // gave up: the copies in flight land before the CTA's shared memory is released
-        for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
-          mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
-        for (int t = 0; t < NT; ++t)
-          if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
-      }
+      // every copy lands before the CTA's shared memory is released, whichever of its threads gives up
+      for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
+        mbar_wait_one(smem_u32(&bars.kv_full[j % kStages]), (j / kStages) & 1, kAttentionWaitLimit);
+      for (int t = 0; t < NT; ++t)
+        if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
     } else if (warp == 4 * NT + 2 && act && edge) {
       // ---- the last step's end: k is a factor of dq -------------------------------------------
       const int st = (n - 1) % kStages;
@@ -235,10 +233,9 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
           else if (++idle > limit) ok = false;
         }
       }
-      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        tc_commit(smem_u32(&bars.drain));
-        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
-      }
+      // no product is in flight when tensor memory is freed, whichever thread gives up
+      tc_commit(smem_u32(&bars.drain));
+      mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
     }
     __syncwarp();
   } else {
@@ -549,12 +546,10 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         row0 += kRows;
         if (row0 >= nq) { row0 = 0; ++h; }
       }
-      if (!ok) {
-        // gave up: the copies in flight land before the CTA's shared memory is released
-        for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-          mbar_wait_one(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
-        if (limit) mbar_wait_one(smem_u32(&bars.kv_full), 0, kAttentionWaitLimit);
-      }
+      // every copy lands before the CTA's shared memory is released, whichever of its threads gives up
+      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
+        mbar_wait_one(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1, kAttentionWaitLimit);
+      if (limit) mbar_wait_one(smem_u32(&bars.kv_full), 0, kAttentionWaitLimit);
     } else if (warp == 4 * NW + 2 && edge) {
       // ---- the end of each head's last step: q and dout are factors of dk and dv ----------------
       for (int i = steps - 1 - step0, g = 0; i < n && ok; i += steps, ++g) {
@@ -618,10 +613,9 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
           tc_commit(smem_u32(&bars.dp_full));
         }
       }
-      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        tc_commit(smem_u32(&bars.drain));
-        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
-      }
+      // no product is in flight when tensor memory is freed, whichever thread gives up
+      tc_commit(smem_u32(&bars.drain));
+      mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
     }
     __syncwarp();
   } else {

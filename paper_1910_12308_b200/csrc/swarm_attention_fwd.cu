@@ -114,13 +114,11 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
         load_tile<DB>(smem_u32(sKV) + st * kTileBytes, f & 1 ? mv : mk, (start + (f >> 1)) * kTile, hk, b, bar);
         issued = f + 1;
       }
-      if (!ok) {
-        // gave up: the copies in flight land before the CTA's shared memory is released
-        for (int f = issued > kStages ? issued - kStages : 0; f < issued; ++f)
-          mbar_wait_one(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
-        for (int t = 0; t < NT; ++t)
-          if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
-      }
+      // every copy lands before the CTA's shared memory is released, whichever of its threads gives up
+      for (int f = issued > kStages ? issued - kStages : 0; f < issued; ++f)
+        mbar_wait_one(smem_u32(&bars.kv_full[f % kStages]), (f / kStages) & 1, kAttentionWaitLimit);
+      for (int t = 0; t < NT; ++t)
+        if (active(t) && limit) mbar_wait_one(smem_u32(&bars.q_full[t]), 0, kAttentionWaitLimit);
     } else if (warp == 4 * NT + 2 && any && edge) {
       // ---- the last tile's end: v is a factor of the sums ---------------------------------------
       const int f = 2 * n - 1;
@@ -182,10 +180,9 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
           if (NT == 2 && j + 1 < n) tc_commit(smem_u32(&bars.kv_empty[sk]));
         }
       }
-      if (!ok) {                                        // gave up: no product may be in flight when tensor memory is freed
-        tc_commit(smem_u32(&bars.drain));
-        mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
-      }
+      // no product is in flight when tensor memory is freed, whichever thread gives up
+      tc_commit(smem_u32(&bars.drain));
+      mbar_wait_one(smem_u32(&bars.drain), 0, kAttentionWaitLimit);
     }
     __syncwarp();
   } else {

@@ -561,3 +561,26 @@ def test_refusals_of_the_tensor_checks():
         with pytest.raises(g.SwarmError):
             bad()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("b,tq,tk,h,hk,d", [(40, 150, 120, 4, 4, 64), (40, 150, 120, 4, 2, 128), (3, 300, 700, 4, 2, 64), (3, 300, 700, 4, 4, 128),
+                                            (1, 140, 4100, 2, 1, 64), (1, 4100, 130, 2, 1, 128)])
+def test_waits_that_give_up_in_mid_call_leave_nothing_in_flight(b, tq, tk, h, hk, d):
+    """Small positive limits: some threads of a CTA give up while others have copies and products under way, or are already
+    through. The call is either reported or right, and so are the calls whose CTAs follow on the same multiprocessors."""
+    q, k, v, do = attention_inputs(b, tq, tk, h, hk, d, BF16, seed=5)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    grads = ops.cross_attention_backward(do, q, k, v, o, lse)
+    ops.check()
+    for limit in (1, 2, 3, 5, 8, 13, 30, 100, 1000):
+        for call, want in ((lambda **kw: ops.cross_attention(q, k, v, need_lse=True, **kw), (o, lse)),
+                           (lambda **kw: ops.cross_attention_backward(do, q, k, v, o, lse, **kw), grads)):
+            short, right = call(wait_limit=limit), call()
+            assert all(torch.equal(x, y) for x, y in zip(right, want)), limit
+            try:
+                ops.check()
+            except g.SwarmError as err:
+                assert err.code == g.ECUDA and g.load().swarm_operator_error() == 702
+            else:
+                assert all(torch.equal(x, y) for x, y in zip(short, want)), limit
+    ops.check()
