@@ -247,7 +247,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const uint32_t tile = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = tile + Shape::kDp;
     const float c = a.scale * kLog2e;
     const bool live = work && row < nq;
-    float delta = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
+    float delta = 0.0f, taken = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
     if (live) {
       const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
       const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, row, head);
@@ -296,6 +296,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < kStep; ++i) sum += i < valid ? p[i] * (dp[i] - delta) : 0.0f;
           delta += sum;
+          taken = sum;
         }
 #pragma unroll
         for (int i = 0; i < kStep; i += 2) {
@@ -340,7 +341,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     if (!exists(t) || !named_barrier_and(1 + t, 128, ok)) {
       // nothing to write
     } else if (SPLIT) {
-      // this CTA's part of the row: dq without its factor, and the sum of ds
+      // this CTA's part of the row: dq without its factor, and delta's error: the sum of ds and what was taken out before
       const int64_t at = (((int64_t)bh * a.queries + row) * a.group + (head - hk * a.group)) * plan.splits + split;
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
@@ -352,7 +353,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
             *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + g * 32 + i) =
                 live ? make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? off[0] + off[1] : 0.0f, 0.0f);
+      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? taken + (off[0] + off[1]) : 0.0f, 0.0f);
       else if (split == 0) {                            // rows of the tile past the tensor's
         store_stat<T>(a.stat_lse + stat, -INFINITY);
         store_stat<T>(a.stat_delta + stat, 0.0f);

@@ -584,3 +584,42 @@ def test_waits_that_give_up_in_mid_call_leave_nothing_in_flight(b, tq, tk, h, hk
             else:
                 assert all(torch.equal(x, y) for x, y in zip(short, want)), limit
     ops.check()
+
+
+# ---- gradients away from unit size ---------------------------------------------------------------------------------
+
+
+def beside_rounding(got, want, factor, what):
+    """The error of `got` as a whole is at most `factor` times what rounding the exact result to its type leaves."""
+    assert torch.isfinite(got).all(), what
+    alone = (want.to(got.dtype).double() - want).norm().item()
+    off = (got.double() - want).norm().item()
+    assert off <= factor * alone, (what, off / alone)
+
+
+def check_gradients_beside_rounding(q, k, v, do, scale=None, nq=None, nk=None, sentences=None, names=("dq", "dk", "dv")):
+    """p and ds are each rounded once before their products, o once before delta: independent errors of the size of the
+    result's own rounding, so that four of them come to twice it, and three times bounds them on any sizes."""
+    b, tq, tk = q.shape[0], q.shape[1], k.shape[1]
+    lq, lk = nq.tolist() if nq is not None else [tq] * b, nk.tolist() if nk is not None else [tk] * b
+    ref = attention_reference(q, k, v, scale or q.shape[3] ** -0.5, lq, lk, do, U[q.dtype])
+    kw = dict(scale=scale, query_lengths=nq, key_lengths=nk)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True, **kw)
+    got = dict(zip(("dq", "dk", "dv"), ops.cross_attention_backward(do, q, k, v, o, lse, **kw)))
+    ops.check()
+    for name in names:
+        for i in sentences or range(b):
+            beside_rounding(got[name][i], ref[name][i], 3.0, (name, i))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_cross_attention_split_states_of_short_sentences(dtype, d):
+    """Sentences of 6 and of 64 states beside a long one, whose states are split over CTAs. The values share a large part,
+    so that the rounding of o would show in dk if it were not taken out of delta."""
+    q, k, v, do = attention_inputs(3, 140, 4100, 2, 1, d, dtype, seed=39)
+    v = (v.float() + 16).to(dtype)
+    nk = torch.tensor([4100, 6, 64], dtype=torch.int32, device="cuda")
+    check_gradients_beside_rounding(q, k, v, do, nk=nk, sentences=(1, 2), names=("dq", "dk"))
+    short = slice(1, 3)
+    check_gradients_beside_rounding(q[short], k[short, :64], v[short, :64], do[short], nk=nk[short], names=("dq", "dk"))
