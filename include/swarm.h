@@ -430,7 +430,8 @@ int swarm_cross_attention(const swarm_attention *desc_host, const void *q_dev, c
                           void *o_dev, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
 /* dq, dk, dv from dout (the gradient of o), q, k, v and the o and lse of the forward call. dk and dv of a key head
  * are the sums over its query heads, added in a fixed order; p, ds and their products as in the formula
- *   p = exp(s - lse),  dv = p^T dout,  ds = scale * p * (dout v^T - rowsum(dout * o)),  dq = ds k,  dk = ds^T q. */
+ *   p = exp(s - lse),  dv = p^T dout,  ds = scale * p * (dout v^T - rowsum(dout * o)),  dq = ds k,  dk = ds^T q.
+ * Errors: EINVAL (as the forward call; a scale below 2^-120). */
 int swarm_cross_attention_backward(const swarm_attention *desc_host, const void *dout_dev, const void *q_dev,
                                    const void *k_dev, const void *v_dev, const void *o_dev, const float *lse_dev,
                                    void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,

@@ -69,6 +69,8 @@ constexpr int64_t kMaxStride = (int64_t)1 << 38;
 bool one_stride_ok(int64_t s, int extent, bool repeats) {
   return extent <= 1 || (s >= 0 && s < kMaxStride && s % 8 == 0 && (repeats || s != 0));
 }
+// The backward kernels hold lse / scale, which has to stay within fp32's range (lse is below 2^7 where that bounds it).
+constexpr float kMinGradScale = 0x1p-120f;
 // A tensor of `tokens` rows and `heads` heads: address and strides; an input may repeat its sentences or heads.
 bool strided_ok(const void* p, const swarm_strides& s, int batch, int tokens, int heads, bool output) {
   return p && ((uintptr_t)p & 15) == 0 && one_stride_ok(s.batch, batch, !output) && one_stride_ok(s.token, tokens, false) &&
@@ -140,7 +142,7 @@ int swarm_cross_attention_backward(const swarm_attention* desc_host, const void*
                                    const void* k_dev, const void* v_dev, const void* o_dev, const float* lse_dev,
                                    void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
                                    size_t workspace_bytes, void* cuda_stream) {
-  if (!desc_ok(desc_host)) return SWARM_EINVAL;
+  if (!desc_ok(desc_host) || desc_host->scale < kMinGradScale) return SWARM_EINVAL;
   const swarm_attention& d = *desc_host;
   if (d.batch == 0) return SWARM_OK;
   size_t need = 0;

@@ -355,12 +355,12 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
       if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? taken + (off[0] + off[1]) : 0.0f, 0.0f);
       else if (split == 0) {                            // rows of the tile past the tensor's
-        store_stat<T>(a.stat_lse + stat, -INFINITY);
-        store_stat<T>(a.stat_delta + stat, 0.0f);
+        store_stat(a.stat_lse + stat, -INFINITY);
+        store_stat(a.stat_delta + stat, 0.0f);
       }
     } else {
-      store_stat<T>(a.stat_lse + stat, (kWeightShift<T> - lse2) / c);    // in units of a score; -infinity in rows that take no part
-      store_stat<T>(a.stat_delta + stat, live ? -(delta + (off[0] + off[1])) : 0.0f);
+      store_stat(a.stat_lse + stat, (kWeightShift<T> - lse2) / c);    // in units of a score; -infinity in rows that take no part
+      store_stat(a.stat_delta + stat, live ? -(delta + (off[0] + off[1])) : 0.0f);
       uint8_t* out = sQ + 2 * t * kTileBytes;
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
@@ -417,8 +417,8 @@ __global__ void __launch_bounds__(128) attention_dq_join_kernel(AttentionArgs a,
   }
   if (lane == 0) {
     const int64_t head = (int64_t)b * a.heads + h, stat = stat_offset(head * row_tiles * kTile + t);
-    store_stat<T>(a.stat_lse + stat, live ? (kWeightShift<T> - a.lse_in[head * a.queries + t] * kLog2e) / (a.scale * kLog2e) : -INFINITY);
-    store_stat<T>(a.stat_delta + stat, live ? -delta : 0.0f);
+    store_stat(a.stat_lse + stat, live ? (kWeightShift<T> - a.lse_in[head * a.queries + t] * kLog2e) / (a.scale * kLog2e) : -INFINITY);
+    store_stat(a.stat_delta + stat, live ? -delta : 0.0f);
   }
 }
 
@@ -507,7 +507,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
   }
   if (warp == 4 * NW + 1) { tmem_alloc(smem_u32(&tmem_slot), Shape::kColumns); tmem_relinquish(); }
   if (tid < kTile) {                                    // the row of ones, for 128 states
-    const uint32_t one = pack2<T>(kStatOne<T>, kStatOne<T>);
+    const uint32_t one = pack2<StatType>(1.0f, 1.0f);
     uint8_t* p = sOnes + stat_offset(tid);
     *reinterpret_cast<uint4*>(p) = make_uint4(one, one & 0xFFFFu, 0u, 0u);
     *reinterpret_cast<uint4*>(p + 128) = make_uint4(0u, 0u, 0u, 0u);
@@ -570,7 +570,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       // d += ones x stat^T: the number `which` (0 lse, 1 delta) of the stage's rows
       auto add_stat = [&](uint32_t d, int stage, int which, int columns) {
         tc_mma(d, d_ones, smem_desc_plain(smem_u32(sStat) + (2 * stage + which) * Shape::kStatBytes, 128, 256),
-               instr_desc_16<T>(kTile, 0, 0, 0) + ((uint32_t)(columns >> 3) << 17), 1);
+               instr_desc_16<StatType>(kTile, 0, 0, 0) + ((uint32_t)(columns >> 3) << 17), 1);
       };
       ok = mbar_wait_one(smem_u32(&bars.kv_full), 0, limit);
       int cols = 0, cols_next = 0, step = step0, head = 0;  // columns of steps i and i + 1; the latter's place

@@ -91,18 +91,16 @@ __device__ __forceinline__ void store_row32(uint8_t* tile, int row, int col, con
   }
 }
 
-// A number per row as an operand of a product: 16 values of T of which the first three add up to it (24 bits or more), against
-// a row of kStatOne in the same places. Rows are stored as the unswizzled operand wants them, eight of them in 256 bytes: their
-// first eight values (16 bytes a row), then the others. fp16 has its range widened by kStatOne.
-template <typename T> constexpr float kStatOne = 1.0f;
-template <> constexpr float kStatOne<__half> = 64.0f;
+// A number per row as an operand of a product: 16 values of bf16 of which the first three add up to it (24 bits), against a row
+// of ones in the same places. bf16 whatever the call's type, so that fp32's range is held (a product of its own: an fp16
+// call's others are fp16). Rows are stored as the unswizzled operand wants them, eight of them in 256 bytes: their first
+// eight values (16 bytes a row), then the others.
+using StatType = __nv_bfloat16;
 __device__ __forceinline__ int64_t stat_offset(int64_t row) { return (row >> 3) * 256 + (row & 7) * 16; }
-template <typename T>
 __device__ __forceinline__ void store_stat(uint8_t* p, float v) {
-  v *= 1.0f / kStatOne<T>;
-  const float hi = to_float<T>(from_float<T>(v)), r1 = isinf(hi) ? 0.0f : v - hi;
-  const float mid = to_float<T>(from_float<T>(r1)), lo = r1 - mid;
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(hi, mid), pack2<T>(lo, 0.0f), 0u, 0u);
+  const float hi = to_float(from_float<StatType>(v)), r1 = isinf(hi) ? 0.0f : v - hi;
+  const float mid = to_float(from_float<StatType>(r1)), lo = r1 - mid;
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2<StatType>(hi, mid), pack2<StatType>(lo, 0.0f), 0u, 0u);
   *reinterpret_cast<uint4*>(p + 128) = make_uint4(0u, 0u, 0u, 0u);
 }
 

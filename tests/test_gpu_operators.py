@@ -623,3 +623,39 @@ def test_cross_attention_split_states_of_short_sentences(dtype, d):
     check_gradients_beside_rounding(q, k, v, do, nk=nk, sentences=(1, 2), names=("dq", "dk"))
     short = slice(1, 3)
     check_gradients_beside_rounding(q[short], k[short, :64], v[short, :64], do[short], nk=nk[short], names=("dq", "dk"))
+
+
+@pytest.mark.parametrize("tq,d,scale,size", [(140, 128, 2.0 ** -20, 360.0), (140, 64, 2.0 ** -20, 420.0), (9, 128, 2.0 ** 12, 0.007)])
+def test_cross_attention_gradients_of_large_and_small_scales_fp16(tq, d, scale, size):
+    """lse / scale, in which one of the kernels keeps a row's statistics, far above and far below the scores of unit normals."""
+    q, k, v, do = attention_inputs(2, tq, 200, 2, 1, d, F16, seed=31)
+    q, k = (q.float() * (size / 1.5)).to(F16), (k.float() * size).to(F16)
+    check_gradients_beside_rounding(q, k, v, (do.float() / 64).to(F16) if scale > 1 else do, scale=scale)
+
+
+def test_cross_attention_gradients_of_scores_in_the_millions_fp16():
+    """Rows that each attend to one state, their products with it 2^23: all of a row's weight is there."""
+    gen = torch.Generator(device="cuda").manual_seed(32)
+    k = (torch.randint(0, 2, (1, 150, 2, 128), generator=gen, device="cuda") * 512 - 256).to(F16)
+    at = torch.randint(0, 150, (140,), generator=gen, device="cuda")
+    q, scale = k[:, at].contiguous(), 2.0 ** -4
+    v, do = randn(1, 150, 2, 128, dtype=F16, seed=33), randn(1, 140, 2, 128, dtype=F16, seed=34)
+    o, lse = ops.cross_attention(q, k, v, scale=scale, need_lse=True)
+    dq, dk, dv = ops.cross_attention_backward(do, q, k, v, o, lse, scale=scale)
+    assert torch.equal(o, v[:, at]) and (lse == 2.0 ** 19).all()
+    want = torch.zeros(1, 150, 2, 128, dtype=torch.float64, device="cuda").index_add_(1, at, do.double())
+    # fp32 numbers of 2^23 are 1 apart: the product, lse / scale, its parts and their sum leave four of them, times the scale
+    size = torch.zeros_like(want).index_add_(1, at, do.double().abs())
+    within(dv, want, size * (math.exp(4 * scale) - 1) + U[F16] * want.abs(), "dv")
+
+
+def test_cross_attention_gradients_with_a_large_common_part_fp16():
+    """rowsum(dout * o) of 2^23, of which the differences between the states are a hundredth."""
+    q, k, v, do = attention_inputs(2, 20, 30, 2, 1, 128, F16, seed=35)
+    v, do = (v.float() + 8).to(F16), (do.float() * 64 + 8192).to(F16)
+    s = 128 ** -0.5
+    ref = attention_reference(q, k, v, s, [20] * 2, [30] * 2, do, U[F16])
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    got = dict(zip(("dq", "dk", "dv"), ops.cross_attention_backward(do, q, k, v, o, lse)))
+    for name in ("dq", "dk"):
+        within(got[name], ref[name], ref[name + "_b"], name)

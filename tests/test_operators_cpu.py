@@ -113,3 +113,11 @@ def test_no_cpu_path():
         ops.add_rms_norm(x, torch.ones(8))
     with pytest.raises(ValueError):
         ops.cross_attention(torch.zeros(1, 1, 1, 8), torch.zeros(1, 1, 1, 8), torch.zeros(1, 1, 1, 8))
+
+
+def test_attention_gradient_refuses_scales_whose_statistics_leave_fp32():
+    L, n = g.load(), C.c_size_t()
+    for scale in (2.0 ** -121, 2.0 ** -149):
+        args = [P] * 10 + [1 << 40, None]
+        assert L.swarm_cross_attention_backward(desc(scale=scale), *args) == g.EINVAL
+        assert L.swarm_cross_attention_workspace(desc(scale=scale), 0, C.byref(n)) == g.OK
