@@ -29,6 +29,10 @@ namespace {
 // taken out: with 6 states it doubled the error of dq), beside the rounding of ds to T; the two together would leave dq 1.55
 // times as far from its value as its own rounding does. So ds is the sum of two numbers of T, both of which dq takes (the
 // second lies beside the first, over the rest of dp): 1.2 times.
+// In fp16 a row's ds is held times a power of two, since its size is that of dout / states and fp16 ends at 2^-24 and 2^16:
+// the first step's largest is brought to 2^7, and where a later one passes 2^15 the row's power and its sums so far come down
+// (their product has completed when the step's dp has). It is taken out with the result's factor. Price: fp16 heads of 64, 512 rows
+// and states, 32 x 16, backward 254 -> 267 us; heads of 128 1 %.
 // =================================================================================================
 constexpr int kStep = 64;                               // states of a step
 constexpr int kStepBlock = kStep * 128;                 // bytes of 64 rows x 64 values
@@ -247,6 +251,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const uint32_t tile = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = tile + Shape::kDp;
     const float c = a.scale * kLog2e;
     const bool live = work && row < nq;
+    float up = 1.0f;                                    // fp16: what ds is held times
     float delta = 0.0f, taken = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
     if (live) {
       const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
@@ -300,12 +305,37 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         }
 #pragma unroll
         for (int i = 0; i < kStep; i += 2) {
-          add2(dp[i], dp[i + 1], dp[i], dp[i + 1], -delta, -delta);
+          if constexpr (kNarrow<T>) fma2(dp[i], dp[i + 1], dp[i], dp[i + 1], up, up, -delta * up, -delta * up);
+          else add2(dp[i], dp[i + 1], dp[i], dp[i + 1], -delta, -delta);
           mul2(p[i], p[i + 1], p[i], p[i + 1], dp[i], dp[i + 1]);
         }
         if (valid < kStep) {
 #pragma unroll
           for (int i = 0; i < kStep; ++i) p[i] = i < valid ? p[i] : 0.0f;
+        }
+        if constexpr (kNarrow<T>) {
+          float top = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kStep; i += 2) top = max3(top, fabsf(p[i]), fabsf(p[i + 1]));
+          if (j == 0 || __any_sync(0xFFFFFFFFu, top > 0x1p15f)) {
+            const float f = j == 0 || top > 0x1p15f ? power_to_2_7(top) : 1.0f;
+            up *= f;
+            off[0] *= f;
+            off[1] *= f;
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) p[i] *= f;
+            if (j > 0) {
+#pragma unroll
+              for (int g = 0; g < DB * 2; ++g) {
+                float o[32];
+                tmem_ld32(tile + Shape::kDq + g * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= f;
+                tmem_st32(tile + Shape::kDq + g * 32, o);
+              }
+            }
+          }
         }
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -338,6 +368,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
     }
     const int64_t stat = stat_offset(((int64_t)b * a.heads + head) * row_tiles * kTile + row);
+    const float down = 1.0f / up;                       // a power of two
     if (!exists(t) || !named_barrier_and(1 + t, 128, ok)) {
       // nothing to write
     } else if (SPLIT) {
@@ -351,22 +382,22 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         for (int i = 0; i < 32; i += 4)
           if (row < a.queries && g * 32 + i < a.head_dim)
             *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + g * 32 + i) =
-                live ? make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                live ? make_float4(o[i] * down, o[i + 1] * down, o[i + 2] * down, o[i + 3] * down) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? taken + (off[0] + off[1]) : 0.0f, 0.0f);
+      if (row < a.queries) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(live ? taken + (off[0] + off[1]) * down : 0.0f, 0.0f);
       else if (split == 0) {                            // rows of the tile past the tensor's
         store_stat(a.stat_lse + stat, -INFINITY);
         store_stat(a.stat_delta + stat, 0.0f);
       }
     } else {
       store_stat(a.stat_lse + stat, (kWeightShift<T> - lse2) / c);    // in units of a score; -infinity in rows that take no part
-      store_stat(a.stat_delta + stat, live ? -(delta + (off[0] + off[1])) : 0.0f);
+      store_stat(a.stat_delta + stat, live ? -(delta + (off[0] + off[1]) * down) : 0.0f);
       uint8_t* out = sQ + 2 * t * kTileBytes;
 #pragma unroll
       for (int g = 0; g < DB * 2; ++g) {
         float o[32];
         if (work) { tmem_ld32(tile + Shape::kDq + g * 32, o); tmem_wait_ld(); }
-        store_row32<T>(out, tile_row, g * 32, o, a.scale, live);
+        store_row32<T>(out, tile_row, g * 32, o, a.scale * down, live);
       }
       fence_proxy_async();
       named_barrier(1 + t, 128);

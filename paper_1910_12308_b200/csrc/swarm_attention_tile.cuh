@@ -24,6 +24,16 @@ template <typename T> constexpr float kRunningShift = 0.0f;
 template <> constexpr float kRunningShift<__half> = 7.0f;              // weights against a running maximum: at most 2^8
 __device__ __forceinline__ constexpr float pow2_of(float shift) { return shift == 15.0f ? 0x1p-15f : 1.0f; }
 
+// Whether numbers of T have so small a range that ds, which follows the size of dout, needs a power of two of its own.
+template <typename T> constexpr bool kNarrow = false;
+template <> constexpr bool kNarrow<__half> = true;
+// The power of two that brings a number (not negative) to at least 2^7 and below 2^8, 2^80 at most: zeros, and with dout of 2^-24
+// beside values of 2^16, stay far inside fp32's range.
+__device__ __forceinline__ float power_to_2_7(float v) {
+  const int n = 134 - (int)(__float_as_uint(v) >> 23);
+  return __uint_as_float((uint32_t)(127 + min(n, 80)) << 23);
+}
+
 // Offset of 16 bytes (8 values) of a row in a block.
 __device__ __forceinline__ uint32_t swizzled(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
 

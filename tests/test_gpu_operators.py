@@ -659,3 +659,58 @@ def test_cross_attention_gradients_with_a_large_common_part_fp16():
     got = dict(zip(("dq", "dk", "dv"), ops.cross_attention_backward(do, q, k, v, o, lse)))
     for name in ("dq", "dk"):
         within(got[name], ref[name], ref[name + "_b"], name)
+
+
+DOUT_SHAPES = [(1, 300, 4096, 4, 2, 128), (1, 140, 4100, 2, 1, 64), (8, 300, 4000, 4, 4, 128), (8, 140, 4000, 20, 4, 64), (1, 4100, 130, 2, 1, 64),
+               (2, 50, 61, 4, 2, 128)]
+
+
+def check_gradients_of_size(shape, size, names):
+    q, k, v, do = attention_inputs(*shape, F16, seed=36)
+    check_gradients_beside_rounding(q, k, v, (do.float() * size).to(F16), sentences=range(min(shape[0], 2)), names=names)
+
+
+def check_gradients_are_linear(tq, tk, d, power, names):
+    """A power of two times dout is the same power of two times the gradients, but for where their last rounding falls:
+    half a step of either side. dout holds multiples of 2^-6, so that all of its multiples here are exact."""
+    q, k, v, do = attention_inputs(2, tq, tk, 2, 1, d, F16, seed=38)
+    do, v = ((do.float() * 64).round() / 64).clamp(-3.5, 3.5).to(F16), (v.float() * 4).to(F16)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    one = ops.cross_attention_backward(do, q, k, v, o, lse)
+    scaled = (do.float() * 2.0 ** power).to(F16)
+    assert torch.equal(scaled.double(), do.double() * 2.0 ** power)
+    other = ops.cross_attention_backward(scaled, q, k, v, o, lse)
+    for name, x, y in zip(("dq", "dk", "dv"), one, other):
+        if name not in names:
+            continue
+        want = x.double() * 2.0 ** power
+        room = want.abs() < 60000                                                   # what fits the type
+        assert room.double().mean() > 0.5, name
+        within(y[room], want[room], 2.01 * U[F16] * want[room].abs() + 2.0 ** (power - 25) + 2.0 ** -25, name)
+
+
+@pytest.mark.parametrize("shape", DOUT_SHAPES)
+@pytest.mark.parametrize("size", [1e-2, 1e-3, 1e-4, 64.0])
+def test_cross_attention_dq_of_small_and_large_dout_fp16(shape, size):
+    check_gradients_of_size(shape, size, ("dq", "dv"))
+
+
+@pytest.mark.parametrize("tq,tk,d", [(4, 2, 128), (4, 130, 64), (140, 200, 128), (20, 4100, 64)])
+@pytest.mark.parametrize("power", [-18, -6, 7, 13])
+def test_cross_attention_dq_is_linear_in_dout_fp16(tq, tk, d, power):
+    check_gradients_are_linear(tq, tk, d, power, ("dq", "dv"))
+
+
+@pytest.mark.parametrize("tk", [700, 5000])
+def test_cross_attention_dq_of_rows_of_unequal_size_fp16(tk):
+    """Rows of dout 2^-14 of the others, and first steps of states that take e^-25 of the weight."""
+    q, k, v, do = attention_inputs(1, 260, tk, 2, 1, 128, F16, seed=37)
+    do, k = do.float(), k.float()
+    do[:, 100:] *= 2.0 ** -14
+    k[:, :130] -= 1.5
+    q, k, do = (q.float() + 1.5).to(F16), k.to(F16), do.to(F16)
+    ref = attention_reference(q, k, v, 128 ** -0.5, [260], [tk], do, U[F16])
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    dq = ops.cross_attention_backward(do, q, k, v, o, lse)[0]
+    beside_rounding(dq[:, :100], ref["dq"][:, :100], 3.0, "large rows")
+    beside_rounding(dq[:, 100:], ref["dq"][:, 100:], 3.0, "small rows")
