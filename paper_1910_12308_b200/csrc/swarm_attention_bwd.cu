@@ -251,7 +251,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const uint32_t tile = tmem + 256 * t + ((uint32_t)(quad * 32) << 16), tdp = tile + Shape::kDp;
     const float c = a.scale * kLog2e;
     const bool live = work && row < nq;
-    float up = 1.0f;                                    // fp16: what ds is held times
+    float up = 1.0f, peak = 0.0f;                       // fp16: what ds is held times, and the largest so far
     float delta = 0.0f, taken = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
     if (live) {
       const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
@@ -318,8 +318,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < kStep; i += 2) top = max3(top, fabsf(p[i]), fabsf(p[i + 1]));
           if (j == 0 || __any_sync(0xFFFFFFFFu, top > 0x1p15f)) {
-            const float f = j == 0 || top > 0x1p15f ? power_to_2_7(top) : 1.0f;
+            const float f = j == 0 || top > 0x1p15f ? power_to<7>(top) : 1.0f;
             up *= f;
+            peak *= f;
+            top *= f;
             off[0] *= f;
             off[1] *= f;
 #pragma unroll
@@ -336,6 +338,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
               }
             }
           }
+          peak = fmaxf(peak, top);
         }
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -369,7 +372,15 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     }
     const int64_t stat = stat_offset(((int64_t)b * a.heads + head) * row_tiles * kTile + row);
     const float down = 1.0f / up;                       // a power of two
-    if (!exists(t) || !named_barrier_and(1 + t, 128, ok)) {
+    const bool write = exists(t) && named_barrier_and(1 + t, 128, ok);
+    if (kNarrow<T> && write) {
+      peak = live ? peak * down : 0.0f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
+      if (lane == 0)
+        a.stat_peak[((((int64_t)b * a.heads + head) * row_tiles + row0 / kTile) * 4 + quad) * plan.splits + split] = peak;
+    }
+    if (!write) {
       // nothing to write
     } else if (SPLIT) {
       // this CTA's part of the row: dq without its factor, and delta's error: the sum of ds and what was taken out before
@@ -477,6 +488,9 @@ SplitPlan make_dq_plan(const AttentionArgs& a) {
 // sixteen of the contraction, q's row with -lse against a row of ones beside k, and dout's with -delta beside v. (Read
 // from shared memory by every thread they took 32 loads a step, which waited behind the special functions: 1.17 ms
 // against 1.05 ms for the backward pass of 4 x 16 heads of 64, 4096 rows and states.)
+// In fp16 ds^T is held times one power of two for all rows that a state's dk sums, which brings the largest |ds| that the dq
+// kernel saw among them to 2^11: room for 16 times as much above (p is formed again here, from scores of another product), 25
+// powers of two below it before bits are lost. It takes the place of the power that p is held times.
 // =================================================================================================
 template <int DB, int NW> struct DkvShape {
   static constexpr int kThreads = 128 * (NW + 1);
@@ -500,7 +514,7 @@ template <typename T, int DB, int NW, bool SPLIT>
 __global__ void __launch_bounds__(DkvShape<DB, NW>::kThreads, DkvShape<DB, NW>::kCtasPerSm)
 attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv,
                      const __grid_constant__ TileMap mdo, const __grid_constant__ TileMap mdk, const __grid_constant__ TileMap mdv,
-                     AttentionArgs a, int key_tiles, int row_tiles, SplitPlan plan) {
+                     AttentionArgs a, int key_tiles, int row_tiles, int dq_splits, SplitPlan plan) {
   using Shape = DkvShape<DB, NW>;
   constexpr int kStages = Shape::kStages, kRows = Shape::kRows;
   constexpr uint32_t kTileBytes = DB * kBlockBytes, kHalfBytes = Shape::kHalfBytes;
@@ -658,6 +672,18 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
     const uint32_t ts = tmem + lane_base + half * 64, tdp = ts + Shape::kDp;
     const float c = a.scale * kLog2e;
     constexpr float kUnshift = pow2_of(kWeightShift<T>);
+    float up = 1.0f;                                    // fp16: what ds is held times
+    if (kNarrow<T> && n) {
+      const int64_t peaks = (int64_t)a.group * row_tiles * 4 * dq_splits;
+      const float* of_head = a.stat_peak + ((int64_t)b * a.kv_heads + hk) * peaks;
+      float peak = 0.0f;
+#pragma unroll 4
+      for (int64_t i = lane; i < peaks; i += 32) peak = fmaxf(peak, of_head[i]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
+      up = isinf(peak) ? 1.0f : power_to<11>(peak);
+    }
+    const float p_to_ds = kUnshift * up, dk_factor = a.scale / up;
     int step = step0;
     for (int i = 0; i < n; ++i) {
       const int cols = (step == steps - 1 ? nq - step * kRows : kRows) - half * 64;   // columns of this warpgroup that exist
@@ -703,7 +729,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         uint32_t w[16];
 #pragma unroll
         for (int q = g * 32; q < g * 32 + 32; q += 2) {
-          if (kUnshift != 1.0f) mul2(dp[q], dp[q + 1], dp[q], dp[q + 1], kUnshift, kUnshift);
+          if constexpr (kNarrow<T>) mul2(dp[q], dp[q + 1], dp[q], dp[q + 1], p_to_ds, p_to_ds);
           mul2(dp[q], dp[q + 1], dp[q], dp[q + 1], p[q], p[q + 1]);
         }
         if (cols < 64) {
@@ -733,7 +759,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
         if (NW == 2 && which != half) continue;
-        const float factor = which == 0 ? kUnshift : a.scale;
+        const float factor = which == 0 ? kUnshift : dk_factor;
 #pragma unroll
         for (int g = 0; g < DB * 2; ++g) {
           float o[32];
@@ -754,7 +780,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
         for (int g = 0; g < DB * 2; ++g) {
           float o[32];
           if (n) { tmem_ld32(tmem + lane_base + (which == 0 ? Shape::kDv : Shape::kDk) + g * 32, o); tmem_wait_ld(); }
-          store_row32<T>(out, tile_row, g * 32, o, which == 0 ? kUnshift : a.scale, live);
+          store_row32<T>(out, tile_row, g * 32, o, which == 0 ? kUnshift : dk_factor, live);
         }
       }
       fence_proxy_async();
@@ -859,20 +885,22 @@ cudaError_t launch_backward(const AttentionArgs& a, const SplitPlan& plan, const
   if (e != cudaSuccess) return e;
   const unsigned dkv_ctas = (unsigned)((int64_t)key_tiles * a.kv_heads * a.batch * dkv.splits);
   if (dkv.splits > 1) {
-    attention_dkv_kernel<T, DB, DB, true><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, dkv);
+    attention_dkv_kernel<T, DB, DB, true><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, plan.splits, dkv);
     attention_dkv_join_kernel<T><<<(unsigned)(((int64_t)a.batch * a.kv_heads * a.keys + 3) / 4), 128, 0, st>>>(a, dkv);
   } else {
-    attention_dkv_kernel<T, DB, DB, false><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, dkv);
+    attention_dkv_kernel<T, DB, DB, false><<<dkv_ctas, Dkv::kThreads, Dkv::kSmem, st>>>(mq, mk, mv, mdo, mdk, mdv, a, key_tiles, row_tiles, plan.splits, dkv);
   }
   return cudaGetLastError();
 }
 
 int64_t stat_count(const AttentionArgs& a) { return (int64_t)a.batch * a.heads * ((a.queries + kTile - 1) / kTile) * kTile; }
+size_t peak_bytes(const AttentionArgs& a, const SplitPlan& dq) { return (size_t)(stat_count(a) / 32) * dq.splits * sizeof(float); }
 
 }  // namespace
 
 size_t attention_backward_workspace(const AttentionArgs& a) {
-  return (size_t)stat_count(a) * 2 * 32 + dkv_part_bytes(a, make_dkv_plan(a)) + split_bytes(a, make_dq_plan(a));
+  const SplitPlan dq = make_dq_plan(a);
+  return (size_t)stat_count(a) * 2 * 32 + dkv_part_bytes(a, make_dkv_plan(a)) + split_bytes(a, dq) + peak_bytes(a, dq);
 }
 
 cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* workspace, cudaStream_t st) {
@@ -882,6 +910,7 @@ cudaError_t launch_attention_backward_tc(AttentionArgs a, int dtype, void* works
   uint8_t* rest = a.stat_delta + stat_count(a) * 32;
   dkv.part_o = reinterpret_cast<float*>(rest);          // head_dim is a multiple of 8: 16-byte boundaries throughout
   if (dq.splits > 1) place_parts(a, &dq, rest + dkv_part_bytes(a, dkv));
+  a.stat_peak = reinterpret_cast<float*>(rest + dkv_part_bytes(a, dkv) + split_bytes(a, dq));
   if (dtype == SWARM_BF16)
     return a.head_dim <= 64 ? launch_backward<__nv_bfloat16, 1>(a, dq, dkv, dtype, st) : launch_backward<__nv_bfloat16, 2>(a, dq, dkv, dtype, st);
   return a.head_dim <= 64 ? launch_backward<__half, 1>(a, dq, dkv, dtype, st) : launch_backward<__half, 2>(a, dq, dkv, dtype, st);

@@ -27,10 +27,11 @@ __device__ __forceinline__ constexpr float pow2_of(float shift) { return shift =
 // Whether numbers of T have so small a range that ds, which follows the size of dout, needs a power of two of its own.
 template <typename T> constexpr bool kNarrow = false;
 template <> constexpr bool kNarrow<__half> = true;
-// The power of two that brings a number (not negative) to at least 2^7 and below 2^8, 2^80 at most: zeros, and with dout of 2^-24
-// beside values of 2^16, stay far inside fp32's range.
-__device__ __forceinline__ float power_to_2_7(float v) {
-  const int n = 134 - (int)(__float_as_uint(v) >> 23);
+// The power of two that brings a number (not negative) to at least 2^TO and below twice that, 2^80 at most: zeros, and with
+// dout of 2^-24 beside values of 2^16, stay far inside fp32's range.
+template <int TO>
+__device__ __forceinline__ float power_to(float v) {
+  const int n = 127 + TO - (int)(__float_as_uint(v) >> 23);
   return __uint_as_float((uint32_t)(127 + min(n, 80)) << 23);
 }
 

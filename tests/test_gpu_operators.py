@@ -714,3 +714,34 @@ def test_cross_attention_dq_of_rows_of_unequal_size_fp16(tk):
     dq = ops.cross_attention_backward(do, q, k, v, o, lse)[0]
     beside_rounding(dq[:, :100], ref["dq"][:, :100], 3.0, "large rows")
     beside_rounding(dq[:, 100:], ref["dq"][:, 100:], 3.0, "small rows")
+
+
+@pytest.mark.parametrize("shape", DOUT_SHAPES)
+@pytest.mark.parametrize("size", [1e-2, 1e-3, 1e-4, 64.0])
+def test_cross_attention_dk_of_small_and_large_dout_fp16(shape, size):
+    check_gradients_of_size(shape, size, ("dk",))
+
+
+@pytest.mark.parametrize("tq,tk,d", [(4, 2, 128), (4, 130, 64), (140, 200, 128), (20, 4100, 64)])
+@pytest.mark.parametrize("power", [-18, -6, 7, 13])
+def test_cross_attention_dk_is_linear_in_dout_fp16(tq, tk, d, power):
+    check_gradients_are_linear(tq, tk, d, power, ("dk",))
+
+
+@pytest.mark.parametrize("tq,tk,h,hk,d", [(260, 700, 2, 1, 128), (140, 5000, 2, 2, 64), (4100, 200, 2, 1, 128)])
+def test_cross_attention_dk_of_unequal_sizes_fp16(tq, tk, h, hk, d):
+    """Rows of dout 2^-12 of the others, alone in the second sentence, and states that take e^-12 of the weight."""
+    q, k, v, do = attention_inputs(2, tq, tk, h, hk, d, F16, seed=40)
+    do, k, shift = do.float() * 1024, k.float(), 12 / 1.5 / d ** 0.5
+    do[:, 100:] *= 2.0 ** -12
+    do[1, :100] = 0
+    k[:, :130] -= shift
+    q, k, do = (q.float() + 1.5).to(F16), k.to(F16), do.to(F16)
+    lengths = torch.tensor([tq, tq - 3], dtype=torch.int32, device="cuda")
+    ref = attention_reference(q, k, v, d ** -0.5, lengths.tolist(), [tk] * 2, do, U[F16])
+    o, lse = ops.cross_attention(q, k, v, need_lse=True, query_lengths=lengths)
+    _, dk, dv = ops.cross_attention_backward(do, q, k, v, o, lse, query_lengths=lengths)
+    for i in range(2):
+        beside_rounding(dk[i, :130], ref["dk"][i, :130], 3.0, ("light states", i))
+        beside_rounding(dk[i, 130:], ref["dk"][i, 130:], 3.0, ("the others", i))
+        beside_rounding(dv[i], ref["dv"][i], 3.0, ("dv", i))
