@@ -206,10 +206,14 @@ def _attention_desc(device, q, k, v, o, scale, query_lengths, key_lengths, wait_
         more = (*_heads(do, "do", device, dtype, whole), *_heads(dq, "dq", device, dtype, whole),
                 *_heads(dk, "dk", device, dtype, states), *_heads(dv, "dv", device, dtype, states))
     batch, dim = whole[0], whole[3]
-    return _DESC.pack(batch, whole[2], states[2], whole[1], states[1], dim, _DTYPES[dtype],
-                      dim ** -0.5 if scale is None else scale, wait_limit,
-                      _lengths(query_lengths, "query_lengths", device, batch), _lengths(key_lengths, "key_lengths", device, batch),
-                      *strides, *more)
+    if dim == 0:
+        raise ValueError("q, k: head_dim is 0")
+    lengths = (_lengths(query_lengths, "query_lengths", device, batch), _lengths(key_lengths, "key_lengths", device, batch))
+    try:
+        return _DESC.pack(batch, whole[2], states[2], whole[1], states[1], dim, _DTYPES[dtype],
+                          dim ** -0.5 if scale is None else scale, wait_limit, *lengths, *strides, *more)
+    except (struct.error, OverflowError) as err:
+        raise ValueError(f"sizes, scale or wait_limit: {err}") from None
 
 
 def _workspace(L, desc, backward, x):

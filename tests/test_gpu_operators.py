@@ -745,3 +745,15 @@ def test_cross_attention_dk_of_unequal_sizes_fp16(tq, tk, h, hk, d):
         beside_rounding(dk[i, :130], ref["dk"][i, :130], 3.0, ("light states", i))
         beside_rounding(dk[i, 130:], ref["dk"][i, 130:], 3.0, ("the others", i))
         beside_rounding(dv[i], ref["dv"][i], 3.0, ("dv", i))
+
+
+def test_refusals_of_numbers_that_the_call_cannot_hold():
+    q, k, v, do = attention_inputs(2, 5, 7, 4, 2, 64, BF16)
+    o, lse = ops.cross_attention(q, k, v, need_lse=True)
+    for bad in (dict(scale=1e300), dict(scale=-1e300), dict(wait_limit=1 << 70), dict(scale="a")):
+        with pytest.raises(ValueError):
+            ops.cross_attention(q, k, v, **bad)
+        with pytest.raises(ValueError):
+            ops.cross_attention_backward(do, q, k, v, o, lse, **bad)
+    with pytest.raises(ValueError):
+        ops.cross_attention(q[..., :0], k[..., :0], v[..., :0])
