@@ -18,7 +18,7 @@ struct AttentionArgs {
   // backward, per (sentence, head) padded to whole row tiles: lse and rowsum(dout * o) as factors of a product (see the
   // backward kernels), 32 bytes a row each
   uint8_t *stat_lse, *stat_delta;
-  // fp16: the largest |ds| (without the factor scale) of 32 rows, [batch][heads][row tiles][4][parts of dq]
+  // fp16: the largest |ds| (without the factor scale; 2^-7 sum |dout| at least) of 32 rows, [batch][heads][row tiles][4][parts of dq]
   float* stat_peak;
   const int32_t *query_lengths, *key_lengths;
   swarm_strides qs, ks, vs, os, dos, dqs, dks, dvs;

@@ -252,7 +252,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const float c = a.scale * kLog2e;
     const bool live = work && row < nq;
     float up = 1.0f, peak = 0.0f;                       // fp16: what ds is held times, and the largest so far
-    float delta = 0.0f, taken = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
+    float delta = 0.0f, size = 0.0f, taken = 0.0f, lse2 = INFINITY, off[2] = {0.0f, 0.0f};
     if (live) {
       const T* g = reinterpret_cast<const T*>(a.dout) + offset_of(a.dos, b, row, head);
       const T* o = reinterpret_cast<const T*>(a.o) + offset_of(a.os, b, row, head);
@@ -263,7 +263,10 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
         unpack8<T>(load_raw8<T>(g + d), x);
         unpack8<T>(load_raw8<T>(o + d), y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
+        for (int i = 0; i < 8; ++i) {
+          delta = fmaf(x[i], y[i], delta);
+          if constexpr (kNarrow<T>) size += fabsf(x[i]);
+        }
       }
     }
     if (work) {
@@ -374,7 +377,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
     const float down = 1.0f / up;                       // a power of two
     const bool write = exists(t) && named_barrier_and(1 + t, 128, ok);
     if (kNarrow<T> && write) {
-      peak = live ? peak * down : 0.0f;
+      peak = live ? fmaxf(peak * down, size * 0x1p-7f) : 0.0f;         // size: sum of |dout|
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
       if (lane == 0)
@@ -489,8 +492,10 @@ SplitPlan make_dq_plan(const AttentionArgs& a) {
 // from shared memory by every thread they took 32 loads a step, which waited behind the special functions: 1.17 ms
 // against 1.05 ms for the backward pass of 4 x 16 heads of 64, 4096 rows and states.)
 // In fp16 ds^T is held times one power of two for all rows that a state's dk sums, which brings the largest |ds| that the dq
-// kernel saw among them to 2^11: room for 16 times as much above (p is formed again here, from scores of another product), 25
-// powers of two below it before bits are lost. It takes the place of the power that p is held times.
+// kernel saw among them to 2^13: room for four times as much above (p is formed again here, from scores of another product), 27
+// powers of two below it before bits are lost. It takes the place of the power that p is held times. Where ds cancels to nothing
+// what is left of it here may be any multiple of what is left there: at most a few roundings of dout v^T, 2^-21 of
+// sum |dout| * 2^16. So the largest |ds| counts as at least 2^-7 of sum |dout|, which keeps that below fp16's end as well.
 // =================================================================================================
 template <int DB, int NW> struct DkvShape {
   static constexpr int kThreads = 128 * (NW + 1);
@@ -681,7 +686,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       for (int64_t i = lane; i < peaks; i += 32) peak = fmaxf(peak, of_head[i]);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
-      up = isinf(peak) ? 1.0f : power_to<11>(peak);
+      up = isinf(peak) ? 1.0f : power_to<13>(peak);
     }
     const float p_to_ds = kUnshift * up, dk_factor = a.scale / up;
     int step = step0;
