@@ -234,7 +234,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
             }
           }
           if (moved) idle = 0;
-          else if (++idle > limit) ok = false;
+          else if (++idle >= limit) ok = false;             // reached for every limit, 2^32 - 1 included
         }
       }
       // no product is in flight when tensor memory is freed, whichever thread gives up
