@@ -787,3 +787,82 @@ def test_cross_attention_gradients_that_cancel_fp16(tk, sharp, tq, d):
             assert not torch.isnan(x).any(), name
             room = ref[name].abs() + ref[name + "_b"] < 65504
             within(x[room], ref[name][room], ref[name + "_b"][room] + TINY[F16], name)
+
+
+# ---- masks over whole grids and wide rows ---------------------------------------------------------------------------
+
+
+def factors_at_once(rows, cols, rate, seed, event):
+    """As `factors`, all generator calls side by side."""
+    import numpy as np
+    u, groups = np.uint64, (cols + 7) // 8
+    low, half = u(0xFFFFFFFF), u(32)
+    c = [np.tile(np.arange(groups, dtype=u), rows), np.repeat(np.arange(rows, dtype=u), groups), np.full(rows * groups, event, dtype=u),
+         np.full(rows * groups, 13, dtype=u)]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(10):
+        p0, p1 = u(0xD2511F53) * c[0], u(0xCD9E8D57) * c[2]
+        c = [(p1 >> half) ^ c[1] ^ u(k[0]), p1 & low, (p0 >> half) ^ c[3] ^ u(k[1]), p0 & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    draws = np.stack([w >> u(16 * i) & u(0xFFFF) for w in c for i in (0, 1)], 1).reshape(rows, groups * 8)[:, :cols]
+    drop = math.floor(rate * 65536 + 0.5)
+    return torch.from_numpy(np.where(draws >= u(drop), 65536 / (65536 - drop), 0.0)).cuda()
+
+
+def test_the_two_ways_to_draw_a_mask_agree():
+    assert torch.equal(factors(5, 83, 0.3, 0xFEDCBA9876543210, 4000000000), factors_at_once(5, 83, 0.3, 0xFEDCBA9876543210, 4000000000))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", [(70001, 48), (30011, 128), (9001, 1000), (5003, 1001), (1201, 8200), (901, 4099)])
+def test_dropout_over_several_passes_of_the_grid(dtype, rows, cols):
+    x = torch.ones(rows, cols, dtype=dtype, device="cuda")
+    got = ops.dropout(x, 0.3, 41, 42)
+    m = factors_at_once(rows, cols, 0.3, 41, 42)
+    within(got, m, U[dtype] * m + 2.0 ** -22 * m)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols", [(5, 1201), (900, 2048), (3, 3000), (400, 4096), (3, 4100), (300, 8192), (2, 16000), (40, 16384), (2, 32768)])
+def test_norm_masks_of_wide_rows(dtype, rows, cols):
+    rate, seed, event = 0.3, 2 ** 40 + 5, 6
+    x, r, dy = (randn(rows, cols, dtype=dtype, seed=s) for s in (1, 2, 3))
+    w = 1 + 0.3 * randn(cols, seed=4)
+    m = factors_at_once(rows, cols, rate, seed, event)
+    total, want = norm_reference(x, r, w, 1e-6, m)
+    how = dict(rate=rate, seed=seed, event=event)
+    y, kept = ops.add_rms_norm(x, w, residual=r, **how)
+    size = (x.double() * m).abs() + r.double().abs()
+    within(kept, total, U[dtype] * total.abs() + 2.0 ** -22 * size + TINY[dtype])
+    rstd = 1 / (total.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    within(y, want, (U[dtype] + E) * want.abs() + 2.0 ** -22 * size * rstd * w.double().abs() + TINY[dtype])
+    assert torch.equal(ops.add_rms_norm(x, w, residual=r, eight_bit=True, **how)[2], kept)
+    t, wdy = kept.double(), w.double() * dy.double()
+    rt = 1 / (t.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    grad = rt * wdy - t * rt ** 3 * (wdy * t).mean(1, keepdim=True)
+    size = rt * wdy.abs() + t.abs() * rt ** 3 * (wdy * t).abs().mean(1, keepdim=True)
+    dx, dres, _ = ops.add_rms_norm_backward(dy, kept, w, **how)
+    within(dres, grad, U[dtype] * grad.abs() + E * size + TINY[dtype])
+    within(dx, grad * m, U[dtype] * (grad * m).abs() + E * size * 2 + TINY[dtype])
+    assert ((dx == 0) | (m > 0)).all()
+
+
+@pytest.mark.parametrize("tq,tk,d,dtype", [(40, 100, 64, F16), (200, 300, 128, F16), (150, 270, 72, F16), (1, 300, 128, F16), (140, 4100, 64, F16),
+                                           (140, 4100, 128, BF16), (2100, 130, 64, BF16), (2100, 130, 128, F16)])
+def test_cross_attention_takes_nothing_from_past_the_ends_in_its_other_forms(tq, tk, d, dtype):
+    """NaN and infinities past the ends, in fp16 and where states or rows are split: the same bits as without them."""
+    clean = attention_inputs(2, tq, tk, 2, 1, d, dtype, seed=9, layout="packed")
+    nk = torch.tensor([tk - 3, max(1, tk // 3)], dtype=torch.int32, device="cuda")
+    nq = torch.tensor([max(1, tq // 2 - 1), max(1, tq - 5)], dtype=torch.int32, device="cuda")
+    dirty = [x.clone() for x in clean]
+    for i in range(2):
+        for x, n in zip(dirty, (nq, nk, nk, nq)):
+            x[i, int(n[i]):] = float("nan")
+            x[i, int(n[i])::2] = float("inf")
+            x[i, int(n[i])::3] = -float("inf")
+    ends = dict(query_lengths=nq, key_lengths=nk)
+    results = []
+    for q, k, v, do in (clean, dirty):
+        o, lse = ops.cross_attention(q, k, v, need_lse=True, **ends)
+        results.append([o, lse, *ops.cross_attention_backward(do, q, k, v, o, lse, **ends)])
+    assert all(torch.equal(x, y) for x, y in zip(*results))
