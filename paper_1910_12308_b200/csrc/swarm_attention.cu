@@ -87,10 +87,18 @@ void fill(AttentionArgs& a, const swarm_attention* d) {
   a.wait_limit = d->wait_limit < 0 ? kAttentionWaitLimit : d->wait_limit < (int64_t)1 << 32 ? (uint32_t)d->wait_limit : 0xFFFFFFFFu;
 }
 
-// Whether a call goes to the kernel that streams the states past 16 rows at a time, instead of that with tiles of 128 rows
-// of one head. Measured (16 sentences, 1024 states, heads of 64, streaming / tiles): one row of 16 heads in batches of 128
-// 103 / 122 us, 16 rows 25 / 23 us, 17 rows 40 / 23 us; four heads to a key head: 2 rows 19 / 38 us, 8 rows 23 / 38 us,
-// 16 rows 41 / 38 us.
+// Whether a call goes to the kernel that streams the states past 16 rows (query tokens x heads of a key head) at a time, instead
+// of that with tiles of 128 rows of one head. The tiles walk all states once for each head of a group, the other kernel once for
+// each 16 rows, so the crossing in tokens hardly moves with the group; at 12 streaming is at most 15 % behind and up to a
+// quarter ahead. Measured, 128 sentences of 1024 states, 16 heads of 64, one token: 103 / 122 us; 16 sentences, 16 key heads, bf16,
+// cold caches, us streaming / tiles:
+//   tokens                            1          8          12         16         24
+//   heads of 64,  1 to a key head   29 /  27   29 /  27   31 /  27   33 /  27   49 /  27
+//   heads of 64,  4 to a key head   29 /  66   51 /  68   55 /  68   72 /  68   92 /  68
+//   heads of 64,  8 to a key head   31 / 119   70 / 121   92 / 121  113 / 121  156 / 121
+//   heads of 128, 1 to a key head   39 /  45   43 /  45   45 /  47   47 /  45   70 /  45
+//   heads of 128, 4 to a key head   41 /  90   74 /  90   98 /  90  125 /  90  178 /  90
+//   heads of 128, 8 to a key head   41 / 150  125 / 152  172 / 152  209 / 152  307 / 154
 bool few_rows(const AttentionArgs& a) { return a.queries <= 12; }
 
 }  // namespace

@@ -6,10 +6,10 @@
 //   attention_dkv_kernel  CTA = 128 states of a key head: the transposed products, over all rows of all its query
 //                         heads: dv = sum p^T dout, dk = sum ds^T q
 // The price is s and dp computed twice: 8 products instead of 5 (one for ds's second part, see dq).
-// Measured: 32 x 16 heads of 64, 512 rows and states, 228 us; 4 x 16 heads of 128 on 4 key heads, 2048 rows, 4096 states,
-// 1034 us (dkv 470), 590 TFLOP/s of the five products. With ds in one part the tensor pipe was busy 40 % (dq) and 59 % (dkv)
-// of the long case; a tile's chain of products, their latency (about 350 cycles from the issue to the barrier) and the
-// warps' arithmetic is what the other tile covers in part.
+// Measured: 32 x 16 heads of 64, 512 rows and states, bf16 227 us (dq 126, dkv 100), fp16 267 us; 4 x 16 heads of 128 on 4 key
+// heads, 2048 rows, 4096 states, fp16, 1046 us (dq 573, dkv 465), 657 TFLOP/s of the five products. There the tensor pipe is
+// busy 43 % (dq) and 59 % (dkv) of the time, in the first case 21 % and 29 %; a tile's chain of products, their latency (about
+// 350 cycles from the issue to the barrier) and the warps' arithmetic is what the other tile covers in part.
 #include <mutex>
 
 #include "swarm_attention_tile.cuh"

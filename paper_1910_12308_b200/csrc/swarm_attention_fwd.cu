@@ -6,7 +6,7 @@
 // about 2700 cycles of which 2048 are both CTAs' exponentials; 4 x 16 heads, 4096 rows and states, 380 us, 720 TFLOP/s.
 // A part of the exponentials as polynomials on the fp32 pipe gave nothing: a warp's other 600 instructions a step
 // then take as long. Heads of 128: a tile's chain of softmax (1900 cycles), products (1024) and their latency is what
-// two tiles in turn cover to 56 %; 460 us there, 1190 TFLOP/s. Sentences of 128: 22 us for 64 x 16 heads, mostly the
+// two tiles in turn cover to 56 %; 460 us there, 1190 TFLOP/s. Sentences of 128: 25 us for 64 x 16 heads, mostly the
 // CTAs' start and end.
 #include <mutex>
 
@@ -359,7 +359,7 @@ cudaError_t launch_forward(const AttentionArgs& a, const SplitPlan& plan, const 
 // Few row tiles leave multiprocessors idle while each CTA walks all states: these are then split, as far as the CTAs still
 // run at once and four steps or more are left to each, where that saves twelve steps (a step is about 1.4 us, the parts'
 // way through memory and the joining kernel 10 to 15). Measured: 8 heads of 64, 128 rows, 4096 states 42 us whole and 24 in
-// parts, 8 heads of 128, 512 rows 66 and 31; 2 x 8 heads of 64, 300 rows, 1000 states (eight steps) 16 and 25.
+// parts, 8 heads of 128, 512 rows 66 and 26; 2 x 8 heads of 64, 300 rows, 1000 states (eight steps) 16 and 25.
 SplitPlan make_forward_plan(const AttentionArgs& a) {
   SplitPlan p{};
   const int nt = a.head_dim <= 64 ? 1 : 2;
