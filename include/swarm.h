@@ -431,6 +431,8 @@ int swarm_cross_attention(const swarm_attention *desc_host, const void *q_dev, c
 /* dq, dk, dv from dout (the gradient of o), q, k, v and the o and lse of the forward call. dk and dv of a key head
  * are the sums over its query heads, added in a fixed order; p, ds and their products as in the formula
  *   p = exp(s - lse),  dv = p^T dout,  ds = scale * p * (dout v^T - rowsum(dout * o)),  dq = ds k,  dk = ds^T q.
+ * o is taken as it was rounded: where values share a large part, dq of sentences of more than 64 states has the error that this
+ * leaves in rowsum(dout * o); dk has it taken out.
  * s and lse are fp32: p is off by a factor of about exp(2^-23 |lse|), which matters for scores beyond 10^4. p and ds enter
  * their products in dtype; in fp16 ds carries a power of two of its own, so that its size (dout's, over the states) does not matter.
  * Errors: EINVAL (as the forward call; a scale below 2^-120). */
