@@ -69,7 +69,7 @@ enum { SWARM_F32 = 0, SWARM_BF16 = 1, SWARM_F16 = 2 };
 enum {
   SWARM_OK = 0,
   SWARM_EINVAL = -1,  /* bad n, d, bits, mode, H, count, NULL pointer, size mismatch          */
-  SWARM_ERANGE = -2,  /* node id outside [0, n)                                                */
+  SWARM_ERANGE = -2,  /* node id outside [0, n); a page of a cache that does not exist         */
   SWARM_EPAIR  = -3,  /* pairs not disjoint, a == b, or (a, b) not an edge of G                */
   SWARM_ESTATE = -4,  /* e.g. non-blocking mode without base snapshots, local steps without an objective */
   SWARM_ENOMEM = -5,  /* device or host allocation failed                                      */
@@ -441,9 +441,84 @@ int swarm_cross_attention_backward(const swarm_attention *desc_host, const void 
                                    void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,
                                    size_t workspace_bytes, void *cuda_stream);
 
+/* A paged cache of keys and values, for models that answer token by token. Sentence b holds lengths[b] tokens, those of the
+ * call included; its row of the table names the pages that hold them: position p lies in slot p mod page_size of page
+ * table[b][p div page_size]. The call's rows are the sentence's newest n = min(counts[b], lengths[b]) tokens (at most `tokens`,
+ * at least 0): row t < n is position lengths[b] - n + t. Sentences may share pages that no call writes.
+ *   A page number outside [0, pages), or a position past the table's columns, is not followed: such a token is not
+ *   written and not read, and a word is raised that swarm_operator_check reads. Table entries that no token of the call
+ *   needs are not read (what a window has left behind may be given up).
+ *   Tensors are addressed by strides (elements) over sentence (of the cache: page), token (slot) and head; the head_dim
+ *   values of a head are consecutive. */
+typedef struct {
+  int32_t batch, heads, kv_heads, tokens, head_dim;          /* as swarm_attention; tokens: rows of a sentence   */
+  int32_t dtype;                                             /* SWARM_BF16 or SWARM_F16                     */
+  int32_t pages, page_size, table_columns;                   /* >= 0, >= 1, >= 0                            */
+  int32_t rotated, interleaved;                              /* swarm_cache_append only                     */
+  int32_t window, sinks;                                     /* swarm_paged_attention only; >= 0            */
+  float scale;                                               /* swarm_paged_attention only; > 0, finite     */
+  int64_t table_pitch;                                       /* elements between rows of the table, >= table_columns */
+  const int32_t *table_dev, *lengths_dev;                    /* [batch][table_columns], [batch]             */
+  const int32_t *counts_dev;                                 /* [batch]; NULL: `tokens` of every sentence   */
+  swarm_strides k_pages, v_pages;                            /* multiples of 8, > 0; .batch: between pages  */
+  swarm_strides q, out;                                      /* multiples of 8; inputs may repeat sentences or heads by strides of 0 */
+  swarm_strides k, v;                                        /* swarm_cache_append only                     */
+} swarm_paged;
+
+/* Writes the call's keys and values into their pages, the keys rotated by their position p, and the queries rotated likewise to
+ * out_dev. Of each head the first `rotated` values (even, <= head_dim) turn in pairs i, values 2 i and 2 i + 1 if
+ * interleaved, else i and i + rotated / 2, by the angle p * frequencies[i]:
+ *   (x, y) -> (x cos - y sin, y cos + x sin),
+ * the angle taken in 64 bits, each result rounded once. The other values, and v, are copied.
+ *   frequencies_dev: rotated / 2 floats (NULL with rotated 0). q_dev and out_dev may both be NULL (heads is then not
+ *   looked at); out_dev may be q_dev with the same strides. Rows t >= n: out is 0, nothing is written to the cache.
+ *   Places that two tokens of a call share (the same page in two rows of the table) hold either.
+ * Errors: EINVAL (sizes, strides, alignment, NULL). */
+int swarm_cache_append(const swarm_paged *desc_host, const void *k_dev, const void *v_dev, void *k_pages_dev,
+                       void *v_pages_dev, const void *q_dev, void *out_dev, const float *frequencies_dev, void *cuda_stream);
+
+/* Attention of the call's rows, which are in the cache already, over it. The row at position p sees positions j <= p; with a
+ * window w > 0 only those of j > p - w, and the sentence's first `sinks` beside them:
+ *   s = scale * q . k,   lse = log sum_j exp(s_j),   o = sum_j exp(s_j - lse) v_j
+ * over what it sees. Rows t >= n, and rows of which no page can be followed, have o = 0 and lse = -infinity. What the
+ * cache holds in places that a row does not see is not used for it (NaN included).
+ *   tokens <= SWARM_PAGED_MAX_TOKENS (a decoding step, drafts that are checked at once, a short piece of a prompt). lse_dev:
+ *   [batch][heads][tokens] floats, or NULL. Addresses: multiples of 16 bytes. out must not overlap inputs.
+ * Errors: EINVAL (sizes, strides, alignment, scale, NULL, workspace too small). */
+#define SWARM_PAGED_MAX_TOKENS 64
+int swarm_paged_attention_workspace(const swarm_paged *desc_host, size_t *bytes_host);
+int swarm_paged_attention(const swarm_paged *desc_host, const void *q_dev, const void *k_pages_dev, const void *v_pages_dev,
+                          void *out_dev, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
+/* Log probabilities of rows of logits: with x = scale * logits (scale = 1 / temperature) and lse = log sum_j exp(x_j),
+ *   log_probs[r] = x[r][tokens[r]] - lse[r],    entropy[r] = lse - sum_j exp(x_j - lse) x_j,
+ *   top_tokens[r][0 .. top - 1]: the tokens of the largest logits in descending order (equal ones: the lowest first; a NaN
+ *   counts as larger than any number), top_log_probs[r] theirs.
+ * Differences are taken from the row's largest logit before anything is scaled, so large logits cost no accuracy.
+ *   stats[r] = (largest logit, log sum_j exp(scale * (logit_j - largest))), kept for the gradient: lse = scale * stats[0] + stats[1].
+ *   A token outside [0, cols) stands for a padded place: log_probs 0. Logits of -infinity are tokens that are ruled out: they add nothing
+ *   to the entropy. A row of nothing else has log probabilities -infinity and entropy 0. A NaN in a row makes its results NaN.
+ *   rows x cols logits of dtype, consecutive in a row, rows at the given pitch (>= cols). tokens_dev and log_probs_dev
+ *   may both be NULL, entropy_dev too; top_*_dev are needed with top > 0 (<= SWARM_MAX_TOP, <= cols).
+ * Errors: EINVAL (rows < 0, cols < 1, either >= 2^31, pitch, dtype, scale not in (0, inf), top, NULL, alignment). */
+#define SWARM_MAX_TOP 32
+int swarm_token_log_probs(const void *logits_dev, const int64_t *tokens_dev, float *log_probs_dev, float *stats_dev,
+                          float *entropy_dev, float *top_log_probs_dev, int64_t *top_tokens_dev, int64_t rows,
+                          int64_t cols, int64_t pitch, int32_t dtype, float scale, int32_t top, void *cuda_stream);
+/* Gradient with respect to the logits, from those of log_probs and of entropy: with p_j = exp(x_j - lse)
+ *   dlogits_j = scale * (dlog_probs * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy)).
+ *   stats_dev (and entropy_dev, with dentropy_dev) as the forward call returned them. Either of dlog_probs_dev (with tokens_dev)
+ *   and dentropy_dev may be NULL. A row whose token is a padded place has no first part; a row of -infinity has gradient 0.
+ *   dlogits_dev may be logits_dev with the same pitch.
+ * Errors: EINVAL (as the forward call). */
+int swarm_token_log_probs_backward(const float *dlog_probs_dev, const float *dentropy_dev, const void *logits_dev,
+                                   const int64_t *tokens_dev, const float *stats_dev, const float *entropy_dev,
+                                   void *dlogits_dev, int64_t rows, int64_t cols, int64_t pitch, int64_t dlogits_pitch,
+                                   int32_t dtype, float scale, void *cuda_stream);
+
 /* Waits for cuda_stream and returns SWARM_ECUDA (swarm_operator_error() == cudaErrorLaunchTimeout) if a device-side
  * wait of an operator has given up on the current device since the last check (its results are then undefined),
- * or a CUDA error of the stream. */
+ * or a CUDA error of the stream; SWARM_ERANGE if a table named a page that does not exist since then. */
 int swarm_operator_check(void *cuda_stream);
 int swarm_operator_error(void);                            /* cudaError_t of this thread's last SWARM_ECUDA from an operator */
 

@@ -33,6 +33,7 @@ EXPORTS = [
     "swarm_sync", "swarm_set_wait_limit", "swarm_potential_static", "swarm_kernel_launches", "swarm_last_cuda_error", "swarm_strerror", "swarm_destroy",
     "swarm_dropout", "swarm_add_rms_norm", "swarm_add_rms_norm_workspace", "swarm_add_rms_norm_backward",
     "swarm_cross_attention", "swarm_cross_attention_workspace", "swarm_cross_attention_backward",
+    "swarm_cache_append", "swarm_paged_attention_workspace", "swarm_paged_attention", "swarm_token_log_probs", "swarm_token_log_probs_backward",
     "swarm_operator_check", "swarm_operator_error",
 ]
 
@@ -126,6 +127,11 @@ def load():
         "swarm_cross_attention_workspace": (C.c_int, [vp, i32, C.POINTER(C.c_size_t)]),
         "swarm_cross_attention": (C.c_int, [vp] * 7 + [C.c_size_t, vp]),
         "swarm_cross_attention_backward": (C.c_int, [vp] * 11 + [C.c_size_t, vp]),
+        "swarm_cache_append": (C.c_int, [vp] * 9),
+        "swarm_paged_attention_workspace": (C.c_int, [vp, C.POINTER(C.c_size_t)]),
+        "swarm_paged_attention": (C.c_int, [vp] * 7 + [C.c_size_t, vp]),
+        "swarm_token_log_probs": (C.c_int, [vp] * 7 + [i64] * 3 + [i32, f32, i32, vp]),
+        "swarm_token_log_probs_backward": (C.c_int, [vp] * 7 + [i64] * 4 + [i32, f32, vp]),
         "swarm_operator_check": (C.c_int, [vp]),
         "swarm_operator_error": (C.c_int, []),
     }

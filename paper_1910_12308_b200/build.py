@@ -9,7 +9,7 @@ LIB = os.path.join(HERE, "libswarm_b200.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["swarm_api.cu", "swarm_interact.cu", "swarm_local.cu", "swarm_reduce.cu", "swarm_noalloc.cu", "swarm_lsq_tc.cu",
            "swarm_rows.cu", "swarm_attention.cu", "swarm_attention_fwd.cu", "swarm_attention_bwd.cu",
-           "swarm_attention_rows.cu"]
+           "swarm_attention_rows.cu", "swarm_paged.cu", "swarm_paged_attention.cu", "swarm_logprobs.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -498,7 +498,7 @@ const char* swarm_strerror(int code) {
   switch (code) {
     case SWARM_OK: return "ok";
     case SWARM_EINVAL: return "invalid argument";
-    case SWARM_ERANGE: return "node id out of range";
+    case SWARM_ERANGE: return "node id or page out of range";
     case SWARM_EPAIR: return "pairs not disjoint, self-pair, or not an edge of the graph";
     case SWARM_ESTATE: return "call not valid in the current configuration";
     case SWARM_ENOMEM: return "out of memory";

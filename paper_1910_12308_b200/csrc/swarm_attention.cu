@@ -13,11 +13,12 @@ namespace swarm {
 namespace {
 
 constexpr int kMaxDevices = 64;
-static __device__ int g_operator_status;               // raised by a kernel of this device whose wait gave up
+static __device__ int g_operator_status;               // raised by kernels of this device
 int* g_status_addr[kMaxDevices] = {};
 std::mutex g_setup_mutex;
 
-// Device address of the status word of the current device.
+}  // namespace
+
 cudaError_t status_word(int** out) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -33,6 +34,8 @@ cudaError_t status_word(int** out) {
   *out = g_status_addr[dev];
   return cudaSuccess;
 }
+
+namespace {
 
 // Zeros into a strided tensor: the outputs of a call that has no rows or no states to sum over.
 __global__ void __launch_bounds__(256) attention_zero_kernel(uint4* p, swarm_strides s, int tokens, int heads, int chunks) {
@@ -193,6 +196,7 @@ int swarm_operator_check(void* cuda_stream) {
   if (e == cudaSuccess && raised) {
     e = cudaMemsetAsync(word, 0, sizeof raised, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && !(raised & kStatusWait)) return SWARM_ERANGE;
     if (e == cudaSuccess) e = cudaErrorLaunchTimeout;
   }
   return operator_result(e);

@@ -63,6 +63,11 @@ inline void place_parts(const AttentionArgs& a, SplitPlan* p, void* workspace) {
   p->part_o = reinterpret_cast<float*>(workspace);
   p->part_ml = p->part_o + split_parts(a, *p) * a.head_dim;
 }
+// Device address of the current device's word that swarm_operator_check reads (defined in swarm_attention.cu): bit 0, a
+// device-side wait gave up; bit 1, a table named a page that does not exist.
+cudaError_t status_word(int** out);
+constexpr int kStatusWait = 1, kStatusPage = 2;
+
 cudaError_t launch_attention_join(const AttentionArgs& a, const SplitPlan& p, int dtype, cudaStream_t st);
 
 size_t attention_forward_workspace(const AttentionArgs& a);

@@ -425,7 +425,7 @@ attention_dq_kernel(const __grid_constant__ TileMap mq, const __grid_constant__ 
       }
     }
   }
-  if (!ok) atomicExch(a.status, 1);
+  if (!ok) atomicOr(a.status, kStatusWait);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);
@@ -801,7 +801,7 @@ attention_dkv_kernel(const __grid_constant__ TileMap mq, const __grid_constant__
       }
     }
   }
-  if (!ok) atomicExch(a.status, 1);
+  if (!ok) atomicOr(a.status, kStatusWait);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NW + 1) tmem_dealloc(tmem, Shape::kColumns);

@@ -320,7 +320,7 @@ attention_forward_kernel(const __grid_constant__ TileMap mq, const __grid_consta
       }
     }
   }
-  if (!ok) atomicExch(a.status, 1);
+  if (!ok) atomicOr(a.status, kStatusWait);
   tc_fence_before();
   __syncthreads();
   if (warp == 4 * NT + 1) tmem_dealloc(tmem, Shape::kColumns);

@@ -1,4 +1,5 @@
-"""Operators of the models that the nodes train: dropout, residual root-mean-square norm, cross attention.
+"""Operators of the models that the nodes train: dropout, residual root-mean-square norm, cross attention; and of the same
+models as they answer token by token: a paged cache of keys and values, attention over it, log probabilities of tokens.
 
 Bindings of the C entry points of the same names (include/swarm.h says what each computes): checks of torch tensors,
 allocation of outputs and scratch through torch, the current stream. Forward and backward are separate calls; nothing
@@ -10,6 +11,7 @@ at through the cheapest attributes that say enough, contiguous ones first.
 """
 import ctypes as C
 import struct
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -18,6 +20,8 @@ from . import binding as _b
 _DTYPES = {torch.float32: _b.F32, torch.bfloat16: _b.BF16, torch.float16: _b.F16}
 _DESC = struct.Struct("=7ifq2Q24q")                        # swarm_attention: 8 tensors of 3 strides at the end
 _NO_GRADS = (0,) * 12
+_PAGED = struct.Struct("=13ifq3Q18q")                       # swarm_paged: 6 tensors of 3 strides at the end
+_NO_STRIDES = (0,) * 3
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -262,7 +266,180 @@ def cross_attention_backward(do, q, k, v, o, lse, scale=None, query_lengths=None
     return dq, dk, dv
 
 
+def _paged_desc(device, heads, x, x_name, k_pages, v_pages, table, lengths, counts, rotated, interleaved, window, sinks, scale,
+                strides):
+    """Descriptor of a call on x [batch, tokens, ., head_dim]; `strides` are those of q, out, k and v."""
+    dtype, whole, pages = x.dtype, x.shape, k_pages.shape
+    if dtype != torch.bfloat16 and dtype != torch.float16:
+        raise ValueError(f"{x_name}: bfloat16 or float16 is needed, got {dtype}")
+    if len(whole) != 4 or len(pages) != 4 or pages[3] != whole[3]:
+        raise ValueError(f"{x_name}, k_pages: [batch, tokens, heads, head_dim] and [pages, page_size, kv_heads, head_dim] are "
+                         f"needed, got {tuple(whole)} and {tuple(pages)}")
+    cache = (*_heads(k_pages, "k_pages", device, dtype, pages), *_heads(v_pages, "v_pages", device, dtype, pages))
+    batch = whole[0]
+    _same(table, "table", device, torch.int32)
+    if table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table: int32 [batch, columns] is needed, each row consecutive")
+    columns = table.shape[1]
+    pitch = table.stride(0) if batch > 1 else columns
+    if lengths is None:
+        raise ValueError("lengths: one int32 for each sentence is needed")
+    try:
+        return _PAGED.pack(batch, heads, pages[2], whole[1], whole[3], _DTYPES[dtype], pages[0], pages[1], columns,
+                           rotated, 1 if interleaved else 0, window, sinks, scale, pitch, table.data_ptr(),
+                           _lengths(lengths, "lengths", device, batch), _lengths(counts, "counts", device, batch), *cache, *strides)
+    except (struct.error, OverflowError) as err:
+        raise ValueError(f"sizes, window, sinks or scale: {err}") from None
+
+
+def append_to_cache(k, v, k_pages, v_pages, table, lengths, counts=None, q=None, frequencies=None, interleaved=False, out=None):
+    """Writes k, v [batch, tokens, kv_heads, head_dim] into the cache, k rotated by its position, and returns q
+    [batch, tokens, heads, head_dim] rotated likewise (None without q).
+
+    k_pages, v_pages: [pages, page_size, kv_heads, head_dim], any strides that are multiples of 8 elements. table: int32
+    [batch, columns] page numbers. lengths: int32 [batch], tokens of each sentence with these; counts: int32 [batch], how
+    many of `tokens` are a sentence's (None: all). frequencies: float32 [rotated / 2], angle of each pair per position;
+    None: nothing is rotated. Pairs are (i, i + rotated / 2), with `interleaved` neighbours. `out` may be q. Rows past a
+    sentence's count are not written to the cache, and zeros in what is returned."""
+    device = _device(k, "k")
+    rotated = 0
+    if frequencies is not None:
+        _same(frequencies, "frequencies", device, torch.float32)
+        if frequencies.dim() != 1 or not frequencies.is_contiguous():
+            raise ValueError("frequencies: consecutive values are needed")
+        rotated = 2 * frequencies.shape[0]
+    shape = k.shape
+    if len(shape) != 4 or k_pages.dim() != 4 or shape[2] != k_pages.shape[2]:
+        raise ValueError(f"k, k_pages: [batch, tokens, kv_heads, head_dim] and [pages, page_size, kv_heads, head_dim] are needed, "
+                         f"got {tuple(shape)} and {tuple(k_pages.shape)}")
+    strides = (*_heads(k, "k", device, k.dtype, shape), *_heads(v, "v", device, k.dtype, shape))
+    if q is None:
+        if out is not None:
+            raise ValueError("out: there is no q to rotate")
+        heads, pq, po, strides = shape[2], None, None, (*_NO_STRIDES, *_NO_STRIDES, *strides)
+    else:
+        if not isinstance(q, torch.Tensor) or q.dim() != 4:
+            raise ValueError("q: [batch, tokens, heads, head_dim] is needed")
+        heads = q.shape[2]
+        out = _empty(q) if out is None else out
+        whole = (shape[0], shape[1], heads, shape[3])
+        strides = (*_heads(q, "q", device, k.dtype, whole), *_heads(out, "out", device, k.dtype, whole), *strides)
+        pq, po = q.data_ptr(), out.data_ptr()
+        if pq == po and strides[0:3] != strides[3:6]:
+            raise ValueError("out: of other strides than q at the same place")
+    desc = _paged_desc(device, heads, k, "k", k_pages, v_pages, table, lengths, counts, rotated, interleaved, 0, 0, 1.0, strides)
+    _check(_b.load().swarm_cache_append(desc, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), pq, po,
+                                        frequencies.data_ptr() if rotated else None, _raw_stream(device)), "swarm_cache_append")
+    return out
+
+
+def paged_attention(q, k_pages, v_pages, table, lengths, counts=None, scale=None, window=0, sinks=0, need_lse=False, out=None):
+    """o (or (o, lse) with `need_lse`) of the newest tokens q [batch, tokens, heads, head_dim] over the cache, which holds their
+    keys and values already (append_to_cache says how it is laid out). A token sees itself and what came before it; with a
+    window w > 0 the last w of these (itself included) and the sentence's first `sinks`. tokens is at most 64: a
+    decoding step, drafts that are checked at once, a piece of a prompt. scale: 1 / sqrt(head_dim) unless given. lse:
+    [batch, heads, tokens]. Rows past a sentence's count are 0, with lse -infinity."""
+    device = _device(q, "q")
+    if q.dim() != 4:
+        raise ValueError(f"q: [batch, tokens, heads, head_dim] is needed, got {tuple(q.shape)}")
+    if out is None:
+        out = _empty(q)
+    whole = q.shape
+    if whole[3] == 0:
+        raise ValueError("q: head_dim is 0")
+    strides = (*_heads(q, "q", device, q.dtype, whole), *_heads(out, "out", device, q.dtype, whole), *_NO_STRIDES, *_NO_STRIDES)
+    desc = _paged_desc(device, whole[2], q, "q", k_pages, v_pages, table, lengths, counts, 0, 0, 0 if window is None else window, sinks,
+                       whole[3] ** -0.5 if scale is None else scale, strides)
+    L = _b.load()
+    lse = q.new_empty((whole[0], whole[2], whole[1]), dtype=torch.float32) if need_lse else None
+    size = C.c_size_t()
+    _check(L.swarm_paged_attention_workspace(desc, C.byref(size)), "swarm_paged_attention_workspace")
+    n = size.value
+    work = q.new_empty((n,), dtype=torch.uint8) if n else None
+    _check(L.swarm_paged_attention(desc, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
+                                   lse.data_ptr() if need_lse else None, work.data_ptr() if n else None, n,
+                                   _raw_stream(device)), "swarm_paged_attention")
+    return (out, lse) if need_lse else out
+
+
+class TokenLogProbs(NamedTuple):
+    """What token_log_probs returns; None where it was not asked for."""
+    log_probs: Optional[torch.Tensor]                      # float32, of the given tokens
+    stats: torch.Tensor                                    # float32 [..., 2]: largest logit, log of the sum; for the gradient
+    entropy: Optional[torch.Tensor]                        # float32
+    top_log_probs: Optional[torch.Tensor]                  # float32 [..., top], in descending order
+    top_tokens: Optional[torch.Tensor]                     # int64 [..., top]
+
+
+def _tokens(tokens, device, lead):
+    if tokens is None:
+        return None
+    _same(tokens, "tokens", device, torch.int64)
+    if tokens.shape != lead or not tokens.is_contiguous():
+        raise ValueError(f"tokens: contiguous {tuple(lead)} is needed, got {tuple(tokens.shape)}")
+    return tokens.data_ptr()
+
+
+def _row_floats(x, name, device, shape):
+    if x is None:
+        return None
+    _same(x, name, device, torch.float32)
+    if x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name}: contiguous {tuple(shape)} is needed, got {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def token_log_probs(logits, tokens=None, scale=1.0, top=0, entropy=False):
+    """TokenLogProbs of the distributions softmax(scale * logits) over the last dimension (scale: 1 / temperature): log
+    probabilities of `tokens` (int64, one for each row; outside the vocabulary: a padded place, log probability 0), with `entropy`
+    the entropies, with `top` (at most 32) the likeliest tokens, equal ones in ascending order."""
+    device = _device(logits, "logits")
+    dtype = _dtype(logits, "logits")
+    px, rows, cols, pitch = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    pt = _tokens(tokens, device, lead)
+    if not isinstance(top, int) or not 0 <= top <= 32 or top > cols:
+        raise ValueError("top: between 0 and 32, and not more than the vocabulary")
+    new = {"dtype": torch.float32, "device": device}
+    log_probs = torch.empty(lead, **new) if tokens is not None else None
+    stats = torch.empty((*lead, 2), **new)
+    spread = torch.empty(lead, **new) if entropy else None
+    best = torch.empty((*lead, top), **new) if top else None
+    which = torch.empty((*lead, top), dtype=torch.int64, device=device) if top else None
+    _check(_b.load().swarm_token_log_probs(px, pt, log_probs.data_ptr() if pt is not None else None, stats.data_ptr(),
+                                           spread.data_ptr() if entropy else None, best.data_ptr() if top else None,
+                                           which.data_ptr() if top else None, rows, cols, pitch, dtype, scale, top,
+                                           _raw_stream(device)), "swarm_token_log_probs")
+    return TokenLogProbs(log_probs, stats, spread, best, which)
+
+
+def token_log_probs_backward(dlog_probs, logits, tokens, stats, entropy=None, dentropy=None, scale=1.0, dlogits=None):
+    """The gradient of the logits from those of log_probs (None: none) and of the entropies, at what the forward call took and
+    returned. `dlogits` may be given, logits itself included."""
+    device = _device(logits, "logits")
+    dtype = _dtype(logits, "logits")
+    px, rows, cols, pitch = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    if dlog_probs is not None and tokens is None:
+        raise ValueError("tokens: the tokens of the forward call are needed with dlog_probs")
+    if dentropy is not None and entropy is None:
+        raise ValueError("entropy: the entropies of the forward call are needed with dentropy")
+    if stats is None:
+        raise ValueError("stats: what the forward call returned is needed")
+    pg, ph = _row_floats(dlog_probs, "dlog_probs", device, lead), _row_floats(dentropy, "dentropy", device, lead)
+    ps, pe = _row_floats(stats, "stats", device, (*lead, 2)), _row_floats(entropy, "entropy", device, lead)
+    if dlogits is None:
+        dlogits = _empty(logits)
+    po, out_pitch = _like(dlogits, "dlogits", device, logits, cols)
+    if po == px and out_pitch != pitch and rows > 1:
+        raise ValueError("dlogits: of another pitch than logits at the same place")
+    _check(_b.load().swarm_token_log_probs_backward(pg, ph, px, _tokens(tokens, device, lead), ps, pe, po, rows, cols, pitch,
+                                                    pitch if po == px else out_pitch, dtype, scale, _raw_stream(device)),
+           "swarm_token_log_probs_backward")
+    return dlogits
+
+
 def check():
-    """Waits for the current stream; raises SwarmError if a device-side wait of an operator has given up since the
-    last check, or the stream holds a CUDA error."""
+    """Waits for the current stream; raises SwarmError if a device-side wait of an operator has given up, or a table named a page
+    that does not exist, since the last check, or the stream holds a CUDA error."""
     _check(_b.load().swarm_operator_check(torch.cuda.current_stream().cuda_stream), "swarm_operator_check")
