@@ -483,7 +483,7 @@ int swarm_cache_append(const swarm_paged *desc_host, const void *k_dev, const vo
  * over what it sees. Rows t >= n, and rows of which no page can be followed, have o = 0 and lse = -infinity. What the
  * cache holds in places that a row does not see is not used for it (NaN included).
  *   tokens <= SWARM_PAGED_MAX_TOKENS (a decoding step, drafts that are checked at once, a short piece of a prompt). lse_dev:
- *   [batch][heads][tokens] floats, or NULL. Addresses: multiples of 16 bytes. out must not overlap inputs.
+ *   [batch][heads][tokens] floats, or NULL. Addresses: multiples of 16 bytes. out must not overlap inputs. batch * heads < 2^25.
  * Errors: EINVAL (sizes, strides, alignment, scale, NULL, workspace too small). */
 #define SWARM_PAGED_MAX_TOKENS 64
 int swarm_paged_attention_workspace(const swarm_paged *desc_host, size_t *bytes_host);

@@ -76,7 +76,8 @@ bool desc_ok(const swarm_paged* d) {
 }
 bool heads_ok(const swarm_paged* d) { return d->heads >= 1 && d->heads <= 65535 && d->heads % d->kv_heads == 0; }
 bool attention_ok(const swarm_paged* d) {
-  return desc_ok(d) && heads_ok(d) && d->tokens <= SWARM_PAGED_MAX_TOKENS && d->window >= 0 && d->sinks >= 0 && d->scale > 0.0f && std::isfinite(d->scale);
+  return desc_ok(d) && heads_ok(d) && d->tokens <= SWARM_PAGED_MAX_TOKENS &&
+         (int64_t)d->batch * d->heads * SWARM_PAGED_MAX_TOKENS < (int64_t)1 << 31 && d->window >= 0 && d->sinks >= 0 && d->scale > 0.0f && std::isfinite(d->scale);
 }
 
 void fill(PagedArgs& a, const swarm_paged* d) {

@@ -69,7 +69,7 @@ def test_paged_attention_refusals():
     def call(d, q=P, kp=P, vp=P, out=P, lse=None, work=P, size=1 << 40):
         return L.swarm_paged_attention(d, q, kp, vp, out, lse, work, size, None)
 
-    for bad in BAD_DESCRIPTORS + [dict(tokens=65), dict(window=-1), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0),
+    for bad in BAD_DESCRIPTORS + [dict(tokens=65), dict(batch=8192, heads=4096), dict(window=-1), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0),
                                   dict(scale=float("inf")), dict(scale=float("nan"))]:
         assert call(desc(**bad)) == g.EINVAL, bad
     for bad in (dict(q=None), dict(kp=None), dict(vp=None), dict(out=None), dict(lse=P + 2), dict(q=P + 8), dict(kp=P + 8), dict(vp=P + 2),
