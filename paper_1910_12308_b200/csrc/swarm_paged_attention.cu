@@ -4,8 +4,9 @@
 // The blocks of all items in a row are dealt to the device's warps in equal runs, whatever the sentences' lengths: a warp may end
 // one item, take several whole ones and begin another. Each warp works alone: a ring of blocks that cp.async fills
 // past the ends of items, so that loads never pause (about 170 KB in flight on a multiprocessor), ldmatrix, m16n8k16 products with
-// the running maximum and sum of the softmax in registers. Items that were cut leave their parts (maximum, sum, o) in
-// the workspace, and a second kernel, whose launch overlaps the first one's end, adds them in order.
+// the running maximum and sum of the softmax in registers. An item that was cut leaves parts (maximum, sum, o): those of
+// a CTA's warps, whose runs follow one another, are joined at the CTA's end, those of several CTAs by a second kernel, whose
+// launch overlaps the first one's end; always in the items' order.
 //
 // Weights enter their product as the sum of two numbers of the type: rounded once, o would be 1.4 times as far from its value as
 // its own rounding leaves it. The products are a small part of a block's time, so the second costs nothing.
@@ -38,9 +39,11 @@ struct PagedPlan {
   int32_t whole;                      // items are not cut
   int32_t ctas;
   int32_t join_warps;                 // for each row
+  uint32_t page_multiplier, page_shift;                 // division by the size of a page
   int64_t* prefix;                    // [batch + 1] blocks of the items before a sentence's
-  float* part_ml;                     // [2 warps][rows][2] maximum and sum
-  float* part_o;                      // [2 warps][rows][head_dim]
+  // parts of the warps, two each, then of the CTAs
+  float* part_ml;                     // [parts][rows][2] maximum and sum
+  float* part_o;                      // [parts][rows][head_dim]
 };
 
 // What a sentence's rows see, in blocks: the first `sink_blocks`, then those from position lo / 16 * 16.
@@ -62,16 +65,17 @@ __device__ __forceinline__ int64_t blocks_of_items(const PagedArgs& a, const Sen
   return (int64_t)s.blocks * a.kv_heads * s.row_groups;
 }
 
-// The runs that `total` blocks are dealt in: the first `more` warps of `warps` have each + 1.
+// The runs that `total` blocks are dealt in: `warps` runs, `per_cta` of them in each CTA, the first `more` one block longer.
 struct Runs {
   int64_t each, more;
-  int warps;
-  __device__ __forceinline__ Runs(int64_t total, int all) {
-    warps = (int)max((int64_t)1, min((int64_t)all, total / kMinShare));
+  int warps, per_cta;
+  __device__ __forceinline__ Runs(int64_t total, int ctas) {
+    warps = (int)max((int64_t)1, min((int64_t)ctas * kWarps, total / kMinShare));
+    per_cta = (warps + ctas - 1) / ctas;                // few runs go to many multiprocessors
     each = total / warps;
     more = total % warps;
   }
-  __device__ __forceinline__ int64_t begin(int w) const { return w >= warps ? warps * each + more : w * each + min((int64_t)w, more); }
+  __device__ __forceinline__ int64_t begin(int w) const { return w * each + min((int64_t)w, more); }
   __device__ __forceinline__ int owner(int64_t x) const {
     const int64_t wide = more * (each + 1);
     return (int)(x < wide ? x / (each + 1) : more + (x - wide) / each);
@@ -98,27 +102,61 @@ template <typename T> __device__ __forceinline__ bool not_finite(uint32_t w) {
 }
 
 // A block in the ring: what it is of, and which of its positions were read.
-struct BlockInfo {
-  int32_t b, item, position;          // item: key head * row_groups(sentence) + group of rows
+struct __align__(16) BlockInfo {
+  int32_t b, head, row0, n;           // sentence, key head, first row of the item; the sentence's rows are n tokens'
+  int32_t position;
+  int32_t first_new;                  // position of the first row: what lies past it, not every row sees
+  int32_t last_gone;                  // what lies before it, the last row does not see
   uint32_t flags;                     // bits 0..15: the position is there
 };
 constexpr uint32_t kFirst = 1u << 16, kLast = 2u << 16, kFromStart = 4u << 16, kToEnd = 8u << 16, kNone = 16u << 16;
 
-template <typename T, int DB>
+// Parts of a cut item that a warp holds: the run's first item may have begun elsewhere (0), its last one may go on (1).
+struct __align__(16) PartInfo {
+  int32_t there, b, head, row0, n, to_end;
+};
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= kBlock ? 0xFFFFu : (1u << n) - 1u; }
+
+// Two parts of a row joined: maximum and sum, and the factors of their o.
+__device__ __forceinline__ void join_ml(float& m, float& l, float m1, float l1, float c, float& f0, float& f1) {
+  const float top = fmaxf(m, m1), base = top == -INFINITY ? 0.0f : top;
+  f0 = ex2((m - base) * c);
+  f1 = ex2((m1 - base) * c);
+  l = l * f0 + l1 * f1;
+  m = top;
+}
+
+// Four values of a row from its sum, and its lse.
+template <typename T>
+__device__ __forceinline__ void write_row(const PagedArgs& a, int b, int t, int h, int lane, float m, float l, const float v[4]) {
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  if (lane * 4 < a.head_dim)
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4) =
+        l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
+  if (a.lse && lane == 0)
+    a.lse[((int64_t)b * a.heads + h) * a.tokens + t] = l != 0.0f ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
+}
+
+// ONE_PAGE: pages hold a multiple of 16 positions, so a block lies in one. Then its page is the same number in every lane and
+// a row's address is one addition away from the last one's; else each position has its own, and a lane gets them by shuffles.
+template <typename T, int DB, bool ONE_PAGE>
 __global__ void __launch_bounds__(kWarps * 32, Shape<DB>::kCtasPerSm)
 paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   using S = Shape<DB>;
   constexpr int kStages = S::kStages, kChunks = DB * 8, kRowsPerCopy = 32 / kChunks;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ BlockInfo s_info[kWarps][kStages];
+  __shared__ PartInfo s_part[kWarps][2];
   __shared__ int64_t s_prefix[kWarps * 32 + 1];
   __shared__ int64_t s_warp[kWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3, chunks = a.head_dim / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (lane < 2) s_part[warp][lane].there = 0;
 
   // rows past a sentence's count
   for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    const int n = rows_in(a, b, length_in(a, b)), chunks = a.head_dim / 8;
+    const int n = rows_in(a, b, length_in(a, b));
     for (int i = tid; i < (a.tokens - n) * a.heads * chunks; i += kWarps * 32) {
       const int ch = i % chunks, h = i / chunks % a.heads, t = n + i / chunks / a.heads;
       *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + ch * 8) = make_uint4(0, 0, 0, 0);
@@ -126,15 +164,15 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     }
   }
 
-  // this warp's run: warps of a multiprocessor are far apart, so that few runs go to many multiprocessors
-  const int all = gridDim.x * kWarps, w = warp * gridDim.x + blockIdx.x;
-  int b = 0, hk = 0, rg = 0, block = 0;
+  // this warp's run
+  int b = 0, hk = 0, rg = 0, block = 0, w = 0;
   int64_t left = 0, item_end = 0;                       // blocks to take; past the last item, where items are not cut
   Sentence s;
   if (plan.whole) {
     const int64_t each = a.kv_heads * (int64_t)plan.row_groups, items = a.batch * each;
-    const int64_t per = items / all, more = items % all, item = w * per + min((int64_t)w, more);
-    item_end = item + per + (w < more);
+    const int all = gridDim.x * kWarps, turn = warp * gridDim.x + blockIdx.x;          // few items go to many multiprocessors
+    const int64_t per = items / all, more = items % all, item = turn * per + min((int64_t)turn, more);
+    item_end = item + per + (turn < more);
     b = (int)(item / each); hk = (int)(item % each) / plan.row_groups; rg = (int)(item % plan.row_groups);
     left = item < item_end;
     if (left) s = sentence_of(a, b);
@@ -160,9 +198,11 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       if (b1 == a.batch && b0 < b1) plan.prefix[a.batch] = at;
     }
     __syncthreads();
-    const Runs runs(s_prefix[kWarps * 32], all);
-    const int64_t begin = runs.begin(w);
-    left = runs.begin(w + 1) - begin;
+    const Runs runs(s_prefix[kWarps * 32], gridDim.x);
+    w = blockIdx.x * runs.per_cta + warp;
+    const bool takes = warp < runs.per_cta && w < runs.warps;
+    const int64_t begin = takes ? runs.begin(w) : 0;
+    left = takes ? runs.begin(w + 1) - begin : 0;
     if (left > 0) {
       int lo = 0, hi = kWarps * 32;                     // the slice of sentences that holds the run's first block
       while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (s_prefix[mid] <= begin) lo = mid; else hi = mid; }
@@ -192,48 +232,81 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   };
   if (left > 0) skip();
 
-  const int page_size = a.page_size, chunks = a.head_dim / 8;
-  auto position = [&]() { return (block < s.sink_blocks ? block : block - s.sink_blocks + s.lo / kBlock) * kBlock; };
-  int page = -1;                                        // lane i < 16: page of position i of the next block, looked up a block ahead
+  // the next block: its position, and its page (ONE_PAGE) or lane i < 16 that of its position i, looked up a block ahead
+  int p0 = 0, page = -1, slot = 0;
   auto look_up = [&]() {
     page = -1;
-    if (left > 0 && lane < kBlock) {
-      const int p = position() + lane, column = p / page_size;
-      if (p < s.length && (p >= s.lo || p < a.sinks) && column < a.table_columns) page = a.table[b * a.table_pitch + column];
-    }
+    if (left <= 0) return;
+    p0 = (block < s.sink_blocks ? block : block - s.sink_blocks + s.lo / kBlock) * kBlock;
+    const int p = ONE_PAGE ? p0 : p0 + (lane & (kBlock - 1));
+    const int column = (int)((__umulhi((uint32_t)p, plan.page_multiplier) + (uint32_t)p) >> plan.page_shift);
+    slot = p - column * a.page_size;
+    if (column < a.table_columns && (ONE_PAGE || (p < s.length && (p >= s.lo || p < a.sinks)))) page = a.table[b * a.table_pitch + column];
   };
   look_up();
 
   uint8_t* ring = smem + warp * kStages * 2 * S::kTileBytes;
+  const int row_of_lane = lane / kChunks, c_of_lane = lane % kChunks;
+  uint32_t spot[kBlock / kRowsPerCopy];                 // where a lane's pieces of a tile go
+#pragma unroll
+  for (int i = 0; i < kBlock / kRowsPerCopy; ++i) spot[i] = smem_u32(ring) + tile_offset<DB>(i * kRowsPerCopy + row_of_lane, c_of_lane);
   // starts the copies of the next block, and moves on
   auto fetch = [&](int stage) {
     if (left > 0) {
-      const int p0 = position(), p = p0 + lane;
-      const bool wanted = lane < kBlock && p < s.length && (p >= s.lo || p < a.sinks), there = (uint32_t)page < (uint32_t)a.pages;
-      if (wanted && !there) atomicOr(a.status, kStatusPage);
-      const uint32_t present = __ballot_sync(0xFFFFFFFFu, wanted && there);
-      const int slot = lane < kBlock ? p % page_size : 0;
-      const uint32_t dst = smem_u32(ring) + stage * 2 * S::kTileBytes;
-      const T* kb = reinterpret_cast<const T*>(a.k_pages) + hk * a.kps.head;
-      const T* vb = reinterpret_cast<const T*>(a.v_pages) + hk * a.vps.head;
-      const int c = lane % kChunks;
-#pragma unroll
-      for (int i = 0; i < kBlock / kRowsPerCopy; ++i) {
-        const int r = i * kRowsPerCopy + lane / kChunks;
-        const int pg = __shfl_sync(0xFFFFFFFFu, page, r), sl = __shfl_sync(0xFFFFFFFFu, slot, r);
-        const bool copy = (present >> r & 1u) && c < chunks;
-        const T *ks = reinterpret_cast<const T*>(a.q), *vs = ks;             // nothing is read there
-        if (copy) {
-          ks = kb + pg * a.kps.batch + sl * a.kps.token + c * 8;
-          vs = vb + pg * a.vps.batch + sl * a.vps.token + c * 8;
+      const uint32_t dst = stage * 2 * S::kTileBytes;
+      const bool there = (uint32_t)page < (uint32_t)a.pages;
+      uint32_t present = 0xFFFFu;                       // wanted by some row
+      if (p0 < s.lo || p0 > s.length - kBlock) present = low_bits(s.length - p0) & (~low_bits(s.lo - p0) | low_bits(a.sinks - p0));
+      if constexpr (ONE_PAGE) {
+        if (!there) {
+          if (lane == 0 && present) atomicOr(a.status, kStatusPage);
+          present = 0;
         }
-        cp_async16_or_zero(dst + tile_offset<DB>(r, c), ks, copy);
-        cp_async16_or_zero(dst + S::kTileBytes + tile_offset<DB>(r, c), vs, copy);
+        const T* kp = reinterpret_cast<const T*>(a.k_pages) + hk * a.kps.head + page * a.kps.batch + (slot + row_of_lane) * a.kps.token + c_of_lane * 8;
+        const T* vp = reinterpret_cast<const T*>(a.v_pages) + hk * a.vps.head + page * a.vps.batch + (slot + row_of_lane) * a.vps.token + c_of_lane * 8;
+        const int64_t kstep = kRowsPerCopy * a.kps.token, vstep = kRowsPerCopy * a.vps.token;
+        if (present == 0xFFFFu && chunks == kChunks) {
+#pragma unroll
+          for (int i = 0; i < kBlock / kRowsPerCopy; ++i) {
+            cp_async16(spot[i] + dst, kp);
+            cp_async16(spot[i] + dst + S::kTileBytes, vp);
+            kp += kstep;
+            vp += vstep;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kBlock / kRowsPerCopy; ++i) {
+            const bool copy = (present >> (i * kRowsPerCopy + row_of_lane) & 1u) && c_of_lane < chunks;
+            const void* none = a.q;                     // nothing is read there
+            cp_async16_or_zero(spot[i] + dst, copy ? kp : none, copy);
+            cp_async16_or_zero(spot[i] + dst + S::kTileBytes, copy ? vp : none, copy);
+            kp += kstep;
+            vp += vstep;
+          }
+        }
+      } else {
+        const bool wanted = lane < kBlock && (present >> lane & 1u);
+        if (wanted && !there) atomicOr(a.status, kStatusPage);
+        present = __ballot_sync(0xFFFFFFFFu, wanted && there);
+        const int64_t ko = page * a.kps.batch + slot * a.kps.token, vo = page * a.vps.batch + slot * a.vps.token;
+        const T* kb = reinterpret_cast<const T*>(a.k_pages) + hk * a.kps.head + c_of_lane * 8;
+        const T* vb = reinterpret_cast<const T*>(a.v_pages) + hk * a.vps.head + c_of_lane * 8;
+#pragma unroll
+        for (int i = 0; i < kBlock / kRowsPerCopy; ++i) {
+          const int r = i * kRowsPerCopy + row_of_lane;
+          const int64_t kr = __shfl_sync(0xFFFFFFFFu, ko, r), vr = __shfl_sync(0xFFFFFFFFu, vo, r);
+          const bool copy = (present >> r & 1u) && c_of_lane < chunks;
+          const void* none = a.q;
+          cp_async16_or_zero(spot[i] + dst, copy ? kb + kr : none, copy);
+          cp_async16_or_zero(spot[i] + dst + S::kTileBytes, copy ? vb + vr : none, copy);
+        }
       }
       const bool ends = block + 1 == s.blocks, last = ends || (!plan.whole && left == 1);
       if (lane == 0) {
         BlockInfo info;
-        info.b = b; info.item = hk * s.row_groups + rg; info.position = p0;
+        info.b = b; info.head = hk; info.row0 = rg * kRows; info.n = s.n; info.position = p0;
+        info.first_new = s.length - s.n;
+        info.last_gone = a.window > 0 ? s.length - a.window : 0;
         info.flags = present | (fresh ? kFirst : 0u) | (fresh && block == 0 ? kFromStart : 0u) | (last ? kLast : 0u) | (ends ? kToEnd : 0u);
         s_info[warp][stage] = info;
       }
@@ -257,8 +330,10 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   uint32_t q[DB * 4][4];                                // operands of the products with the keys
   float o[DB * 8][4], m[2], l[2];
   const float c = a.scale * kLog2e;
-  int first_new = 0, see_all = 0, last_gone = 0, t_of[2] = {0, 0};     // of the item, see below
+  int t_of[2] = {0, 0};
   bool from_start = false;
+  // a lane's addresses for ldmatrix: keys, 8 positions x 8 values four times; values likewise, transposed
+  const int key_row = (lane & 7) + (lane >> 4) * 8, key_half = lane >> 3 & 1, value_row = lane & 15, value_half = lane >> 4;
   for (int stage = 0;; stage = stage + 1 == kStages ? 0 : stage + 1) {
     cp_async_wait<kStages - 2>();
     __syncwarp();
@@ -266,20 +341,16 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     const BlockInfo info = s_info[warp][stage];
     if (info.flags & kNone) break;
     if (info.flags & kFirst) {
-      const Sentence it = sentence_of(a, info.b);
-      const int head = info.item / it.row_groups, row0 = info.item % it.row_groups * kRows;
-      first_new = it.length - it.n;                     // the first row's position: what lies past it, not every row sees
-      last_gone = a.window > 0 ? it.length - a.window : 0;              // what lies before it, the last row does not see
       from_start = info.flags & kFromStart;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int r = row0 + r8 + 8 * u, t = r / a.group;
+        const int r = info.row0 + r8 + 8 * u, t = r / a.group;
         t_of[u] = t;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const T*>(a.q) + offset_of(a.qs, info.b, t, head * a.group + r % a.group)) + c4;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const T*>(a.q) + offset_of(a.qs, info.b, t, info.head * a.group + r % a.group)) + c4;
 #pragma unroll
         for (int ks = 0; ks < DB * 4; ++ks)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) q[ks][u + 2 * e] = t < it.n && ks * 2 + e < chunks ? src[ks * 8 + e * 4] : 0u;
+          for (int e = 0; e < 2; ++e) q[ks][u + 2 * e] = t < info.n && ks * 2 + e < chunks ? src[ks * 8 + e * 4] : 0u;
         m[u] = -INFINITY;
         l[u] = 0.0f;
       }
@@ -294,15 +365,15 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
     for (int ks = 0; ks < DB * 4; ++ks) {
       uint32_t k[4];                                    // positions 0..7, values 0..7 and 8..15 of sixteen; positions 8..15
-      ldmatrix4(tile_k + tile_offset<DB>((lane & 7) + (lane >> 4) * 8, ks * 2 + (lane >> 3 & 1)), k);
+      ldmatrix4(tile_k + tile_offset<DB>(key_row, ks * 2 + key_half), k);
       mma16816<T>(sc[0], q[ks], k[0], k[1]);
       mma16816<T>(sc[1], q[ks], k[2], k[3]);
     }
     // some position of the block is hidden from some row
-    const bool edge = (info.flags & 0xFFFFu) != 0xFFFFu || info.position + (kBlock - 1) > first_new ||
-                      (a.window > 0 && info.position < last_gone && info.position + (kBlock - 1) >= a.sinks);
+    const bool edge = (info.flags & 0xFFFFu) != 0xFFFFu || info.position + (kBlock - 1) > info.first_new ||
+                      (a.window > 0 && info.position < info.last_gone && info.position + (kBlock - 1) >= a.sinks);
     auto sees = [&](int p, int t) {
-      const int own = first_new + t;
+      const int own = info.first_new + t;
       return p <= own && (a.window == 0 || p > own - a.window || p < a.sinks);
     };
     if (edge) {
@@ -353,9 +424,8 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     if (edge && a.tokens > 1) {
       bool bad = false;
 #pragma unroll
-      for (int i = 0; i < kBlock * kChunks / 32; ++i) {
-        const int r = i * kRowsPerCopy + lane / kChunks;
-        const uint4 x = *reinterpret_cast<const uint4*>(ring + stage * 2 * S::kTileBytes + S::kTileBytes + tile_offset<DB>(r, lane % kChunks));
+      for (int i = 0; i < kBlock / kRowsPerCopy; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(ring + stage * 2 * S::kTileBytes + S::kTileBytes + tile_offset<DB>(i * kRowsPerCopy + row_of_lane, c_of_lane));
         bad |= not_finite<T>(x.x) || not_finite<T>(x.y) || not_finite<T>(x.z) || not_finite<T>(x.w);
       }
       apart = __any_sync(0xFFFFFFFFu, bad);
@@ -364,7 +434,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
       for (int d = 0; d < DB * 4; ++d) {
         uint32_t v[4];                                  // sixteen values: the first eight of positions 0..7 and 8..15, the others
-        ldmatrix4_trans(tile_v + tile_offset<DB>(lane & 15, d * 2 + (lane >> 4)), v);
+        ldmatrix4_trans(tile_v + tile_offset<DB>(value_row, d * 2 + value_half), v);
         mma16816<T>(o[2 * d], hi, v[0], v[1]);
         mma16816<T>(o[2 * d + 1], hi, v[2], v[3]);
         mma16816<T>(o[2 * d], lo, v[0], v[1]);
@@ -382,7 +452,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
         for (int d = 0; d < DB * 4; ++d) {
           uint32_t v[4];
-          ldmatrix4_trans(tile_v + tile_offset<DB>(lane & 15, d * 2 + (lane >> 4)), v);
+          ldmatrix4_trans(tile_v + tile_offset<DB>(value_row, d * 2 + value_half), v);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float x[4] = {o[2 * d + e][0], o[2 * d + e][1], o[2 * d + e][2], o[2 * d + e][3]};
@@ -395,17 +465,21 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       }
     }
     if (info.flags & kLast) {
-      const Sentence it = sentence_of(a, info.b);
-      const int head = info.item / it.row_groups, row0 = info.item % it.row_groups * kRows;
       const bool done = from_start && (info.flags & kToEnd);
+      if (!done && lane == 0) {
+        PartInfo part;
+        part.there = 1; part.b = info.b; part.head = info.head; part.row0 = info.row0; part.n = info.n;
+        part.to_end = (info.flags & kToEnd) != 0;
+        s_part[warp][from_start] = part;
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 1);
         l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 2);
-        const int r = row0 + r8 + 8 * u, t = t_of[u];
-        if (t >= it.n) continue;
+        const int r = info.row0 + r8 + 8 * u, t = t_of[u];
+        if (t >= info.n) continue;
         if (done) {
-          const int h = head * a.group + r % a.group;
+          const int h = info.head * a.group + r % a.group;
           const float inv = l[u] != 0.0f ? 1.0f / l[u] : 0.0f;
           uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, info.b, t, h)) + c4;
 #pragma unroll
@@ -414,8 +488,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
           if (a.lse && c4 == 0)
             a.lse[((int64_t)info.b * a.heads + h) * a.tokens + t] = l[u] != 0.0f ? m[u] * a.scale + (logf(l[u]) - kRunningShift<T> * 0.69314718f) : -INFINITY;
         } else {
-          // the run's first item may have begun elsewhere (part 2 w), its last one may go on (part 2 w + 1)
-          const int64_t at = (int64_t)(2 * w + (from_start ? 1 : 0)) * plan.rows + r8 + 8 * u;
+          const int64_t at = (int64_t)(2 * (blockIdx.x * kWarps + warp) + from_start) * plan.rows + r8 + 8 * u;
           if (c4 == 0) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(m[u], l[u]);
           float2* dst = reinterpret_cast<float2*>(plan.part_o + at * a.head_dim) + c4;
 #pragma unroll
@@ -426,79 +499,102 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     }
   }
   cp_async_wait<0>();
+  if (plan.whole) return;
+
+  // the CTA's parts: an item's are warp j's second and the first of those after it, up to one that ends it. warp = one row of an item
+  __syncthreads();
+  int turn = 0;
+  for (int j = 0; j < kWarps; ++j)
+#pragma unroll 1
+    for (int second = 0; second < 2; ++second) {
+      if (!s_part[j][second].there || (second == 0 && j > 0)) continue;      // a later warp's first part follows another
+      int last = j;
+      bool ended = s_part[j][second].to_end;
+      while (!ended && last + 1 < kWarps && s_part[last + 1][0].there) ended = s_part[++last][0].to_end;
+      const PartInfo item = s_part[j][second];
+      const int rows = min(kRows, item.n * a.group - item.row0);
+      for (int r = 0; r < rows; ++r, ++turn) {
+        if (turn % kWarps != warp) continue;
+        float m0 = -INFINITY, l0 = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int k = j; k <= last; ++k) {
+          const int64_t at = (int64_t)(2 * (blockIdx.x * kWarps + k) + (k == j ? second : 0)) * plan.rows + r;
+          const float2 ml = __ldcg(reinterpret_cast<const float2*>(plan.part_ml + at * 2));
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (lane * 4 < a.head_dim) x = __ldcg(reinterpret_cast<const float4*>(plan.part_o + at * a.head_dim + lane * 4));
+          float f0, f1;
+          join_ml(m0, l0, ml.x, ml.y, c, f0, f1);
+          v[0] = v[0] * f0 + x.x * f1; v[1] = v[1] * f0 + x.y * f1; v[2] = v[2] * f0 + x.z * f1; v[3] = v[3] * f0 + x.w * f1;
+        }
+        if (second && ended) {
+          const int row = item.row0 + r;
+          write_row<T>(a, item.b, row / a.group, item.head * a.group + row % a.group, lane, m0, l0, v);
+        } else {
+          const int64_t at = (int64_t)(2 * (gridDim.x * kWarps + blockIdx.x) + second) * plan.rows + r;
+          if (lane == 0) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(m0, l0);
+          if (lane * 4 < a.head_dim) *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    }
 }
 
-// Joins the parts of a row: `join_warps` warps for each, lane = four values, the parts in order; the warps meet in shared memory.
+// Joins the CTAs' parts of a row: `join_warps` warps for each, lane = four values, the parts in order; the warps meet in shared memory.
 template <typename T>
 __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan plan) {
   extern __shared__ float s_join[];                     // [warps][head_dim + 2]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % plan.join_warps, pitch = a.head_dim + 2;
-  const int rows = a.tokens * a.group;
-  const int64_t row_index = (int64_t)blockIdx.x * (blockDim.x / 32 / plan.join_warps) + warp / plan.join_warps;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const bool exists = row_index < (int64_t)a.batch * a.kv_heads * rows;
-  const int row = (int)(row_index % rows), hk = (int)(row_index / rows % a.kv_heads), b = exists ? (int)(row_index / rows / a.kv_heads) : 0;
-  const Runs runs(plan.prefix[a.batch], plan.ctas * kWarps);
-  const Sentence s = sentence_of(a, b);
+  const uint32_t rows = a.tokens * a.group, index = blockIdx.x * (blockDim.x / 32 / plan.join_warps) + warp / plan.join_warps;
+  const bool exists = index < (uint32_t)a.batch * a.kv_heads * rows;
+  const int row = index % rows, hk = index / rows % a.kv_heads, b = exists ? index / rows / a.kv_heads : 0;
   const int t = row / a.group, h = hk * a.group + row % a.group;
-  int w0 = 0, w1 = 0;
+  const Sentence s = sentence_of(a, b);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int c0 = 0, c1 = 0;                                   // the CTAs that hold parts
   if (exists && t < s.n) {
+    const Runs runs(plan.prefix[a.batch], plan.ctas);
     const int64_t start = plan.prefix[b] + ((int64_t)hk * s.row_groups + row / kRows) * s.blocks;
-    w0 = runs.owner(start);
-    w1 = runs.owner(start + s.blocks - 1);
+    c0 = runs.owner(start) / runs.per_cta;
+    c1 = runs.owner(start + s.blocks - 1) / runs.per_cta;
   }
   const float c = a.scale * kLog2e;
   float top = -INFINITY, sum = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (w1 > w0) {
-    const int count = w1 - w0 + 1, from = count * sub / plan.join_warps, to = count * (sub + 1) / plan.join_warps;
-    for (int p0 = from; p0 < to; p0 += 32) {
-      const int here = min(32, to - p0);
-      auto part = [&](int i) { return ((int64_t)2 * (w0 + p0 + i) + (p0 + i == 0 ? 1 : 0)) * plan.rows + row % kRows; };
-      float2 ml = make_float2(-INFINITY, 0.0f);
-      if (lane < here) ml = *reinterpret_cast<const float2*>(plan.part_ml + part(lane) * 2);
-      float most = ml.x;
+  if (c1 > c0) {
+    const int count = c1 - c0 + 1, from = count * sub / plan.join_warps, to = count * (sub + 1) / plan.join_warps;
+    for (int p0 = from; p0 < to; p0 += 8) {
+      float2 ml[8];
+      float4 x[8];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-      const float m_new = fmaxf(top, most), base = m_new == -INFINITY ? 0.0f : m_new, f0 = ex2((top - base) * c);
-      const float f = ex2((ml.x - base) * c);
-      top = m_new;
-      sum = fmaf(sum, f0, warp_sum(ml.y * f));
+      for (int i = 0; i < 8; ++i) {
+        const int k = p0 + i;
+        const int64_t at = (int64_t)(2 * (plan.ctas * kWarps + c0 + k) + (k == 0)) * plan.rows + row % kRows;
+        ml[i] = k < to ? *reinterpret_cast<const float2*>(plan.part_ml + at * 2) : make_float2(-INFINITY, 0.0f);
+        x[i] = k < to && lane * 4 < a.head_dim ? *reinterpret_cast<const float4*>(plan.part_o + at * a.head_dim + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= f0;
-#pragma unroll 8
-      for (int i = 0; i < here; ++i) {
-        const float fs = __shfl_sync(0xFFFFFFFFu, f, i);
-        if (lane * 4 < a.head_dim) {
-          const float4 x = *reinterpret_cast<const float4*>(plan.part_o + part(i) * a.head_dim + lane * 4);
-          v[0] = fmaf(x.x, fs, v[0]); v[1] = fmaf(x.y, fs, v[1]); v[2] = fmaf(x.z, fs, v[2]); v[3] = fmaf(x.w, fs, v[3]);
-        }
+      for (int i = 0; i < 8; ++i) {
+        float f0, f1;
+        join_ml(top, sum, ml[i].x, ml[i].y, c, f0, f1);
+        v[0] = v[0] * f0 + x[i].x * f1; v[1] = v[1] * f0 + x[i].y * f1; v[2] = v[2] * f0 + x[i].z * f1; v[3] = v[3] * f0 + x[i].w * f1;
       }
     }
   }
   if (plan.join_warps > 1) {
     float* mine = s_join + warp * pitch;
-    if (lane * 4 < a.head_dim) for (int e = 0; e < 4; ++e) mine[2 + lane * 4 + e] = v[e];
+    if (lane * 4 < a.head_dim)
+      for (int e = 0; e < 4; ++e) mine[2 + lane * 4 + e] = v[e];
     if (lane == 0) { mine[0] = top; mine[1] = sum; }
     __syncthreads();
     if (sub == 0) {
       for (int i = 1; i < plan.join_warps; ++i) {
         const float* x = mine + i * pitch;
-        const float m_new = fmaxf(top, x[0]), base = m_new == -INFINITY ? 0.0f : m_new, f0 = ex2((top - base) * c), f1 = ex2((x[0] - base) * c);
-        top = m_new;
-        sum = sum * f0 + x[1] * f1;
+        float f0, f1;
+        join_ml(top, sum, x[0], x[1], c, f0, f1);
         if (lane * 4 < a.head_dim)
           for (int e = 0; e < 4; ++e) v[e] = v[e] * f0 + x[2 + lane * 4 + e] * f1;
       }
     }
   }
-  if (w1 <= w0 || sub != 0) return;
-  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  if (lane * 4 < a.head_dim) {
-    T* out = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4;
-    *reinterpret_cast<uint2*>(out) = sum != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
-  }
-  if (a.lse && lane == 0)
-    a.lse[((int64_t)b * a.heads + h) * a.tokens + t] = sum != 0.0f ? top * a.scale + (logf(sum) - kRunningShift<T> * 0.69314718f) : -INFINITY;
+  if (c1 > c0 && sub == 0) write_row<T>(a, b, t, h, lane, top, sum, v);
 }
 
 PagedPlan make_plan(const PagedArgs& a) {
@@ -516,13 +612,16 @@ PagedPlan make_plan(const PagedArgs& a) {
   p.whole = most <= kWholeBlocks;
   const int64_t warps = p.whole ? items : items * (most / kMinShare + 1);
   p.ctas = (int32_t)(warps < room ? (warps < 1 ? 1 : warps) : room);
-  int64_t join = p.ctas * kWarps / (items > 0 ? items : 1) / 16;       // about 16 parts or more to a warp
+  const int64_t join = p.ctas / (items > 0 ? items : 1) / 8;           // about 8 parts or more to a warp
   p.join_warps = 1;
   while (p.join_warps < 32 && p.join_warps < join) p.join_warps *= 2;
+  // x / size = (high word of x * multiplier + x) >> shift for every x below 2^31 (Granlund and Montgomery's division by invariants)
+  while (p.page_shift < 31 && (1u << p.page_shift) < (uint32_t)a.page_size) ++p.page_shift;
+  p.page_multiplier = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << p.page_shift) - (uint64_t)a.page_size)) / (uint64_t)a.page_size + 1);
   return p;
 }
 
-template <typename T, int DB>
+template <typename T, int DB, bool ONE_PAGE>
 cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
   using S = Shape<DB>;
   static bool attr_set[64] = {};
@@ -533,12 +632,12 @@ cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+      const cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<T, DB, ONE_PAGE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
   }
-  paged_attention_kernel<T, DB><<<p.ctas, kWarps * 32, S::kSmem, st>>>(a, p);
+  paged_attention_kernel<T, DB, ONE_PAGE><<<p.ctas, kWarps * 32, S::kSmem, st>>>(a, p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || p.whole) return e;
   const int warps = p.join_warps > 8 ? p.join_warps : 8;
@@ -556,7 +655,7 @@ cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, paged_join_kernel<T>, a, p);
 }
 
-size_t parts_of(const PagedPlan& p) { return (size_t)2 * p.ctas * kWarps * p.rows; }
+size_t parts_of(const PagedPlan& p) { return (size_t)2 * p.ctas * (kWarps + 1) * p.rows; }
 
 }  // namespace
 
@@ -572,8 +671,11 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, void* workspac
     p.part_ml = p.part_o + parts_of(p) * a.head_dim;
     p.prefix = reinterpret_cast<int64_t*>(p.part_ml + parts_of(p) * 2);
   }
-  if (dtype == SWARM_BF16) return a.head_dim <= 64 ? launch<__nv_bfloat16, 1>(a, p, st) : launch<__nv_bfloat16, 2>(a, p, st);
-  return a.head_dim <= 64 ? launch<__half, 1>(a, p, st) : launch<__half, 2>(a, p, st);
+#define SWARM_PAGED_LAUNCH(T)                                                                                             \
+  (a.page_size % kBlock == 0 ? a.head_dim <= 64 ? launch<T, 1, true>(a, p, st) : launch<T, 2, true>(a, p, st)             \
+                             : a.head_dim <= 64 ? launch<T, 1, false>(a, p, st) : launch<T, 2, false>(a, p, st))
+  return dtype == SWARM_BF16 ? SWARM_PAGED_LAUNCH(__nv_bfloat16) : SWARM_PAGED_LAUNCH(__half);
+#undef SWARM_PAGED_LAUNCH
 }
 
 }  // namespace swarm
