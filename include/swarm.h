@@ -447,7 +447,7 @@ int swarm_cross_attention_backward(const swarm_attention *desc_host, const void 
  * at least 0): row t < n is position lengths[b] - n + t. Sentences may share pages that no call writes.
  *   A page number outside [0, pages), or a position past the table's columns, is not followed: such a token is not
  *   written and not read, and a word is raised that swarm_operator_check reads. Table entries that no token of the call
- *   needs are not read (what a window has left behind may be given up).
+ *   needs are not followed, whatever they hold (what a window has left behind may be given up).
  *   Tensors are addressed by strides (elements) over sentence (of the cache: page), token (slot) and head; the head_dim
  *   values of a head are consecutive. */
 typedef struct {

@@ -23,7 +23,8 @@ namespace swarm {
 namespace {
 
 constexpr int kRows = 16;
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
+constexpr int kCtasPerSm = 2;
 constexpr int kMinShare = 64;                           // positions that a warp's run has at least
 constexpr int kWholePositions = 128;                    // items of no more are not cut
 constexpr int kSms = 148;
@@ -42,12 +43,15 @@ struct PagedPlan {
   int32_t rows;                       // that a part holds
   int32_t whole;                      // items are not cut
   int32_t ctas;
-  int32_t join_warps;                 // for each row
+  int32_t beside;                     // key heads that warps of a CTA take side by side (a divisor of kv_heads, up to kWarps)
+  int32_t joined;                     // items that the joining kernel has at most, those side by side counted once
+  int32_t join_warps;                 // for each row of them
   uint32_t page_multiplier, page_shift;                 // division by the size of a page
   int32_t* joins;                     // [ctas][8], see JoinInfo
-  // parts: two for each warp, then two for each CTA
+  // parts: two for each CTA and key head side by side; then, without ml, the first of each warp
   float* part_ml;                     // [parts][rows][2] maximum and sum
-  float* part_o;                      // [parts][rows][head_dim]
+  float* part_o;                      // [parts][rows][pitch], the warps' as their lanes hold them
+  int32_t pitch;
 };
 
 // What a sentence's rows see, in blocks of B: the first `sink_blocks`, then those from position lo / B * B.
@@ -65,24 +69,25 @@ template <int B> __device__ __forceinline__ Sentence sentence_of(const PagedArgs
   s.row_groups = (s.n * a.group + kRows - 1) / kRows;
   return s;
 }
-__device__ __forceinline__ int64_t blocks_of_items(const PagedArgs& a, const Sentence& s) {
-  return (int64_t)s.blocks * a.kv_heads * s.row_groups;
+// Blocks of a sentence's items, those of the key heads beside one another counted once.
+__device__ __forceinline__ int64_t blocks_of_items(const PagedArgs& a, const PagedPlan& p, const Sentence& s) {
+  return (int64_t)s.blocks * (a.kv_heads / p.beside) * s.row_groups;
 }
 __device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {      // of numbers that are not negative
   return ((x | d) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
 }
 
-// The runs that `total` blocks are dealt in: `warps` runs, `per_cta` of them in each CTA, the first `more` one block longer.
+// The runs that `total` blocks are dealt in, `per_cta` of them in each CTA, the first `more` one block longer.
 struct Runs {
   int64_t each, more;
-  int warps, per_cta;
-  __device__ __forceinline__ Runs(int64_t total, int ctas, int min_share) {
-    warps = (int)max((int64_t)1, min((int64_t)ctas * kWarps, total / min_share));
-    per_cta = (warps + ctas - 1) / ctas;                // few runs go to many multiprocessors
-    each = divide(total, warps);
-    more = total - each * warps;
+  int count, per_cta;
+  __device__ __forceinline__ Runs(int64_t total, int most, int ctas, int min_share) {
+    count = (int)max((int64_t)1, min((int64_t)most, total / min_share));
+    per_cta = (count + ctas - 1) / ctas;                // few runs go to many multiprocessors
+    each = divide(total, count);
+    more = total - each * count;
   }
-  __device__ __forceinline__ int64_t begin(int w) const { return w * each + min((int64_t)w, more); }
+  __device__ __forceinline__ int64_t begin(int r) const { return r * each + min((int64_t)r, more); }
   __device__ __forceinline__ int owner(int64_t x) const {
     const int64_t wide = more * (each + 1);
     return (int)(x < wide ? divide(x, each + 1) : more + divide(x - wide, each));
@@ -98,6 +103,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t r[4]) {
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t r[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" :: "l"(p)); }
 // An 8 x 8 matrix of 16-bit numbers (lane: two neighbours of row lane / 4) transposed. All lanes of the warp.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t r;
@@ -131,9 +137,9 @@ enum : uint32_t {
 
 // Parts of a cut item that a warp holds: the run's first item may have begun elsewhere (0), its last one may go on (1).
 struct __align__(16) PartInfo {
-  int32_t there, b, head, row0, n, to_end, in_ring;      // in_ring: in shared memory, else in the workspace
+  int32_t there, b, head, row0, rows, to_end, in_ring;   // rows: from row0 on; in_ring: in shared memory, else in the workspace
 };
-// An item that CTAs begin with `cta` and go on past it, for the joining kernel; rows 0: none.
+// The item (of the first of the key heads beside one another) that a CTA begins and does not end, for the joining kernel; rows 0: none.
 struct __align__(16) JoinInfo {
   int32_t b, head, row0, rows, last_cta, unused[3];
 };
@@ -154,31 +160,34 @@ template <typename T>
 __device__ __forceinline__ void write_lse(const PagedArgs& a, int b, int t, int h, float m, float l) {
   a.lse[((int64_t)b * a.heads + h) * a.tokens + t] = l != 0.0f ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
 }
-// A row from its sum, four values a lane, and its lse.
+// A lane's four values of a row, from the row's sum.
 template <typename T>
-__device__ __forceinline__ void write_row(const PagedArgs& a, int b, int t, int h, int lane, float m, float l, const float v[4]) {
+__device__ __forceinline__ void write_values(const PagedArgs& a, int b, int t, int h, int lane, float l, const float v[4]) {
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-  if (lane * 4 < a.head_dim)
-    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4) =
-        l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
-  if (a.lse && lane == 0) write_lse<T>(a, b, t, h, m, l);
+  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4) =
+      l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
 }
 
 // NT: items of up to 8 NT rows. ONE_PAGE: pages hold a multiple of 16 positions, so sixteen of a block lie in one. Then a row's
 // address is one addition away from the last one's; else each position has its own, and a lane gets them by shuffles.
 template <typename T, int DB, int NT, bool ONE_PAGE>
-__global__ void __launch_bounds__(kWarps * 32, 1)
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
 paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   using S = Shape<DB>;
+  constexpr int kPartBytes = kRows * DB * 64 * 4;
+  static_assert(2 * kPartBytes <= S::kRing, "a warp's two parts fit its ring");
   constexpr int B = S::kBlock, kSixteens = B / 16, kStages = S::kStages, kChunks = DB * 8, kRowsPerCopy = 32 / kChunks;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ BlockInfo s_info[kWarps][kStages];
   __shared__ PartInfo s_part[kWarps][2];
   __shared__ int64_t s_prefix[kWarps * 32 + 1];
   __shared__ int64_t s_warp[kWarps];
+  __shared__ int s_last_cta;
+  __shared__ float2 s_ml[kWarps][2][kRows];             // maximum and sum of the rows of a part, then their o's factor and, in the last one, the whole sum
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3, chunks = a.head_dim / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane < 2) s_part[warp][lane].there = 0;
+  const int beside = plan.beside, sub_runs = kWarps / beside, side = warp % beside, sub = warp / beside;
 
   // this warp's run
   int b = 0, hk = 0, rg = 0, block = 0;
@@ -196,7 +205,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     const int per = (a.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
     int64_t before = 0;
-    for (int i = b0; i < b1; ++i) before += blocks_of_items(a, sentence_of<B>(a, i));
+    for (int i = b0; i < b1; ++i) before += blocks_of_items(a, plan, sentence_of<B>(a, i));
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t x = __shfl_up_sync(0xFFFFFFFFu, before, o);
@@ -208,21 +217,21 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     s_prefix[tid + 1] = before;
     if (tid == 0) s_prefix[0] = 0;
     __syncthreads();
-    const Runs runs(s_prefix[kWarps * 32], gridDim.x, kMinShare / B);
-    const int w = blockIdx.x * runs.per_cta + warp;
-    const bool takes = warp < runs.per_cta && w < runs.warps;
-    const int64_t begin = takes ? runs.begin(w) : 0;
-    left = takes ? runs.begin(w + 1) - begin : 0;
+    const Runs runs(s_prefix[kWarps * 32], gridDim.x * sub_runs, gridDim.x, kMinShare / B);
+    const int run = blockIdx.x * runs.per_cta + sub;
+    const bool takes = sub < runs.per_cta && run < runs.count;
+    const int64_t begin = takes ? runs.begin(run) : 0;
+    left = takes ? runs.begin(run + 1) - begin : 0;
     if (left > 0) {
       int lo = 0, hi = kWarps * 32;                     // the slice of sentences that holds the run's first block
       while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (s_prefix[mid] <= begin) lo = mid; else hi = mid; }
       int64_t at = begin - s_prefix[lo];
       b = lo * per;
       s = sentence_of<B>(a, b);
-      while (at >= blocks_of_items(a, s)) { at -= blocks_of_items(a, s); ++b; s = sentence_of<B>(a, b); }
+      while (at >= blocks_of_items(a, plan, s)) { at -= blocks_of_items(a, plan, s); ++b; s = sentence_of<B>(a, b); }
       const int item = (int)divide(at, s.blocks);
       block = (int)(at - (int64_t)item * s.blocks);
-      hk = item / s.row_groups;
+      hk = item / s.row_groups * beside + side;
       rg = item % s.row_groups;
     }
   }
@@ -231,9 +240,9 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   auto skip = [&]() {
     while (rg >= s.row_groups) {                        // none in a sentence without rows
       rg = 0;
-      ++hk;
+      hk += beside;
       if (hk >= a.kv_heads || s.row_groups == 0) {
-        hk = 0;
+        hk = side;
         if (++b >= a.batch) { left = 0; return; }
         s = sentence_of<B>(a, b);
       }
@@ -242,20 +251,32 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   };
   if (left > 0) skip();
 
-  // the next block: its position, and the pages of its sixteens (ONE_PAGE), or lane i that of position i; looked up a block ahead
-  int p0 = 0, page[ONE_PAGE ? kSixteens : 1], slot[ONE_PAGE ? kSixteens : 1];
+  // The next block: its position, and the pages of its sixteens (ONE_PAGE), or lane i that of position i. The table is read 64
+  // columns at a time, the second 32 before they are needed: lane i holds columns seen + i and seen + 32 + i of row seen_b.
+  int p0 = 0, page[ONE_PAGE ? kSixteens : 1], slot[ONE_PAGE ? kSixteens : 1], near = 0, far = 0, seen = 0, seen_b = -1;
   auto look_up = [&]() {
     if (left <= 0) return;
     p0 = (block < s.sink_blocks ? block : block - s.sink_blocks + s.lo / B) * B;
+    auto column_of = [&](int p) { return (int)((__umulhi((uint32_t)p, plan.page_multiplier) + (uint32_t)p) >> plan.page_shift); };
+    auto entries = [&](uint32_t column) { return column + lane < (uint32_t)a.table_columns ? a.table[b * a.table_pitch + column + lane] : -1; };
+    const int first = column_of(p0);
+    const uint32_t ahead = (uint32_t)(first - seen);
+    if (b != seen_b || ahead >= 64u) {
+      seen_b = b;
+      seen = first;
+      near = entries(first);
+      far = entries((uint32_t)first + 32u);
+    } else if (ahead >= 32u) {
+      seen += 32;
+      near = far;
+      far = entries((uint32_t)seen + 32u);
+    }
 #pragma unroll
     for (int g = 0; g < (ONE_PAGE ? kSixteens : 1); ++g) {
-      const int p = ONE_PAGE ? p0 + g * 16 : p0 + (lane & (B - 1));
-      const int column = (int)((__umulhi((uint32_t)p, plan.page_multiplier) + (uint32_t)p) >> plan.page_shift);
+      const int p = ONE_PAGE ? p0 + g * 16 : p0 + (lane & (B - 1)), column = column_of(p), at = column - seen;
       slot[g] = p - column * a.page_size;
-      page[g] = -1;
-      // of a block's sixteens, or positions, some may be seen by no row
-      const bool some = ONE_PAGE ? (kSixteens == 1 || (p < s.length && (p + 15 >= s.lo || p < a.sinks))) : p < s.length && (p >= s.lo || p < a.sinks);
-      if (some && column < a.table_columns) page[g] = a.table[b * a.table_pitch + column];
+      const int x = __shfl_sync(0xFFFFFFFFu, near, at & 31), y = __shfl_sync(0xFFFFFFFFu, far, at & 31);
+      page[g] = at < 32 ? x : y;                        // a block has at most 32 columns from its first one on
     }
   };
   look_up();
@@ -337,6 +358,17 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
         info.flags = (fresh ? kFirst : 0u) | (fresh && block == 0 ? kFromStart : 0u) | (last ? kLast : 0u) | (ends ? kToEnd : 0u) | (run_ends ? kRunEnds : 0u);
         s_info[warp][stage] = info;
       }
+      if (fresh) {                                      // its rows, needed two blocks from now, behind what is in flight
+        const int r = rg * kRows + lane / DB, t = r / a.group;
+        if (lane < NT * 8 * DB && t < s.n && lane % DB * 64 < a.head_dim)
+          prefetch_l2(reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, hk * a.group + r % a.group) + lane % DB * 64);
+      }
+      if (run_ends && !ends && lane == 0 && side == 0) {
+        // the CTA that holds the item's last block; of a CTA's runs the last one's counts
+        const Runs runs(s_prefix[kWarps * 32], gridDim.x * sub_runs, gridDim.x, kMinShare / B);
+        const int run = blockIdx.x * runs.per_cta + sub;
+        if (sub + 1 == runs.per_cta || run + 1 == runs.count) s_last_cta = runs.owner(runs.begin(run + 1) + (s.blocks - 2 - block)) / runs.per_cta;
+      }
       fresh = last;
       ++block;
       if (!plan.whole) --left;
@@ -369,6 +401,20 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   int t_of[NT][2];                                      // the tokens of these rows
   const float c = a.scale * kLog2e;
   bool from_start = false;
+  // a part of a cut item, as rows, in the ring when the run has ended; one that ends earlier is kept in the workspace till then
+  auto store_part = [&](int second, auto value) {
+    float* to = reinterpret_cast<float*>(ring) + second * (kPartBytes / 4);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int d = 0; d < DB * 4; ++d) {
+        const float4 x = value(nt, d);
+        const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) to[(nt * 8 + c4 * 2 + (u & 1)) * (DB * 64) + d * 16 + (u >> 1) * 8 + r8] = xs[u];
+      }
+  };
+  float4* kept = reinterpret_cast<float4*>(plan.part_o + ((int64_t)2 * gridDim.x * beside * plan.rows + (int64_t)(blockIdx.x * kWarps + warp) * kRows) * (DB * 64)) + lane;
   // a lane's rows and halves for ldmatrix: eight rows x 8 values four times
   const int key_row = lane & 15, key_half = lane >> 4, value_row = (lane & 7) + (lane >> 4) * 8, value_half = lane >> 3 & 1;
   for (int stage = 0;; stage = stage + 1 == kStages ? 0 : stage + 1) {
@@ -562,112 +608,109 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
         const bool in_ring = info.flags & kRunEnds;
         if (lane == 0) {
           PartInfo part;
-          part.there = 1; part.b = info.b; part.head = info.head; part.row0 = info.row0; part.n = info.n;
+          part.there = 1; part.b = info.b; part.head = info.head; part.row0 = info.row0; part.rows = min(kRows, info.n * a.group - info.row0);
           part.to_end = (info.flags & kToEnd) != 0; part.in_ring = in_ring;
           s_part[warp][from_start] = part;
         }
         __syncwarp();
-        const int64_t at = (int64_t)(2 * (blockIdx.x * kWarps + warp)) * plan.rows;      // only a first part goes there
-        float* po = in_ring ? reinterpret_cast<float*>(ring) : plan.part_o + at * a.head_dim;
-        float* pml = in_ring ? reinterpret_cast<float*>(ring) + kRows * a.head_dim : plan.part_ml + at * 2;
+        if (r8 == 0) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int r = nt * 8 + c4 * 2 + u;
-            if (t_of[nt][u] >= info.n) continue;
-            if (r8 == 0) *reinterpret_cast<float2*>(pml + r * 2) = make_float2(m[nt][u], l[nt][u]);
+            for (int u = 0; u < 2; ++u) s_ml[warp][from_start][nt * 8 + c4 * 2 + u] = make_float2(m[nt][u], l[nt][u]);
+        }
+        if (in_ring) {
+          store_part(from_start, [&](int nt, int d) { return make_float4(o[nt][d][0], o[nt][d][1], o[nt][d][2], o[nt][d][3]); });
+        } else {
 #pragma unroll
-            for (int d = 0; d < DB * 4; ++d)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (d * 2 + e < chunks) po[r * a.head_dim + d * 16 + e * 8 + r8] = o[nt][d][2 * e + u];
-          }
+            for (int d = 0; d < DB * 4; ++d) kept[(nt * DB * 4 + d) * 32] = make_float4(o[nt][d][0], o[nt][d][1], o[nt][d][2], o[nt][d][3]);
+        }
       }
     }
   }
   cp_async_wait<0>();
   if (plan.whole) return;
+  __syncwarp();
+  if (s_part[warp][0].there && !s_part[warp][0].in_ring) {
+    float4 x[NT][DB * 4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int d = 0; d < DB * 4; ++d) x[nt][d] = kept[(nt * DB * 4 + d) * 32];
+    store_part(0, [&](int nt, int d) { return x[nt][d]; });
+  }
 
-  // The CTA's parts. An item's are warp j's second, or the first warp's first, and the first of those after it up to one
-  // that ends it; only that last one may be in the workspace. warp = a row of an item, four at a time.
-  __shared__ struct { int32_t first, second, last, ended, units; } s_item[kWarps + 1];
-  __shared__ int s_items;
+  // The CTA's parts. Those of an item: the second of the warp that begins it here, or the first warp's first, and the first of
+  // the warps after it up to one that ends it. A row of an item: (its key head beside the others, k: its first warp's first
+  // part (0) or that of the k-1-th warp's second, row).
+  if (tid == 0) reinterpret_cast<JoinInfo*>(plan.joins)[blockIdx.x] = JoinInfo{};
   __syncthreads();
-  if (tid == 0) {
-    int items = 0, units = 0;
-    for (int j = 0; j < kWarps; ++j)
-      for (int second = j > 0; second < 2; ++second) {
-        if (!s_part[j][second].there) continue;
-        int last = j, ended = s_part[j][second].to_end;
-        while (!ended && last + 1 < kWarps && s_part[last + 1][0].there) ended = s_part[++last][0].to_end;
-        units += min(kRows, s_part[j][second].n * a.group - s_part[j][second].row0);
-        s_item[items].first = j; s_item[items].second = second; s_item[items].last = last; s_item[items].ended = ended; s_item[items].units = units;
-        ++items;
-      }
-    s_items = items;
-    JoinInfo join{};
-    if (items > 0 && s_item[items - 1].second && !s_item[items - 1].ended) {
-      const PartInfo x = s_part[s_item[items - 1].first][1];
-      join.b = x.b; join.head = x.head; join.row0 = x.row0;
-      join.rows = min(kRows, x.n * a.group - x.row0);
-      // the item's last block
-      const Sentence it = sentence_of<B>(a, x.b);
-      const int per = (a.batch + kWarps * 32 - 1) / (kWarps * 32);
-      int64_t at = s_prefix[x.b / per];
-      for (int i = x.b / per * per; i < x.b; ++i) at += blocks_of_items(a, sentence_of<B>(a, i));
-      at += ((int64_t)x.head * it.row_groups + x.row0 / kRows + 1) * it.blocks - 1;
-      const Runs runs(s_prefix[kWarps * 32], gridDim.x, kMinShare / B);
-      join.last_cta = runs.owner(at) / runs.per_cta;
+  auto chain = [&](int at, int& first, int& second, int& last, bool& ended) {
+    const int k = at % (sub_runs + 1);
+    second = k > 0;
+    first = last = (k > 0 ? k - 1 : 0) * beside + at / (sub_runs + 1);
+    if (!s_part[first][second].there) return false;
+    ended = s_part[first][second].to_end;
+    while (!ended && last + beside < kWarps && s_part[last + beside][0].there) {
+      last += beside;
+      ended = s_part[last][0].to_end;
     }
-    *reinterpret_cast<JoinInfo*>(plan.joins + blockIdx.x * 8) = join;
+    return true;
+  };
+  const int chains = beside * (sub_runs + 1);
+  // thread = a row: maximum and sum over its parts, and the parts' factors
+  for (int unit = tid; unit < chains * kRows; unit += kWarps * 32) {
+    int first, second, last;
+    bool ended;
+    const int row = unit % kRows;
+    if (!chain(unit / kRows, first, second, last, ended) || row >= s_part[first][second].rows) continue;
+    float most = -INFINITY, sum = 0.0f;
+    for (int j = first; j <= last; j += beside) most = fmaxf(most, s_ml[j][j == first && second][row].x);
+    const float base = most == -INFINITY ? 0.0f : most;
+    for (int j = first; j <= last; j += beside) {
+      float2& ml = s_ml[j][j == first && second][row];
+      const float f = ex2((ml.x - base) * c);
+      sum = fmaf(ml.y, f, sum);
+      ml.x = f;
+    }
+    s_ml[last][last == first && second][row].y = sum;
+    const PartInfo of = s_part[first][second];
+    if (second && ended) {
+      const int r = of.row0 + row;
+      if (a.lse) write_lse<T>(a, of.b, r / a.group, of.head * a.group + r % a.group, most, sum);
+    } else {
+      *reinterpret_cast<float2*>(plan.part_ml + ((int64_t)(2 * (blockIdx.x * beside + first % beside) + second) * plan.rows + row) * 2) = make_float2(most, sum);
+      if (second && row == 0 && first % beside == 0) {
+        JoinInfo join{};
+        join.b = of.b; join.head = of.head; join.row0 = of.row0; join.rows = of.rows; join.last_cta = s_last_cta;
+        reinterpret_cast<JoinInfo*>(plan.joins)[blockIdx.x] = join;
+      }
+    }
   }
   __syncthreads();
-  const int items = s_items, units = items > 0 ? s_item[items - 1].units : 0;
-  for (int u0 = warp; u0 < units; u0 += 4 * kWarps) {
-    float2 ml[4];
-    float4 x[4];
-    int item[4], row[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int unit = u0 + i * kWarps;
-      int k = 0;
-      while (k < items - 1 && unit >= s_item[k].units) ++k;
-      item[i] = k;
-      row[i] = unit - (k > 0 ? s_item[k - 1].units : 0);
-      const int j = s_item[k].last;
-      ml[i] = make_float2(-INFINITY, 0.0f);
-      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (unit < units && !s_part[j][j == s_item[k].first ? s_item[k].second : 0].in_ring) {
-        const int64_t at = (int64_t)(2 * (blockIdx.x * kWarps + j)) * plan.rows + row[i];
-        ml[i] = __ldcg(reinterpret_cast<const float2*>(plan.part_ml + at * 2));
-        if (lane * 4 < a.head_dim) x[i] = __ldcg(reinterpret_cast<const float4*>(plan.part_o + at * a.head_dim + lane * 4));
+  // a warp takes rows of an item, a lane four values of them
+  for (int at = 0; at < chains; ++at) {
+    int first, second, last;
+    bool ended;
+    if (!chain(at, first, second, last, ended) || lane * 4 >= a.head_dim) continue;
+    const PartInfo of = s_part[first][second];
+    const int last_second = last == first && second;
+#pragma unroll 4
+    for (int row = warp; row < of.rows; row += kWarps) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int j = first; j <= last; j += beside) {
+        const float f = s_ml[j][j == first && second][row].x;
+        const float4 x = *reinterpret_cast<const float4*>(smem + j * S::kRing + (j == first && second) * kPartBytes + (row * (DB * 64) + lane * 4) * 4);
+        v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (u0 + i * kWarps >= units) break;
-      const auto it = s_item[item[i]];
-      float m0 = -INFINITY, l0 = 0.0f, f0, f1, v[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int j = it.first; j <= it.last; ++j) {
-        if (!s_part[j][j == it.first ? it.second : 0].in_ring) break;        // the last one
-        const float* po = reinterpret_cast<const float*>(smem + j * S::kRing);
-        const float2 pm = *reinterpret_cast<const float2*>(po + kRows * a.head_dim + row[i] * 2);
-        float4 px = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (lane * 4 < a.head_dim) px = *reinterpret_cast<const float4*>(po + row[i] * a.head_dim + lane * 4);
-        join_ml(m0, l0, pm.x, pm.y, c, f0, f1);
-        v[0] = v[0] * f0 + px.x * f1; v[1] = v[1] * f0 + px.y * f1; v[2] = v[2] * f0 + px.z * f1; v[3] = v[3] * f0 + px.w * f1;
-      }
-      join_ml(m0, l0, ml[i].x, ml[i].y, c, f0, f1);
-      v[0] = v[0] * f0 + x[i].x * f1; v[1] = v[1] * f0 + x[i].y * f1; v[2] = v[2] * f0 + x[i].z * f1; v[3] = v[3] * f0 + x[i].w * f1;
-      const PartInfo of = s_part[it.first][it.second];
-      if (it.second && it.ended) {
-        const int r = of.row0 + row[i];
-        write_row<T>(a, of.b, r / a.group, of.head * a.group + r % a.group, lane, m0, l0, v);
+      const int r = of.row0 + row;
+      if (second && ended) {
+        write_values<T>(a, of.b, r / a.group, of.head * a.group + r % a.group, lane, s_ml[last][last_second][row].y, v);
       } else {
-        const int64_t at = (int64_t)(2 * (gridDim.x * kWarps + blockIdx.x) + it.second) * plan.rows + row[i];
-        if (lane == 0) *reinterpret_cast<float2*>(plan.part_ml + at * 2) = make_float2(m0, l0);
-        if (lane * 4 < a.head_dim) *reinterpret_cast<float4*>(plan.part_o + at * a.head_dim + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
+        const int64_t part = (int64_t)(2 * (blockIdx.x * beside + first % beside) + second) * plan.rows + row;
+        *reinterpret_cast<float4*>(plan.part_o + part * (DB * 64) + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
   }
@@ -680,10 +723,21 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
   extern __shared__ float s_join[];                     // [warps][head_dim + 2]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % plan.join_warps, pitch = a.head_dim + 2;
   const int index = blockIdx.x * (blockDim.x / 32 / plan.join_warps) + warp / plan.join_warps;
-  const int c0 = index / plan.rows, r = index % plan.rows;
+  int c0 = index / plan.rows / plan.beside;             // of the items that have to be joined
+  const int side = index / plan.rows % plan.beside, r = index % plan.rows;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (plan.joined < plan.ctas) {                        // fewer than CTAs: which CTA begins the c0-th
+    int seen = 0, found = plan.ctas;
+    for (int i = 0; i < plan.ctas && found == plan.ctas; i += 32) {
+      const uint32_t has = __ballot_sync(0xFFFFFFFFu, i + lane < plan.ctas && reinterpret_cast<const JoinInfo*>(plan.joins)[i + lane].rows > 0);
+      const int here = __popc(has);
+      if (seen + here > c0) found = i + __fns(has, 0, c0 - seen + 1);
+      seen += here;
+    }
+    c0 = found;
+  }
   JoinInfo join{};
-  if (c0 < plan.ctas) join = *reinterpret_cast<const JoinInfo*>(plan.joins + c0 * 8);
+  if (c0 < plan.ctas) join = reinterpret_cast<const JoinInfo*>(plan.joins)[c0];
   const bool works = r < join.rows;
   const float c = a.scale * kLog2e;
   float top = -INFINITY, sum = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -695,9 +749,9 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int k = p0 + i;
-        const int64_t at = (int64_t)(2 * (plan.ctas * kWarps + c0 + k) + (k == 0)) * plan.rows + r;
+        const int64_t at = (int64_t)(2 * ((c0 + k) * plan.beside + side) + (k == 0)) * plan.rows + r;
         ml[i] = k < to ? *reinterpret_cast<const float2*>(plan.part_ml + at * 2) : make_float2(-INFINITY, 0.0f);
-        x[i] = k < to && lane * 4 < a.head_dim ? *reinterpret_cast<const float4*>(plan.part_o + at * a.head_dim + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        x[i] = k < to && lane * 4 < a.head_dim ? *reinterpret_cast<const float4*>(plan.part_o + at * plan.pitch + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -723,7 +777,10 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
       }
     }
   }
-  if (works && sub == 0) write_row<T>(a, join.b, (join.row0 + r) / a.group, join.head * a.group + (join.row0 + r) % a.group, lane, top, sum, v);
+  if (!works || sub != 0) return;
+  const int t = (join.row0 + r) / a.group, h = (join.head + side) * a.group + (join.row0 + r) % a.group;
+  if (lane * 4 < a.head_dim) write_values<T>(a, join.b, t, h, lane, sum, v);
+  if (a.lse && lane == 0) write_lse<T>(a, join.b, t, h, top, sum);
 }
 
 PagedPlan make_plan(const PagedArgs& a) {
@@ -739,10 +796,20 @@ PagedPlan make_plan(const PagedArgs& a) {
   }
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_groups;
   p.whole = most <= kWholePositions;
+  p.beside = 1;
+  p.pitch = a.head_dim <= 64 ? 64 : 128;
+  if (!p.whole) {
+    // A position's heads of up to 64 values are 128 bytes each; where they lie side by side, two warps that take two of them at
+    // a time ask for 256 bytes together: 16 heads of 64, 128 sentences 74 -> 68 us, 8 of 16384 positions 101 -> 96 us; four
+    // at a time 68 and 96, eight 68 and 102. Heads of 128 on their own 95 us, two at a time 97.
+    if (a.head_dim <= 64 && a.kv_heads % 2 == 0 && a.kps.head < a.kps.token) p.beside = 2;
+  }
   const int64_t warps = p.whole ? items : items * (most / kMinShare + 2);
-  p.ctas = (int32_t)(warps < kSms ? (warps < 1 ? 1 : warps) : kSms);
-  const int64_t join = p.ctas / (items > 0 ? items : 1) / 8;           // about 8 parts or more to a warp
+  const int64_t room = (int64_t)kSms * kCtasPerSm;
+  p.ctas = (int32_t)(warps < room ? (warps < 1 ? 1 : warps) : room);
+  const int64_t join = p.ctas * p.beside / (items > 0 ? items : 1) / 8;           // about 8 parts or more to a warp
   p.join_warps = 1;
+  p.joined = (int32_t)(items / p.beside < p.ctas ? items / p.beside : p.ctas);
   while (p.join_warps < 32 && p.join_warps < join) p.join_warps *= 2;
   // x / size = (high word of x * multiplier + x) >> shift for every x below 2^31 (Granlund and Montgomery's division by invariants)
   while (p.page_shift < 31 && (1u << p.page_shift) < (uint32_t)a.page_size) ++p.page_shift;
@@ -784,7 +851,7 @@ cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
   if (e != cudaSuccess || p.whole || p.ctas == 1) return e;
   const int warps = p.join_warps > 8 ? p.join_warps : 8, each = warps / p.join_warps;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((p.ctas * p.rows + each - 1) / each);
+  cfg.gridDim = dim3((p.joined * p.beside * p.rows + each - 1) / each);
   cfg.blockDim = dim3(warps * 32);
   cfg.dynamicSmemBytes = p.join_warps > 1 ? warps * (a.head_dim + 2) * sizeof(float) : 0;
   cfg.stream = st;
@@ -796,13 +863,14 @@ cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, paged_join_kernel<T>, a, p);
 }
 
-size_t parts_of(const PagedPlan& p) { return (size_t)2 * p.ctas * (kWarps + 1) * p.rows; }
+size_t cta_rows(const PagedPlan& p) { return (size_t)2 * p.ctas * p.beside * p.rows; }
+size_t all_rows(const PagedPlan& p) { return cta_rows(p) + (size_t)p.ctas * kWarps * kRows; }
 
 }  // namespace
 
 size_t paged_attention_workspace(const PagedArgs& a) {
   const PagedPlan p = make_plan(a);
-  return p.whole ? 0 : parts_of(p) * (a.head_dim + 2) * sizeof(float) + (size_t)p.ctas * sizeof(JoinInfo) + 16;
+  return p.whole ? 0 : (all_rows(p) * p.pitch + cta_rows(p) * 2) * sizeof(float) + (size_t)p.ctas * sizeof(JoinInfo);
 }
 
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, void* workspace, cudaStream_t st) {
@@ -810,7 +878,7 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, void* workspac
   if (!p.whole) {
     p.joins = reinterpret_cast<int32_t*>(workspace);
     p.part_o = reinterpret_cast<float*>(p.joins + p.ctas * 8);
-    p.part_ml = p.part_o + parts_of(p) * a.head_dim;
+    p.part_ml = p.part_o + all_rows(p) * p.pitch;
   }
   return dtype == SWARM_BF16 ? launch<__nv_bfloat16>(a, p, st) : launch<__half>(a, p, st);
 }
