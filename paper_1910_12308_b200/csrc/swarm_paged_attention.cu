@@ -43,7 +43,8 @@ struct PagedPlan {
   int32_t rows;                       // that a part holds
   int32_t whole;                      // items are not cut
   int32_t ctas;
-  int32_t beside;                     // key heads that warps of a CTA take side by side (a divisor of kv_heads, up to kWarps)
+  int32_t beside;                     // key heads that warps of a CTA take side by side: 1 or 2
+  int32_t head_groups;                // kv_heads / beside
   int32_t joined;                     // items that the joining kernel has at most, those side by side counted once
   int32_t join_warps;                 // for each row of them
   uint32_t page_multiplier, page_shift;                 // division by the size of a page
@@ -70,8 +71,8 @@ template <int B> __device__ __forceinline__ Sentence sentence_of(const PagedArgs
   return s;
 }
 // Blocks of a sentence's items, those of the key heads beside one another counted once.
-__device__ __forceinline__ int64_t blocks_of_items(const PagedArgs& a, const PagedPlan& p, const Sentence& s) {
-  return (int64_t)s.blocks * (a.kv_heads / p.beside) * s.row_groups;
+__device__ __forceinline__ int64_t blocks_of_items(const PagedPlan& p, const Sentence& s) {
+  return (int64_t)s.blocks * (p.head_groups * s.row_groups);
 }
 __device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {      // of numbers that are not negative
   return ((x | d) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
@@ -83,7 +84,7 @@ struct Runs {
   int count, per_cta;
   __device__ __forceinline__ Runs(int64_t total, int most, int ctas, int min_share) {
     count = (int)max((int64_t)1, min((int64_t)most, total / min_share));
-    per_cta = (count + ctas - 1) / ctas;                // few runs go to many multiprocessors
+    per_cta = count == most ? most / ctas : (count + ctas - 1) / ctas;        // few runs go to many multiprocessors
     each = divide(total, count);
     more = total - each * count;
   }
@@ -139,6 +140,12 @@ enum : uint32_t {
 struct __align__(16) PartInfo {
   int32_t there, b, head, row0, rows, to_end, in_ring;   // rows: from row0 on; in_ring: in shared memory, else in the workspace
 };
+// A row of a cut item: where it goes (values of out, or below 0 the CTA's part -1 - row), its parts' first and last warp.
+struct __align__(16) CutRow {
+  int64_t to;
+  float sum;
+  int8_t first, last, second, there;
+};
 // The item (of the first of the key heads beside one another) that a CTA begins and does not end, for the joining kernel; rows 0: none.
 struct __align__(16) JoinInfo {
   int32_t b, head, row0, rows, last_cta, unused[3];
@@ -160,12 +167,11 @@ template <typename T>
 __device__ __forceinline__ void write_lse(const PagedArgs& a, int b, int t, int h, float m, float l) {
   a.lse[((int64_t)b * a.heads + h) * a.tokens + t] = l != 0.0f ? m * a.scale + (logf(l) - kRunningShift<T> * 0.69314718f) : -INFINITY;
 }
-// A lane's four values of a row, from the row's sum.
+// Four values of a row, from the row's sum.
 template <typename T>
-__device__ __forceinline__ void write_values(const PagedArgs& a, int b, int t, int h, int lane, float l, const float v[4]) {
+__device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + lane * 4) =
-      l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
+  *reinterpret_cast<uint2*>(to) = l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
 }
 
 // NT: items of up to 8 NT rows. ONE_PAGE: pages hold a multiple of 16 positions, so sixteen of a block lie in one. Then a row's
@@ -183,11 +189,12 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   __shared__ int64_t s_prefix[kWarps * 32 + 1];
   __shared__ int64_t s_warp[kWarps];
   __shared__ int s_last_cta;
-  __shared__ float2 s_ml[kWarps][2][kRows];             // maximum and sum of the rows of a part, then their o's factor and, in the last one, the whole sum
+  __shared__ float2 s_ml[kWarps][2][kRows];             // maximum and sum of the rows of a part, then (factor of their o, .)
+  __shared__ CutRow s_rows[(kWarps + 2) * kRows];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3, chunks = a.head_dim / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane < 2) s_part[warp][lane].there = 0;
-  const int beside = plan.beside, sub_runs = kWarps / beside, side = warp % beside, sub = warp / beside;
+  const int beside = plan.beside, sub_runs = beside == 2 ? kWarps / 2 : kWarps, side = warp & (beside - 1), sub = warp >> (beside - 1);
 
   // this warp's run
   int b = 0, hk = 0, rg = 0, block = 0;
@@ -205,7 +212,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     const int per = (a.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
     int64_t before = 0;
-    for (int i = b0; i < b1; ++i) before += blocks_of_items(a, plan, sentence_of<B>(a, i));
+    for (int i = b0; i < b1; ++i) before += blocks_of_items(plan, sentence_of<B>(a, i));
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t x = __shfl_up_sync(0xFFFFFFFFu, before, o);
@@ -228,7 +235,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       int64_t at = begin - s_prefix[lo];
       b = lo * per;
       s = sentence_of<B>(a, b);
-      while (at >= blocks_of_items(a, plan, s)) { at -= blocks_of_items(a, plan, s); ++b; s = sentence_of<B>(a, b); }
+      while (at >= blocks_of_items(plan, s)) { at -= blocks_of_items(plan, s); ++b; s = sentence_of<B>(a, b); }
       const int item = (int)divide(at, s.blocks);
       block = (int)(at - (int64_t)item * s.blocks);
       hk = item / s.row_groups * beside + side;
@@ -647,72 +654,68 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   // part (0) or that of the k-1-th warp's second, row).
   if (tid == 0) reinterpret_cast<JoinInfo*>(plan.joins)[blockIdx.x] = JoinInfo{};
   __syncthreads();
-  auto chain = [&](int at, int& first, int& second, int& last, bool& ended) {
-    const int k = at % (sub_runs + 1);
-    second = k > 0;
-    first = last = (k > 0 ? k - 1 : 0) * beside + at / (sub_runs + 1);
-    if (!s_part[first][second].there) return false;
-    ended = s_part[first][second].to_end;
-    while (!ended && last + beside < kWarps && s_part[last + beside][0].there) {
-      last += beside;
-      ended = s_part[last][0].to_end;
-    }
-    return true;
-  };
-  const int chains = beside * (sub_runs + 1);
   // thread = a row: maximum and sum over its parts, and the parts' factors
-  for (int unit = tid; unit < chains * kRows; unit += kWarps * 32) {
-    int first, second, last;
-    bool ended;
-    const int row = unit % kRows;
-    if (!chain(unit / kRows, first, second, last, ended) || row >= s_part[first][second].rows) continue;
-    float most = -INFINITY, sum = 0.0f;
-    for (int j = first; j <= last; j += beside) most = fmaxf(most, s_ml[j][j == first && second][row].x);
-    const float base = most == -INFINITY ? 0.0f : most;
-    for (int j = first; j <= last; j += beside) {
-      float2& ml = s_ml[j][j == first && second][row];
-      const float f = ex2((ml.x - base) * c);
-      sum = fmaf(ml.y, f, sum);
-      ml.x = f;
-    }
-    s_ml[last][last == first && second][row].y = sum;
+  const int rows = (sub_runs + 1) * beside * plan.rows;
+  for (int unit = tid; unit < rows; unit += kWarps * 32) {
+    CutRow x{};
+    int k = unit / plan.rows;
+    const int row = unit - k * plan.rows, i0 = k > sub_runs;
+    k -= i0 * (sub_runs + 1);
+    const int second = k > 0, first = (k > 0 ? k - 1 : 0) * beside + i0;
+    int last = first;
     const PartInfo of = s_part[first][second];
-    if (second && ended) {
-      const int r = of.row0 + row;
-      if (a.lse) write_lse<T>(a, of.b, r / a.group, of.head * a.group + r % a.group, most, sum);
-    } else {
-      *reinterpret_cast<float2*>(plan.part_ml + ((int64_t)(2 * (blockIdx.x * beside + first % beside) + second) * plan.rows + row) * 2) = make_float2(most, sum);
-      if (second && row == 0 && first % beside == 0) {
-        JoinInfo join{};
-        join.b = of.b; join.head = of.head; join.row0 = of.row0; join.rows = of.rows; join.last_cta = s_last_cta;
-        reinterpret_cast<JoinInfo*>(plan.joins)[blockIdx.x] = join;
+    if (of.there && row < of.rows) {
+      bool ended = of.to_end;
+      float most = s_ml[first][second][row].x, sum = 0.0f;
+      while (!ended && last + beside < kWarps && s_part[last + beside][0].there) {
+        last += beside;
+        ended = s_part[last][0].to_end;
+        most = fmaxf(most, s_ml[last][0][row].x);
+      }
+      const float base = most == -INFINITY ? 0.0f : most;
+      for (int j = first; j <= last; j += beside) {
+        float2& ml = s_ml[j][j == first && second][row];
+        const float f = ex2((ml.x - base) * c);
+        sum = fmaf(ml.y, f, sum);
+        ml.x = f;
+      }
+      x.sum = sum; x.first = first; x.last = last; x.second = second; x.there = 1;
+      const int r = of.row0 + row, t = r / a.group, h = of.head * a.group + r - t * a.group;
+      if (second && ended) {
+        x.to = offset_of(a.os, of.b, t, h);
+        if (a.lse) write_lse<T>(a, of.b, t, h, most, sum);
+      } else {
+        const int64_t part = (int64_t)(2 * (blockIdx.x * beside + i0) + second) * plan.rows + row;
+        x.to = -1 - part;
+        *reinterpret_cast<float2*>(plan.part_ml + part * 2) = make_float2(most, sum);
+        if (second && row == 0 && i0 == 0) {
+          JoinInfo join{};
+          join.b = of.b; join.head = of.head; join.row0 = of.row0; join.rows = of.rows; join.last_cta = s_last_cta;
+          reinterpret_cast<JoinInfo*>(plan.joins)[blockIdx.x] = join;
+        }
       }
     }
+    s_rows[unit] = x;
   }
   __syncthreads();
-  // a warp takes rows of an item, a lane four values of them
-  for (int at = 0; at < chains; ++at) {
-    int first, second, last;
-    bool ended;
-    if (!chain(at, first, second, last, ended) || lane * 4 >= a.head_dim) continue;
-    const PartInfo of = s_part[first][second];
-    const int last_second = last == first && second;
-#pragma unroll 4
-    for (int row = warp; row < of.rows; row += kWarps) {
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int j = first; j <= last; j += beside) {
-        const float f = s_ml[j][j == first && second][row].x;
-        const float4 x = *reinterpret_cast<const float4*>(smem + j * S::kRing + (j == first && second) * kPartBytes + (row * (DB * 64) + lane * 4) * 4);
-        v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
-      }
-      const int r = of.row0 + row;
-      if (second && ended) {
-        write_values<T>(a, of.b, r / a.group, of.head * a.group + r % a.group, lane, s_ml[last][last_second][row].y, v);
-      } else {
-        const int64_t part = (int64_t)(2 * (blockIdx.x * beside + first % beside) + second) * plan.rows + row;
-        *reinterpret_cast<float4*>(plan.part_o + part * (DB * 64) + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
-      }
+  // 16 or 32 lanes take a row, four values each
+  constexpr int kLanes = DB * 16;
+  const int l4 = tid % kLanes * 4;
+  if (l4 >= a.head_dim) return;
+#pragma unroll 2
+  for (int unit = tid / kLanes; unit < rows; unit += kWarps * 32 / kLanes) {
+    const CutRow x = s_rows[unit];
+    if (!x.there) continue;
+    const int row = unit % plan.rows;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    int second = x.second;
+    for (int j = x.first; j <= x.last; j += beside, second = 0) {
+      const float f = s_ml[j][second][row].x;
+      const float4 y = *reinterpret_cast<const float4*>(smem + j * S::kRing + second * kPartBytes + (row * (DB * 64) + l4) * 4);
+      v[0] = fmaf(y.x, f, v[0]); v[1] = fmaf(y.y, f, v[1]); v[2] = fmaf(y.z, f, v[2]); v[3] = fmaf(y.w, f, v[3]);
     }
+    if (x.to >= 0) write_values<T>(reinterpret_cast<T*>(a.out) + x.to + l4, x.sum, v);
+    else *reinterpret_cast<float4*>(plan.part_o + (-1 - x.to) * (DB * 64) + l4) = make_float4(v[0], v[1], v[2], v[3]);
   }
 }
 
@@ -779,7 +782,7 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
   }
   if (!works || sub != 0) return;
   const int t = (join.row0 + r) / a.group, h = (join.head + side) * a.group + (join.row0 + r) % a.group;
-  if (lane * 4 < a.head_dim) write_values<T>(a, join.b, t, h, lane, sum, v);
+  if (lane * 4 < a.head_dim) write_values<T>(reinterpret_cast<T*>(a.out) + offset_of(a.os, join.b, t, h) + lane * 4, sum, v);
   if (a.lse && lane == 0) write_lse<T>(a, join.b, t, h, top, sum);
 }
 
@@ -804,6 +807,7 @@ PagedPlan make_plan(const PagedArgs& a) {
     // at a time 68 and 96, eight 68 and 102. Heads of 128 on their own 95 us, two at a time 97.
     if (a.head_dim <= 64 && a.kv_heads % 2 == 0 && a.kps.head < a.kps.token) p.beside = 2;
   }
+  p.head_groups = a.kv_heads / p.beside;
   const int64_t warps = p.whole ? items : items * (most / kMinShare + 2);
   const int64_t room = (int64_t)kSms * kCtasPerSm;
   p.ctas = (int32_t)(warps < room ? (warps < 1 ? 1 : warps) : room);
