@@ -23,8 +23,8 @@ namespace swarm {
 namespace {
 
 constexpr int kRows = 16;
-constexpr int kWarps = 4;
-constexpr int kCtasPerSm = 2;
+constexpr int kWarps = 8;
+constexpr int kCtasPerSm = 1;                         // two of four warps: long documents 96 -> 101 us
 constexpr int kMinShare = 64;                           // positions that a warp's run has at least
 constexpr int kWholePositions = 128;                    // items of no more are not cut
 constexpr int kSms = 148;
@@ -177,7 +177,7 @@ __device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
 // NT: items of up to 8 NT rows. ONE_PAGE: pages hold a multiple of 16 positions, so sixteen of a block lie in one. Then a row's
 // address is one addition away from the last one's; else each position has its own, and a lane gets them by shuffles.
 template <typename T, int DB, int NT, bool ONE_PAGE>
-__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
+__global__ void __launch_bounds__(kWarps * 32 + 32, kCtasPerSm)         // a CTA of the joining kernel fits beside: 8192 registers
 paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   using S = Shape<DB>;
   constexpr int kPartBytes = kRows * DB * 64 * 4;
@@ -730,11 +730,16 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
   const int side = index / plan.rows % plan.beside, r = index % plan.rows;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (plan.joined < plan.ctas) {                        // fewer than CTAs: which CTA begins the c0-th
-    int seen = 0, found = plan.ctas;
-    for (int i = 0; i < plan.ctas && found == plan.ctas; i += 32) {
-      const uint32_t has = __ballot_sync(0xFFFFFFFFu, i + lane < plan.ctas && reinterpret_cast<const JoinInfo*>(plan.joins)[i + lane].rows > 0);
+    int there[(kSms * kCtasPerSm + 31) / 32], seen = 0, found = plan.ctas;
+#pragma unroll
+    for (int i = 0; i < (kSms * kCtasPerSm + 31) / 32; ++i)
+      there[i] = i * 32 + lane < plan.ctas ? reinterpret_cast<const JoinInfo*>(plan.joins)[i * 32 + lane].rows : 0;
+#pragma unroll
+    for (int i = 0; i < (kSms * kCtasPerSm + 31) / 32; ++i) {
+      const uint32_t has = __ballot_sync(0xFFFFFFFFu, there[i] > 0);
       const int here = __popc(has);
-      if (seen + here > c0) found = i + __fns(has, 0, c0 - seen + 1);
+      const uint32_t at = __ballot_sync(0xFFFFFFFFu, there[i] > 0 && __popc(has & ((1u << lane) - 1u)) == c0 - seen);
+      if (at) found = i * 32 + __ffs(at) - 1;
       seen += here;
     }
     c0 = found;
@@ -770,13 +775,20 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
       for (int e = 0; e < 4; ++e) mine[2 + lane * 4 + e] = v[e];
     if (lane == 0) { mine[0] = top; mine[1] = sum; }
     __syncthreads();
-    if (sub == 0) {
-      for (int i = 1; i < plan.join_warps; ++i) {
-        const float* x = mine + i * pitch;
-        float f0, f1;
-        join_ml(top, sum, x[0], x[1], c, f0, f1);
+    if (works && sub == 0) {                            // lane = a warp's part
+      const float m0 = lane < plan.join_warps ? mine[lane * pitch] : -INFINITY;
+      top = m0;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+      const float f = ex2((m0 - (top == -INFINITY ? 0.0f : top)) * c);
+      sum = warp_sum(lane < plan.join_warps ? mine[lane * pitch + 1] * f : 0.0f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = 0.0f;
+#pragma unroll 8
+      for (int i = 0; i < plan.join_warps; ++i) {
+        const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
         if (lane * 4 < a.head_dim)
-          for (int e = 0; e < 4; ++e) v[e] = v[e] * f0 + x[2 + lane * 4 + e] * f1;
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(mine[i * pitch + 2 + lane * 4 + e], fi, v[e]);
       }
     }
   }
@@ -853,7 +865,7 @@ cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
     else e = one_page ? launch_as<T, 2, 2, true>(a, p, st) : launch_as<T, 2, 2, false>(a, p, st);
   }
   if (e != cudaSuccess || p.whole || p.ctas == 1) return e;
-  const int warps = p.join_warps > 8 ? p.join_warps : 8, each = warps / p.join_warps;
+  const int warps = p.join_warps > 4 ? p.join_warps : 4, each = warps / p.join_warps;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((p.joined * p.beside * p.rows + each - 1) / each);
   cfg.blockDim = dim3(warps * 32);
