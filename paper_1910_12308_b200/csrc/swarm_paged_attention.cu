@@ -177,7 +177,7 @@ __device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
 // NT: items of up to 8 NT rows. ONE_PAGE: pages hold a multiple of 16 positions, so sixteen of a block lie in one. Then a row's
 // address is one addition away from the last one's; else each position has its own, and a lane gets them by shuffles.
 template <typename T, int DB, int NT, bool ONE_PAGE>
-__global__ void __launch_bounds__(kWarps * 32 + 32, kCtasPerSm)         // a CTA of the joining kernel fits beside: 8192 registers
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
 paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   using S = Shape<DB>;
   constexpr int kPartBytes = kRows * DB * 64 * 4;
