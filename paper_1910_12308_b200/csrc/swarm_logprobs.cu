@@ -1,12 +1,23 @@
 // Log probabilities of given tokens with entropy and the likeliest tokens, and their gradient with respect to the logits.
+//
+// Forward: one walk over a row with the running maximum, sum and weighted sum of each thread's logits; HBM is the bound where rows are
+// many. Rows of up to 1024 logits take a warp each, longer ones a CTA, and where these are too few for the device a
+// cluster of up to eight CTAs, which meet in shared memory of the first. The likeliest tokens take a second walk (over L2):
+// the first leaves a number that at least `top` logits of the CTA reach, so of the second's logits hardly more than `top` are
+// looked at twice. They are kept as (logit, place) in one 64-bit key, a lane each, so that their order is that of numbers.
+// Gradient: one walk, a logit read and a gradient written.
 #include <cmath>
+#include <mutex>
 
 #include "swarm_opsup.cuh"
+#include "swarm_tc.cuh"
 
 namespace swarm {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr float kFar = -3.402823466e38f;                // stands for differences of -infinity, whose exponential 0 they are multiplied with
 
 __device__ __forceinline__ float ex2(float x) {
   float r;
@@ -27,94 +38,414 @@ struct LogProbsArgs {
 };
 
 // A logit and its place as one number: larger logits first, of equal ones the lowest place; NaN above all, -0 as 0. 0 is no key.
-__device__ __forceinline__ uint64_t key_of(float v, uint32_t place) {
-  uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);
-  u = isnan(v) ? 0xFFFFFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
-  return (uint64_t)u << 32 | (uint32_t)~place;
+__device__ __forceinline__ uint32_t rank_of(float v) {
+  const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);
+  return isnan(v) ? 0xFFFFFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t key_of(float v, uint32_t place) { return (uint64_t)rank_of(v) << 32 | (uint32_t)~place; }
+
+// What a part of a row adds up to: its largest logit, and with d = logit - largest the sums of exp(scale d) and exp(scale d) d.
+// A part of nothing but -infinity has sums of 0. c = scale * log2(e).
+struct Sums {
+  float m, s, w;
+};
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+// The sums taken against a larger maximum.
+template <bool ENTROPY>
+__device__ __forceinline__ void rebase(Sums& x, float m, float c) {
+  if (x.m == m) return;
+  const float d = x.m - m, f = ex2(d * c);
+  if (ENTROPY) x.w = f == 0.0f ? 0.0f : (x.w + x.s * d) * f;
+  x.s *= f;
+  x.m = m;
+}
+template <bool ENTROPY>
+__device__ __forceinline__ Sums joined(Sums a, Sums b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  rebase<ENTROPY>(a, m, c);
+  rebase<ENTROPY>(b, m, c);
+  return Sums{m, a.s + b.s, ENTROPY ? a.w + b.w : 0.0f};
+}
+template <bool ENTROPY>
+__device__ __forceinline__ Sums warp_joined(Sums x, float c) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Sums y;
+    y.m = __shfl_xor_sync(kAll, x.m, o);
+    y.s = __shfl_xor_sync(kAll, x.s, o);
+    y.w = ENTROPY ? __shfl_xor_sync(kAll, x.w, o) : 0.0f;
+    x = joined<ENTROPY>(x, y, c);
+  }
+  return x;
 }
 
-// CTA = one row, three walks over it: its largest logit, its sums, and one for each of the likeliest tokens.
-template <typename T>
-__global__ void __launch_bounds__(256) log_probs_kernel(LogProbsArgs a) {
-  __shared__ float s_f[8], s_g[8];
-  __shared__ uint64_t s_k[8];
-  const int64_t row = blockIdx.x;
-  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.pitch;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  auto largest_below = [&](uint64_t bound) {
-    uint64_t best = 0;
-    for (int64_t i = threadIdx.x; i < a.cols; i += 256) {
-      const uint64_t k = key_of(to_float<T>(x[i]), (uint32_t)i);
-      if (k < bound && k > best) best = k;
-    }
-    for (int o = 16; o > 0; o >>= 1) { const uint64_t k = __shfl_xor_sync(0xFFFFFFFFu, best, o); best = k > best ? k : best; }
-    __syncthreads();
-    if (lane == 0) s_k[warp] = best;
-    __syncthreads();
-    for (int w = 0; w < 8; ++w) best = s_k[w] > best ? s_k[w] : best;
-    return best;
-  };
-  const uint64_t first = largest_below(~0ull);
-  const float top = to_float<T>(x[~(uint32_t)first]), base = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, weighted = 0.0f;
-  for (int64_t i = threadIdx.x; i < a.cols; i += 256) {
-    const float d = (to_float<T>(x[i]) - base) * a.scale, e = ex2(d * kLog2e);
-    sum += e;
-    weighted += e == 0.0f ? 0.0f : e * d;
+// Elements [0, n) of a row whose first one may lie anywhere: `head` elements up to a 16-byte boundary, `vectors` of 16 bytes, a tail.
+template <typename T> struct Span {
+  static constexpr int kPer = 16 / (int)sizeof(T);
+  const T* p;
+  int head, vectors, n;
+  __device__ __forceinline__ Span(const T* row, int64_t cols) {
+    p = row;
+    n = (int)cols;
+    head = min(n, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));
+    vectors = (n - head) / kPer;
   }
-  sum = warp_sum(sum);
-  weighted = warp_sum(weighted);
-  if (lane == 0) { s_f[warp] = sum; s_g[warp] = weighted; }
-  __syncthreads();
-  sum = weighted = 0.0f;
-  for (int w = 0; w < 8; ++w) { sum += s_f[w]; weighted += s_g[w]; }
-  const float log_sum = logf(sum);
-  auto log_prob = [&](float v) { return top == -INFINITY ? -INFINITY : (v - base) * a.scale - log_sum; };
-  if (threadIdx.x == 0) {
-    a.stats[row * 2] = top;
+  __device__ __forceinline__ const uint4* at(int v) const { return reinterpret_cast<const uint4*>(p + head) + v; }
+  // the elements outside the vectors, at most 2 (kPer - 1): number i of them
+  __device__ __forceinline__ int loose() const { return n - vectors * kPer; }
+  __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + vectors * kPer; }
+};
+template <typename T> __device__ __forceinline__ void unpack(const uint4& r, float* v) {
+  if constexpr (sizeof(T) == 4) {
+    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+  } else {
+    unpack2<T>(r.x, v[0], v[1]); unpack2<T>(r.y, v[2], v[3]); unpack2<T>(r.z, v[4], v[5]); unpack2<T>(r.w, v[6], v[7]);
+  }
+}
+
+// N logits into a thread's sums.
+template <bool ENTROPY, int N>
+__device__ __forceinline__ void add_logits(Sums& x, const float* v, float c) {
+  float m[2] = {v[0], v[1 % N]};
+#pragma unroll
+  for (int i = 2; i + 1 < N; i += 2) { m[0] = fmaxf(m[0], v[i]); m[1] = fmaxf(m[1], v[i + 1]); }
+  const float most = fmaxf(m[0], m[1]);
+  if (most > x.m) rebase<ENTROPY>(x, most, c);          // rarely after the first few
+  const float base = base_of(x.m);
+  float s[2] = {0.0f, 0.0f}, w[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    if (N == 1) {
+      const float d = v[0] - base, e = ex2(d * c);
+      s[0] = e;
+      if (ENTROPY) w[0] = e * fmaxf(d, kFar);
+      break;
+    }
+    float d0, d1, e0, e1;
+    add2(d0, d1, v[i], v[i + 1], -base, -base);
+    mul2(e0, e1, d0, d1, c, c);
+    e0 = ex2(e0);
+    e1 = ex2(e1);
+    add2(s[0], s[1], s[0], s[1], e0, e1);
+    if (ENTROPY) {                                      // a NaN comes in through the exponential
+      d0 = fmaxf(d0, kFar);
+      d1 = fmaxf(d1, kFar);
+      fma2(w[0], w[1], e0, e1, d0, d1, w[0], w[1]);
+    }
+  }
+  x.s += s[0] + s[1];
+  if (ENTROPY) x.w += w[0] + w[1];
+}
+
+// The likeliest of what a warp has seen: lane i holds the i-th key, in descending order.
+struct Best {
+  uint64_t key;
+  // all lanes; keys of the lanes where `has`
+  __device__ __forceinline__ void add(uint64_t k, bool has, int top, int lane) {
+    const uint64_t least = __shfl_sync(kAll, key, top - 1);
+    uint32_t todo = __ballot_sync(kAll, has && k > least);
+    while (todo) {
+      const int from = __ffs(todo) - 1;
+      todo &= todo - 1;
+      const uint64_t x = __shfl_sync(kAll, k, from), before = __shfl_up_sync(kAll, key, 1);
+      const int at = __popc(__ballot_sync(kAll, key > x));
+      key = lane < at ? key : lane == at ? x : before;
+    }
+  }
+  // with another list in descending order: the 32 largest of both, in descending order
+  __device__ __forceinline__ void merge(uint64_t other, int lane) {
+    const uint64_t y = __shfl_sync(kAll, other, 31 - lane);
+    uint64_t x = key > y ? key : y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const uint64_t z = __shfl_xor_sync(kAll, x, o);
+      x = (lane & o) == 0 ? (x > z ? x : z) : (x < z ? x : z);
+    }
+    key = x;
+  }
+};
+
+// Writes a row's results; one warp, the row's sums and its best keys in every lane.
+template <typename T>
+__device__ __forceinline__ void write_results(const LogProbsArgs& a, int64_t row, const T* x, const Sums& sums, const Best& best, int lane) {
+  const float base = base_of(sums.m), log_sum = logf(sums.s);
+  const bool none = sums.s == 0.0f;                     // not a token is left: else the largest one's exponential is 1
+  auto log_prob = [&](float v) { return none ? -INFINITY : (v - base) * a.scale - log_sum; };
+  if (lane == 0) {
+    a.stats[row * 2] = isnan(sums.s) && sums.m != INFINITY ? sums.s : sums.m;       // maxima pass NaN by
     a.stats[row * 2 + 1] = log_sum;
     if (a.log_probs) {
       const int64_t t = a.tokens[row];
       a.log_probs[row] = t >= 0 && t < a.cols ? log_prob(to_float<T>(x[t])) : 0.0f;
     }
-    if (a.entropy) a.entropy[row] = top == -INFINITY ? 0.0f : log_sum - weighted / sum;
+    if (a.entropy) a.entropy[row] = none ? 0.0f : log_sum - a.scale * (sums.w / sums.s);
   }
-  uint64_t key = first;
-  for (int k = 0; k < a.top; ++k) {
-    if (k > 0) key = largest_below(key);
-    if (threadIdx.x == 0) {
-      const uint32_t place = ~(uint32_t)key;
-      a.top_tokens[row * a.top + k] = place;
-      a.top_log_probs[row * a.top + k] = log_prob(to_float<T>(x[place]));
+  if (lane < a.top) {
+    const uint32_t place = ~(uint32_t)best.key;
+    a.top_tokens[row * a.top + lane] = place;
+    a.top_log_probs[row * a.top + lane] = log_prob(to_float<T>(x[place]));
+  }
+}
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+// Warp = a row of at most 1024 logits.
+template <typename T, bool ENTROPY>
+__global__ void __launch_bounds__(kThreads) log_probs_short_kernel(LogProbsArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (row >= a.rows) return;
+  const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
+  constexpr int kPer = Span<T>::kPer;
+  const float c = a.scale * kLog2e;
+  Sums sums{-INFINITY, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = lane; i < span.vectors; i += 32) {
+    float v[kPer];
+    unpack<T>(*span.at(i), v);
+    add_logits<ENTROPY, kPer>(sums, v, c);
+  }
+  if (lane < span.loose()) {
+    const float v = to_float<T>(span.p[span.loose_at(lane)]);
+    add_logits<ENTROPY, 1>(sums, &v, c);
+  }
+  const uint32_t r = rank_of(sums.m);
+  sums = warp_joined<ENTROPY>(sums, c);
+  Best best{0};
+  if (a.top > 0) {
+    // the top-th largest of the lanes' largest logits: `top` logits reach it
+    int before = 0;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+      const uint32_t x = __shfl_sync(kAll, r, i);
+      before += x > r || (x == r && i < lane);
+    }
+    const uint32_t floor = __shfl_sync(kAll, r, __ffs(__ballot_sync(kAll, before == a.top - 1)) - 1);
+    for (int i0 = 0; i0 < span.n; i0 += 32) {
+      const int i = i0 + lane;
+      const float v = i < span.n ? to_float<T>(span.p[i]) : 0.0f;
+      best.add(key_of(v, (uint32_t)i), i < span.n && rank_of(v) >= floor, a.top, lane);
     }
   }
+  write_results<T>(a, row, span.p, sums, best, lane);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) log_probs_grad_kernel(LogProbsArgs a) {
-  const int64_t row = blockIdx.x;
-  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.pitch;
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// The address of the first CTA's copy of a variable in shared memory.
+__device__ __forceinline__ uint32_t in_first(const void* p) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  return r;
+}
+__device__ __forceinline__ void store_remote(uint32_t at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(at), "f"(v) : "memory"); }
+__device__ __forceinline__ void store_remote(uint32_t at, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(at), "l"(v) : "memory"); }
+
+// CTA, or cluster of CTAS of them, = a row.
+template <typename T, bool ENTROPY, int CTAS>
+__global__ void __launch_bounds__(kThreads) log_probs_kernel(LogProbsArgs a) {
+  constexpr int kPer = Span<T>::kPer;
+  __shared__ Sums s_sums[kWarps], s_row[8];
+  __shared__ uint64_t s_keys[kWarps][32], s_row_keys[8][32];
+  __shared__ __align__(16) uint32_t s_ranks[kThreads];
+  __shared__ uint32_t s_floor;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if constexpr (CTAS > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+  const int64_t row = blockIdx.x / CTAS;
+  const int part = CTAS > 1 ? (int)cluster_rank() : 0;
+  const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
+  // this CTA's vectors; the elements outside them are the first one's
+  const int begin = (int)((int64_t)span.vectors * part / CTAS), end = (int)((int64_t)span.vectors * (part + 1) / CTAS);
+  const float c = a.scale * kLog2e;
+  Sums sums{-INFINITY, 0.0f, 0.0f};
+  constexpr int kAhead = 4;
+  for (int i0 = begin + tid; i0 < end; i0 += kAhead * kThreads) {
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * kThreads < end) raw[u] = *span.at(i0 + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * kThreads < end) {
+        float v[kPer];
+        unpack<T>(raw[u], v);
+        add_logits<ENTROPY, kPer>(sums, v, c);
+      }
+  }
+  const bool loose = part == 0 && tid < span.loose();
+  const float loose_logit = loose ? to_float<T>(span.p[span.loose_at(tid)]) : 0.0f;
+  if (loose) add_logits<ENTROPY, 1>(sums, &loose_logit, c);
+  const float mine = sums.m;
+  sums = warp_joined<ENTROPY>(sums, c);
+  if (lane == 0) s_sums[warp] = sums;
+  if (a.top > 0) s_ranks[tid] = rank_of(mine);
+  __syncthreads();
+  Best best{0};
+  if (a.top > 0) {
+    // the top-th largest of the threads' largest logits: `top` logits of this CTA reach it
+    const uint32_t r = s_ranks[tid];
+    int before = 0;
+#pragma unroll 8
+    for (int i = 0; i < kThreads; i += 4) {
+      const uint4 x = *reinterpret_cast<const uint4*>(s_ranks + i);
+      before += (x.x > r || (x.x == r && i < tid)) + (x.y > r || (x.y == r && i + 1 < tid)) + (x.z > r || (x.z == r && i + 2 < tid)) + (x.w > r || (x.w == r && i + 3 < tid));
+    }
+    if (before == a.top - 1) s_floor = r;
+    __syncthreads();
+    const uint32_t floor = s_floor;
+    uint32_t last = 0;                                  // rank of the warp's top-th best so far
+    auto look = [&](float v, int place, bool has) {
+      best.add(key_of(v, (uint32_t)place), has && rank_of(v) >= floor, a.top, lane);
+      last = (uint32_t)(__shfl_sync(kAll, best.key, a.top - 1) >> 32);
+    };
+    if (__any_sync(kAll, loose)) look(loose_logit, loose ? span.loose_at(tid) : 0, loose);
+    for (int i0 = begin + warp * 32; i0 < end; i0 += kThreads) {
+      const int i = i0 + lane;
+      float v[kPer];
+      uint32_t ranks = 0;
+      if (i < end) {
+        unpack<T>(*span.at(i), v);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) ranks = max(ranks, rank_of(v[u]));
+      }
+      // equal to the top-th best: a later place, unless the list has it from the loose elements behind the vectors
+      if (!__any_sync(kAll, ranks >= floor && ranks >= last)) continue;
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) look(v[u], span.head + i * kPer + u, i < end);
+    }
+    s_keys[warp][lane] = best.key;
+    __syncthreads();
+  }
+  if (warp == 0) {
+    sums = s_sums[0];
+    for (int w = 1; w < kWarps; ++w) sums = joined<ENTROPY>(sums, s_sums[w], c);
+    if (a.top > 0)
+      for (int w = 1; w < kWarps; ++w) best.merge(s_keys[w][lane], lane);
+  }
+  if constexpr (CTAS > 1) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");       // the first CTA has begun: its shared memory is there
+    if (warp == 0) {
+      if (lane == 0) {
+        store_remote(in_first(&s_row[part].m), sums.m);
+        store_remote(in_first(&s_row[part].s), sums.s);
+        store_remote(in_first(&s_row[part].w), sums.w);
+      }
+      if (a.top > 0) store_remote(in_first(&s_row_keys[part][lane]), best.key);
+    }
+    cluster_sync();
+    if (part != 0 || warp != 0) return;
+    for (int i = 1; i < CTAS; ++i) {
+      sums = joined<ENTROPY>(sums, s_row[i], c);
+      if (a.top > 0) best.merge(s_row_keys[i][lane], lane);
+    }
+  }
+  if (warp == 0) write_results<T>(a, row, span.p, sums, best, lane);
+}
+
+// Gradient: CTA = a row, or `parts` CTAs for long ones. SAME: rows of logits and gradients lie alike to 16 bytes.
+template <typename T, bool ENTROPY>
+__global__ void __launch_bounds__(kThreads) log_probs_grad_kernel(LogProbsArgs a, int parts, int threads_per_row) {
+  constexpr int kPer = Span<T>::kPer;
+  const int rows_here = kThreads / threads_per_row, tid = threadIdx.x % threads_per_row;
+  const int64_t row = (int64_t)(blockIdx.x / parts) * rows_here + threadIdx.x / threads_per_row;
+  const int part = blockIdx.x % parts;
+  if (row >= a.rows) return;
+  const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
   T* dx = reinterpret_cast<T*>(a.dlogits) + row * a.dlogits_pitch;
+  const bool same = (((uintptr_t)dx ^ (uintptr_t)span.p) & 15) == 0;
   const float top = a.stats[row * 2], log_sum = a.stats[row * 2 + 1];
-  const int64_t t = a.tokens ? a.tokens[row] : -1;
-  const float g = a.dlog_probs && t >= 0 && t < a.cols ? a.dlog_probs[row] : 0.0f;
-  const float h = a.dentropy ? a.dentropy[row] : 0.0f, entropy = a.dentropy ? a.entropy[row] : 0.0f;
-  for (int64_t i = threadIdx.x; i < a.cols; i += 256) {
-    const float logp = (to_float<T>(x[i]) - top) * a.scale - log_sum, p = ex2(logp * kLog2e);
-    float v = (i == t ? g : 0.0f) - g * p;
-    if (a.dentropy && p != 0.0f) v -= h * p * (logp + entropy);
-    dx[i] = from_float<T>(top == -INFINITY ? 0.0f : v * a.scale);
+  const int64_t t64 = a.tokens ? a.tokens[row] : -1;
+  const int t = t64 >= 0 && t64 < a.cols ? (int)t64 : -1;
+  const float g = a.dlog_probs && t >= 0 ? a.dlog_probs[row] * a.scale : 0.0f;
+  const float h = ENTROPY ? a.dentropy[row] * a.scale : 0.0f, entropy = ENTROPY ? a.entropy[row] : 0.0f;
+  const bool none = top == -INFINITY;
+  // with l = log p: p (-g - h (l + entropy)), and g more at the token. The token's is g (1 - p), not g - g p of rounded parts
+  auto gradient = [&](float v, int i) {
+    const float l = (v - top) * a.scale - log_sum, p = ex2(l * kLog2e);
+    float r = i == t ? g * (1.0f - p) : -g * p;
+    if (ENTROPY) r -= p == 0.0f ? 0.0f : p * (h * (l + entropy));
+    return none ? 0.0f : r;
+  };
+  const int begin = (int)((int64_t)span.vectors * part / parts), end = (int)((int64_t)span.vectors * (part + 1) / parts);
+  constexpr int kAhead = 4;
+  for (int i0 = begin + tid; i0 < end; i0 += kAhead * threads_per_row) {
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * threads_per_row < end) raw[u] = *span.at(i0 + u * threads_per_row);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * threads_per_row < end) {
+        const int first = span.head + (i0 + u * threads_per_row) * kPer;
+        float v[kPer];
+        unpack<T>(raw[u], v);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] = gradient(v[e], first + e);
+        if (same) {
+          uint4 w;
+          if constexpr (sizeof(T) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+          else w = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4 % kPer], v[5 % kPer]), pack2<T>(v[6 % kPer], v[7 % kPer]));
+          *reinterpret_cast<uint4*>(dx + first) = w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) dx[first + e] = from_float<T>(v[e]);
+        }
+      }
+  }
+  if (part == 0 && tid < span.loose()) {
+    const int i = span.loose_at(tid);
+    dx[i] = from_float<T>(gradient(to_float<T>(span.p[i]), i));
   }
 }
 
+template <typename T, bool ENTROPY, int CTAS>
+cudaError_t launch_rows(const LogProbsArgs& a, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.rows * CTAS));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = CTAS;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = CTAS > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, log_probs_kernel<T, ENTROPY, CTAS>, a);
+}
+
+constexpr int kShort = 1024;                            // logits of a row that a warp takes
+template <typename T, bool ENTROPY>
+cudaError_t launch_forward_as(const LogProbsArgs& a, cudaStream_t st) {
+  if (a.cols <= kShort) {
+    log_probs_short_kernel<T, ENTROPY><<<(unsigned)((a.rows + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  // as many CTAs to a row as leave two thousand logits to each and fill the device's 148 multiprocessors twice over
+  int ctas = 1;
+  while (ctas < 8 && a.rows * ctas < 296 && a.cols >= ctas * 4096) ctas *= 2;
+  return ctas == 1 ? launch_rows<T, ENTROPY, 1>(a, st) : ctas == 2 ? launch_rows<T, ENTROPY, 2>(a, st)
+       : ctas == 4 ? launch_rows<T, ENTROPY, 4>(a, st) : launch_rows<T, ENTROPY, 8>(a, st);
+}
 template <typename T>
 cudaError_t launch_forward(const LogProbsArgs& a, cudaStream_t st) {
-  log_probs_kernel<T><<<(unsigned)a.rows, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  return a.entropy ? launch_forward_as<T, true>(a, st) : launch_forward_as<T, false>(a, st);
 }
 template <typename T>
 cudaError_t launch_backward(const LogProbsArgs& a, cudaStream_t st) {
-  log_probs_grad_kernel<T><<<(unsigned)a.rows, 256, 0, st>>>(a);
+  // a warp for short rows; several CTAs for a long row where rows are few
+  const int threads = a.cols <= kShort ? 32 : kThreads;
+  const int64_t groups = (a.rows * threads + kThreads - 1) / kThreads;
+  int parts = 1;
+  while (threads == kThreads && groups * parts < 1184 && a.cols >= (int64_t)parts * 8192 && parts < 64) parts *= 2;
+  if (groups * parts >= (int64_t)1 << 31) return cudaErrorInvalidConfiguration;
+  if (a.dentropy) log_probs_grad_kernel<T, true><<<(unsigned)(groups * parts), kThreads, 0, st>>>(a, parts, threads);
+  else log_probs_grad_kernel<T, false><<<(unsigned)(groups * parts), kThreads, 0, st>>>(a, parts, threads);
   return cudaGetLastError();
 }
 
