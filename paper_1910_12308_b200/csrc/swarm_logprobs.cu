@@ -42,6 +42,7 @@ __device__ __forceinline__ uint32_t rank_of(float v) {
   const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);
   return isnan(v) ? 0xFFFFFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of(uint32_t rank) { return __uint_as_float(rank & 0x80000000u ? rank & 0x7FFFFFFFu : ~rank); }
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t place) { return (uint64_t)rank_of(v) << 32 | (uint32_t)~place; }
 
 // What a part of a row adds up to: its largest logit, and with d = logit - largest the sums of exp(scale d) and exp(scale d) d.
@@ -59,22 +60,17 @@ __device__ __forceinline__ void rebase(Sums& x, float m, float c) {
   x.s *= f;
   x.m = m;
 }
-template <bool ENTROPY>
-__device__ __forceinline__ Sums joined(Sums a, Sums b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  rebase<ENTROPY>(a, m, c);
-  rebase<ENTROPY>(b, m, c);
-  return Sums{m, a.s + b.s, ENTROPY ? a.w + b.w : 0.0f};
-}
-template <bool ENTROPY>
-__device__ __forceinline__ Sums warp_joined(Sums x, float c) {
+// The sums of LANES neighbouring lanes, in each of them.
+template <bool ENTROPY, int LANES>
+__device__ __forceinline__ Sums lanes_joined(Sums x, float c) {
+  float m = x.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Sums y;
-    y.m = __shfl_xor_sync(kAll, x.m, o);
-    y.s = __shfl_xor_sync(kAll, x.s, o);
-    y.w = ENTROPY ? __shfl_xor_sync(kAll, x.w, o) : 0.0f;
-    x = joined<ENTROPY>(x, y, c);
+  for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
+  rebase<ENTROPY>(x, m, c);
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    x.s += __shfl_xor_sync(kAll, x.s, o);
+    if (ENTROPY) x.w += __shfl_xor_sync(kAll, x.w, o);
   }
   return x;
 }
@@ -137,11 +133,23 @@ __device__ __forceinline__ void add_logits(Sums& x, const float* v, float c) {
   if (ENTROPY) x.w += w[0] + w[1];
 }
 
+// How many of the lanes' numbers come before this one in descending order (of equal ones the lower lane's).
+__device__ __forceinline__ int place_among(uint32_t x, int lane) {
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t y = __shfl_sync(kAll, x, i);
+    before += y > x || (y == x && i < lane);
+  }
+  return before;
+}
+
 // The likeliest of what a warp has seen: lane i holds the i-th key, in descending order.
 struct Best {
   uint64_t key;
   // all lanes; keys of the lanes where `has`
   __device__ __forceinline__ void add(uint64_t k, bool has, int top, int lane) {
+    if (!__any_sync(kAll, has)) return;
     const uint64_t least = __shfl_sync(kAll, key, top - 1);
     uint32_t todo = __ballot_sync(kAll, has && k > least);
     while (todo) {
@@ -165,69 +173,91 @@ struct Best {
   }
 };
 
+// The token that is given for a row and its logit, looked up ahead of time; -1: none, or a padded place.
+template <typename T> struct Given {
+  int64_t token;
+  float logit;
+  __device__ __forceinline__ Given(const LogProbsArgs& a, int64_t row, const T* x) {
+    token = a.tokens ? a.tokens[row] : -1;
+    if (token >= a.cols) token = -1;
+    logit = token >= 0 ? to_float<T>(x[token]) : 0.0f;
+  }
+};
+
+// N lists, list w < N held by warp w and in shared memory, into the first warp's; all warps of a CTA.
+template <int N>
+__device__ __forceinline__ void merge_lists(uint64_t (*lists)[32], Best& mine, int warp, int lane) {
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (warp < n) {
+      mine.merge(lists[warp + n][lane], lane);
+      lists[warp][lane] = mine.key;
+    }
+  }
+}
+
 // Writes a row's results; one warp, the row's sums and its best keys in every lane.
 template <typename T>
-__device__ __forceinline__ void write_results(const LogProbsArgs& a, int64_t row, const T* x, const Sums& sums, const Best& best, int lane) {
+__device__ __forceinline__ void write_results(const LogProbsArgs& a, int64_t row, const Given<T>& given, const Sums& sums, const Best& best, int lane) {
   const float base = base_of(sums.m), log_sum = logf(sums.s);
   const bool none = sums.s == 0.0f;                     // not a token is left: else the largest one's exponential is 1
   auto log_prob = [&](float v) { return none ? -INFINITY : (v - base) * a.scale - log_sum; };
   if (lane == 0) {
     a.stats[row * 2] = isnan(sums.s) && sums.m != INFINITY ? sums.s : sums.m;       // maxima pass NaN by
     a.stats[row * 2 + 1] = log_sum;
-    if (a.log_probs) {
-      const int64_t t = a.tokens[row];
-      a.log_probs[row] = t >= 0 && t < a.cols ? log_prob(to_float<T>(x[t])) : 0.0f;
-    }
+    if (a.log_probs) a.log_probs[row] = given.token >= 0 ? log_prob(given.logit) : 0.0f;
     if (a.entropy) a.entropy[row] = none ? 0.0f : log_sum - a.scale * (sums.w / sums.s);
   }
   if (lane < a.top) {
-    const uint32_t place = ~(uint32_t)best.key;
-    a.top_tokens[row * a.top + lane] = place;
-    a.top_log_probs[row * a.top + lane] = log_prob(to_float<T>(x[place]));
+    a.top_tokens[row * a.top + lane] = ~(uint32_t)best.key;
+    a.top_log_probs[row * a.top + lane] = log_prob(logit_of((uint32_t)(best.key >> 32)));
   }
 }
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // Warp = a row of at most 1024 logits.
-template <typename T, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads) log_probs_short_kernel(LogProbsArgs a) {
+template <typename T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_short_kernel(LogProbsArgs a) {
   const int lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (row >= a.rows) return;
   const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
-  constexpr int kPer = Span<T>::kPer;
+  constexpr int kPer = Span<T>::kPer, kAhead = 4;
+  const Given<T> given(a, row, span.p);
   const float c = a.scale * kLog2e;
   Sums sums{-INFINITY, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int i = lane; i < span.vectors; i += 32) {
-    float v[kPer];
-    unpack<T>(*span.at(i), v);
-    add_logits<ENTROPY, kPer>(sums, v, c);
+  for (int i0 = lane; i0 < span.vectors; i0 += kAhead * 32) {
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * 32 < span.vectors) raw[u] = *span.at(i0 + u * 32);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u * 32 < span.vectors) {
+        float v[kPer];
+        unpack<T>(raw[u], v);
+        add_logits<ENTROPY, kPer>(sums, v, c);
+      }
   }
   if (lane < span.loose()) {
     const float v = to_float<T>(span.p[span.loose_at(lane)]);
     add_logits<ENTROPY, 1>(sums, &v, c);
   }
-  const uint32_t r = rank_of(sums.m);
-  sums = warp_joined<ENTROPY>(sums, c);
+  const uint32_t mine = rank_of(sums.m);
+  sums = lanes_joined<ENTROPY, 32>(sums, c);
   Best best{0};
-  if (a.top > 0) {
+  if constexpr (TOP) {
     // the top-th largest of the lanes' largest logits: `top` logits reach it
-    int before = 0;
-#pragma unroll 8
-    for (int i = 0; i < 32; ++i) {
-      const uint32_t x = __shfl_sync(kAll, r, i);
-      before += x > r || (x == r && i < lane);
-    }
-    const uint32_t floor = __shfl_sync(kAll, r, __ffs(__ballot_sync(kAll, before == a.top - 1)) - 1);
+    const float floor = logit_of(__shfl_sync(kAll, mine, __ffs(__ballot_sync(kAll, place_among(mine, lane) == a.top - 1)) - 1));
     for (int i0 = 0; i0 < span.n; i0 += 32) {
       const int i = i0 + lane;
       const float v = i < span.n ? to_float<T>(span.p[i]) : 0.0f;
-      best.add(key_of(v, (uint32_t)i), i < span.n && rank_of(v) >= floor, a.top, lane);
+      best.add(key_of(v, (uint32_t)i), i < span.n && !(v < floor), a.top, lane);
     }
   }
-  write_results<T>(a, row, span.p, sums, best, lane);
+  write_results<T>(a, row, given, sums, best, lane);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -248,18 +278,19 @@ __device__ __forceinline__ void store_remote(uint32_t at, float v) { asm volatil
 __device__ __forceinline__ void store_remote(uint32_t at, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(at), "l"(v) : "memory"); }
 
 // CTA, or cluster of CTAS of them, = a row.
-template <typename T, bool ENTROPY, int CTAS>
-__global__ void __launch_bounds__(kThreads) log_probs_kernel(LogProbsArgs a) {
+template <typename T, bool ENTROPY, bool TOP, int CTAS>
+__global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(LogProbsArgs a) {
   constexpr int kPer = Span<T>::kPer;
   __shared__ Sums s_sums[kWarps], s_row[8];
-  __shared__ uint64_t s_keys[kWarps][32], s_row_keys[8][32];
-  __shared__ __align__(16) uint32_t s_ranks[kThreads];
-  __shared__ uint32_t s_floor;
+  __shared__ uint64_t s_keys[TOP ? kWarps : 1][32], s_row_keys[TOP ? CTAS : 1][32];
+  __shared__ __align__(16) uint32_t s_largest[kWarps][8];
+  __shared__ float s_floor;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if constexpr (CTAS > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
   const int64_t row = blockIdx.x / CTAS;
   const int part = CTAS > 1 ? (int)cluster_rank() : 0;
   const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
+  const Given<T> given(a, row, span.p);
   // this CTA's vectors; the elements outside them are the first one's
   const int begin = (int)((int64_t)span.vectors * part / CTAS), end = (int)((int64_t)span.vectors * (part + 1) / CTAS);
   const float c = a.scale * kLog2e;
@@ -282,51 +313,60 @@ __global__ void __launch_bounds__(kThreads) log_probs_kernel(LogProbsArgs a) {
   const float loose_logit = loose ? to_float<T>(span.p[span.loose_at(tid)]) : 0.0f;
   if (loose) add_logits<ENTROPY, 1>(sums, &loose_logit, c);
   const float mine = sums.m;
-  sums = warp_joined<ENTROPY>(sums, c);
+  sums = lanes_joined<ENTROPY, 32>(sums, c);
   if (lane == 0) s_sums[warp] = sums;
-  if (a.top > 0) s_ranks[tid] = rank_of(mine);
+  if constexpr (TOP) {
+    // the top-th largest of the eight largest of each warp's threads' largest logits: `top` logits of this CTA reach it
+    const uint32_t r = rank_of(mine);
+    const int before = place_among(r, lane);
+    if (before < 8) s_largest[warp][before] = r;
+  }
   __syncthreads();
   Best best{0};
-  if (a.top > 0) {
-    // the top-th largest of the threads' largest logits: `top` logits of this CTA reach it
-    const uint32_t r = s_ranks[tid];
-    int before = 0;
-#pragma unroll 8
-    for (int i = 0; i < kThreads; i += 4) {
-      const uint4 x = *reinterpret_cast<const uint4*>(s_ranks + i);
-      before += (x.x > r || (x.x == r && i < tid)) + (x.y > r || (x.y == r && i + 1 < tid)) + (x.z > r || (x.z == r && i + 2 < tid)) + (x.w > r || (x.w == r && i + 3 < tid));
-    }
-    if (before == a.top - 1) s_floor = r;
-    __syncthreads();
-    const uint32_t floor = s_floor;
-    uint32_t last = 0;                                  // rank of the warp's top-th best so far
-    auto look = [&](float v, int place, bool has) {
-      best.add(key_of(v, (uint32_t)place), has && rank_of(v) >= floor, a.top, lane);
-      last = (uint32_t)(__shfl_sync(kAll, best.key, a.top - 1) >> 32);
-    };
-    if (__any_sync(kAll, loose)) look(loose_logit, loose ? span.loose_at(tid) : 0, loose);
-    for (int i0 = begin + warp * 32; i0 < end; i0 += kThreads) {
-      const int i = i0 + lane;
-      float v[kPer];
-      uint32_t ranks = 0;
-      if (i < end) {
-        unpack<T>(*span.at(i), v);
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) ranks = max(ranks, rank_of(v[u]));
+  if constexpr (TOP) {
+    static_assert(kWarps * 8 == 64, "two warps take one of them each");
+    if (tid < 64) {
+      const uint32_t r = s_largest[0][tid];
+      int before = 0;
+#pragma unroll 4
+      for (int i = 0; i < 64; i += 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(&s_largest[0][i]);
+        before += (x.x > r || (x.x == r && i < tid)) + (x.y > r || (x.y == r && i + 1 < tid)) + (x.z > r || (x.z == r && i + 2 < tid)) + (x.w > r || (x.w == r && i + 3 < tid));
       }
-      // equal to the top-th best: a later place, unless the list has it from the loose elements behind the vectors
-      if (!__any_sync(kAll, ranks >= floor && ranks >= last)) continue;
+      if (before == a.top - 1) s_floor = logit_of(r);
+    }
+    __syncthreads();
+    float floor = s_floor;                              // from here on the larger of that and the warp's top-th best so far
+    best.add(key_of(loose_logit, (uint32_t)span.loose_at(tid)), loose && !(loose_logit < floor), a.top, lane);
+    for (int i0 = begin + tid; i0 - lane < end; i0 += kAhead * kThreads) {
+      uint4 raw[kAhead];
 #pragma unroll
-      for (int u = 0; u < kPer; ++u) look(v[u], span.head + i * kPer + u, i < end);
+      for (int u = 0; u < kAhead; ++u)
+        if (i0 + u * kThreads < end) raw[u] = *span.at(i0 + u * kThreads);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + u * kThreads;
+        float v[kPer];
+        uint32_t some = 0;                              // which of the lane's reach it, a NaN too
+        if (i < end) {
+          unpack<T>(raw[u], v);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) some |= !(v[e] < floor) ? 1u << e : 0u;
+        }
+        const uint32_t any = __reduce_or_sync(kAll, some);
+        if (!any) continue;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          if (any >> e & 1u) best.add(key_of(v[e], (uint32_t)(span.head + i * kPer + e)), some >> e & 1u, a.top, lane);
+        const uint64_t least = __shfl_sync(kAll, best.key, a.top - 1);
+        if (least != 0) floor = fmaxf(floor, logit_of((uint32_t)(least >> 32)));       // of a NaN: stays
+      }
     }
     s_keys[warp][lane] = best.key;
-    __syncthreads();
+    merge_lists<kWarps>(s_keys, best, warp, lane);
   }
   if (warp == 0) {
-    sums = s_sums[0];
-    for (int w = 1; w < kWarps; ++w) sums = joined<ENTROPY>(sums, s_sums[w], c);
-    if (a.top > 0)
-      for (int w = 1; w < kWarps; ++w) best.merge(s_keys[w][lane], lane);
+    sums = lanes_joined<ENTROPY, kWarps>(s_sums[lane % kWarps], c);
   }
   if constexpr (CTAS > 1) {
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");       // the first CTA has begun: its shared memory is there
@@ -336,21 +376,22 @@ __global__ void __launch_bounds__(kThreads) log_probs_kernel(LogProbsArgs a) {
         store_remote(in_first(&s_row[part].s), sums.s);
         store_remote(in_first(&s_row[part].w), sums.w);
       }
-      if (a.top > 0) store_remote(in_first(&s_row_keys[part][lane]), best.key);
+      if constexpr (TOP) store_remote(in_first(&s_row_keys[part][lane]), best.key);
     }
     cluster_sync();
-    if (part != 0 || warp != 0) return;
-    for (int i = 1; i < CTAS; ++i) {
-      sums = joined<ENTROPY>(sums, s_row[i], c);
-      if (a.top > 0) best.merge(s_row_keys[i][lane], lane);
+    if (part != 0) return;
+    if (warp == 0) sums = lanes_joined<ENTROPY, CTAS>(s_row[lane % CTAS], c);
+    if constexpr (TOP) {
+      best.key = s_row_keys[warp % CTAS][lane];
+      merge_lists<CTAS>(s_row_keys, best, warp, lane);
     }
   }
-  if (warp == 0) write_results<T>(a, row, span.p, sums, best, lane);
+  if (warp == 0) write_results<T>(a, row, given, sums, best, lane);
 }
 
 // Gradient: CTA = a row, or `parts` CTAs for long ones. SAME: rows of logits and gradients lie alike to 16 bytes.
 template <typename T, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads) log_probs_grad_kernel(LogProbsArgs a, int parts, int threads_per_row) {
+__global__ void __launch_bounds__(kThreads, 4) log_probs_grad_kernel(LogProbsArgs a, int parts, int threads_per_row) {
   constexpr int kPer = Span<T>::kPer;
   const int rows_here = kThreads / threads_per_row, tid = threadIdx.x % threads_per_row;
   const int64_t row = (int64_t)(blockIdx.x / parts) * rows_here + threadIdx.x / threads_per_row;
@@ -404,7 +445,7 @@ __global__ void __launch_bounds__(kThreads) log_probs_grad_kernel(LogProbsArgs a
   }
 }
 
-template <typename T, bool ENTROPY, int CTAS>
+template <typename T, bool ENTROPY, bool TOP, int CTAS>
 cudaError_t launch_rows(const LogProbsArgs& a, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(a.rows * CTAS));
@@ -416,25 +457,26 @@ cudaError_t launch_rows(const LogProbsArgs& a, cudaStream_t st) {
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cfg.attrs = &cluster;
   cfg.numAttrs = CTAS > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, log_probs_kernel<T, ENTROPY, CTAS>, a);
+  return cudaLaunchKernelEx(&cfg, log_probs_kernel<T, ENTROPY, TOP, CTAS>, a);
 }
 
 constexpr int kShort = 1024;                            // logits of a row that a warp takes
-template <typename T, bool ENTROPY>
+template <typename T, bool ENTROPY, bool TOP>
 cudaError_t launch_forward_as(const LogProbsArgs& a, cudaStream_t st) {
   if (a.cols <= kShort) {
-    log_probs_short_kernel<T, ENTROPY><<<(unsigned)((a.rows + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
+    log_probs_short_kernel<T, ENTROPY, TOP><<<(unsigned)((a.rows + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
   // as many CTAs to a row as leave two thousand logits to each and fill the device's 148 multiprocessors twice over
   int ctas = 1;
   while (ctas < 8 && a.rows * ctas < 296 && a.cols >= ctas * 4096) ctas *= 2;
-  return ctas == 1 ? launch_rows<T, ENTROPY, 1>(a, st) : ctas == 2 ? launch_rows<T, ENTROPY, 2>(a, st)
-       : ctas == 4 ? launch_rows<T, ENTROPY, 4>(a, st) : launch_rows<T, ENTROPY, 8>(a, st);
+  return ctas == 1 ? launch_rows<T, ENTROPY, TOP, 1>(a, st) : ctas == 2 ? launch_rows<T, ENTROPY, TOP, 2>(a, st)
+       : ctas == 4 ? launch_rows<T, ENTROPY, TOP, 4>(a, st) : launch_rows<T, ENTROPY, TOP, 8>(a, st);
 }
 template <typename T>
 cudaError_t launch_forward(const LogProbsArgs& a, cudaStream_t st) {
-  return a.entropy ? launch_forward_as<T, true>(a, st) : launch_forward_as<T, false>(a, st);
+  if (a.top > 0) return a.entropy ? launch_forward_as<T, true, true>(a, st) : launch_forward_as<T, false, true>(a, st);
+  return a.entropy ? launch_forward_as<T, true, false>(a, st) : launch_forward_as<T, false, false>(a, st);
 }
 template <typename T>
 cudaError_t launch_backward(const LogProbsArgs& a, cudaStream_t st) {
