@@ -6,51 +6,131 @@
 namespace swarm {
 namespace {
 
-// Keys and values of new tokens into their pages, keys and queries rotated on the way: thread = one pair of a head of a token.
-template <typename T>
-__global__ void __launch_bounds__(256) cache_append_kernel(PagedArgs a, int heads) {
-  const int half = a.rotated / 2, pairs = a.head_dim / 2, all = heads + 2 * a.kv_heads;
-  const int64_t count = (int64_t)a.batch * a.tokens * all * pairs;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-    const int u = (int)(i % pairs), vh = (int)(i / pairs % all);
-    const int64_t token = i / pairs / all;
-    const int t = (int)(token % a.tokens), b = (int)(token / a.tokens);
+// Keys and values of new tokens into their pages, keys and queries rotated on the way: each value is read and written once, HBM is
+// the bound. A warp takes a token (or, where tokens are few, some heads of it). Its angles are computed once and wait in shared
+// memory for all heads; a lane then takes W pairs of a head at a time, as two vectors of W values half a rotation apart, or as one
+// of 2 W neighbours. Values that do not turn go the same way.
+//
+// The angle p f is taken in 64 bits as half turns, t = p (f / pi), brought to [-1, 1] by an exact subtraction and only then rounded
+// to fp32: a rotation at position 2^31 is as good as one at the start, but for the 22 bits that t has left behind the point there.
+constexpr int kAppendWarps = 4, kAppendSms = 148;
+
+struct AppendPlan {
+  int32_t heads, units, parts;                          // heads of q, k and v together; units of a head; warps for a token
+  uint32_t unit_multiplier;                             // x / units = high word of x * multiplier, for x below 2^26 and units above 1
+};
+
+template <int BYTES> struct VectorOf;
+struct __align__(16) Two16 { uint4 a, b; };
+template <> struct VectorOf<32> { using Type = Two16; };
+template <> struct VectorOf<16> { using Type = uint4; };
+template <> struct VectorOf<8> { using Type = uint2; };
+template <> struct VectorOf<4> { using Type = uint32_t; };
+template <> struct VectorOf<2> { using Type = uint16_t; };
+
+template <typename T, int N> struct Pieces {            // N consecutive values, N * 2 bytes aligned (16 at most)
+  using Raw = typename VectorOf<N * 2>::Type;
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const { return to_float<T>(reinterpret_cast<const T*>(&raw)[i]); }
+  __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&raw)[i] = from_float<T>(v); }
+};
+
+template <typename T, int W, bool INTERLEAVED>
+__global__ void __launch_bounds__(kAppendWarps * 32)
+cache_append_kernel(PagedArgs a, AppendPlan plan) {
+  __shared__ __align__(16) float2 s_turn[kAppendWarps][kMaxDim / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = a.rotated / 2, pairs = a.head_dim / 2;
+  const int q_heads = plan.heads - 2 * a.kv_heads;
+  float2* turn = s_turn[warp];
+  const int64_t items = (int64_t)a.batch * a.tokens * plan.parts, all = (int64_t)gridDim.x * kAppendWarps;
+  for (int64_t item = (int64_t)blockIdx.x * kAppendWarps + warp; item < items; item += all) {
+    const int part = (int)(item % plan.parts), t = (int)(item / plan.parts % a.tokens), b = (int)(item / plan.parts / a.tokens);
+    const int units = plan.heads * plan.units;
+    const int begin = (int)((int64_t)units * part / plan.parts) + lane, end = (int)((int64_t)units * (part + 1) / plan.parts);
     const int length = length_in(a, b), n = rows_in(a, b, length), at = length - n + t;
-    const bool live = t < n, is_q = vh < heads, is_v = vh >= heads + a.kv_heads;
-    const int h = is_q ? vh : is_v ? vh - heads - a.kv_heads : vh - heads;
-    // pair u: of the rotated values, or two neighbours of the others
-    int first = 2 * u, second = 2 * u + 1;
-    if (u < half && !a.interleaved) { first = u; second = u + half; }
-    const T* src = reinterpret_cast<const T*>(is_q ? a.q : is_v ? a.v : a.k) + offset_of(is_q ? a.qs : is_v ? a.vs : a.ks, b, t, h);
-    T* dst;
-    if (is_q) {
-      dst = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h);
-    } else {
-      if (!live) continue;
-      const int page = page_of(a, b, at / a.page_size);
-      if (page < 0) { atomicOr(a.status, kStatusPage); continue; }
-      dst = reinterpret_cast<T*>(is_v ? a.v_pages : a.k_pages) + offset_of(is_v ? a.vps : a.kps, page, at % a.page_size, h);
+    const bool live = t < n;
+    int page = -1;
+    if (live) page = page_of(a, b, at / a.page_size);
+    const int slot = live ? at % a.page_size : 0;
+    if (live && page < 0 && lane == 0) atomicOr(a.status, kStatusPage);
+    __syncwarp();                                       // the last token's angles have been read
+    for (int i = lane; i < half; i += 32) {
+      const double v = (double)at * ((double)a.frequencies[i] * 0.31830988618379067154);
+      float s, c;
+      sincospif((float)(v - 2.0 * rint(0.5 * v)), &s, &c);
+      turn[i] = make_float2(c, s);
     }
-    float x = live ? to_float<T>(src[first]) : 0.0f, y = live ? to_float<T>(src[second]) : 0.0f;
-    if (live && !is_v && u < half) {
-      const double angle = (double)at * (double)a.frequencies[u];
-      double s, c;
-      sincos(angle, &s, &c);
-      const float fs = (float)s, fc = (float)c, x0 = x;
-      x = fmaf(x0, fc, -(y * fs));
-      y = fmaf(y, fc, x0 * fs);
+    __syncwarp();
+    for (int i = begin; i < end; i += 32) {
+      // head h of q (0), k (1) or v (2), the unit's first pair, and where that lies: pairs of the rotated values, then those of
+      // the others, which lie half of what is left apart
+      const int head = plan.units == 1 ? i : (int)__umulhi((uint32_t)i, plan.unit_multiplier);
+      const int of = head < q_heads ? 0 : head < q_heads + a.kv_heads ? 1 : 2, h = of == 0 ? head : of == 1 ? head - q_heads : head - q_heads - a.kv_heads;
+      const int pair = (i - head * plan.units) * W, first = INTERLEAVED ? 2 * pair : pair < half ? pair : pair + half, apart = pair < half ? half : pairs - half;
+      Pieces<T, INTERLEAVED ? 2 * W : W> x{}, y{};
+      if (live) {
+        const T* from = reinterpret_cast<const T*>(of == 0 ? a.q : of == 1 ? a.k : a.v) + offset_of(of == 0 ? a.qs : of == 1 ? a.ks : a.vs, b, t, h) + first;
+        x.load(from);
+        if (!INTERLEAVED) y.load(from + apart);
+      }
+      T* to = nullptr;
+      if (of == 0) to = reinterpret_cast<T*>(a.out) + offset_of(a.os, b, t, h) + first;
+      else if (page >= 0) to = reinterpret_cast<T*>(of == 1 ? a.k_pages : a.v_pages) + offset_of(of == 1 ? a.kps : a.vps, page, slot, h) + first;
+      if (!to) continue;
+      if (live && of != 2 && pair < half) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          float2 cs;
+          if (W == 1) {
+            cs = turn[pair];
+          } else {                                      // two pairs' at a time
+            const float4 two = *reinterpret_cast<const float4*>(turn + pair + (e & ~1));
+            cs = e & 1 ? make_float2(two.z, two.w) : make_float2(two.x, two.y);
+          }
+          if (INTERLEAVED) {
+            const float u = x.get(2 * e), v = x.get(2 * e + 1);
+            x.set(2 * e, fmaf(u, cs.x, -(v * cs.y)));
+            x.set(2 * e + 1, fmaf(v, cs.x, u * cs.y));
+          } else {
+            const float u = x.get(e), v = y.get(e);
+            x.set(e, fmaf(u, cs.x, -(v * cs.y)));
+            y.set(e, fmaf(v, cs.x, u * cs.y));
+          }
+        }
+      }
+      x.store(to);
+      if (!INTERLEAVED) y.store(to + apart);
     }
-    dst[first] = from_float<T>(x);
-    dst[second] = from_float<T>(y);
   }
 }
 
+template <typename T, int W, bool INTERLEAVED>
+cudaError_t launch_append_as(const PagedArgs& a, cudaStream_t st) {
+  AppendPlan p{};
+  p.heads = (a.out ? a.heads : 0) + 2 * a.kv_heads;
+  p.units = a.head_dim / (2 * W);
+  p.unit_multiplier = (uint32_t)((((uint64_t)1 << 32) + p.units - 1) / p.units);
+  // as many warps to a token as have a unit for each lane, while the device has room for them
+  const int64_t tokens = (int64_t)a.batch * a.tokens, most = ((int64_t)p.heads * p.units + 31) / 32, room = (int64_t)kAppendSms * 16 / (tokens > 0 ? tokens : 1);
+  p.parts = (int32_t)(room < 1 ? 1 : room < most ? room : most);
+  const int64_t ctas = (tokens * p.parts + kAppendWarps - 1) / kAppendWarps, cap = (int64_t)kAppendSms * 64;
+  cache_append_kernel<T, W, INTERLEAVED><<<(unsigned)(ctas < cap ? ctas : cap), kAppendWarps * 32, 0, st>>>(a, p);
+  return cudaGetLastError();
+}
+
+// The widest vectors that the pairs of a head allow.
 template <typename T>
 cudaError_t launch_append(const PagedArgs& a, cudaStream_t st) {
-  const int heads = a.out ? a.heads : 0;
-  const int64_t count = (int64_t)a.batch * a.tokens * (heads + 2 * a.kv_heads) * (a.head_dim / 2);
-  cache_append_kernel<T><<<(unsigned)((count + 255) / 256 < 65535 ? (count + 255) / 256 : 65535), 256, 0, st>>>(a, heads);
-  return cudaGetLastError();
+  const int half = a.rotated / 2, rest = (a.head_dim - a.rotated) / 2;
+  if (a.interleaved && a.rotated > 0) {
+    if (half % 8 == 0 && rest % 8 == 0) return launch_append_as<T, 8, true>(a, st);
+    return half % 4 == 0 ? launch_append_as<T, 4, true>(a, st) : half % 2 == 0 ? launch_append_as<T, 2, true>(a, st) : launch_append_as<T, 1, true>(a, st);
+  }
+  if (half % 8 == 0 && rest % 8 == 0) return launch_append_as<T, 8, false>(a, st);
+  return half % 4 == 0 && rest % 4 == 0 ? launch_append_as<T, 4, false>(a, st) : half % 2 == 0 && rest % 2 == 0 ? launch_append_as<T, 2, false>(a, st)
+                                                                             : launch_append_as<T, 1, false>(a, st);
 }
 
 // ---- argument checks ------------------------------------------------------------------------
