@@ -400,12 +400,12 @@ def token_log_probs(logits, tokens=None, scale=1.0, top=0, entropy=False):
     pt = _tokens(tokens, device, lead)
     if not isinstance(top, int) or not 0 <= top <= 32 or top > cols:
         raise ValueError("top: between 0 and 32, and not more than the vocabulary")
-    new = {"dtype": torch.float32, "device": device}
-    log_probs = torch.empty(lead, **new) if tokens is not None else None
-    stats = torch.empty((*lead, 2), **new)
-    spread = torch.empty(lead, **new) if entropy else None
-    best = torch.empty((*lead, top), **new) if top else None
-    which = torch.empty((*lead, top), dtype=torch.int64, device=device) if top else None
+    new, floats = logits.new_empty, torch.float32
+    log_probs = new(lead, dtype=floats) if pt is not None else None
+    stats = new((*lead, 2), dtype=floats)
+    spread = new(lead, dtype=floats) if entropy else None
+    best = new((*lead, top), dtype=floats) if top else None
+    which = new((*lead, top), dtype=torch.int64) if top else None
     _check(_b.load().swarm_token_log_probs(px, pt, log_probs.data_ptr() if pt is not None else None, stats.data_ptr(),
                                            spread.data_ptr() if entropy else None, best.data_ptr() if top else None,
                                            which.data_ptr() if top else None, rows, cols, pitch, dtype, scale, top,
