@@ -29,10 +29,12 @@ constexpr int kMinShare = 64;                           // positions that a warp
 constexpr int kWholePositions = 128;                    // items of no more are not cut
 constexpr int kSms = 148;
 
-// DB: heads of up to 64 DB values.
-template <int DB> struct Shape {
+// DB: heads of up to 64 DB values. Blocks in flight to a warp, measured with one page to sixteen positions: heads of 128, pages of 64,
+// long documents two ahead 95 us, one 89; drafts through a window 61 and 60. Heads of 64, 8 sentences of 16384, 88 and 91;
+// with a page to each position, heads of 128, 88 and 90.
+template <int DB, bool ONE_PAGE> struct Shape {
   static constexpr int kBlock = 32 / DB;                // positions of a block
-  static constexpr int kStages = 3;
+  static constexpr int kStages = DB == 2 && ONE_PAGE ? 2 : 3;
   static constexpr int kTileBytes = kBlock * DB * 128;  // of keys, and of values
   static constexpr int kRing = kStages * 2 * kTileBytes;
   static constexpr int kSmem = kWarps * kRing;
@@ -42,6 +44,7 @@ struct PagedPlan {
   int32_t row_groups;                 // of `tokens` rows
   int32_t rows;                       // that a part holds
   int32_t whole;                      // items are not cut
+  int32_t streams;                    // the cache is larger than L2
   int32_t ctas;
   int32_t beside;                     // key heads that warps of a CTA take side by side: 1 or 2
   int32_t head_groups;                // kv_heads / beside
@@ -95,8 +98,12 @@ struct Runs {
   }
 };
 
-__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// Copies of 16 bytes under a cache policy; zeros where nothing is there.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool there, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" :: "r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t r[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -179,7 +186,7 @@ __device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
 template <typename T, int DB, int NT, bool ONE_PAGE>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
 paged_attention_kernel(PagedArgs a, PagedPlan plan) {
-  using S = Shape<DB>;
+  using S = Shape<DB, ONE_PAGE>;
   constexpr int kPartBytes = kRows * DB * 64 * 4;
   static_assert(2 * kPartBytes <= S::kRing, "a warp's two parts fit its ring");
   constexpr int B = S::kBlock, kSixteens = B / 16, kStages = S::kStages, kChunks = DB * 8, kRowsPerCopy = 32 / kChunks;
@@ -195,6 +202,10 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane < 2) s_part[warp][lane].there = 0;
   const int beside = plan.beside, sub_runs = beside == 2 ? kWarps / 2 : kWarps, side = warp & (beside - 1), sub = warp >> (beside - 1);
+
+  uint64_t policy;
+  if (plan.streams) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
 
   // this warp's run
   int b = 0, hk = 0, rg = 0, block = 0;
@@ -320,8 +331,8 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
             for (int i = 0; i < 16 / kRowsPerCopy; ++i) {
               const uint32_t to = spot_of(g * (16 / kRowsPerCopy) + i);
-              cp_async16(to, kp);
-              cp_async16(to + S::kTileBytes, vp);
+              copy16(to, kp, policy);
+              copy16(to + S::kTileBytes, vp, policy);
               kp += kstep;
               vp += vstep;
             }
@@ -331,8 +342,8 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
               const bool copy = (present >> (g * 16 + i * kRowsPerCopy + row_of_lane) & 1u) && c_of_lane < chunks;
               const void* none = a.q;                   // nothing is read there
               const uint32_t to = spot_of(g * (16 / kRowsPerCopy) + i);
-              cp_async16_or_zero(to, copy ? kp : none, copy);
-              cp_async16_or_zero(to + S::kTileBytes, copy ? vp : none, copy);
+              copy16_or_zero(to, copy ? kp : none, copy, policy);
+              copy16_or_zero(to + S::kTileBytes, copy ? vp : none, copy, policy);
               kp += kstep;
               vp += vstep;
             }
@@ -351,8 +362,8 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
           const int64_t kr = __shfl_sync(0xFFFFFFFFu, ko, r), vr = __shfl_sync(0xFFFFFFFFu, vo, r);
           const bool copy = (present >> r & 1u) && c_of_lane < chunks;
           const void* none = a.q;
-          cp_async16_or_zero(spot_of(i), copy ? kb + kr : none, copy);
-          cp_async16_or_zero(spot_of(i) + S::kTileBytes, copy ? vb + vr : none, copy);
+          copy16_or_zero(spot_of(i), copy ? kb + kr : none, copy, policy);
+          copy16_or_zero(spot_of(i) + S::kTileBytes, copy ? vb + vr : none, copy, policy);
         }
       }
       const bool ends = block + 1 == s.blocks, run_ends = !plan.whole && left == 1, last = ends || run_ends;
@@ -811,6 +822,10 @@ PagedPlan make_plan(const PagedArgs& a) {
   }
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_groups;
   p.whole = most <= kWholePositions;
+  // A cache that does not fit into L2 passes through it without displacing what other kernels, and the tables, rows and parts
+  // of this one, have there: 128 sentences x 16 heads of 64 67 -> 62 us, drafts through a window 65 -> 61, long documents
+  // 95 -> 92. One that fits stays for the next step: 100001 positions 24 us, else 25.
+  p.streams = (int64_t)a.pages * a.page_size * a.kv_heads * a.head_dim * 4 > (int64_t)96 << 20;
   p.beside = 1;
   p.pitch = a.head_dim <= 64 ? 64 : 128;
   if (!p.whole) {
@@ -835,7 +850,7 @@ PagedPlan make_plan(const PagedArgs& a) {
 
 template <typename T, int DB, int NT, bool ONE_PAGE>
 cudaError_t launch_as(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
-  using S = Shape<DB>;
+  using S = Shape<DB, ONE_PAGE>;
   static bool attr_set[64] = {};
   static std::mutex attr_mutex;
   {
