@@ -389,14 +389,15 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(LogPro
   if (warp == 0) write_results<T>(a, row, given, sums, best, lane);
 }
 
-// Gradient: CTA = a row, or `parts` CTAs for long ones. SAME: rows of logits and gradients lie alike to 16 bytes.
+// Gradient: CTA = a row, or `parts` CTAs for long ones, a warp for short ones. The last rows come first: they are what the forward
+// call has left in L2, and the gradients pass through it first to go.
 template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(kThreads, 4) log_probs_grad_kernel(LogProbsArgs a, int parts, int threads_per_row) {
   constexpr int kPer = Span<T>::kPer;
   const int rows_here = kThreads / threads_per_row, tid = threadIdx.x % threads_per_row;
-  const int64_t row = (int64_t)(blockIdx.x / parts) * rows_here + threadIdx.x / threads_per_row;
+  const int64_t turn = (int64_t)(blockIdx.x / parts) * rows_here + threadIdx.x / threads_per_row, row = a.rows - 1 - turn;
   const int part = blockIdx.x % parts;
-  if (row >= a.rows) return;
+  if (row < 0) return;
   const Span<T> span(reinterpret_cast<const T*>(a.logits) + row * a.pitch, a.cols);
   T* dx = reinterpret_cast<T*>(a.dlogits) + row * a.dlogits_pitch;
   const bool same = (((uintptr_t)dx ^ (uintptr_t)span.p) & 15) == 0;
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 4) log_probs_grad_kernel(LogProbsArg
           uint4 w;
           if constexpr (sizeof(T) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
           else w = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4 % kPer], v[5 % kPer]), pack2<T>(v[6 % kPer], v[7 % kPer]));
-          *reinterpret_cast<uint4*>(dx + first) = w;
+          __stcs(reinterpret_cast<uint4*>(dx + first), w);
         } else {
 #pragma unroll
           for (int e = 0; e < kPer; ++e) dx[first + e] = from_float<T>(v[e]);
@@ -485,7 +486,6 @@ cudaError_t launch_backward(const LogProbsArgs& a, cudaStream_t st) {
   const int64_t groups = (a.rows * threads + kThreads - 1) / kThreads;
   int parts = 1;
   while (threads == kThreads && groups * parts < 1184 && a.cols >= (int64_t)parts * 8192 && parts < 64) parts *= 2;
-  if (groups * parts >= (int64_t)1 << 31) return cudaErrorInvalidConfiguration;
   if (a.dentropy) log_probs_grad_kernel<T, true><<<(unsigned)(groups * parts), kThreads, 0, st>>>(a, parts, threads);
   else log_probs_grad_kernel<T, false><<<(unsigned)(groups * parts), kThreads, 0, st>>>(a, parts, threads);
   return cudaGetLastError();

@@ -269,6 +269,8 @@ def cross_attention_backward(do, q, k, v, o, lse, scale=None, query_lengths=None
 def _paged_desc(device, heads, x, x_name, k_pages, v_pages, table, lengths, counts, rotated, interleaved, window, sinks, scale,
                 strides):
     """Descriptor of a call on x [batch, tokens, ., head_dim]; `strides` are those of q, out, k and v."""
+    if not isinstance(k_pages, torch.Tensor):
+        raise ValueError("k_pages: a tensor on the call's CUDA device is needed")
     dtype, whole, pages = x.dtype, x.shape, k_pages.shape
     if dtype != torch.bfloat16 and dtype != torch.float16:
         raise ValueError(f"{x_name}: bfloat16 or float16 is needed, got {dtype}")
@@ -309,9 +311,9 @@ def append_to_cache(k, v, k_pages, v_pages, table, lengths, counts=None, q=None,
             raise ValueError("frequencies: consecutive values are needed")
         rotated = 2 * frequencies.shape[0]
     shape = k.shape
-    if len(shape) != 4 or k_pages.dim() != 4 or shape[2] != k_pages.shape[2]:
+    if len(shape) != 4 or not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4 or shape[2] != k_pages.shape[2]:
         raise ValueError(f"k, k_pages: [batch, tokens, kv_heads, head_dim] and [pages, page_size, kv_heads, head_dim] are needed, "
-                         f"got {tuple(shape)} and {tuple(k_pages.shape)}")
+                         f"got {tuple(shape)} and {tuple(getattr(k_pages, 'shape', ()))}")
     strides = (*_heads(k, "k", device, k.dtype, shape), *_heads(v, "v", device, k.dtype, shape))
     if q is None:
         if out is not None:
