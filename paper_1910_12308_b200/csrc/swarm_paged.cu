@@ -165,6 +165,8 @@ void fill(PagedArgs& a, const swarm_paged* d) {
   a.kps = d->k_pages; a.vps = d->v_pages; a.qs = d->q; a.os = d->out; a.ks = d->k; a.vs = d->v;
   a.batch = d->batch; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads;
   a.tokens = d->tokens; a.head_dim = d->head_dim; a.pages = d->pages; a.page_size = d->page_size; a.table_columns = d->table_columns;
+  const int64_t room = (int64_t)d->table_columns * d->page_size;
+  a.capacity = (int32_t)(room < 0x7FFFFFFF ? room : 0x7FFFFFFF);
   a.rotated = d->rotated; a.interleaved = d->interleaved; a.window = d->window; a.sinks = d->window > 0 ? d->sinks : 0;
   a.scale = d->scale;
 }

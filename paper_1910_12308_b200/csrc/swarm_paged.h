@@ -13,6 +13,7 @@ struct PagedArgs {
   int64_t table_pitch;
   swarm_strides kps, vps, qs, os, ks, vs;               // of the pages: .batch is the page's
   int32_t batch, heads, kv_heads, group, tokens, head_dim, pages, page_size, table_columns;
+  int32_t capacity;                                     // positions that a row of the table has room for
   int32_t rotated, interleaved, window, sinks;
   float scale;
   int* status;                                          // kStatusPage is raised for pages that do not exist

@@ -58,7 +58,8 @@ struct PagedPlan {
   int32_t pitch;
 };
 
-// What a sentence's rows see, in blocks of B: the first `sink_blocks`, then those from position lo / B * B.
+// What a sentence's rows see, in blocks of B: the first `sink_blocks`, then those from position lo / B * B. A length beyond what the
+// table has room for adds no blocks, and a sentence without blocks has no items.
 struct Sentence {
   int length, n, lo, sink_blocks, blocks, row_groups;
 };
@@ -67,10 +68,15 @@ template <int B> __device__ __forceinline__ Sentence sentence_of(const PagedArgs
   s.length = length_in(a, b);
   s.n = rows_in(a, b, s.length);
   s.lo = a.window > 0 ? max(0, s.length - s.n - a.window + 1) : 0;
-  const int sinks = min(a.sinks, s.lo);
-  s.sink_blocks = min(sinks / B + (sinks % B != 0), s.lo / B);
-  s.blocks = s.n > 0 ? s.sink_blocks + (s.length - 1) / B + 1 - s.lo / B : 0;
-  s.row_groups = (s.n * a.group + kRows - 1) / kRows;
+  const int sinks = min(min(a.sinks, s.lo), a.capacity), end = min(s.length, a.capacity);
+  s.sink_blocks = sinks / B + (sinks % B != 0);
+  s.blocks = s.sink_blocks;
+  if (end > s.lo) {
+    s.sink_blocks = min(s.sink_blocks, s.lo / B);
+    s.blocks = s.sink_blocks + (end - 1) / B + 1 - s.lo / B;
+  }
+  if (s.n == 0) s.blocks = 0;
+  s.row_groups = s.blocks > 0 ? (s.n * a.group + kRows - 1) / kRows : 0;
   return s;
 }
 // Blocks of a sentence's items, those of the key heads beside one another counted once.
@@ -404,9 +410,11 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) fetch(i);
 
-  // rows past a sentence's count
+  // rows past a sentence's count, or of a sentence of which nothing is there
   for (int z = blockIdx.x; z < a.batch; z += gridDim.x) {
-    const int n = rows_in(a, z, length_in(a, z));
+    const Sentence x = sentence_of<B>(a, z);
+    const int n = x.blocks > 0 ? x.n : 0;
+    if (x.n > 0 && x.length > a.capacity && tid == 0) atomicOr(a.status, kStatusPage);
     for (int i = tid; i < (a.tokens - n) * a.heads * chunks; i += kWarps * 32) {
       const int ch = i % chunks, h = i / chunks % a.heads, t = n + i / chunks / a.heads;
       *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + offset_of(a.os, z, t, h) + ch * 8) = make_uint4(0, 0, 0, 0);
@@ -815,7 +823,7 @@ PagedPlan make_plan(const PagedArgs& a) {
   p.row_groups = (int32_t)((rows + kRows - 1) / kRows);
   p.rows = (int32_t)(rows < kRows ? rows : kRows);
   // the most positions that an item can have: the table's, or the window's with the first tokens'
-  int64_t most = (int64_t)a.table_columns * a.page_size;
+  int64_t most = a.capacity;
   if (a.window > 0) {
     const int64_t seen = (int64_t)a.window + a.tokens - 1 + a.sinks;
     if (seen < most) most = seen;

@@ -425,6 +425,49 @@ def test_a_window_far_into_a_sentence_of_2_31_tokens():
     ops.check()
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (10, 0), (10, 5), (1000, 30)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 2, 64), (16, 2, 128)])
+def test_lengths_beyond_the_table_add_nothing(window, sinks, heads, kv_heads, dim):
+    """Positions that the table has no room for are not there: what a row sees of the others is, and nothing is waited for."""
+    page, columns = 8, 40
+    lengths = [columns * page, columns * page + 3, columns * page + 500, 2 ** 31 - 1, 100]
+    table = torch.randperm(5 * columns, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(5, columns).cuda()
+    k_pages, v_pages = (randn(5 * columns, page, kv_heads, dim, dtype=F16, seed=s) for s in (1, 2))
+    q = randn(5, 2, heads, dim, dtype=F16, seed=3)
+    o, lse = ops.paged_attention(q, k_pages, v_pages, table, ints(*lengths), window=window, sinks=sinks, need_lse=True)
+    with pytest.raises(g.SwarmError):
+        ops.check()
+    for b, n in enumerate(lengths):
+        room = min(n, columns * page)
+        k, v = (held(x, table, b, room) for x in (k_pages, v_pages))
+        for t in range(2):
+            p, seen = n - 2 + t, torch.arange(room, device="cuda")
+            seen = seen[seen <= p]
+            if window:
+                seen = seen[(seen > p - window) | (seen < sinks)]
+            w, l, size = attention_of(q[b, t], k[seen], v[seen], dim ** -0.5)
+            within(o[b, t], w, U[F16] * w.abs() + E * size + TINY[F16], (b, t))
+            assert torch.equal(torch.isneginf(lse[b, :, t]), torch.isneginf(l))
+    ops.paged_attention(q, k_pages, v_pages, table, ints(320, 0, 5, 319, 100), window=window, sinks=sinks)
+    ops.check()
+
+
+def test_keys_and_values_of_different_layouts_and_a_wide_table():
+    lengths, hk, d = [50, 7, 200], 4, 64
+    k_pages, v_pages, table = make_cache(lengths, 16, hk, d, BF16)
+    q = randn(3, 1, 8, d, dtype=BF16, seed=5)
+    want = ops.paged_attention(q, k_pages, v_pages, table, ints(*lengths))
+    by_head = v_pages.transpose(1, 2).contiguous().transpose(1, 2)
+    wide = torch.full((3, table.shape[1] + 9), 2 ** 30, dtype=torch.int32, device="cuda")
+    wide[:, 5:5 + table.shape[1]] = table
+    assert torch.equal(ops.paged_attention(q, k_pages, by_head, wide[:, 5:5 + table.shape[1]], ints(*lengths)), want)
+    k_by_head = k_pages.transpose(1, 2).contiguous().transpose(1, 2)
+    other = ops.paged_attention(q, k_by_head, by_head, table, ints(*lengths))   # heads one by one instead of in pairs
+    size = torch.stack([attention_of(q[b, 0], held(k_pages, table, b, n), held(v_pages, table, b, n), d ** -0.5)[2] for b, n in enumerate(lengths)])
+    within(other[:, 0], want[:, 0], 2 * U[BF16] * want[:, 0].double().abs() + 2 * E * size)
+    ops.check()
+
+
 def test_attention_refusals():
     q, pages = randn(2, 3, 4, 64, dtype=BF16), randn(5, 16, 2, 64, dtype=BF16)
     table, lengths = torch.zeros(2, 2, dtype=torch.int32, device="cuda"), ints(3, 3)
