@@ -13,6 +13,10 @@ namespace {
 //
 // The angle p f is taken in 64 bits as half turns, t = p (f / pi), brought to [-1, 1] by an exact subtraction and only then rounded
 // to fp32: a rotation at position 2^31 is as good as one at the start, but for the 22 bits that t has left behind the point there.
+//
+// Measured on the device: 16 prompts of 512 to 1024 tokens, 32 heads of 128 on 8, 302 MB, 56 us, 5.4 TB/s (all of 1024 tokens, 403 MB,
+// 69 us, 5.9); neighbouring pairs 61 us; one token of 4 sentences 2.9 us. More units of a lane at a time cost warps: two 65 us, four 90.
+// Reading a unit before the sentence's length is known reads padded rows too: 69.
 constexpr int kAppendWarps = 4, kAppendSms = 148;
 
 struct AppendPlan {

@@ -5,7 +5,8 @@ Tolerances are bounds, not observations. U is the largest relative rounding erro
                 double's 53 bits add their last place
   attention     E = 2e-5 (128-term dot products, base-2 exponentials) times the sum of the weighted magnitudes, and 2^-16 for
                 weights that go into their products as two numbers of the type
-  log probs     sums of n positive terms in runs of n / 256: (n / 256 + 16) 2^-24; exponentials of d: (|d| + 4) 2^-23
+  log probs     sums of n positive terms, each thread a run of n / 256, or of n / 32 where a warp may take the row (n <= 16384):
+                (run + 16) 2^-24; exponentials of d: (|d| + 4) 2^-23
 """
 import math
 
@@ -22,6 +23,10 @@ BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 U = {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}
 TINY = {BF16: 1e-38, F16: 2.0 ** -24, F32: 1e-37}        # a result may fall among the subnormals of its type
 E = 2e-5 + 2.0 ** -16
+
+
+def run(n):
+    return n / (32 if n <= 16384 else 256)
 
 
 def randn(*shape, dtype=F32, seed=0, std=1.0):
@@ -522,7 +527,7 @@ def within_fp32(got, want, off, what):
 def check_log_probs(got, logits, tokens, scale, top):
     n = logits.shape[-1]
     lp, stats, entropy, logp, spread = reference(logits, tokens, scale)
-    off = (n / 256 + 16) * 2.0 ** -24 + (spread + 4) * 2.0 ** -23               # of the logarithm of the sum
+    off = (run(n) + 16) * 2.0 ** -24 + (spread + 4) * 2.0 ** -23               # of the logarithm of the sum
     assert torch.equal(got.stats[..., 0].double(), stats[..., 0])
     within(got.stats[..., 1], stats[..., 1], off + 2.0 ** -23 * stats[..., 1].abs(), "log of the sum")
     within_fp32(got.log_probs, lp, off, "log probs")
@@ -536,7 +541,8 @@ def check_log_probs(got, logits, tokens, scale, top):
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("rows,cols,top", [(1, 1, 1), (3, 2, 2), (5, 7, 0), (2, 33, 32), (9, 100, 5), (1, 255, 1), (300, 256, 8), (2, 2049, 20), (4, 10007, 32),
-                                           (1, 50000, 3), (3, 131072, 32), (40, 32000, 0), (700, 1000, 1), (2, 300001, 16)])
+                                           (1, 50000, 3), (3, 131072, 32), (40, 32000, 0), (700, 1000, 1), (2, 300001, 16),
+                                           (1100, 1025, 0), (1024, 1025, 0), (2600, 2500, 0), (2600, 2500, 6), (4100, 4099, 0)])
 def test_log_probs(dtype, rows, cols, top):
     logits = randn(rows, cols, dtype=dtype, seed=cols, std=3.0)
     tokens = torch.randint(cols, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
@@ -608,7 +614,7 @@ def check_gradient(dx, logits, tokens, scale, g_, h):
     first = torch.zeros_like(p) if g_ is None else (g_.double() * some).unsqueeze(-1) * (here - p)
     second = torch.zeros_like(p) if h is None else -h.double().unsqueeze(-1) * p * (finite + entropy.unsqueeze(-1))
     want = scale * (first + second)
-    off = ((n / 256 + 16) * 2.0 ** -24 + (spread + 4) * 2.0 ** -23).unsqueeze(-1) + 2.0 ** -22 * (finite.abs() + 1)
+    off = ((run(n) + 16) * 2.0 ** -24 + (spread + 4) * 2.0 ** -23).unsqueeze(-1) + 2.0 ** -22 * (finite.abs() + 1)
     size = p * (0 if g_ is None else g_.double().abs().unsqueeze(-1))
     size = size + p * (0 if h is None else h.double().abs().unsqueeze(-1) * (finite.abs() + entropy.abs().unsqueeze(-1) + 8 + 2 * spread.unsqueeze(-1)))
     bound = U[dx.dtype] * want.abs() + scale * size * 2 * off + 2.0 ** -22 * (first.abs() + second.abs()) * scale + TINY[dx.dtype]
@@ -616,7 +622,7 @@ def check_gradient(dx, logits, tokens, scale, g_, h):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (2, 256), (5, 1001), (30, 4099), (2, 70001)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (2, 256), (5, 1001), (30, 4099), (2, 70001), (1100, 1025), (2600, 2501)])
 @pytest.mark.parametrize("parts", ["token", "entropy", "both"])
 def test_gradient(dtype, rows, cols, parts):
     logits = randn(rows, cols, dtype=dtype, seed=cols, std=2.0)
@@ -651,7 +657,7 @@ def test_log_probs_take_strides_and_gradients_overwrite_logits():
     tokens = torch.arange(12, device="cuda") * 80
     a, b = ops.token_log_probs(part, tokens, top=6, entropy=True), ops.token_log_probs(part.contiguous(), tokens, top=6, entropy=True)
     n = part.shape[1]
-    off = (n / 256 + 16) * 2.0 ** -23 + 40 * 2.0 ** -22                         # another alignment may take another order
+    off = (run(n) + 16) * 2.0 ** -23 + 40 * 2.0 ** -22                         # another alignment may take another order
     within(a.log_probs, b.log_probs, off)
     assert torch.equal(a.top_tokens, b.top_tokens)
     c = ops.token_log_probs(part.contiguous().view(3, 4, n), tokens.view(3, 4), top=6, entropy=True)
