@@ -177,7 +177,8 @@ def add_rms_norm_backward(dy, total, weight, dtotal=None, eps=1e-6, rate=0.0, se
 
 def _heads(x, name, device, dtype, shape):
     """Strides over sentence, token and head."""
-    _same(x, name, device, dtype)
+    if not isinstance(x, torch.Tensor) or x.dtype != dtype or x.get_device() != device:
+        _same(x, name, device, dtype)
     if x.shape != shape:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected {tuple(shape)}")
     s = x.stride()
