@@ -258,11 +258,16 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       int64_t at = begin - s_prefix[lo];
       b = lo * per;
       s = sentence_of<B>(a, b);
-      while (at >= blocks_of_items(plan, s)) { at -= blocks_of_items(plan, s); ++b; s = sentence_of<B>(a, b); }
-      const int item = (int)divide(at, s.blocks);
-      block = (int)(at - (int64_t)item * s.blocks);
-      hk = item / s.row_groups * beside + side;
-      rg = item % s.row_groups;
+      while (at >= blocks_of_items(plan, s) && b + 1 < a.batch) { at -= blocks_of_items(plan, s); ++b; s = sentence_of<B>(a, b); }
+      // lengths are read more than once: should somebody write them meanwhile, nothing out of range is touched
+      if (at >= blocks_of_items(plan, s)) {
+        left = 0;
+      } else {
+        const int item = (int)divide(at, s.blocks);
+        block = (int)(at - (int64_t)item * s.blocks);
+        hk = item / s.row_groups * beside + side;
+        rg = item % s.row_groups;
+      }
     }
   }
   bool fresh = true;                                    // the next block is the first of its item here
@@ -388,7 +393,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
         info.flags = (fresh ? kFirst : 0u) | (fresh && block == 0 ? kFromStart : 0u) | (last ? kLast : 0u) | (ends ? kToEnd : 0u) | (run_ends ? kRunEnds : 0u);
         s_info[warp][stage] = info;
       }
-      if (fresh) {                                      // its rows, needed two blocks from now, behind what is in flight
+      if (fresh) {                                      // its rows, needed a block or two from now, behind what is in flight
         const int r = rg * kRows + lane / DB, t = r / a.group;
         if (lane < NT * 8 * DB && t < s.n && lane % DB * 64 < a.head_dim)
           prefetch_l2(reinterpret_cast<const T*>(a.q) + offset_of(a.qs, b, t, hk * a.group + r % a.group) + lane % DB * 64);
@@ -397,7 +402,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
         // the CTA that holds the item's last block; of a CTA's runs the last one's counts
         const Runs runs(s_prefix[kWarps * 32], gridDim.x * sub_runs, gridDim.x, kMinShare / B);
         const int run = blockIdx.x * runs.per_cta + sub;
-        if (sub + 1 == runs.per_cta || run + 1 == runs.count) s_last_cta = runs.owner(runs.begin(run + 1) + (s.blocks - 2 - block)) / runs.per_cta;
+        if (sub + 1 == runs.per_cta || run + 1 == runs.count) s_last_cta = min(runs.owner(runs.begin(run + 1) + (s.blocks - 2 - block)) / runs.per_cta, (int)gridDim.x - 1);
       }
       fresh = last;
       ++block;
