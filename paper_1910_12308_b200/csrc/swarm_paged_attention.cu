@@ -31,8 +31,12 @@ namespace {
 constexpr int kRows = 16;
 constexpr int kWarps = 8;
 constexpr int kCtasPerSm = 1;                         // two of four warps: long documents 96 -> 101 us
-constexpr int kMinShare = 64;                           // positions that a warp's run has at least
-constexpr int kWholePositions = 128;                    // items of no more are not cut
+// Positions that a warp's run has at least. Small calls, 32 / 64 / 128: 4 x 8 heads of 64 on 490 positions 12.2 / 14.0 / 15.0 us, 32 x 4
+// key heads of 128 on 230 14.1 / 16.0 / 20.0; large ones are the same.
+constexpr int kMinShare = 32;
+// Items of no more positions are not cut: a warp takes each, and no kernel joins. 4 x 8 heads of 64 on 100 positions 9.2 us, cut 11.2;
+// on 230 positions 13.4 and 12.2, 32 x 4 key heads of 128 on 230 20.5 and 16.0.
+constexpr int kWholePositions = 128;
 constexpr int kSms = 148;
 
 // DB: heads of up to 64 DB values. Blocks in flight to a warp, measured with one page to sixteen positions: heads of 128, pages of 64,
