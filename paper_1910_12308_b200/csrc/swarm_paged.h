@@ -31,6 +31,12 @@ __device__ __forceinline__ int page_of(const PagedArgs& a, int b, int column) {
   return (uint32_t)page < (uint32_t)a.pages ? page : -1;
 }
 
+// How many CTAs, from CTA `first` on, hold parts of an item that `first` begins and `last` ends. What a CTA says of the last one
+// is a number in memory: whatever it is, no part outside the `ctas` that the workspace has is read.
+__host__ __device__ inline int parts_between(int first, int last, int ctas) {
+  return (last < first ? first : last < ctas ? last : ctas - 1) - first + 1;
+}
+
 size_t paged_attention_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, void* workspace, cudaStream_t st);
 

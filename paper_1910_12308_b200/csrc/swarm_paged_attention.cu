@@ -217,6 +217,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3, chunks = a.head_dim / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane < 2) s_part[warp][lane].there = 0;
+  if (tid == 0) s_last_cta = blockIdx.x;                // no run of the CTA ends inside an item
   const int beside = plan.beside, sub_runs = beside == 2 ? kWarps / 2 : kWarps, side = warp & (beside - 1), sub = warp >> (beside - 1);
 
   uint64_t policy;
@@ -263,7 +264,8 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       b = lo * per;
       s = sentence_of<B>(a, b);
       while (at >= blocks_of_items(plan, s) && b + 1 < a.batch) { at -= blocks_of_items(plan, s); ++b; s = sentence_of<B>(a, b); }
-      // lengths are read more than once: should somebody write them meanwhile, nothing out of range is touched
+      // Lengths are read more than once: should somebody write them meanwhile, the results are undefined, but nothing out of
+      // range is touched. Runs and items then may not fit together: this run is left out, items begun before it are not ended.
       if (at >= blocks_of_items(plan, s)) {
         left = 0;
       } else {
@@ -784,7 +786,7 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
   const float c = a.scale * kLog2e;
   float top = -INFINITY, sum = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
   if (works) {
-    const int count = join.last_cta - c0 + 1, from = count * sub / plan.join_warps, to = count * (sub + 1) / plan.join_warps;
+    const int count = parts_between(c0, join.last_cta, plan.ctas), from = count * sub / plan.join_warps, to = count * (sub + 1) / plan.join_warps;
     for (int p0 = from; p0 < to; p0 += 8) {
       float2 ml[8];
       float4 x[8];
