@@ -578,44 +578,54 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       }
       apart = __any_sync(0xFFFFFFFFu, bad);
     }
+    // A block's products are added up from nothing, and then to o in fp32: the tensor core cuts off what its sum has no bits
+    // for, always towards 0, and a long run's sums shrank by as many cuts (2^20 positions in one run, fp16: o 0.8 % too small).
+    // Sixteen rows, drafts through a window, 62 -> 65 us, eight rows the same.
+    // products: the sums of values 16 d on; `masked` leaves of the cache's values what is to be seen
+    auto products = [&](float x[NT][4], int d, auto masked) {
+#pragma unroll
+      for (int g = 0; g < kSixteens; ++g) {
+        uint32_t v[4];
+        ldmatrix4_trans(tile_v + g * (16 * DB * 128) + tile_offset<DB>(value_row, d * 2 + value_half), v);
+        masked(g, v);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (g == 0) mma16816_first<T>(x[nt], v, hi[nt][g][0], hi[nt][g][1]);
+          else mma16816<T>(x[nt], v, hi[nt][g][0], hi[nt][g][1]);
+          mma16816<T>(x[nt], v, lo[nt][g][0], lo[nt][g][1]);
+        }
+      }
+    };
     if (!apart) {
 #pragma unroll
-      for (int g = 0; g < kSixteens; ++g)
+      for (int d = 0; d < DB * 4; ++d) {
+        float x[NT][4];
+        products(x, d, [](int, uint32_t*) {});
 #pragma unroll
-        for (int d = 0; d < DB * 4; ++d) {
-          uint32_t v[4];
-          ldmatrix4_trans(tile_v + g * (16 * DB * 128) + tile_offset<DB>(value_row, d * 2 + value_half), v);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma16816<T>(o[nt][d], v, hi[nt][g][0], hi[nt][g][1]);
-            mma16816<T>(o[nt][d], v, lo[nt][g][0], lo[nt][g][1]);
-          }
+        for (int nt = 0; nt < NT; ++nt) {
+          add2(o[nt][d][0], o[nt][d][1], o[nt][d][0], o[nt][d][1], x[nt][0], x[nt][1]);
+          add2(o[nt][d][2], o[nt][d][3], o[nt][d][2], o[nt][d][3], x[nt][2], x[nt][3]);
         }
+      }
     } else {
       // one token after the other, its rows alone and what it does not see as zeros: the same bits as above for these
       for (int t = 0; t < a.tokens; ++t) {
+        uint32_t keep[kSixteens][2];
 #pragma unroll
-        for (int g = 0; g < kSixteens; ++g) {
-          uint32_t keep[2];
+        for (int g = 0; g < kSixteens; ++g)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int p = info.position + g * 16 + e * 8 + c4 * 2;
-            keep[e] = (sees(p, t) ? 0xFFFFu : 0u) | (sees(p + 1, t) ? 0xFFFF0000u : 0u);
+            keep[g][e] = (sees(p, t) ? 0xFFFFu : 0u) | (sees(p + 1, t) ? 0xFFFF0000u : 0u);
           }
 #pragma unroll
-          for (int d = 0; d < DB * 4; ++d) {
-            uint32_t v[4];
-            ldmatrix4_trans(tile_v + g * (16 * DB * 128) + tile_offset<DB>(value_row, d * 2 + value_half), v);
-            v[0] &= keep[0]; v[1] &= keep[0]; v[2] &= keep[1]; v[3] &= keep[1];
+        for (int d = 0; d < DB * 4; ++d) {
+          float x[NT][4];
+          products(x, d, [&](int g, uint32_t* v) { v[0] &= keep[g][0]; v[1] &= keep[g][0]; v[2] &= keep[g][1]; v[3] &= keep[g][1]; });
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float x[4] = {o[nt][d][0], o[nt][d][1], o[nt][d][2], o[nt][d][3]};
-              mma16816<T>(x, v, hi[nt][g][0], hi[nt][g][1]);
-              mma16816<T>(x, v, lo[nt][g][0], lo[nt][g][1]);
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int u = 0; u < 4; ++u) o[nt][d][u] = t_of[nt][u & 1] == t ? x[u] : o[nt][d][u];
-            }
-          }
+            for (int u = 0; u < 4; ++u) o[nt][d][u] = t_of[nt][u & 1] == t ? o[nt][d][u] + x[nt][u] : o[nt][d][u];
         }
       }
     }
