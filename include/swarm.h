@@ -481,7 +481,8 @@ int swarm_cache_append(const swarm_paged *desc_host, const void *k_dev, const vo
  * window w > 0 only those of j > p - w, and the sentence's first `sinks` beside them:
  *   s = scale * q . k,   lse = log sum_j exp(s_j),   o = sum_j exp(s_j - lse) v_j
  * over what it sees. Rows t >= n, and rows of which no page can be followed, have o = 0 and lse = -infinity. What the
- * cache holds in places that a row does not see is not used for it (NaN included).
+ * cache holds in places that a row does not see is not used for it (NaN included). An infinite value that it sees makes o
+ * infinite, whatever its weight, and NaN where both signs meet.
  *   tokens <= SWARM_PAGED_MAX_TOKENS (a decoding step, drafts that are checked at once, a short piece of a prompt). lse_dev:
  *   [batch][heads][tokens] floats, or NULL. Addresses: multiples of 16 bytes. out must not overlap inputs. batch * heads < 2^25.
  * Errors: EINVAL (sizes, strides, alignment, scale, NULL, workspace too small). */

@@ -144,9 +144,18 @@ template <typename T> __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (w & e) == e || ((w >> 16) & e) == e;
 }
 
+// The numbers of a word that are NaN or the infinity with this sign bit (in each half), as ones of the type.
+template <typename T> __device__ __forceinline__ uint32_t infinities(uint32_t w, uint32_t sign) {
+  constexpr uint32_t e = kNarrow<T> ? 0x7C007C00u : 0x7F807F80u, least = e & ~(e << 1), one = kNarrow<T> ? 0x3C00u : 0x3F80u;
+  const uint32_t all = (w & e) + least;                 // the top bit: an exponent of ones
+  const uint32_t some = ((w & ~e & 0x7FFF7FFFu) + 0x7FFF7FFFu) | ~(w ^ sign);           // the top bit: a NaN, or that sign
+  return ((all & some) >> 15 & 0x00010001u) * one;
+}
+
 // A block in the ring: what it is of, and which of its positions were read.
 struct __align__(16) BlockInfo {
   int32_t b, head, row0, n;           // sentence, key head, first row of the item; the sentence's rows are n tokens'
+  int32_t block;                      // of the item
   int32_t position;
   int32_t first_new;                  // position of the first row: what lies past it, not every row sees
   int32_t last_gone;                  // what lies before it, the last row does not see
@@ -176,11 +185,13 @@ struct __align__(16) JoinInfo {
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
+// The factor of a part's sums whose maximum is `m` beside one of `base`; never 0, so that infinities of its o stay.
+__device__ __forceinline__ float part_factor(float m, float base, float c) { return fmaxf(ex2((m - base) * c), 1.17549435e-38f); }
 // Two parts of a row joined: maximum and sum, and the factors of their o.
 __device__ __forceinline__ void join_ml(float& m, float& l, float m1, float l1, float c, float& f0, float& f1) {
   const float top = fmaxf(m, m1), base = top == -INFINITY ? 0.0f : top;
-  f0 = ex2((m - base) * c);
-  f1 = ex2((m1 - base) * c);
+  f0 = part_factor(m, base, c);
+  f1 = part_factor(m1, base, c);
   l = l * f0 + l1 * f1;
   m = top;
 }
@@ -212,6 +223,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
   __shared__ int64_t s_prefix[kWarps * 32 + 1];
   __shared__ int64_t s_warp[kWarps];
   __shared__ int s_last_cta;
+  __shared__ int s_first_block[kWarps];                 // that a run has of its item
   __shared__ float2 s_ml[kWarps][2][kRows];             // maximum and sum of the rows of a part, then (factor of their o, .)
   __shared__ CutRow s_rows[(kWarps + 2) * kRows];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r8 = lane >> 2, c4 = lane & 3, chunks = a.head_dim / 8;
@@ -392,7 +404,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       const bool ends = block + 1 == s.blocks, run_ends = !plan.whole && left == 1, last = ends || run_ends;
       if (lane == 0) {
         BlockInfo info;
-        info.b = b; info.head = hk; info.row0 = rg * kRows; info.n = s.n; info.position = p0;
+        info.b = b; info.head = hk; info.row0 = rg * kRows; info.n = s.n; info.block = block; info.position = p0;
         info.first_new = s.length - s.n;
         info.last_gone = a.window > 0 ? s.length - a.window : 0;
         info.present = present;
@@ -468,6 +480,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     if (info.flags & kNone) break;
     if (info.flags & kFirst) {
       from_start = info.flags & kFromStart;
+      if (lane == 0) s_first_block[warp] = info.block;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int r = info.row0 + nt * 8 + r8, t = r / a.group;
@@ -631,6 +644,78 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     }
     if (info.flags & kLast) {
       const bool done = from_start && (info.flags & kToEnd);
+      // An infinite value that a row sees has become NaN if what rounding left of its weight was 0 or of the other sign. Where that
+      // may be, the values are read once more: the visible infinities of either sign are counted by products with ones, and
+      // take the place of NaN.
+      float zero[2] = {0.0f, 0.0f};                     // as long as all sums are finite
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int d = 0; d < DB * 4; ++d) {
+          fma2(zero[0], zero[1], o[nt][d][0], o[nt][d][1], 0.0f, 0.0f, zero[0], zero[1]);
+          fma2(zero[0], zero[1], o[nt][d][2], o[nt][d][3], 0.0f, 0.0f, zero[0], zero[1]);
+        }
+      if (__any_sync(0xFFFFFFFFu, zero[0] + zero[1] != 0.0f)) {
+        const Sentence of = sentence_of<B>(a, info.b);
+        const T* values = reinterpret_cast<const T*>(a.v_pages) + info.head * a.vps.head;
+        // -0 stands for a NaN that nothing has taken the place of
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int d = 0; d < DB * 4; ++d)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[nt][d][u] = isnan(o[nt][d][u]) ? -0.0f : o[nt][d][u] + 0.0f;
+#pragma unroll 1
+        for (int sixteen = s_first_block[warp] * kSixteens; sixteen < (info.block + 1) * kSixteens; ++sixteen) {
+          const int at = sixteen / kSixteens, p0 = (at < of.sink_blocks ? at : at - of.sink_blocks + of.lo / B) * B + sixteen % kSixteens * 16;
+          const T* row[4];                              // of positions 2 c4, + 1, + 8, + 9
+          uint32_t see[NT][2];                          // row r8 sees them
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int p = p0 + c4 * 2 + (i & 1) + (i >> 1) * 8, page = p >= 0 ? page_of(a, info.b, p / a.page_size) : -1;
+            row[i] = page >= 0 ? values + page * a.vps.batch + p % a.page_size * a.vps.token : nullptr;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint32_t one = page >= 0 && sees(p, (info.row0 + nt * 8 + r8) / a.group) ? (kNarrow<T> ? 0x3C00u : 0x3F80u) : 0u;
+              see[nt][i >> 1] = i & 1 ? see[nt][i >> 1] | one << 16 : one;
+            }
+          }
+#pragma unroll 1
+          for (int d = 0; d < DB * 4; ++d) {
+            uint32_t up[4], down[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {               // values r8 (and 8 more), positions as in `see`
+              const int value = d * 16 + r8 + (e & 1) * 8;
+              uint32_t w = 0;
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                if (row[(e >> 1) * 2 + i] && value < a.head_dim) w |= (uint32_t)reinterpret_cast<const uint16_t*>(row[(e >> 1) * 2 + i])[value] << (16 * i);
+              up[e] = infinities<T>(w, 0u);
+              down[e] = infinities<T>(w, 0x80008000u);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float plus[4], minus[4];
+              mma16816_first<T>(plus, up, see[nt][0], see[nt][1]);
+              mma16816_first<T>(minus, down, see[nt][0], see[nt][1]);
+#pragma unroll
+              for (int i = 0; i < DB * 4; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  if (i == d) {
+                    if (plus[u] > 0.0f) o[nt][i][u] += INFINITY;
+                    if (minus[u] > 0.0f) o[nt][i][u] -= INFINITY;
+                  }
+            }
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int d = 0; d < DB * 4; ++d)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[nt][d][u] = __float_as_uint(o[nt][d][u]) == 0x80000000u ? NAN : o[nt][d][u];
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -721,7 +806,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       const float base = most == -INFINITY ? 0.0f : most;
       for (int j = first; j <= last; j += beside) {
         float2& ml = s_ml[j][j == first && second][row];
-        const float f = ex2((ml.x - base) * c);
+        const float f = part_factor(ml.x, base, c);
         sum = fmaf(ml.y, f, sum);
         ml.x = f;
       }
@@ -826,7 +911,7 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(PagedArgs a, PagedPlan
       top = m0;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-      const float f = ex2((m0 - (top == -INFINITY ? 0.0f : top)) * c);
+      const float f = part_factor(m0, top == -INFINITY ? 0.0f : top, c);
       sum = warp_sum(lane < plan.join_warps ? mine[lane * pitch + 1] * f : 0.0f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = 0.0f;

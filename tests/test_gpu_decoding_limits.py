@@ -48,3 +48,45 @@ def test_sums_of_a_million_positions(dtype, dim):
         within(o[b, 0, 0], want, (U[dtype] + slack) * want, (b, "o"))
         within(lse[b, 0, 0], torch.logsumexp(s, 0), slack * 20, (b, "lse"))
     ops.check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim,page,kv_heads", [(64, 16, 2), (64, 24, 1), (128, 64, 1), (40, 10, 2)])
+@pytest.mark.parametrize("tokens,window,std", [(1, 0, 0.3), (4, 0, 0.3), (5, 70, 0.3), (1, 0, 60.0), (3, 300, 60.0)])
+def test_infinite_values_that_a_row_sees_make_it_infinite(dtype, dim, page, kv_heads, tokens, window, std):
+    """What the formula says: +infinity, -infinity, NaN where both meet or a NaN is seen; all else as if they were 0."""
+    lengths = [tokens, 33, 200, 5000]                                           # one weight of 1 alone (tokens 1), and cut sentences
+    columns = -(-max(lengths) // page)
+    table = torch.randperm(4 * columns, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(4, columns).cuda()
+    k, v = (randn(4 * columns, page, kv_heads, dim, dtype=dtype, seed=s) for s in (1, 2))
+    q = randn(4, tokens, 3 * kv_heads, dim, dtype=dtype, seed=3, std=std)       # 60: weights that are 0 in fp32 beside the largest
+    clean = v.clone()
+    inf, nan = math.inf, math.nan
+    # (position from the end, value's place, what stands there): the newest token is seen by the last row alone
+    spoiled = [(0, 0, inf), (0, 1, -inf), (0, 2, nan), (tokens, 3, inf), (tokens, 4, -inf), (tokens, 5, nan), (tokens, 6, inf), (0, 6, -inf),
+               (17, 8, inf), (60, 9, -inf), (150, 10, inf), (4000, 11, -inf), (4500, 7, inf), (16, 7, inf)]
+    for b, n in enumerate(lengths):
+        for back, d, x in spoiled:
+            p = n - 1 - back
+            if p >= 0:
+                page_of, slot = table[b, p // page].long(), p % page
+                v[page_of, slot, :, d], clean[page_of, slot, :, d] = x, 0.0
+    length = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got, lse = ops.paged_attention(q, k, v, table, length, window=window, need_lse=True)
+    base, lse2 = ops.paged_attention(q, k, clean, table, length, window=window, need_lse=True)
+    assert torch.isfinite(base).all() and torch.equal(lse, lse2)
+    for b, n in enumerate(lengths):
+        for t in range(tokens):
+            own = n - tokens + t
+            seen = [[] for _ in range(dim)]
+            for back, d, x in spoiled:
+                p = n - 1 - back
+                if 0 <= p <= own and (not window or p > own - window):
+                    seen[d].append(x)
+            want = base[b, t].clone()
+            for d, xs in enumerate(seen):
+                if xs:
+                    want[:, d] = sum(xs)
+            assert torch.equal(torch.isnan(got[b, t]), torch.isnan(want)), (b, t)
+            assert torch.equal(torch.nan_to_num(got[b, t], nan=1.0, posinf=2e4, neginf=-2e4), torch.nan_to_num(want, nan=1.0, posinf=2e4, neginf=-2e4)), (b, t)
+    ops.check()
