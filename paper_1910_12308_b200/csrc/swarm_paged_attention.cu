@@ -656,6 +656,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
           fma2(zero[0], zero[1], o[nt][d][2], o[nt][d][3], 0.0f, 0.0f, zero[0], zero[1]);
         }
       if (__any_sync(0xFFFFFFFFu, zero[0] + zero[1] != 0.0f)) {
+        __syncwarp();                                   // the run's first block of the item has been written down
         const Sentence of = sentence_of<B>(a, info.b);
         const T* values = reinterpret_cast<const T*>(a.v_pages) + info.head * a.vps.head;
         // -0 stands for a NaN that nothing has taken the place of
