@@ -94,7 +94,10 @@ class Decoder:
         return -got.log_probs.mean()
 
     def answer(self, flat, prompts, counts, steps):
-        """Continues prompts [batch, n], of which counts [batch] tokens are each sequence's: (tokens, their log probabilities), [batch, steps]."""
+        """Continues prompts [batch, n], of which counts [batch] tokens, one at least, are each sequence's: (tokens, their log
+        probabilities), [batch, steps]."""
+        if counts.min().item() < 1 or counts.max().item() > prompts.shape[1]:
+            raise ValueError("counts: between 1 and the prompts' width")
         cache = Cache(self, prompts.shape[0], prompts.shape[1] + steps)
         h, a = self.attend(prompts, cache, counts)
         last = (counts.long() - 1).view(-1, 1, 1).expand(-1, 1, self.width)
