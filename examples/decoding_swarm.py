@@ -25,6 +25,7 @@ from paper_1910_12308_b200 import BLOCKING, Swarm  # noqa: E402
 from paper_1910_12308_b200 import operators as ops  # noqa: E402
 
 DTYPE = torch.bfloat16
+PIECE = 64                                  # tokens of a sequence that one call of attention over the cache takes
 
 
 class Cache:
@@ -70,8 +71,19 @@ class Decoder:
         q, k, v = heads.split((self.heads, self.kv_heads, self.kv_heads), 2)
         cache.lengths += tokens.shape[1] if counts is None else counts
         q = ops.append_to_cache(k, v, cache.k, cache.v, cache.table, cache.lengths, counts=counts, q=q, frequencies=self.frequencies)
-        a = ops.paged_attention(q, cache.k, cache.v, cache.table, cache.lengths, counts=counts)
-        return h, a.flatten(2) @ self.o
+        return h, self.look(q, cache, counts).flatten(2) @ self.o
+
+    def look(self, q, cache, counts):
+        """Attention of the newest tokens, which are in the cache, piece by piece: a piece ends the cache for its own call."""
+        n = q.shape[1]
+        if n <= PIECE:
+            return ops.paged_attention(q, cache.k, cache.v, cache.table, cache.lengths, counts=counts)
+        counts = torch.full_like(cache.lengths, n) if counts is None else counts
+        before, pieces = cache.lengths - counts, []
+        for at in range(0, n, PIECE):
+            here = (counts - at).clamp(0, PIECE)
+            pieces.append(ops.paged_attention(q[:, at:at + PIECE], cache.k, cache.v, cache.table, before + counts.clamp(max=at + PIECE), counts=here))
+        return torch.cat(pieces, 1)
 
     def logits(self, flat, h, a):
         norm, w = self.views(flat)
