@@ -118,3 +118,17 @@ def test_no_cpu_path():
                  lambda: ops.token_log_probs_backward(torch.zeros(2), torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(2, 2))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_paged_attention_refuses_every_workspace_that_does_not_do():
+    """Room for 16384 positions of 8 sentences: items are cut, so there is a workspace, and it has to be there, whole and aligned."""
+    L, n = g.load(), C.c_size_t()
+    big = dict(batch=8, pages=8192, table_columns=1024, table_pitch=1024)
+    assert L.swarm_paged_attention_workspace(desc(**big), C.byref(n)) == g.OK
+    assert n.value > 0
+
+    def call(work, size):
+        return L.swarm_paged_attention(desc(**big), P, P, P, P, None, work, size, None)
+
+    for work, size in ((P, 0), (P, n.value - 1), (None, n.value), (P + 8, n.value), (P + 4, 1 << 40)):
+        assert call(work, size) == g.EINVAL, (work, size)

@@ -90,3 +90,56 @@ def test_infinite_values_that_a_row_sees_make_it_infinite(dtype, dim, page, kv_h
             assert torch.equal(torch.isnan(got[b, t]), torch.isnan(want)), (b, t)
             assert torch.equal(torch.nan_to_num(got[b, t], nan=1.0, posinf=2e4, neginf=-2e4), torch.nan_to_num(want, nan=1.0, posinf=2e4, neginf=-2e4)), (b, t)
     ops.check()
+
+
+def run(rows, cols, top):
+    """Terms that one thread adds up of a row: a warp walks short rows, and longer ones where there are as many and nothing is searched for."""
+    warp = cols <= 1024 or (cols <= 16384 and rows >= cols and not top)
+    return cols / (32 if warp else 256)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("rows,cols,top", [(3, 700, 4), (2, 1025, 0), (4, 10007, 0), (4, 10007, 32), (1, 16384, 0), (1024, 1025, 0), (1100, 1025, 3), (2600, 2500, 0),
+                                           (5, 131072, 0), (40, 32000, 20)])
+def test_log_probs_are_as_near_as_their_threads_runs(dtype, rows, cols, top):
+    """A sum of n positive terms is off by n 2^-24 of it, an exponential of d by (|d| + 4) 2^-23, the joining of threads by 16 2^-24."""
+    scale = 0.9
+    logits = randn(rows, cols, dtype=dtype, seed=cols, std=3.0)
+    tokens = torch.randint(cols, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
+    got = ops.token_log_probs(logits, tokens, scale=scale, top=top, entropy=True)
+    x = logits.double() * scale
+    logp = torch.log_softmax(x, -1)
+    p, most = logp.exp(), x.max(-1).values
+    spread = (p * (x - most.unsqueeze(-1)).abs()).sum(-1)
+    off = (run(rows, cols, top) + 16) * 2.0 ** -24 + (spread + 4) * 2.0 ** -23
+    log_sum = torch.logsumexp(x, -1) - most
+    assert torch.equal(got.stats[:, 0].double(), logits.double().max(-1).values)
+    within(got.stats[:, 1], log_sum, off + 2.0 ** -23 * log_sum.abs(), "log of the sum")
+    want = logp.gather(1, tokens[:, None])[:, 0]
+    within(got.log_probs, want, off + 2.0 ** -22 * (want.abs() + 1), "log probs")
+    entropy = -(p * logp).sum(-1)
+    within(got.entropy, entropy, (off + 2.0 ** -22) * (4 + 2 * spread + entropy.abs()), "entropy")
+    if top:
+        order = torch.sort(logits.double(), dim=-1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(got.top_tokens, order)
+        want = logp.gather(1, order)
+        within(got.top_log_probs, want, off[:, None] + 2.0 ** -22 * (want.abs() + 1), "top")
+
+
+@pytest.mark.parametrize("cols,top", [(700, 20), (131072, 20), (32000, 32), (5000, 3)])
+def test_likeliest_tokens_of_rows_with_fewer_that_are_allowed(cols, top):
+    """Rows in which almost everything is ruled out, and rows of equal logits: the bound of the search leaves them all."""
+    logits = torch.full((6, cols), -math.inf, dtype=BF16, device="cuda")
+    allowed = [0, cols // 3, cols - 1]
+    logits[0, allowed] = torch.tensor([1.0, 3.0, 1.0], dtype=BF16, device="cuda")
+    logits[1, 7] = -2.0
+    logits[3], logits[4] = 0.0, torch.finfo(BF16).min
+    logits[5, ::5] = 0.5
+    got = ops.token_log_probs(logits, torch.zeros(6, dtype=torch.int64, device="cuda"), top=top)
+    order = torch.sort(logits.double(), dim=-1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(got.top_tokens, order)
+    want = torch.log_softmax(logits.double(), -1).gather(1, order)
+    want[2] = -math.inf                                                         # nothing is allowed
+    assert torch.equal(torch.isneginf(got.top_log_probs), torch.isneginf(want))
+    here = ~torch.isneginf(want)
+    assert (got.top_log_probs.double() - want)[here].abs().max().item() <= (cols / 32 + 64) * 2.0 ** -23
