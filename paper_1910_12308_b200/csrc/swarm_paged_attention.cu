@@ -37,6 +37,11 @@ constexpr int kMinShare = 32;
 // Items of no more positions are not cut: a warp takes each, and no kernel joins. 4 x 8 heads of 64 on 100 positions 9.2 us, cut 11.2;
 // on 230 positions 13.4 and 12.2, 32 x 4 key heads of 128 on 230 20.5 and 16.0.
 constexpr int kWholePositions = 128;
+// The tensor core cuts off what its sum has no bits for, always towards 0, so sums shrink by as many cuts as a warp takes products
+// of an item: 2^20 positions in one run, fp16, left o 0.8 % too small. Where a run may be longer than this, a block's products
+// are added up from nothing and then to o in fp32; below, it is at most 512 cuts of some 2^-25 of a growing sum, 8e-6. Added
+// always, drafts through a window 61 -> 63 us, 8 sentences of 16384 positions, heads of 64, 88 -> 92.
+constexpr int kLongRun = 4096;
 constexpr int kSms = 148;
 
 // DB: heads of up to 64 DB values. Blocks in flight to a warp, measured with one page to sixteen positions: heads of 128, pages of 64,
@@ -54,6 +59,7 @@ struct PagedPlan {
   int32_t row_groups;                 // of `tokens` rows
   int32_t rows;                       // that a part holds
   int32_t whole;                      // items are not cut
+  int32_t long_runs;                  // a warp may take more than kLongRun positions of an item
   int32_t streams;                    // the cache is larger than L2
   int32_t ctas;
   int32_t beside;                     // key heads that warps of a CTA take side by side: 1 or 2
@@ -168,6 +174,12 @@ enum : uint32_t {
   kRunEnds = 16, kNone = 32
 };
 
+// Whether the row of token t sees position p.
+__device__ __forceinline__ bool sees(const PagedArgs& a, const BlockInfo& info, int p, int t) {
+  const int own = info.first_new + t;
+  return p <= own && (a.window == 0 || p > own - a.window || p < a.sinks);
+}
+
 // Parts of a cut item that a warp holds: the run's first item may have begun elsewhere (0), its last one may go on (1).
 struct __align__(16) PartInfo {
   int32_t there, b, head, row0, rows, to_end, in_ring;   // rows: from row0 on; in_ring: in shared memory, else in the workspace
@@ -208,11 +220,67 @@ __device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
   *reinterpret_cast<uint2*>(to) = l != 0.0f ? make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv)) : make_uint2(0, 0);
 }
 
+// Puts infinities in the places of NaN that stand for them. A row's infinite value becomes NaN where what rounding left of its weight
+// is 0 or of the other sign. The item's values are read once more, the infinities of either sign that a row sees are counted by
+// products with ones. sums: a warp's, [NT][DB * 4][4], of the blocks from `first_block` to the one of `block`. Not inlined: where
+// all is finite it would cost 2 us of 90 by being there.
+template <typename T, int DB, int NT>
+__device__ __noinline__ void put_infinities(const PagedArgs& a, const BlockInfo* block, int first_block, float* sums) {
+  constexpr int B = 32 / DB, kSixteens = B / 16;
+  constexpr uint32_t kOne = kNarrow<T> ? 0x3C00u : 0x3F80u;
+  const BlockInfo info = *block;
+  const int lane = threadIdx.x & 31, r8 = lane >> 2, c4 = lane & 3;
+  const Sentence of = sentence_of<B>(a, info.b);
+  const T* values = reinterpret_cast<const T*>(a.v_pages) + info.head * a.vps.head;
+  // -0 stands for a NaN that nothing has taken the place of
+  for (int i = 0; i < NT * DB * 16; ++i) sums[i] = isnan(sums[i]) ? -0.0f : sums[i] + 0.0f;
+  for (int sixteen = first_block * kSixteens; sixteen < (info.block + 1) * kSixteens; ++sixteen) {
+    const int at = sixteen / kSixteens, p0 = (at < of.sink_blocks ? at : at - of.sink_blocks + of.lo / B) * B + sixteen % kSixteens * 16;
+    const T* row[4];                                    // of positions 2 c4, + 1, + 8, + 9
+    uint32_t see[NT][2];                                // row r8 sees them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + c4 * 2 + (i & 1) + (i >> 1) * 8, page = p >= 0 ? page_of(a, info.b, p / a.page_size) : -1;
+      row[i] = page >= 0 ? values + page * a.vps.batch + p % a.page_size * a.vps.token : nullptr;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint32_t one = page >= 0 && sees(a, info, p, (info.row0 + nt * 8 + r8) / a.group) ? kOne : 0u;
+        see[nt][i >> 1] = i & 1 ? see[nt][i >> 1] | one << 16 : one;
+      }
+    }
+    for (int d = 0; d < DB * 4; ++d) {
+      uint32_t up[4], down[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {                     // values r8 (and 8 more), positions as in `see`
+        const int value = d * 16 + r8 + (e & 1) * 8;
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (row[(e >> 1) * 2 + i] && value < a.head_dim) w |= (uint32_t)reinterpret_cast<const uint16_t*>(row[(e >> 1) * 2 + i])[value] << (16 * i);
+        up[e] = infinities<T>(w, 0u);
+        down[e] = infinities<T>(w, 0x80008000u);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float plus[4] = {}, minus[4] = {}, *to = sums + (nt * DB * 4 + d) * 4;
+        mma16816<T>(plus, up, see[nt][0], see[nt][1]);
+        mma16816<T>(minus, down, see[nt][0], see[nt][1]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (plus[u] > 0.0f) to[u] += INFINITY;
+          if (minus[u] > 0.0f) to[u] -= INFINITY;
+        }
+      }
+    }
+  }
+  for (int i = 0; i < NT * DB * 16; ++i) sums[i] = __float_as_uint(sums[i]) == 0x80000000u ? NAN : sums[i];
+}
+
 // NT: items of up to 8 NT rows. ONE_PAGE: pages hold a multiple of 16 positions, so sixteen of a block lie in one. Then a row's
 // address is one addition away from the last one's; else each position has its own, and a lane gets them by shuffles.
-template <typename T, int DB, int NT, bool ONE_PAGE>
+template <typename T, int DB, int NT, bool ONE_PAGE, bool LONG>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
-paged_attention_kernel(PagedArgs a, PagedPlan plan) {
+paged_attention_kernel(const __grid_constant__ PagedArgs a, const PagedPlan plan) {
   using S = Shape<DB, ONE_PAGE>;
   constexpr int kPartBytes = kRows * DB * 64 * 4;
   static_assert(2 * kPartBytes <= S::kRing, "a warp's two parts fit its ring");
@@ -522,10 +590,6 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
     // some position of the block is hidden from some row
     const bool edge = info.present != low_bits(B) || info.position + (B - 1) > info.first_new ||
                       (a.window > 0 && info.position < info.last_gone && info.position + (B - 1) >= a.sinks);
-    auto sees = [&](int p, int t) {
-      const int own = info.first_new + t;
-      return p <= own && (a.window == 0 || p > own - a.window || p < a.sinks);
-    };
     if (edge) {
 #pragma unroll
       for (int g = 0; g < kSixteens; ++g)
@@ -534,7 +598,7 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
           const int i = g * 16 + r8 + (u >> 1) * 8;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
-            if (!(info.present >> i & 1u) || !sees(info.position + i, t_of[nt][u & 1])) sc[nt][g][u] = -INFINITY;
+            if (!(info.present >> i & 1u) || !sees(a, info, info.position + i, t_of[nt][u & 1])) sc[nt][g][u] = -INFINITY;
         }
     }
     bool moved = false;
@@ -591,35 +655,43 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
       }
       apart = __any_sync(0xFFFFFFFFu, bad);
     }
-    // A block's products are added up from nothing, and then to o in fp32: the tensor core cuts off what its sum has no bits
-    // for, always towards 0, and a long run's sums shrank by as many cuts (2^20 positions in one run, fp16: o 0.8 % too small).
-    // Sixteen rows, drafts through a window, 62 -> 65 us, eight rows the same.
-    // products: the sums of values 16 d on; `masked` leaves of the cache's values what is to be seen
-    auto products = [&](float x[NT][4], int d, auto masked) {
+    // Adds the block's products to o, for the rows that `of_rows` says; `masked` leaves of the cache's values what is to be seen.
+    // Sums of 64 values side by side: they wait for one another less often.
+    constexpr int kSide = DB == 1 ? 4 : 1;
+    auto add_products = [&](auto masked, auto of_rows) {
 #pragma unroll
-      for (int g = 0; g < kSixteens; ++g) {
-        uint32_t v[4];
-        ldmatrix4_trans(tile_v + g * (16 * DB * 128) + tile_offset<DB>(value_row, d * 2 + value_half), v);
-        masked(g, v);
+      for (int d0 = 0; d0 < DB * 4; d0 += kSide) {
+        float x[kSide][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (g == 0) mma16816_first<T>(x[nt], v, hi[nt][g][0], hi[nt][g][1]);
-          else mma16816<T>(x[nt], v, hi[nt][g][0], hi[nt][g][1]);
-          mma16816<T>(x[nt], v, lo[nt][g][0], lo[nt][g][1]);
-        }
+        for (int d = 0; d < kSide; ++d)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[d][nt][u] = LONG ? 0.0f : o[nt][d0 + d][u];
+#pragma unroll
+        for (int g = 0; g < kSixteens; ++g)
+#pragma unroll
+          for (int d = 0; d < kSide; ++d) {
+            uint32_t v[4];
+            ldmatrix4_trans(tile_v + g * (16 * DB * 128) + tile_offset<DB>(value_row, (d0 + d) * 2 + value_half), v);
+            masked(g, v);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma16816<T>(x[d][nt], v, hi[nt][g][0], hi[nt][g][1]);
+              mma16816<T>(x[d][nt], v, lo[nt][g][0], lo[nt][g][1]);
+            }
+          }
+#pragma unroll
+        for (int d = 0; d < kSide; ++d)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (of_rows(t_of[nt][u & 1])) o[nt][d0 + d][u] = LONG ? o[nt][d0 + d][u] + x[d][nt][u] : x[d][nt][u];
       }
     };
     if (!apart) {
-#pragma unroll
-      for (int d = 0; d < DB * 4; ++d) {
-        float x[NT][4];
-        products(x, d, [](int, uint32_t*) {});
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          add2(o[nt][d][0], o[nt][d][1], o[nt][d][0], o[nt][d][1], x[nt][0], x[nt][1]);
-          add2(o[nt][d][2], o[nt][d][3], o[nt][d][2], o[nt][d][3], x[nt][2], x[nt][3]);
-        }
-      }
+      add_products([](int, uint32_t*) {}, [](int) { return true; });
     } else {
       // one token after the other, its rows alone and what it does not see as zeros: the same bits as above for these
       for (int t = 0; t < a.tokens; ++t) {
@@ -629,24 +701,15 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int p = info.position + g * 16 + e * 8 + c4 * 2;
-            keep[g][e] = (sees(p, t) ? 0xFFFFu : 0u) | (sees(p + 1, t) ? 0xFFFF0000u : 0u);
+            keep[g][e] = (sees(a, info, p, t) ? 0xFFFFu : 0u) | (sees(a, info, p + 1, t) ? 0xFFFF0000u : 0u);
           }
-#pragma unroll
-        for (int d = 0; d < DB * 4; ++d) {
-          float x[NT][4];
-          products(x, d, [&](int g, uint32_t* v) { v[0] &= keep[g][0]; v[1] &= keep[g][0]; v[2] &= keep[g][1]; v[3] &= keep[g][1]; });
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) o[nt][d][u] = t_of[nt][u & 1] == t ? o[nt][d][u] + x[nt][u] : o[nt][d][u];
-        }
+        add_products([&](int g, uint32_t* v) { v[0] &= keep[g][0]; v[1] &= keep[g][0]; v[2] &= keep[g][1]; v[3] &= keep[g][1]; },
+                     [&](int token) { return token == t; });
       }
     }
     if (info.flags & kLast) {
       const bool done = from_start && (info.flags & kToEnd);
-      // An infinite value that a row sees has become NaN if what rounding left of its weight was 0 or of the other sign. Where that
-      // may be, the values are read once more: the visible infinities of either sign are counted by products with ones, and
-      // take the place of NaN.
+      // NaN among the sums may stand for an infinite value
       float zero[2] = {0.0f, 0.0f};                     // as long as all sums are finite
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -657,65 +720,12 @@ paged_attention_kernel(PagedArgs a, PagedPlan plan) {
         }
       if (__any_sync(0xFFFFFFFFu, zero[0] + zero[1] != 0.0f)) {
         __syncwarp();                                   // the run's first block of the item has been written down
-        const Sentence of = sentence_of<B>(a, info.b);
-        const T* values = reinterpret_cast<const T*>(a.v_pages) + info.head * a.vps.head;
-        // -0 stands for a NaN that nothing has taken the place of
+        float sums[NT * DB * 16];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < NT * DB * 16; ++i) sums[i] = o[i / (DB * 16)][i / 4 % (DB * 4)][i % 4];
+        put_infinities<T, DB, NT>(a, &s_info[warp][stage], s_first_block[warp], sums);
 #pragma unroll
-          for (int d = 0; d < DB * 4; ++d)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) o[nt][d][u] = isnan(o[nt][d][u]) ? -0.0f : o[nt][d][u] + 0.0f;
-#pragma unroll 1
-        for (int sixteen = s_first_block[warp] * kSixteens; sixteen < (info.block + 1) * kSixteens; ++sixteen) {
-          const int at = sixteen / kSixteens, p0 = (at < of.sink_blocks ? at : at - of.sink_blocks + of.lo / B) * B + sixteen % kSixteens * 16;
-          const T* row[4];                              // of positions 2 c4, + 1, + 8, + 9
-          uint32_t see[NT][2];                          // row r8 sees them
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int p = p0 + c4 * 2 + (i & 1) + (i >> 1) * 8, page = p >= 0 ? page_of(a, info.b, p / a.page_size) : -1;
-            row[i] = page >= 0 ? values + page * a.vps.batch + p % a.page_size * a.vps.token : nullptr;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const uint32_t one = page >= 0 && sees(p, (info.row0 + nt * 8 + r8) / a.group) ? (kNarrow<T> ? 0x3C00u : 0x3F80u) : 0u;
-              see[nt][i >> 1] = i & 1 ? see[nt][i >> 1] | one << 16 : one;
-            }
-          }
-#pragma unroll 1
-          for (int d = 0; d < DB * 4; ++d) {
-            uint32_t up[4], down[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {               // values r8 (and 8 more), positions as in `see`
-              const int value = d * 16 + r8 + (e & 1) * 8;
-              uint32_t w = 0;
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                if (row[(e >> 1) * 2 + i] && value < a.head_dim) w |= (uint32_t)reinterpret_cast<const uint16_t*>(row[(e >> 1) * 2 + i])[value] << (16 * i);
-              up[e] = infinities<T>(w, 0u);
-              down[e] = infinities<T>(w, 0x80008000u);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float plus[4], minus[4];
-              mma16816_first<T>(plus, up, see[nt][0], see[nt][1]);
-              mma16816_first<T>(minus, down, see[nt][0], see[nt][1]);
-#pragma unroll
-              for (int i = 0; i < DB * 4; ++i)
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                  if (i == d) {
-                    if (plus[u] > 0.0f) o[nt][i][u] += INFINITY;
-                    if (minus[u] > 0.0f) o[nt][i][u] -= INFINITY;
-                  }
-            }
-          }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int d = 0; d < DB * 4; ++d)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) o[nt][d][u] = __float_as_uint(o[nt][d][u]) == 0x80000000u ? NAN : o[nt][d][u];
+        for (int i = 0; i < NT * DB * 16; ++i) o[i / (DB * 16)][i / 4 % (DB * 4)][i % 4] = sums[i];
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -956,6 +966,8 @@ PagedPlan make_plan(const PagedArgs& a) {
     if (a.head_dim <= 64 && a.kv_heads % 2 == 0 && a.kps.head < a.kps.token) p.beside = 2;
   }
   p.head_groups = a.kv_heads / p.beside;
+  // a run is a warp's equal share of all positions that there can be (or kMinShare of them, and the device is not filled)
+  p.long_runs = most > kLongRun && items * most / (kSms * kCtasPerSm * kWarps) > kLongRun;
   const int64_t warps = p.whole ? items : items * (most / kMinShare + 2);
   const int64_t room = (int64_t)kSms * kCtasPerSm;
   p.ctas = (int32_t)(warps < room ? (warps < 1 ? 1 : warps) : room);
@@ -969,7 +981,7 @@ PagedPlan make_plan(const PagedArgs& a) {
   return p;
 }
 
-template <typename T, int DB, int NT, bool ONE_PAGE>
+template <typename T, int DB, int NT, bool ONE_PAGE, bool LONG>
 cudaError_t launch_as(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
   using S = Shape<DB, ONE_PAGE>;
   static bool attr_set[64] = {};
@@ -980,26 +992,26 @@ cudaError_t launch_as(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<T, DB, NT, ONE_PAGE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+      const cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<T, DB, NT, ONE_PAGE, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
       if (e != cudaSuccess) return e;
       attr_set[dev] = true;
     }
   }
-  paged_attention_kernel<T, DB, NT, ONE_PAGE><<<p.ctas, kWarps * 32, S::kSmem, st>>>(a, p);
+  paged_attention_kernel<T, DB, NT, ONE_PAGE, LONG><<<p.ctas, kWarps * 32, S::kSmem, st>>>(a, p);
   return cudaGetLastError();
+}
+
+template <typename T, int DB, int NT>
+cudaError_t launch_of(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
+  if (a.page_size % 16 == 0) return p.long_runs ? launch_as<T, DB, NT, true, true>(a, p, st) : launch_as<T, DB, NT, true, false>(a, p, st);
+  return p.long_runs ? launch_as<T, DB, NT, false, true>(a, p, st) : launch_as<T, DB, NT, false, false>(a, p, st);
 }
 
 template <typename T>
 cudaError_t launch(const PagedArgs& a, const PagedPlan& p, cudaStream_t st) {
-  const bool one_page = a.page_size % 16 == 0;
   cudaError_t e;
-  if (a.head_dim <= 64) {
-    if (p.rows <= 8) e = one_page ? launch_as<T, 1, 1, true>(a, p, st) : launch_as<T, 1, 1, false>(a, p, st);
-    else e = one_page ? launch_as<T, 1, 2, true>(a, p, st) : launch_as<T, 1, 2, false>(a, p, st);
-  } else {
-    if (p.rows <= 8) e = one_page ? launch_as<T, 2, 1, true>(a, p, st) : launch_as<T, 2, 1, false>(a, p, st);
-    else e = one_page ? launch_as<T, 2, 2, true>(a, p, st) : launch_as<T, 2, 2, false>(a, p, st);
-  }
+  if (a.head_dim <= 64) e = p.rows <= 8 ? launch_of<T, 1, 1>(a, p, st) : launch_of<T, 1, 2>(a, p, st);
+  else e = p.rows <= 8 ? launch_of<T, 2, 1>(a, p, st) : launch_of<T, 2, 2>(a, p, st);
   if (e != cudaSuccess || p.whole || p.ctas == 1) return e;
   const int warps = p.join_warps > 4 ? p.join_warps : 4, each = warps / p.join_warps;
   cudaLaunchConfig_t cfg{};

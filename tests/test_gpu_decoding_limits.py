@@ -143,3 +143,49 @@ def test_likeliest_tokens_of_rows_with_fewer_that_are_allowed(cols, top):
     assert torch.equal(torch.isneginf(got.top_log_probs), torch.isneginf(want))
     here = ~torch.isneginf(want)
     assert (got.top_log_probs.double() - want)[here].abs().max().item() <= (cols / 32 + 64) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim,page", [(BF16, 4, 2, 64, 16), (F16, 12, 1, 64, 48), (F16, 6, 2, 128, 16), (BF16, 16, 1, 128, 32), (BF16, 9, 3, 40, 10),
+                                                           (F16, 32, 2, 96, 7)])
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_tables_with_room_for_long_sentences(dtype, heads, kv_heads, dim, page, tokens):
+    """Room for 2^20 tokens of each sentence, as a loop has it that is captured once: the kernel for long runs, over short sentences."""
+    lengths = [tokens, 17, 1024, 1023, 2500, 0, 33, 700, 2049, 64, 1, 100]
+    batch, columns = len(lengths), -(-(1 << 20) // page)
+    need = [-(-n // page) for n in lengths]
+    pages = sum(need)
+    order, at = torch.randperm(pages, generator=torch.Generator().manual_seed(1)).to(torch.int32), 0
+    table = torch.full((batch, columns), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    table = table.cuda()
+    k, v = (randn(pages, page, kv_heads, dim, dtype=dtype, seed=s) for s in (1, 2))
+    q = randn(batch, tokens, heads, dim, dtype=dtype, seed=3, std=1.5)
+    length = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    for window, sinks in ((0, 0), (1 << 19, 5)):
+        o, lse = ops.paged_attention(q, k, v, table, length, window=window, sinks=sinks, need_lse=True)
+        for b, n in enumerate(lengths):
+            here, p = min(n, tokens), torch.arange(n, device="cuda")
+            assert not o[b, here:].any() and torch.isneginf(lse[b, :, here:]).all()
+            kb, vb = (x[table[b][p // page].long(), p % page].double().repeat_interleave(heads // kv_heads, 1) for x in (k, v))
+            for t in range(here):
+                m = n - here + t + 1
+                s = torch.einsum("hd,nhd->hn", q[b, t].double(), kb[:m]) * dim ** -0.5
+                w = torch.softmax(s, -1)
+                want, size = torch.einsum("hn,nhd->hd", w, vb[:m]), torch.einsum("hn,nhd->hd", w, vb[:m].abs())
+                within(o[b, t], want, U[dtype] * want.abs() + E * size + 2.0 ** -24, (b, t))
+                l = torch.logsumexp(s, -1)
+                within(lse[b, :, t], l, E * (1 + l.abs()), (b, t))
+    if tokens > 1:                                                              # what earlier rows do not see: the same bits
+        bad = v.clone()
+        for b, n in enumerate(lengths):
+            if n > 1:
+                bad[table[b, (n - 1) // page].long(), (n - 1) % page] = math.inf
+        again = ops.paged_attention(q, k, bad, table, length)
+        plain = ops.paged_attention(q, k, v, table, length)
+        for b, n in enumerate(lengths):
+            here = min(n, tokens)
+            if n > 1:
+                assert torch.equal(again[b, :here - 1], plain[b, :here - 1]) and torch.isposinf(again[b, here - 1]).all()
+    ops.check()
