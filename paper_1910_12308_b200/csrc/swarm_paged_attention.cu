@@ -3,7 +3,7 @@
 // An item is up to 16 rows (tokens x query heads of a key head) of a sentence and all the positions that one of them sees, in
 // blocks of 16 or 32. The blocks of all items in a row are dealt to the device's warps in equal runs, whatever the sentences'
 // lengths: a warp may end one item, take several whole ones and begin another. Each warp works alone: a ring of blocks that
-// cp.async fills past the ends of items, so that loads never pause (128 to 192 KB in flight on a multiprocessor), ldmatrix,
+// cp.async fills past the ends of items, so that loads never pause (64 to 128 KB in flight on a multiprocessor), ldmatrix,
 // m16n8k16 products with the running maximum and sum of the softmax in registers. An item that was cut leaves parts (maximum,
 // sum, o): those of a CTA's warps, whose runs follow one another, are joined at the CTA's end, those of several CTAs by a
 // second kernel, which may be launched before the first has ended (up to 1 us less); always in the items' order.
@@ -15,9 +15,9 @@
 // Weights enter their product as the sum of two numbers of the type: rounded once, o would be 1.4 times as far from its value as
 // its own rounding leaves it. The products are a small part of a block's time, so the second costs nothing.
 //
-// Measured on the device, whole call: 8 sentences of 16384 positions, 8 key heads of 128 with four query heads each, 537 MB, 89 us, 6.0
-// TB/s; 128 sentences of 128 to 1024 positions, 16 heads of 64, 327 MB, 62 us, 5.2 TB/s; 64 sentences' drafts of four
-// tokens through a window of 1024, 32 heads of 128 on 8, 264 MB, 60 us. Of these 5 us pass until the first copies are on their way, 4 us in
+// Measured on the device, whole call: 8 sentences of 16384 positions, 8 key heads of 128 with four query heads each, 537 MB, 90 us, 6.0
+// TB/s; 128 sentences of 128 to 1024 positions, 16 heads of 64, 327 MB, 63 us, 5.2 TB/s; 64 sentences' drafts of four
+// tokens through a window of 1024, 32 heads of 128 on 8, 264 MB, 61 us. Of these 5 us pass until the first copies are on their way, 4 us in
 // the joining kernel, and about 8 us while some multiprocessors have ended: runs are equal, not what HBM gives each
 // multiprocessor. Runs given to whoever is free would change the order of sums from call to call. The tensor pipe is 10 to 18 % busy.
 #include <mutex>
@@ -34,14 +34,15 @@ constexpr int kCtasPerSm = 1;                         // two of four warps: long
 // Positions that a warp's run has at least. Small calls, 32 / 64 / 128: 4 x 8 heads of 64 on 490 positions 12.2 / 14.0 / 15.0 us, 32 x 4
 // key heads of 128 on 230 14.1 / 16.0 / 20.0; large ones are the same.
 constexpr int kMinShare = 32;
-// Items of no more positions are not cut: a warp takes each, and no kernel joins. 4 x 8 heads of 64 on 100 positions 9.2 us, cut 11.2;
-// on 230 positions 13.4 and 12.2, 32 x 4 key heads of 128 on 230 20.5 and 16.0.
+// Items of no more positions are not cut: a warp takes each, and no kernel joins. 4 x 8 heads of 64 on 100 positions 9.1 us, cut 10.7;
+// on 230 positions 13.6 and 12.1, 32 x 4 key heads of 128 on 230 20.6 and 14.1. The host knows no lengths: this, and what is kept in L2, go
+// by the room that the table and the pages have (77 positions 8.0 us, in a table for more 10.4).
 constexpr int kWholePositions = 128;
 // The tensor core cuts off what its sum has no bits for, always towards 0, so sums shrink by as many cuts as a warp takes products
 // of an item: 2^20 positions in one run, fp16, left o 0.8 % too small. Where a run may be longer than this, a block's products
-// are added up from nothing and then to o in fp32; below, it is at most 512 cuts of some 2^-25 of a growing sum, 8e-6. Added
-// always, drafts through a window 61 -> 63 us, 8 sentences of 16384 positions, heads of 64, 88 -> 92.
-constexpr int kLongRun = 4096;
+// are added up from nothing and then to o in fp32; below, it is 256 cuts and by that measure 1.6e-5, a thirtieth of fp16's
+// own rounding. Added always, drafts through a window 61 -> 63 us, 8 sentences of 16384 positions, heads of 64, 88 -> 92.
+constexpr int kLongRun = 2048;
 constexpr int kSms = 148;
 
 // DB: heads of up to 64 DB values. Blocks in flight to a warp, measured with one page to sixteen positions: heads of 128, pages of 64,
