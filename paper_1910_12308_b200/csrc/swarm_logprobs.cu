@@ -8,8 +8,9 @@
 // Gradient: one walk, a logit read and a gradient written.
 //
 // Measured on the device: 8192 rows of 32000 in bf16 forward 88 us, 6.0 TB/s (the special-function unit is 72 % busy; in fp32 6.6 TB/s),
-// with entropies 102, gradient 165 us, 6.4 TB/s; 128 rows of 131072 9 us, with entropies and the 20 likeliest 18: the bound, the second
-// walk and the merging of lists are chains of latencies; 8 rows of 32000 with four likeliest 5.9 us.
+// with entropies 102, gradient 165 us, 6.4 TB/s; 128 rows of 131072 9 us, with entropies and the 20 likeliest 19: the bound, the second
+// walk and the merging of lists are chains of latencies; 8 rows of 32000 with four likeliest 5.9 us. Where fewer logits are finite than
+// wanted, or all are equal, the bound leaves every logit: the 128 rows take 72 us.
 #include <cmath>
 #include <mutex>
 
@@ -507,6 +508,15 @@ cudaError_t launch_rows(const LogProbsArgs& a, cudaStream_t st) {
 //   of 8000                                  14 / 15     32 / 29     61 / 47      117 / 85
 //   of 16000                                             50 / 54     94 / 87      184 / 161
 //   of 32000                                             88 / 116    165 / 182
+// The gradient, and fp32, turn at about the same sizes. us with a CTA / a warp to a row:
+//                      bf16 gradient   fp32 forward   fp32 gradient
+//   1000 of 2000         4.6 / 3.3       4.3 / 4.2      4.9 / 4.4
+//   1000 of 4000         5.5 / 5.1       4.8 / 6.5      5.6 / 6.4
+//   4000 of 4000          17 / 11         11 / 10        24 / 22
+//   4000 of 8000          28 / 25         25 / 24        38 / 46
+//   8000 of 8000          53 / 45         45 / 50        82 / 88
+//   16000 of 16000       178 / 175       148 / 163      302 / 352
+// The rule gives away up to 1.3 us of 4.6 at 1000 rows of 2000, and up to a sixth at the longest rows of fp32.
 bool warp_takes_row(const LogProbsArgs& a) { return a.cols <= 1024 || (a.cols <= 16384 && a.rows >= a.cols); }
 template <typename T, bool ENTROPY, bool TOP>
 cudaError_t launch_forward_as(const LogProbsArgs& a, cudaStream_t st) {
