@@ -224,7 +224,7 @@ __device__ __forceinline__ void write_values(T* to, float l, const float v[4]) {
 // Puts infinities in the places of NaN that stand for them. A row's infinite value becomes NaN where what rounding left of its weight
 // is 0 or of the other sign. The item's values are read once more, the infinities of either sign that a row sees are counted by
 // products with ones. sums: a warp's, [NT][DB * 4][4], of the blocks from `first_block` to the one of `block`. Not inlined: where
-// all is finite it would cost 2 us of 90 by being there.
+// all is finite it would cost 2 us of 90 by being there. With infinities in every page those 90 us are 750.
 template <typename T, int DB, int NT>
 __device__ __noinline__ void put_infinities(const PagedArgs& a, const BlockInfo* block, int first_block, float* sums) {
   constexpr int B = 32 / DB, kSixteens = B / 16;
@@ -710,7 +710,13 @@ paged_attention_kernel(const __grid_constant__ PagedArgs a, const PagedPlan plan
     }
     if (info.flags & kLast) {
       const bool done = from_start && (info.flags & kToEnd);
-      // NaN among the sums may stand for an infinite value
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l[nt][u] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][u], x);
+      // NaN among the sums of a row whose weights are none may stand for an infinite value
       float zero[2] = {0.0f, 0.0f};                     // as long as all sums are finite
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -720,20 +726,18 @@ paged_attention_kernel(const __grid_constant__ PagedArgs a, const PagedPlan plan
           fma2(zero[0], zero[1], o[nt][d][2], o[nt][d][3], 0.0f, 0.0f, zero[0], zero[1]);
         }
       if (__any_sync(0xFFFFFFFFu, zero[0] + zero[1] != 0.0f)) {
-        __syncwarp();                                   // the run's first block of the item has been written down
         float sums[NT * DB * 16];
+        bool some = false;
 #pragma unroll
-        for (int i = 0; i < NT * DB * 16; ++i) sums[i] = o[i / (DB * 16)][i / 4 % (DB * 4)][i % 4];
-        put_infinities<T, DB, NT>(a, &s_info[warp][stage], s_first_block[warp], sums);
+        for (int i = 0; i < NT * DB * 16; ++i) {
+          sums[i] = o[i / (DB * 16)][i / 4 % (DB * 4)][i % 4];
+          some |= isnan(sums[i]) && !isnan(l[i / (DB * 16)][i & 1]);
+        }
+        __syncwarp();                                   // the run's first block of the item has been written down
+        if (__any_sync(0xFFFFFFFFu, some)) put_infinities<T, DB, NT>(a, &s_info[warp][stage], s_first_block[warp], sums);
 #pragma unroll
         for (int i = 0; i < NT * DB * 16; ++i) o[i / (DB * 16)][i / 4 % (DB * 4)][i % 4] = sums[i];
       }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int x = 4; x < 32; x <<= 1) l[nt][u] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][u], x);
       if (done) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

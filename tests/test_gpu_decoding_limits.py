@@ -189,3 +189,22 @@ def test_tables_with_room_for_long_sentences(dtype, heads, kv_heads, dim, page, 
             if n > 1:
                 assert torch.equal(again[b, :here - 1], plain[b, :here - 1]) and torch.isposinf(again[b, here - 1]).all()
     ops.check()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_that_are_none_stay_so_beside_infinite_values(dim):
+    """A NaN in one query head makes that head's rows NaN, whatever the values; the others see the infinities."""
+    n, page = 3000, 16
+    k, v = (randn(n // page + 1, page, 1, dim, dtype=BF16, seed=s) for s in (1, 2))
+    v[7, 3, 0, 5], v[90, 0, 0, 6] = math.inf, -math.inf
+    table = torch.arange(n // page + 1, dtype=torch.int32, device="cuda")[None]
+    q = randn(1, 2, 6, dim, dtype=BF16, seed=3)
+    q[0, 1, 2, 0] = math.nan
+    o, lse = ops.paged_attention(q, k, v, table, torch.tensor([n], dtype=torch.int32, device="cuda"), need_lse=True)
+    none = torch.zeros(1, 2, 6, dtype=torch.bool, device="cuda")
+    none[0, 1, 2] = True
+    assert torch.equal(torch.isnan(o).all(-1), none) and torch.equal(torch.isnan(o).any(-1), none) and torch.equal(torch.isnan(lse).transpose(1, 2), none)
+    seen = o[~none]
+    assert (seen[:, 5] == math.inf).all() and (seen[:, 6] == -math.inf).all()
+    rest = [d for d in range(dim) if d not in (5, 6)]
+    assert torch.isfinite(seen[:, rest]).all()
