@@ -509,8 +509,8 @@ int swarm_token_log_probs(const void *logits_dev, const int64_t *tokens_dev, flo
 /* Gradient with respect to the logits, from those of log_probs and of entropy: with p_j = exp(x_j - lse)
  *   dlogits_j = scale * (dlog_probs * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy)).
  *   p_j below 2^-126 count as 0. stats_dev (and entropy_dev, with dentropy_dev) as the forward call returned them.
- *   Either of dlog_probs_dev (with tokens_dev) and dentropy_dev may be NULL. A row whose token is a padded place has no first part; a row of -infinity has gradient 0.
- *   dlogits_dev may be logits_dev with the same pitch.
+ *   Either of dlog_probs_dev (with tokens_dev) and dentropy_dev may be NULL. A row whose token is a padded place has no
+ *   first part; a row of -infinity has gradient 0. dlogits_dev may be logits_dev with the same pitch.
  * Errors: EINVAL (as the forward call). */
 int swarm_token_log_probs_backward(const float *dlog_probs_dev, const float *dentropy_dev, const void *logits_dev,
                                    const int64_t *tokens_dev, const float *stats_dev, const float *entropy_dev,
